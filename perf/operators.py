@@ -310,7 +310,7 @@ def prepare(case, seed):
         s["context"] = max(a + n for a, n in zip(committed, counts))
     if own:          # the handle that a program keeps for its cache
         from paper_2605_10793_amd import attention as A
-        s["cache"] = A.KVCache(s["k_pool"], s["v_pool"], s["k_scale"], s["v_scale"])
+        s["cache"] = A.KVCache(s["k_pool"], s["v_pool"], s["k_scale"], s["v_scale"], bits=c["bits"])
     return s
 
 
