@@ -296,6 +296,173 @@ conqur_status conqur_get_last_corners(conqur_ctx* ctx, int8_t* signs_host, float
 conqur_status conqur_score_rows_static(const void* Y_dev, uint32_t dtype, uint64_t T, uint64_t d, uint64_t row_stride_elems,
                                        uint32_t bits, uint32_t zero_point, float clip_ratio, double* out_dev, void* stream);
 
+/* ---- One attention layer around the calibrated heads -------------------------------------------
+ * What stands between a layer's projections and the rows that o_proj (and the per-head rotations above) receive: positions
+ * and norms of queries and keys, a paged cache that holds keys and values in 16 bits or in the zero-point codes of 8 or 4
+ * bits, and the attention of new tokens over it.  These calls need no context.  They run on the CURRENT device, on `stream`
+ * (NULL = its default stream), which must belong to it; they allocate nothing, copy nothing to the host and return without
+ * waiting, so they may be captured into a HIP graph.  All memory they name is DEVICE memory of the caller's, except where
+ * HOST is said; it must stay until the stream has passed the call.  `conqur_rotary_call` and its like are HOST structs, read
+ * before the call returns.  Errors: CONQUR_EINVAL (nothing was enqueued), CONQUR_EHIP.                                    */
+
+/* Rows of several heads: entry e of head h of token t lies at data + t * token_stride + h * head_stride + e, in elements of the
+ * call's dtype.  Inputs may have any strides from 0 (one row for all) to below 2^40; an output's rows must not overlap (an
+ * output may be its own input).  heads = 0: absent, the rest is ignored.  A base and strides that are multiples of 16 bytes are the fast case; any
+ * multiple of the element's size is allowed.                                                                            */
+typedef struct {
+  void* data;
+  int64_t token_stride;
+  int64_t head_stride;
+  uint64_t heads;
+} conqur_heads;
+
+/* Which entries of a head's rotated part form pair j: (j, j + part/2), or (2j, 2j + 1). */
+typedef enum { CONQUR_HALF = 0, CONQUR_INTERLEAVED = 1 } conqur_rotary_layout;
+
+/* How the frequencies theta^(-2j/part) are stretched by `factor` for contexts longer than the trained one:
+ *   LINEAR  all divided by factor
+ *   BASE    theta is replaced by theta * factor^(part / (part - 2)): the lowest is divided by factor, the highest kept
+ *   BANDS   pairs that make more than `high` turns within `context` tokens are kept, those that make fewer than `low` are divided by
+ *           factor, and between them the share kept is linear in the number of turns
+ *   RAMP    as BANDS, but the share kept is linear in the number of the pair, between the (rounded) pairs that make `high` and
+ *           `low` turns; the result is multiplied by 0.1 ln(factor) + 1 (queries and keys alike)                          */
+typedef enum {
+  CONQUR_SCALE_NONE = 0,
+  CONQUR_SCALE_LINEAR = 1,
+  CONQUR_SCALE_BASE = 2,
+  CONQUR_SCALE_BANDS = 3,
+  CONQUR_SCALE_RAMP = 4
+} conqur_rotary_scaling;
+
+/*
+ * The frequencies of a rotary plan, computed on the HOST: turns_host (HOST, part/2 doubles) receives the turns (angle / 2 pi) that
+ * one position adds to each pair, magnitude_host (HOST) the factor on the rotated entries.  part: even, 2 to 512.  theta > 1;
+ * factor >= 1 (ignored for NONE); 0 < low < high and context > 0 for BANDS and RAMP (ignored otherwise); BASE needs part >= 4.
+ */
+conqur_status conqur_rotary_frequencies(uint32_t part, uint32_t scaling, double theta, double factor, double low, double high, double context,
+                                        double* turns_host, float* magnitude_host);
+
+typedef struct {
+  conqur_heads q, k;            /* queries and keys, [tokens][heads][width]; either may be absent                        */
+  conqur_heads q_out, k_out;    /* results, the same numbers of heads                                                     */
+  conqur_heads q_grad, k_grad;  /* conqur_qk_norm_rotary_backward only: gradients of the results                          */
+  const void* q_weight;         /* norms only: `width` weights of the queries' norm, in the call's dtype                  */
+  const void* k_weight;         /* ... of the keys'                                                                       */
+  const int64_t* positions;     /* one per token, any value whose product with a frequency a double holds to 2^-24 turns  */
+  const double* turns;          /* part/2 frequencies as conqur_rotary_frequencies gives them                             */
+  uint64_t tokens;              /* below 2^31; 0: nothing is done                                                         */
+  uint32_t width;               /* entries of a head, even, 2 to 512                                                      */
+  uint32_t part;                /* entries that are rotated, the first of a head: even, 2 to width; the others are copied */
+  uint32_t layout;              /* conqur_rotary_layout                                                                   */
+  uint32_t dtype;               /* conqur_dtype of the rows and the weights                                               */
+  uint32_t transposed;          /* 1 (conqur_rotary only): the transposed rotation, which takes gradients back            */
+  float magnitude;              /* factor on the rotated entries                                                          */
+  float eps;                    /* norms only, >= 0                                                                       */
+  uint32_t reserved;
+} conqur_rotary_call;
+
+/*
+ * Rotary positions: y_a = m (x_a cos t - x_b sin t), y_b = m (x_b cos t + x_a sin t) for every pair (a, b), t = position *
+ * frequency (whole turns are dropped in 64 bits, so that far positions keep 32-bit angles).  32-bit arithmetic, one rounding.
+ */
+conqur_status conqur_rotary(const conqur_rotary_call* call, void* stream);
+
+/*
+ * Norms of queries and keys over each head, and the rotation, in one pass: y = rotary(w x / sqrt(mean x^2 + eps)), 32-bit arithmetic,
+ * one rounding at the end.  With eps = 0 a row of zeros gives NaN.
+ */
+conqur_status conqur_qk_norm_rotary(const conqur_rotary_call* call, void* stream);
+
+/*
+ * Its gradients: q, k are the inputs of the forward call, q_grad, k_grad the gradients of its results, q_out, k_out receive the gradients
+ * of q and k (an out may be the grad or the input itself), q_weight_grad and k_weight_grad (`width` floats each, overwritten) those
+ * of the weights, summed over tokens and heads in 32 bits in an order that depends on the sizes alone.  workspace: 16-byte aligned,
+ * at least conqur_qk_norm_rotary_workspace(width) bytes; its content does not matter.  Calls that overlap in time need one each.
+ */
+uint64_t conqur_qk_norm_rotary_workspace(uint32_t width);
+conqur_status conqur_qk_norm_rotary_backward(const conqur_rotary_call* call, float* q_weight_grad, float* k_weight_grad, void* workspace,
+                                             uint64_t workspace_bytes, void* stream);
+
+/*
+ * A paged cache of keys and values.  Page p, head h, slot t, entry e:
+ *   bits 16  k: bf16 [pages][heads][page_tokens][width]      v: bf16 [pages][heads][width][page_tokens]
+ *   bits 8   k: one byte [pages][heads][page_tokens][width]  v: one byte [pages][heads][width][page_tokens]
+ *   bits 4   k: [pages][heads][page_tokens][width/2], v: [pages][heads][width/2][page_tokens]; byte j holds the codes of entries j (low
+ *            half) and j + width/2 (high half)
+ * Values lie with the tokens side by side because attention contracts over tokens.  With codes, k_scale and v_scale hold two floats
+ * { step, offset } for [pages][heads][page_tokens]: the value is step * code + offset.  One range per token and head, by the zero-point
+ * quantiser of conqur_quant_error_zp over the head's entries (ratio 1): step = (hi - lo) / (2^bits - 1), code = clamp(rint(y / step) + zeta),
+ * zeta = -rint(lo / step), offset = -step * zeta; a constant row has step 0, code 0 and offset lo.  All pools 16-byte aligned.
+ * A sequence's token i lies in slot i % page_tokens of page table[i / page_tokens].  A table entry outside [0, pages) names no
+ * page: tokens there are not written and not seen.
+ */
+typedef struct {
+  void* k;
+  void* v;
+  float* k_scale;        /* NULL for bits 16 */
+  float* v_scale;
+  uint64_t pages;        /* below 2^31 */
+  uint32_t heads;        /* up to 65535 */
+  uint32_t width;        /* 64 or 128 */
+  uint32_t page_tokens;  /* a power of two, 16 to 256 */
+  uint32_t bits;         /* 16, 8 or 4 */
+} conqur_cache;
+
+/* New tokens of several sequences, packed: sequence b's are [start[b], start[b + 1]) of the call's rows and become the tokens prefix[b],
+ * prefix[b] + 1, ... of that sequence.  Entries are clamped to [0, tokens]; a negative count means none; tokens beyond the table's
+ * row (table_columns * page_tokens) are dropped.                                                                        */
+typedef struct {
+  const int32_t* start;      /* sequences + 1 */
+  const int32_t* prefix;     /* sequences: tokens committed already, >= 0 */
+  const int32_t* table;      /* [sequences][table_stride], the first table_columns of a row used */
+  int64_t table_stride;
+  uint32_t table_columns;
+  uint32_t sequences;        /* 1 to 65535 */
+} conqur_batch;
+
+typedef struct {
+  conqur_cache cache;
+  conqur_batch batch;
+  conqur_heads k, v;                /* bf16, [tokens][cache.heads][width] */
+  conqur_heads k_values, v_values;  /* optional (heads 0: not wanted; codes only): what the cache holds of them, rounded to bf16 */
+  uint64_t tokens;                  /* rows of k and v, below 2^31; 0: nothing is done */
+} conqur_append_call;
+
+/*
+ * Put new keys and values into the cache, and optionally write out the values that it holds of them (what a quantisation-aware stream goes
+ * on with, Sec. 3.4).  Tokens of no sequence leave their rows of k_values / v_values as they are.  A row with a NaN or an infinity gives
+ * unspecified codes for that row.  Two sequences must not share a page that either appends to.
+ */
+conqur_status conqur_cache_append(const conqur_append_call* call, void* stream);
+
+typedef struct {
+  conqur_cache cache;
+  conqur_batch batch;
+  conqur_heads q, out;       /* bf16, [tokens][heads][width]; heads a multiple of cache.heads, at most 64 times it: query head j reads
+                                head j / (heads / cache.heads) of the cache.  out may be q                                */
+  const uint64_t* mask;      /* one per token: bit j is set if the token sees new token j of its sequence.  NULL: a chain, every token sees
+                                itself and those before it                                                                */
+  uint64_t tokens;           /* rows of q, below 2^31; 0: nothing is done */
+  uint64_t max_context;      /* largest prefix + count of a sequence (at most table_columns * page_tokens is used); tokens of a
+                                sequence beyond it are not seen                                                           */
+  void* workspace;           /* 16-byte aligned, conqur_tree_attention_workspace bytes; its content does not matter.  Calls that overlap
+                                in time need one each                                                                     */
+  uint64_t workspace_bytes;
+  uint32_t max_query;        /* largest count of new tokens of a sequence, 1 to 64; tokens beyond it get no result (their rows of
+                                `out` stay as they are)                                                                   */
+  float scale;               /* on the scores, finite */
+} conqur_tree_call;
+
+/*
+ * Attention of new tokens over a cache that holds them already (conqur_cache_append first): token i of a sequence sees all `prefix`
+ * committed tokens and those new ones that its mask names, for drafted tokens its ancestors in their tree and itself; one token per
+ * sequence is plain decoding.  out = sum_j p_j v_j / sum_j p_j, p_j = exp(scale (q k_j - max)), over the tokens seen; what is not
+ * seen has no influence, whatever it holds.  A token that sees nothing, or whose every score is -inf, gets zeros.  Scores, maxima, sums and
+ * results in 32 bits; the weights p (times the step, with codes) are rounded to bf16 as factors of the second product.
+ */
+uint64_t conqur_tree_attention_workspace(const conqur_tree_call* call);
+conqur_status conqur_tree_attention(const conqur_tree_call* call, void* stream);
+
 /* Device times (ms) of the most recent call of each kind, measured with HIP events on the
  * context's stream.  level 0: off.  level 1: one event pair around each whole call (what a
  * caller's pipeline sees: the call's kernels run back to back).  level 2: additionally one

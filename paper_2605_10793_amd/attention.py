@@ -1,0 +1,240 @@
+"""The attention layer around the calibrated heads, over libconqur.so (the C ABI declared in include/conqur.h).
+
+Argument marshalling only, like `binding`: every step runs in the library's HIP kernels, PyTorch supplies device memory and
+the stream (the current one of the tensors' device).  Nothing synchronises, nothing falls back to the CPU.
+
+  Rotary                              the plan of a rotary position encoding (frequencies on the device)
+  rotary                              positions into queries and keys, or back out of their gradients
+  qk_norm_rotary, .._backward         per-head norms and positions in one pass, and that pass's gradients
+  KVCache, append                     a paged cache of keys and values in bf16 or in 8- or 4-bit zero-point codes
+  tree_attention                      attention of new tokens (a tree of drafted ones, a chain, a single one) over the cache
+
+Rows are [tokens, heads, width] tensors of any token and head stride, e.g. slices of a fused projection's output.
+"""
+from __future__ import annotations
+
+import ctypes
+import struct
+from typing import Optional, Tuple
+
+import torch
+
+from . import binding
+
+SCALINGS = {"none": 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
+
+# The HOST structs of the header, field by field (conqur_heads: pointer, two strides, heads).
+_HEADS = "QqqQ"
+_ROTARY = struct.Struct("=" + 6 * _HEADS + "QQQQ" + "Q" + "IIIII" + "ff" + "I")
+_CACHE_BATCH = "QQQQQIIII" + "QQQqII"
+_APPEND = struct.Struct("=" + _CACHE_BATCH + 4 * _HEADS + "Q")
+_TREE = struct.Struct("=" + _CACHE_BATCH + 2 * _HEADS + "QQQQQ" + "If")
+_ABSENT = (0, 0, 0, 0)
+
+
+def _check(status: int, what: str) -> None:
+    if status != binding.OK:
+        raise binding.ConqurError(status, f"{what} failed")
+
+
+def _rows(x, name: str, dtype=None) -> Tuple[int, int, int, int]:
+    if x.dim() != 3 or x.stride(2) != 1 or not x.is_cuda or (dtype is not None and x.dtype != dtype):
+        raise ValueError(f"{name} must be a [tokens, heads, width] device tensor{'' if dtype is None else f' of {dtype}'} with unit stride along the width")
+    ts, hs, _ = x.stride()
+    return x.data_ptr(), ts, hs, x.shape[1]
+
+
+def _vector(x, name: str, dtype, n: Optional[int] = None) -> int:
+    if x.dtype != dtype or not x.is_cuda or not x.is_contiguous() or (n is not None and x.numel() != n):
+        raise ValueError(f"{name} must be a contiguous {dtype} device tensor" + ("" if n is None else f" of {n} entries"))
+    return x.data_ptr()
+
+
+class _On:
+    """The tensors' device made current for a call, where it is not already."""
+
+    def __init__(self, device):
+        self.index = device.index
+        self.back = torch.cuda.current_device()
+
+    def __enter__(self):
+        if self.index != self.back:
+            torch.cuda.set_device(self.index)
+        return torch.cuda.current_stream(self.index).cuda_stream
+
+    def __exit__(self, *exc):
+        if self.index != self.back:
+            torch.cuda.set_device(self.back)
+
+
+class Rotary:
+    """Frequencies of a rotary position encoding over the first `part` entries of a head.  interleaved: pairs (2j, 2j + 1) instead of
+    (j, j + part/2).  scaling: "none", "linear", "base", "bands" or "ramp", for contexts `factor` times the trained `context`
+    (conqur_rotary_scaling in the header says what `low` and `high` are)."""
+
+    def __init__(self, part: int, theta: float = 10000.0, interleaved: bool = False, scaling: str = "none", factor: float = 1.0, low: float = 1.0,
+                 high: float = 4.0, context: float = 8192.0, device: str = "cuda:0"):
+        if scaling not in SCALINGS:
+            raise ValueError(f"scaling must be one of {sorted(SCALINGS)}")
+        turns = torch.empty(max(part // 2, 1), dtype=torch.float64)
+        magnitude = ctypes.c_float()
+        _check(binding.load().conqur_rotary_frequencies(part, SCALINGS[scaling], theta, factor, low, high, context, turns.data_ptr(),
+                                                        ctypes.byref(magnitude)), "conqur_rotary_frequencies")
+        self.part, self.layout, self.magnitude = part, 1 if interleaved else 0, magnitude.value
+        self.turns = turns.to(device)
+
+
+def _rotary_call(plan, q, k, positions, q_out, k_out, q_grad=None, k_grad=None, q_weight=None, k_weight=None, transposed=0, eps=0.0) -> bytes:
+    dtype, tokens, width = q.dtype, q.shape[0], q.shape[2]
+    if dtype is not torch.bfloat16 and dtype is not torch.float32:
+        raise ValueError("queries and keys must be bf16 or fp32")
+
+    def rows(x, name, like):
+        if x is None:
+            return _ABSENT
+        if x.shape[0] != tokens or x.shape[2] != width or (like is not None and x.shape[1] != like.shape[1]):
+            raise ValueError(f"{name} must hold {tokens} tokens of heads of width {width}, as many as its input")
+        return _rows(x, name, dtype)
+
+    def weight(w, name):
+        return 0 if w is None else _vector(w, name, dtype, width)
+
+    return _ROTARY.pack(*rows(q, "q", None), *rows(k, "k", None), *rows(q_out, "the result of q", q), *rows(k_out, "the result of k", k),
+                        *rows(q_grad, "the gradient of q", q), *rows(k_grad, "the gradient of k", k), weight(q_weight, "q_weight"),
+                        weight(k_weight, "k_weight"), _vector(positions, "positions", torch.int64, tokens), plan.turns.data_ptr(), tokens, width, plan.part,
+                        plan.layout, 1 if dtype is torch.bfloat16 else 0, transposed, plan.magnitude, eps, 0)
+
+
+def _like(x):
+    return None if x is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+
+
+def rotary(plan: Rotary, q, positions, k=None, out=None, k_out=None, transposed: bool = False):
+    """Queries (and keys) rotated by their positions (int64, one per token), into new tensors unless `out` / `k_out` are given (they may
+    be the inputs).  transposed: the transposed rotation, for gradients.  Returns the result of q, or of (q, k)."""
+    out = _like(q) if out is None else out
+    k_out = _like(k) if k_out is None else k_out
+    call = _rotary_call(plan, q, k, positions, out, k_out, transposed=1 if transposed else 0)
+    with _On(q.device) as stream:
+        _check(binding.load().conqur_rotary(call, stream), "conqur_rotary")
+    return out if k is None else (out, k_out)
+
+
+def qk_norm_rotary(plan: Rotary, q, k, q_weight, k_weight, positions, eps: float = 1e-6, out=None, k_out=None):
+    """rotary(w x / sqrt(mean x^2 + eps)) of queries and keys; returns (q, k)."""
+    out = _like(q) if out is None else out
+    k_out = _like(k) if k_out is None else k_out
+    call = _rotary_call(plan, q, k, positions, out, k_out, q_weight=q_weight, k_weight=k_weight, eps=eps)
+    with _On(q.device) as stream:
+        _check(binding.load().conqur_qk_norm_rotary(call, stream), "conqur_qk_norm_rotary")
+    return out, k_out
+
+
+def qk_norm_rotary_backward(plan: Rotary, q, k, q_weight, k_weight, positions, q_grad, k_grad, eps: float = 1e-6):
+    """Gradients of qk_norm_rotary at inputs q, k, for the gradients q_grad, k_grad of its results: (of q, of k, of q_weight, of k_weight), the
+    last two in fp32."""
+    lib = binding.load()
+    dq, dk = _like(q), _like(k)
+    width = q.shape[2]
+    dw = torch.empty((2, width), dtype=torch.float32, device=q.device)
+    size = lib.conqur_qk_norm_rotary_workspace(width)
+    workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
+    call = _rotary_call(plan, q, k, positions, dq, dk, q_grad, k_grad, q_weight, k_weight, eps=eps)
+    with _On(q.device) as stream:
+        _check(lib.conqur_qk_norm_rotary_backward(call, dw.data_ptr(), dw.data_ptr() + 4 * width, workspace.data_ptr(), size, stream),
+               "conqur_qk_norm_rotary_backward")
+    return dq, dk, dw[0], dw[1]
+
+
+class KVCache:
+    """A pool of pages.  bits 16: k [pages, heads, page_tokens, width] and v [pages, heads, width, page_tokens] in bf16; bits 8: uint8 codes in
+    the same layout; bits 4: two codes a byte, width/2 bytes in place of width.  Codes have k_scale and v_scale [pages, heads, page_tokens,
+    2] in fp32, (step, offset) of every token.  page_tokens: a power of two, 16 to 256; width 64 or 128.  `empty` allocates one.
+    The workspace that tree_attention needs is kept here, one for each stream it is called on."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None, bits: int = 16):
+        if bits not in (16, 8, 4):
+            raise ValueError("bits must be 16, 8 or 4")
+        dtype = torch.bfloat16 if bits == 16 else torch.uint8
+        if k.dim() != 4 or not k.is_cuda or k.dtype != dtype or not k.is_contiguous():
+            raise ValueError(f"k must be a contiguous 4-D device tensor of {dtype}")
+        pages, heads, page_tokens, n = k.shape
+        if tuple(v.shape) != (pages, heads, n, page_tokens) or v.dtype != dtype or v.device != k.device or not v.is_contiguous():
+            raise ValueError("k must be [pages, heads, page_tokens, n] and v [pages, heads, n, page_tokens], contiguous, of one type and device")
+        for s in (k_scale, v_scale):
+            if bits == 16:
+                if s is not None:
+                    raise ValueError("a bf16 cache has no scales")
+            elif s is None or s.dtype != torch.float32 or tuple(s.shape) != (pages, heads, page_tokens, 2) or s.device != k.device or not s.is_contiguous():
+                raise ValueError("codes need contiguous fp32 k_scale and v_scale [pages, heads, page_tokens, 2]")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.pages, self.heads, self.page_tokens, self.bits = pages, heads, page_tokens, bits
+        self.width = n * 2 if bits == 4 else n
+        self._fields = (k.data_ptr(), v.data_ptr(), 0 if k_scale is None else k_scale.data_ptr(), 0 if v_scale is None else v_scale.data_ptr(),
+                        pages, heads, self.width, page_tokens, bits)
+        self._workspace = {}
+
+    @classmethod
+    def empty(cls, pages: int, heads: int, page_tokens: int, width: int, bits: int = 16, device: str = "cuda:0") -> "KVCache":
+        n, dtype = (width // 2, torch.uint8) if bits == 4 else (width, torch.uint8 if bits == 8 else torch.bfloat16)
+        k = torch.empty((pages, heads, page_tokens, n), dtype=dtype, device=device)
+        v = torch.empty((pages, heads, n, page_tokens), dtype=dtype, device=device)
+        scales = [None if bits == 16 else torch.empty((pages, heads, page_tokens, 2), dtype=torch.float32, device=device) for _ in range(2)]
+        return cls(k, v, *scales, bits=bits)
+
+
+def _batch(start, prefix, table) -> Tuple:
+    sequences = prefix.shape[0]
+    if table.dim() != 2 or table.dtype != torch.int32 or not table.is_cuda or table.stride(1) != 1 or table.shape[0] != sequences:
+        raise ValueError("table must be a [sequences, columns] int32 device tensor with unit column stride")
+    stride = table.stride(0) if sequences > 1 else max(table.stride(0), table.shape[1])
+    return (_vector(start, "start", torch.int32, sequences + 1), _vector(prefix, "prefix", torch.int32, sequences), table.data_ptr(), stride,
+            table.shape[1], sequences)
+
+
+def append(cache: KVCache, k, v, start, prefix, table, values: bool = False, k_values=None, v_values=None):
+    """New keys and values (bf16) into the cache.  Sequence b's rows are [start[b], start[b + 1]) and become its tokens prefix[b] and on;
+    token i lies in slot i % page_tokens of page table[b, i // page_tokens] (int32 device tensors).  values (8 or 4 bits): also returns
+    what the cache holds of them, (k_values, v_values), in the given or in new bf16 tensors."""
+    tokens = k.shape[0]
+    for x, name in ((k, "k"), (v, "v"), (k_values, "k_values"), (v_values, "v_values")):
+        if x is not None and tuple(x.shape) != (tokens, cache.heads, cache.width):
+            raise ValueError(f"{name} must be [tokens, {cache.heads}, {cache.width}]")
+    if values:
+        k_values = _like(k) if k_values is None else k_values
+        v_values = _like(v) if v_values is None else v_values
+    dtype = torch.bfloat16
+    call = _APPEND.pack(*cache._fields, *_batch(start, prefix, table), *_rows(k, "k", dtype), *_rows(v, "v", dtype),
+                        *(_ABSENT if k_values is None else _rows(k_values, "k_values", dtype)),
+                        *(_ABSENT if v_values is None else _rows(v_values, "v_values", dtype)), tokens)
+    with _On(k.device) as stream:
+        _check(binding.load().conqur_cache_append(call, stream), "conqur_cache_append")
+    return (k_values, v_values) if values else None
+
+
+def tree_attention(q, cache: KVCache, start, prefix, table, mask=None, max_query: int = 64, max_context: Optional[int] = None,
+                   scale: Optional[float] = None, out=None):
+    """Attention of new tokens q (bf16 [tokens, heads, width]; packed as in `append`, which has put their keys and values into the cache) over
+    the committed tokens and those new ones that mask (int64, bit j: new token j of the sequence) names; None: each sees itself and those
+    before it.  max_query: most new tokens of a sequence (up to 64); max_context: most tokens, committed and new (default: what the table
+    holds; a closer bound shares the work out better).  scale: 1 / sqrt(width) unless given.  Returns out."""
+    tokens, heads, width = q.shape
+    if width != cache.width:
+        raise ValueError(f"q must be [tokens, heads, {cache.width}]")
+    out = _like(q) if out is None else out
+    if out.shape != q.shape:
+        raise ValueError("out must have the shape of q")
+    dtype = torch.bfloat16
+    fields = (*cache._fields, *_batch(start, prefix, table), *_rows(q, "q", dtype), *_rows(out, "out", dtype),
+              0 if mask is None else _vector(mask, "mask", torch.int64, tokens), tokens,
+              table.shape[1] * cache.page_tokens if max_context is None else max_context)
+    scale = width ** -0.5 if scale is None else scale
+    lib = binding.load()
+    with _On(q.device) as stream:
+        size = lib.conqur_tree_attention_workspace(_TREE.pack(*fields, 0, 0, max_query, scale))
+        workspace = cache._workspace.get(stream)
+        if size and (workspace is None or workspace.numel() < size):
+            workspace = cache._workspace[stream] = torch.empty(size, dtype=torch.uint8, device=q.device)
+        call = _TREE.pack(*fields, workspace.data_ptr() if size else 0, size, max_query, scale)
+        _check(lib.conqur_tree_attention(call, stream), "conqur_tree_attention")
+    return out

@@ -24,7 +24,8 @@ F32, BF16 = 0, 1
 EXPORTS = [
     "conqur_init", "conqur_step_batch", "conqur_step_batch_heads", "conqur_step_batch_quant", "conqur_get_batch_stats", "conqur_update_rotation",
     "conqur_quant_error", "conqur_quant_error_zp", "conqur_rotate", "conqur_rotate_quant", "conqur_row_diagnostics", "conqur_get_state", "conqur_set_state", "conqur_get_last_corners",
-    "conqur_score_rows_static", "conqur_set_taps", "conqur_set_timing", "conqur_get_timing", "conqur_get_clock_probe", "conqur_last_error", "conqur_destroy", "conqur_version",
+    "conqur_score_rows_static", "conqur_rotary_frequencies", "conqur_rotary", "conqur_qk_norm_rotary", "conqur_qk_norm_rotary_workspace", "conqur_qk_norm_rotary_backward",
+    "conqur_cache_append", "conqur_tree_attention_workspace", "conqur_tree_attention", "conqur_set_taps", "conqur_set_timing", "conqur_get_timing", "conqur_get_clock_probe", "conqur_last_error", "conqur_destroy", "conqur_version",
 ]
 
 
@@ -99,6 +100,18 @@ def load() -> ctypes.CDLL:
         L.conqur_get_last_corners.argtypes = [vp, vp, vp]
         L.conqur_score_rows_static.restype = i32
         L.conqur_score_rows_static.argtypes = [vp, u32, u64, u64, u64, u32, u32, ctypes.c_float, vp, vp]
+        f64 = ctypes.c_double
+        L.conqur_rotary_frequencies.restype = i32
+        L.conqur_rotary_frequencies.argtypes = [u32, u32, f64, f64, f64, f64, f64, vp, vp]
+        for name in ("conqur_rotary", "conqur_qk_norm_rotary", "conqur_cache_append", "conqur_tree_attention"):
+            getattr(L, name).restype = i32
+            getattr(L, name).argtypes = [vp, vp]
+        L.conqur_qk_norm_rotary_workspace.restype = u64
+        L.conqur_qk_norm_rotary_workspace.argtypes = [u32]
+        L.conqur_qk_norm_rotary_backward.restype = i32
+        L.conqur_qk_norm_rotary_backward.argtypes = [vp, vp, vp, vp, u64, vp]
+        L.conqur_tree_attention_workspace.restype = u64
+        L.conqur_tree_attention_workspace.argtypes = [vp]
         L.conqur_set_taps.restype = i32
         L.conqur_set_taps.argtypes = [vp, i32]
         L.conqur_set_timing.restype = i32

@@ -1,0 +1,319 @@
+// Appending keys and values to a paged cache of bf16 rows or of zero-point codes of 8 or 4 bits.
+//
+//   per token and head: lo, hi over the row, step = (hi - lo) / (2^b - 1), zeta = -rint(lo / step), offset = -step zeta,
+//   code = clamp(rint(y / step) + zeta, 0, 2^b - 1); value = step code + offset
+//
+// Bound by HBM: rows are read once, codes written once.  Keys lie as they come, but values lie with the tokens of a page side by
+// side (attention contracts over tokens and reads them straight into matrix operands), so a workgroup takes the tokens of one head
+// that fall into one block of 64 slots and turns them round in LDS; whole groups of 16 slots leave as 16-byte stores, the slots
+// at a batch's ragged ends one by one.  W/16 lanes hold a row, both halves' entries of a code byte in the same lane, so that packing and
+// the row's extremes stay in registers.
+#include "../../include/conqur.h"
+
+#include "kernels.h"
+
+using namespace conqur;
+
+namespace {
+
+constexpr int kBlock = 64;        // slots of a workgroup
+constexpr int kThreads = 256;
+
+struct AppendArgs {
+  conqur_cache cache;
+  conqur_batch batch;
+  const bf16_bits* in[2];
+  int64_t in_ts[2], in_hs[2];
+  bf16_bits* val[2];              // null: not wanted
+  int64_t val_ts[2], val_hs[2];
+  int64_t tokens;
+  int wide[2], val_wide[2];       // rows start at multiples of 16 bytes
+};
+
+__device__ __forceinline__ int clamp_to(int v, int64_t hi) { return v < 0 ? 0 : v > hi ? (int)hi : v; }
+
+template <int CTRL>
+__device__ __forceinline__ float lane_perm(float v) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+// Over the 4 or 8 neighbouring lanes of a row.
+template <int LANES, typename Op>
+__device__ __forceinline__ float row_reduce(float v, Op op) {
+  v = op(v, lane_perm<0xB1>(v));
+  v = op(v, lane_perm<0x4E>(v));
+  if constexpr (LANES > 4) v = op(v, lane_perm<0x141>(v));
+  return v;
+}
+
+__device__ __forceinline__ void load16(const bf16_bits* p, int half, bool wide, uint32_t* u) {
+  if (wide) {
+    const uint4 a = *reinterpret_cast<const uint4*>(p), b = *reinterpret_cast<const uint4*>(p + half);
+    u[0] = a.x; u[1] = a.y; u[2] = a.z; u[3] = a.w;
+    u[4] = b.x; u[5] = b.y; u[6] = b.z; u[7] = b.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      u[i] = p[2 * i] | (uint32_t)p[2 * i + 1] << 16;
+      u[4 + i] = p[half + 2 * i] | (uint32_t)p[half + 2 * i + 1] << 16;
+    }
+  }
+}
+__device__ __forceinline__ void store16(bf16_bits* p, int half, bool wide, const uint32_t* u) {
+  if (wide) {
+    *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+    *reinterpret_cast<uint4*>(p + half) = make_uint4(u[4], u[5], u[6], u[7]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      p[2 * i] = (bf16_bits)u[i];
+      p[2 * i + 1] = (bf16_bits)(u[i] >> 16);
+      p[half + 2 * i] = (bf16_bits)u[4 + i];
+      p[half + 2 * i + 1] = (bf16_bits)(u[4 + i] >> 16);
+    }
+  }
+}
+
+// Codes of a lane's 16 entries (two runs of 8), four to a word, and the row's pair; every operation rounds on its own, as the
+// definition has it.
+template <int BITS, int LANES>
+__device__ __forceinline__ void quantise(const uint32_t* u, uint32_t* code, float2* pair, uint32_t* values) {
+#pragma clang fp contract(off)
+  float y[16];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) { y[2 * i] = __uint_as_float(u[i] << 16); y[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
+  float lo = y[0], hi = y[0];
+#pragma unroll
+  for (int i = 1; i < 16; ++i) { lo = fminf(lo, y[i]); hi = fmaxf(hi, y[i]); }
+  lo = row_reduce<LANES>(lo, [](float a, float b) { return fminf(a, b); });
+  hi = row_reduce<LANES>(hi, [](float a, float b) { return fmaxf(a, b); });
+  constexpr float kTop = (float)((1 << BITS) - 1);
+  const float step = (hi - lo) / kTop;
+  const bool flat = step == 0.0f;
+  const float safe = flat ? 1.0f : step;
+  const float zeta = -rintf(lo / safe);
+  const float offset = flat ? lo : -(step * zeta);
+  *pair = make_float2(step, offset);
+  float q[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const float c = fminf(fmaxf(rintf(y[i] / safe) + zeta, 0.0f), kTop);
+    q[i] = flat ? 0.0f : c;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    code[i] = (uint32_t)q[4 * i] | (uint32_t)q[4 * i + 1] << 8 | (uint32_t)q[4 * i + 2] << 16 | (uint32_t)q[4 * i + 3] << 24;
+  if (values) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float a = step * q[2 * i], b = step * q[2 * i + 1];
+      values[i] = f32x2_to_bf16x2(a + offset, b + offset);
+    }
+  }
+}
+
+template <int BITS, int W>
+__global__ void __launch_bounds__(kThreads) k_append(const AppendArgs a) {
+  constexpr int kLanes = W / 16;                                   // lanes of a row
+  constexpr int kRows = kThreads / kLanes;                         // rows at a time
+  constexpr int kBytes = BITS == 16 ? 2 * W : W * BITS / 8;        // bytes of a row in the cache
+  constexpr int kPitch = kBytes + 4;                               // in LDS
+  __shared__ __attribute__((aligned(16))) unsigned char s_v[kBlock * kPitch];
+
+  // The block's sequence: blocks start[b] / 64 + 2b and on are b's, enough for every count and place (a sequence of n tokens
+  // touches at most n / 64 + 2 blocks of slots).
+  const int64_t id = blockIdx.x;
+  const int head = blockIdx.y;
+  int b = 0;
+  for (int lo = 0, hi = (int)a.batch.sequences - 1; lo <= hi;) {
+    const int mid = (lo + hi) / 2;
+    if (clamp_to(a.batch.start[mid], a.tokens) / kBlock + 2 * (int64_t)mid <= id) {
+      b = mid;
+      lo = mid + 1;
+    } else {
+      hi = mid - 1;
+    }
+  }
+  const int64_t first = clamp_to(a.batch.start[b], a.tokens);
+  const int64_t count = clamp_to(a.batch.start[b + 1], a.tokens) - first;
+  const int64_t prefix = a.batch.prefix[b] < 0 ? 0 : a.batch.prefix[b];
+  const int page_tokens = (int)a.cache.page_tokens;
+  const int64_t room = (int64_t)a.batch.table_columns * page_tokens;
+  const int64_t end = prefix + count < room ? prefix + count : room;
+  const int64_t k = id - (first / kBlock + 2 * (int64_t)b);
+  const int64_t base = (prefix / kBlock + k) * kBlock;             // first slot of the block, as a token number of the sequence
+  if (base >= end || k < 0 || base + kBlock <= prefix) return;
+  const int32_t* table = a.batch.table + (int64_t)b * a.batch.table_stride;
+  const int64_t heads = a.cache.heads;
+
+  const int lane = threadIdx.x % kLanes, row0 = threadIdx.x / kLanes;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    for (int r = row0; r < kBlock; r += kRows) {
+      const int64_t pos = base + r;
+      if (pos < prefix || pos >= end) continue;
+      const int32_t page = table[pos / page_tokens];
+      if (page < 0 || (uint64_t)page >= a.cache.pages) continue;
+      const int64_t token = first + pos - prefix;
+      const int64_t at = ((int64_t)page * heads + head) * page_tokens + pos % page_tokens;
+      uint32_t u[8];
+      load16(a.in[which] + token * a.in_ts[which] + head * a.in_hs[which] + 8 * lane, W / 2, a.wide[which], u);
+      if constexpr (BITS == 16) {
+        if (which == 0) {
+          store16(static_cast<bf16_bits*>(a.cache.k) + at * W + 8 * lane, W / 2, true, u);
+        } else {
+          uint32_t* s = reinterpret_cast<uint32_t*>(s_v + r * kPitch);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) { s[4 * lane + i] = u[i]; s[W / 4 + 4 * lane + i] = u[4 + i]; }
+        }
+      } else {
+        uint32_t code[4], values[8];
+        float2 pair;
+        const bool emit = a.val[which] != nullptr;
+        quantise<BITS, kLanes>(u, code, &pair, values);
+        if (emit) store16(a.val[which] + token * a.val_ts[which] + head * a.val_hs[which] + 8 * lane, W / 2, a.val_wide[which], values);
+        if (lane == 0) reinterpret_cast<float2*>(which ? a.cache.v_scale : a.cache.k_scale)[at] = pair;
+        uint32_t* s = reinterpret_cast<uint32_t*>(s_v + r * kPitch);
+        if constexpr (BITS == 4) {
+          const uint32_t x = code[0] | code[2] << 4, y = code[1] | code[3] << 4;
+          if (which == 0) {
+            *reinterpret_cast<uint2*>(static_cast<unsigned char*>(a.cache.k) + at * (W / 2) + 8 * lane) = make_uint2(x, y);
+          } else {
+            s[2 * lane] = x;
+            s[2 * lane + 1] = y;
+          }
+        } else {
+          if (which == 0) {
+            unsigned char* p = static_cast<unsigned char*>(a.cache.k) + at * W + 8 * lane;
+            *reinterpret_cast<uint2*>(p) = make_uint2(code[0], code[1]);
+            *reinterpret_cast<uint2*>(p + W / 2) = make_uint2(code[2], code[3]);
+          } else {
+            s[2 * lane] = code[0];
+            s[2 * lane + 1] = code[1];
+            s[W / 8 + 2 * lane] = code[2];
+            s[W / 8 + 2 * lane + 1] = code[3];
+          }
+        }
+      }
+    }
+  }
+  __syncthreads();
+
+  // Values: row d of the page holds byte (bf16: entry) d of every token; a unit is 16 slots of one row.
+  constexpr int kSize = BITS == 16 ? 2 : 1;
+  constexpr int kOut = kBytes / kSize;
+  for (int u = threadIdx.x; u < kOut * (kBlock / 16); u += kThreads) {
+    const int d = u / (kBlock / 16), group = u % (kBlock / 16);
+    const int64_t pos = base + group * 16;
+    if (pos + 16 <= prefix || pos >= end) continue;
+    const int32_t page = table[pos / page_tokens];
+    if (page < 0 || (uint64_t)page >= a.cache.pages) continue;
+    unsigned char* out = static_cast<unsigned char*>(a.cache.v) +
+                         ((((int64_t)page * heads + head) * kOut + d) * page_tokens + pos % page_tokens) * kSize;
+    const unsigned char* s = s_v + group * 16 * kPitch + d * kSize;
+    if (pos >= prefix && pos + 16 <= end) {
+      uint32_t w[4 * kSize];
+      if constexpr (BITS == 16) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          w[i] = *reinterpret_cast<const bf16_bits*>(s + 2 * i * kPitch) | (uint32_t)*reinterpret_cast<const bf16_bits*>(s + (2 * i + 1) * kPitch) << 16;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          w[i] = s[4 * i * kPitch] | (uint32_t)s[(4 * i + 1) * kPitch] << 8 | (uint32_t)s[(4 * i + 2) * kPitch] << 16 |
+                 (uint32_t)s[(4 * i + 3) * kPitch] << 24;
+      }
+#pragma unroll
+      for (int i = 0; i < kSize; ++i) reinterpret_cast<uint4*>(out)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    } else {
+      for (int i = 0; i < 16; ++i) {
+        if (pos + i < prefix || pos + i >= end) continue;
+        if constexpr (BITS == 16)
+          reinterpret_cast<bf16_bits*>(out)[i] = *reinterpret_cast<const bf16_bits*>(s + i * kPitch);
+        else
+          out[i] = s[i * kPitch];
+      }
+    }
+  }
+}
+
+constexpr int64_t kMaxStride = 1ll << 40;
+
+bool strides_fine(const conqur_heads& h, uint32_t width, uint64_t tokens, bool output) {
+  if (!h.data || reinterpret_cast<uintptr_t>(h.data) % 2) return false;
+  if (h.token_stride < 0 || h.token_stride >= kMaxStride || h.head_stride < 0 || h.head_stride >= kMaxStride) return false;
+  if (!output) return true;
+  const __int128 w = width, ts = h.token_stride, hs = h.head_stride, heads = h.heads, n = tokens;
+  if ((heads > 1 && hs < w) || (n > 1 && ts < w)) return false;
+  return !(heads > 1 && n > 1 && ts < (heads - 1) * hs + w && hs < (n - 1) * ts + w);
+}
+
+bool is_wide(const conqur_heads& h) {
+  return reinterpret_cast<uintptr_t>(h.data) % 16 == 0 && h.token_stride % 8 == 0 && h.head_stride % 8 == 0;
+}
+
+template <int BITS>
+void launch_width(const AppendArgs& a, dim3 grid, hipStream_t s) {
+  if (a.cache.width == 128)
+    k_append<BITS, 128><<<grid, kThreads, 0, s>>>(a);
+  else
+    k_append<BITS, 64><<<grid, kThreads, 0, s>>>(a);
+}
+
+}  // namespace
+
+namespace conqur {
+
+bool cache_fine(const conqur_cache& c) {
+  if (c.bits != 16 && c.bits != 8 && c.bits != 4) return false;
+  if (c.width != 64 && c.width != 128) return false;
+  if (c.page_tokens < 16 || c.page_tokens > 256 || (c.page_tokens & (c.page_tokens - 1))) return false;
+  if (c.heads < 1 || c.heads > 65535 || c.pages < 1 || c.pages >= (1ull << 31)) return false;
+  if (!c.k || !c.v || reinterpret_cast<uintptr_t>(c.k) % 16 || reinterpret_cast<uintptr_t>(c.v) % 16) return false;
+  if (c.bits != 16 && (!c.k_scale || !c.v_scale || reinterpret_cast<uintptr_t>(c.k_scale) % 16 || reinterpret_cast<uintptr_t>(c.v_scale) % 16)) return false;
+  return true;
+}
+
+bool batch_fine(const conqur_batch& b) {
+  if (!b.start || !b.prefix || !b.table) return false;
+  if ((reinterpret_cast<uintptr_t>(b.start) | reinterpret_cast<uintptr_t>(b.prefix) | reinterpret_cast<uintptr_t>(b.table)) % 4) return false;
+  if (b.sequences < 1 || b.sequences > 65535 || b.table_columns < 1 || b.table_columns >= (1u << 31)) return false;
+  return b.table_stride >= (int64_t)b.table_columns && b.table_stride < kMaxStride;
+}
+
+}  // namespace conqur
+
+extern "C" conqur_status conqur_cache_append(const conqur_append_call* c, void* stream) {
+  if (!c || !cache_fine(c->cache) || !batch_fine(c->batch) || c->tokens >= (1ull << 31)) return CONQUR_EINVAL;
+  if (c->tokens == 0) return CONQUR_OK;
+  AppendArgs a;
+  a.cache = c->cache;
+  a.batch = c->batch;
+  a.tokens = (int64_t)c->tokens;
+  const conqur_heads* in[2] = {&c->k, &c->v};
+  const conqur_heads* val[2] = {&c->k_values, &c->v_values};
+  for (int i = 0; i < 2; ++i) {
+    if (in[i]->heads != c->cache.heads || !strides_fine(*in[i], c->cache.width, c->tokens, false)) return CONQUR_EINVAL;
+    a.in[i] = static_cast<const bf16_bits*>(in[i]->data);
+    a.in_ts[i] = in[i]->token_stride;
+    a.in_hs[i] = in[i]->head_stride;
+    a.wide[i] = is_wide(*in[i]);
+    a.val[i] = nullptr;
+    a.val_ts[i] = a.val_hs[i] = 0;
+    a.val_wide[i] = 0;
+    if (!val[i]->heads) continue;
+    if (c->cache.bits == 16 || val[i]->heads != c->cache.heads || !strides_fine(*val[i], c->cache.width, c->tokens, true)) return CONQUR_EINVAL;
+    a.val[i] = static_cast<bf16_bits*>(val[i]->data);
+    a.val_ts[i] = val[i]->token_stride;
+    a.val_hs[i] = val[i]->head_stride;
+    a.val_wide[i] = is_wide(*val[i]);
+  }
+  const dim3 grid((uint32_t)(c->tokens / kBlock + 2 * (uint64_t)c->batch.sequences), c->cache.heads);
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  if (c->cache.bits == 16)
+    launch_width<16>(a, grid, s);
+  else if (c->cache.bits == 8)
+    launch_width<8>(a, grid, s);
+  else
+    launch_width<4>(a, grid, s);
+  return hipGetLastError() == hipSuccess ? CONQUR_OK : CONQUR_EHIP;
+}
