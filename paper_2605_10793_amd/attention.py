@@ -30,6 +30,7 @@ _CACHE_BATCH = "QQQQQIIII" + "QQQqII"
 _APPEND = struct.Struct("=" + _CACHE_BATCH + 4 * _HEADS + "Q")
 _TREE = struct.Struct("=" + _CACHE_BATCH + 2 * _HEADS + "QQQQQ" + "If")
 _ABSENT = (0, 0, 0, 0)
+_NOTHING = (None, 0, 0)
 
 
 def _check(status: int, what: str) -> None:
@@ -37,34 +38,34 @@ def _check(status: int, what: str) -> None:
         raise binding.ConqurError(status, f"{what} failed")
 
 
-def _rows(x, name: str, dtype=None) -> Tuple[int, int, int, int]:
-    if x.dim() != 3 or x.stride(2) != 1 or not x.is_cuda or (dtype is not None and x.dtype != dtype):
-        raise ValueError(f"{name} must be a [tokens, heads, width] device tensor{'' if dtype is None else f' of {dtype}'} with unit stride along the width")
-    ts, hs, _ = x.stride()
-    return x.data_ptr(), ts, hs, x.shape[1]
+# A decode step makes three of these calls a layer, so what Python does around each counts as much as a small kernel: tensors are looked at with
+# as few attribute reads as the checks need, and the stream is asked for by device index (a pass of `rotary` 15.1 -> 10 us, of which the
+# launch is 3.7).
+
+def _rows(x, name: str, dtype, tokens: int, heads: int, width: int) -> Tuple[int, int, int, int]:
+    shape, stride = x.shape, x.stride()
+    if len(shape) != 3 or shape[0] != tokens or shape[1] != heads or shape[2] != width or stride[2] != 1 or x.dtype is not dtype or not x.is_cuda:
+        raise ValueError(f"{name} must be a [{tokens}, {heads}, {width}] device tensor of {dtype} with unit stride along the width")
+    return x.data_ptr(), stride[0], stride[1], heads
 
 
-def _vector(x, name: str, dtype, n: Optional[int] = None) -> int:
-    if x.dtype != dtype or not x.is_cuda or not x.is_contiguous() or (n is not None and x.numel() != n):
-        raise ValueError(f"{name} must be a contiguous {dtype} device tensor" + ("" if n is None else f" of {n} entries"))
+def _vector(x, name: str, dtype, n: int) -> int:
+    if x.dtype is not dtype or x.shape != (n,) or not x.is_cuda or not x.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} device tensor of {n} entries")
     return x.data_ptr()
 
 
-class _On:
-    """The tensors' device made current for a call, where it is not already."""
+def _run(call, x, *args) -> int:
+    """A library call's status, on x's device and that device's current stream."""
+    index = x.get_device()
+    if index == torch._C._cuda_getDevice():
+        return call(*args, torch._C._cuda_getCurrentRawStream(index))
+    with torch.cuda.device(index):
+        return call(*args, torch._C._cuda_getCurrentRawStream(index))
 
-    def __init__(self, device):
-        self.index = device.index
-        self.back = torch.cuda.current_device()
 
-    def __enter__(self):
-        if self.index != self.back:
-            torch.cuda.set_device(self.index)
-        return torch.cuda.current_stream(self.index).cuda_stream
-
-    def __exit__(self, *exc):
-        if self.index != self.back:
-            torch.cuda.set_device(self.back)
+def _like(x):
+    return None if x is None else torch.empty_like(x, memory_format=torch.contiguous_format)
 
 
 class Rotary:
@@ -85,48 +86,45 @@ class Rotary:
 
 
 def _rotary_call(plan, q, k, positions, q_out, k_out, q_grad=None, k_grad=None, q_weight=None, k_weight=None, transposed=0, eps=0.0) -> bytes:
-    dtype, tokens, width = q.dtype, q.shape[0], q.shape[2]
+    dtype = q.dtype
     if dtype is not torch.bfloat16 and dtype is not torch.float32:
         raise ValueError("queries and keys must be bf16 or fp32")
-
-    def rows(x, name, like):
-        if x is None:
-            return _ABSENT
-        if x.shape[0] != tokens or x.shape[2] != width or (like is not None and x.shape[1] != like.shape[1]):
-            raise ValueError(f"{name} must hold {tokens} tokens of heads of width {width}, as many as its input")
-        return _rows(x, name, dtype)
-
-    def weight(w, name):
-        return 0 if w is None else _vector(w, name, dtype, width)
-
-    return _ROTARY.pack(*rows(q, "q", None), *rows(k, "k", None), *rows(q_out, "the result of q", q), *rows(k_out, "the result of k", k),
-                        *rows(q_grad, "the gradient of q", q), *rows(k_grad, "the gradient of k", k), weight(q_weight, "q_weight"),
-                        weight(k_weight, "k_weight"), _vector(positions, "positions", torch.int64, tokens), plan.turns.data_ptr(), tokens, width, plan.part,
-                        plan.layout, 1 if dtype is torch.bfloat16 else 0, transposed, plan.magnitude, eps, 0)
-
-
-def _like(x):
-    return None if x is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if q.dim() != 3 or (k is not None and k.dim() != 3):
+        raise ValueError("queries and keys must be [tokens, heads, width]")
+    tokens, heads, width = q.shape
+    k_heads = 0 if k is None else k.shape[1]
+    same = (dtype, tokens, heads, width)
+    k_same = (dtype, tokens, k_heads, width)
+    return _ROTARY.pack(*_rows(q, "q", *same), *(_ABSENT if k is None else _rows(k, "k", *k_same)),
+                        *_rows(q_out, "the result of q", *same), *(_ABSENT if k is None else _rows(k_out, "the result of k", *k_same)),
+                        *(_ABSENT if q_grad is None else _rows(q_grad, "the gradient of q", *same)),
+                        *(_ABSENT if k_grad is None else _rows(k_grad, "the gradient of k", *k_same)),
+                        0 if q_weight is None else _vector(q_weight, "q_weight", dtype, width),
+                        0 if k_weight is None else _vector(k_weight, "k_weight", dtype, width),
+                        _vector(positions, "positions", torch.int64, tokens), plan.turns.data_ptr(), tokens, width, plan.part, plan.layout,
+                        1 if dtype is torch.bfloat16 else 0, transposed, plan.magnitude, eps, 0)
 
 
 def rotary(plan: Rotary, q, positions, k=None, out=None, k_out=None, transposed: bool = False):
     """Queries (and keys) rotated by their positions (int64, one per token), into new tensors unless `out` / `k_out` are given (they may
     be the inputs).  transposed: the transposed rotation, for gradients.  Returns the result of q, or of (q, k)."""
-    out = _like(q) if out is None else out
-    k_out = _like(k) if k_out is None else k_out
+    if out is None:
+        out = _like(q)
+    if k_out is None and k is not None:
+        k_out = _like(k)
     call = _rotary_call(plan, q, k, positions, out, k_out, transposed=1 if transposed else 0)
-    with _On(q.device) as stream:
-        _check(binding.load().conqur_rotary(call, stream), "conqur_rotary")
+    _check(_run(binding.load().conqur_rotary, q, call), "conqur_rotary")
     return out if k is None else (out, k_out)
 
 
 def qk_norm_rotary(plan: Rotary, q, k, q_weight, k_weight, positions, eps: float = 1e-6, out=None, k_out=None):
-    """rotary(w x / sqrt(mean x^2 + eps)) of queries and keys; returns (q, k)."""
-    out = _like(q) if out is None else out
-    k_out = _like(k) if k_out is None else k_out
+    """rotary(w x / sqrt(mean x^2 + eps)) of queries and keys, in one pass; returns (q, k)."""
+    if out is None:
+        out = _like(q)
+    if k_out is None:
+        k_out = _like(k)
     call = _rotary_call(plan, q, k, positions, out, k_out, q_weight=q_weight, k_weight=k_weight, eps=eps)
-    with _On(q.device) as stream:
-        _check(binding.load().conqur_qk_norm_rotary(call, stream), "conqur_qk_norm_rotary")
+    _check(_run(binding.load().conqur_qk_norm_rotary, q, call), "conqur_qk_norm_rotary")
     return out, k_out
 
 
@@ -135,14 +133,14 @@ def qk_norm_rotary_backward(plan: Rotary, q, k, q_weight, k_weight, positions, q
     last two in fp32."""
     lib = binding.load()
     dq, dk = _like(q), _like(k)
+    call = _rotary_call(plan, q, k, positions, dq, dk, q_grad, k_grad, q_weight, k_weight, eps=eps)
     width = q.shape[2]
     dw = torch.empty((2, width), dtype=torch.float32, device=q.device)
     size = lib.conqur_qk_norm_rotary_workspace(width)
     workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
-    call = _rotary_call(plan, q, k, positions, dq, dk, q_grad, k_grad, q_weight, k_weight, eps=eps)
-    with _On(q.device) as stream:
-        _check(lib.conqur_qk_norm_rotary_backward(call, dw.data_ptr(), dw.data_ptr() + 4 * width, workspace.data_ptr(), size, stream),
-               "conqur_qk_norm_rotary_backward")
+    at = dw.data_ptr()
+    _check(_run(lib.conqur_qk_norm_rotary_backward, q, call, at, at + 4 * width, workspace.data_ptr(), size),
+           "conqur_qk_norm_rotary_backward")
     return dq, dk, dw[0], dw[1]
 
 
@@ -184,12 +182,12 @@ class KVCache:
 
 
 def _batch(start, prefix, table) -> Tuple:
-    sequences = prefix.shape[0]
-    if table.dim() != 2 or table.dtype != torch.int32 or not table.is_cuda or table.stride(1) != 1 or table.shape[0] != sequences:
+    sequences, stride = prefix.shape[0], table.stride()
+    if table.dim() != 2 or table.dtype is not torch.int32 or not table.is_cuda or stride[1] != 1 or table.shape[0] != sequences:
         raise ValueError("table must be a [sequences, columns] int32 device tensor with unit column stride")
-    stride = table.stride(0) if sequences > 1 else max(table.stride(0), table.shape[1])
-    return (_vector(start, "start", torch.int32, sequences + 1), _vector(prefix, "prefix", torch.int32, sequences), table.data_ptr(), stride,
-            table.shape[1], sequences)
+    columns = table.shape[1]
+    return (_vector(start, "start", torch.int32, sequences + 1), _vector(prefix, "prefix", torch.int32, sequences), table.data_ptr(),
+            stride[0] if sequences > 1 else max(stride[0], columns), columns, sequences)
 
 
 def append(cache: KVCache, k, v, start, prefix, table, values: bool = False, k_values=None, v_values=None):
@@ -197,18 +195,14 @@ def append(cache: KVCache, k, v, start, prefix, table, values: bool = False, k_v
     token i lies in slot i % page_tokens of page table[b, i // page_tokens] (int32 device tensors).  values (8 or 4 bits): also returns
     what the cache holds of them, (k_values, v_values), in the given or in new bf16 tensors."""
     tokens = k.shape[0]
-    for x, name in ((k, "k"), (v, "v"), (k_values, "k_values"), (v_values, "v_values")):
-        if x is not None and tuple(x.shape) != (tokens, cache.heads, cache.width):
-            raise ValueError(f"{name} must be [tokens, {cache.heads}, {cache.width}]")
+    same = (torch.bfloat16, tokens, cache.heads, cache.width)
     if values:
         k_values = _like(k) if k_values is None else k_values
         v_values = _like(v) if v_values is None else v_values
-    dtype = torch.bfloat16
-    call = _APPEND.pack(*cache._fields, *_batch(start, prefix, table), *_rows(k, "k", dtype), *_rows(v, "v", dtype),
-                        *(_ABSENT if k_values is None else _rows(k_values, "k_values", dtype)),
-                        *(_ABSENT if v_values is None else _rows(v_values, "v_values", dtype)), tokens)
-    with _On(k.device) as stream:
-        _check(binding.load().conqur_cache_append(call, stream), "conqur_cache_append")
+    call = _APPEND.pack(*cache._fields, *_batch(start, prefix, table), *_rows(k, "k", *same), *_rows(v, "v", *same),
+                        *(_ABSENT if k_values is None else _rows(k_values, "k_values", *same)),
+                        *(_ABSENT if v_values is None else _rows(v_values, "v_values", *same)), tokens)
+    _check(_run(binding.load().conqur_cache_append, k, call), "conqur_cache_append")
     return (k_values, v_values) if values else None
 
 
@@ -218,23 +212,30 @@ def tree_attention(q, cache: KVCache, start, prefix, table, mask=None, max_query
     the committed tokens and those new ones that mask (int64, bit j: new token j of the sequence) names; None: each sees itself and those
     before it.  max_query: most new tokens of a sequence (up to 64); max_context: most tokens, committed and new (default: what the table
     holds; a closer bound shares the work out better).  scale: 1 / sqrt(width) unless given.  Returns out."""
-    tokens, heads, width = q.shape
-    if width != cache.width:
-        raise ValueError(f"q must be [tokens, heads, {cache.width}]")
-    out = _like(q) if out is None else out
-    if out.shape != q.shape:
-        raise ValueError("out must have the shape of q")
-    dtype = torch.bfloat16
-    fields = (*cache._fields, *_batch(start, prefix, table), *_rows(q, "q", dtype), *_rows(out, "out", dtype),
+    if q.dim() != 3:
+        raise ValueError("q must be [tokens, heads, width]")
+    tokens, heads, _ = q.shape
+    width = cache.width
+    if out is None:
+        out = _like(q)
+    same = (torch.bfloat16, tokens, heads, width)
+    fields = (*cache._fields, *_batch(start, prefix, table), *_rows(q, "q", *same), *_rows(out, "out", *same),
               0 if mask is None else _vector(mask, "mask", torch.int64, tokens), tokens,
               table.shape[1] * cache.page_tokens if max_context is None else max_context)
-    scale = width ** -0.5 if scale is None else scale
+    tail = (max_query, width ** -0.5 if scale is None else scale)
     lib = binding.load()
-    with _On(q.device) as stream:
-        size = lib.conqur_tree_attention_workspace(_TREE.pack(*fields, 0, 0, max_query, scale))
-        workspace = cache._workspace.get(stream)
-        if size and (workspace is None or workspace.numel() < size):
-            workspace = cache._workspace[stream] = torch.empty(size, dtype=torch.uint8, device=q.device)
-        call = _TREE.pack(*fields, workspace.data_ptr() if size else 0, size, max_query, scale)
-        _check(lib.conqur_tree_attention(call, stream), "conqur_tree_attention")
+    stream = torch._C._cuda_getCurrentRawStream(q.get_device())
+    # (a graph keeps the room it was captured with: it takes its own, from its memory pool)
+    capturing = torch._C._cuda_isCurrentStreamCapturing()
+    have = _NOTHING if capturing else cache._workspace.get(stream, _NOTHING)
+    status = _run(lib.conqur_tree_attention, q, _TREE.pack(*fields, *have[1:], *tail))
+    if status == binding.EINVAL:       # perhaps for want of room alone: one that is large enough stays with the cache
+        size = lib.conqur_tree_attention_workspace(_TREE.pack(*fields, 0, 0, *tail))
+        if size > have[2]:
+            room = torch.empty(size, dtype=torch.uint8, device=q.device)
+            have = (room, room.data_ptr(), size)
+            if not capturing:
+                cache._workspace[stream] = have
+            status = _run(lib.conqur_tree_attention, q, _TREE.pack(*fields, *have[1:], *tail))
+    _check(status, "conqur_tree_attention")
     return out

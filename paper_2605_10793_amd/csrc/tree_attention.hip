@@ -16,7 +16,8 @@
 // scores and V's to the weights:
 //   q k_j = step_j (q c_j) + offset_j sum q,   sum_j p_j v_j = sum_j w_j c_j + sum_j w_j offset_j / step_j,   w = p step
 // The second sum, a scalar a row, takes the weights as they are rounded for the first: so the rounding of a weight is multiplied
-// by the value, as with bf16 values, and not by the code (whose zero may lie far from the values' own).
+// by the value, as with bf16 values, and not by the code (whose zero may lie far from the values' own).  The sum of the weights that
+// divides the result takes them so too, over step, so that a row with one large weight gets that token's value unharmed.
 #include "../../include/conqur.h"
 
 #include <math.h>
@@ -36,6 +37,7 @@ constexpr int kWaves = 4;
 constexpr int kBlock = 64;                        // keys a wavefront takes at a time
 constexpr int kStep = kBlock * kWaves;            // keys a workgroup takes at a time
 constexpr int kMaxQuery = 64;
+constexpr int kMaxChunks = 256;                   // that one workgroup joins
 
 struct TreeArgs {
   conqur_cache cache;
@@ -50,7 +52,7 @@ struct TreeArgs {
   int64_t chunk;             // keys of a chunk, a multiple of kStep
   int chunks;                // of the longest context
   int max_query, group, rows;
-  int row_tiles, q_wide;
+  int row_tiles, q_wide, out_wide;
   float scale_log2;
 };
 
@@ -213,6 +215,21 @@ __device__ __forceinline__ void pack_weights(const float* w, uint32_t* out) {
 
 // Two halves of a word that hold infinities or NaNs.
 __device__ __forceinline__ bool any_nonfinite(uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
+
+// Four neighbouring entries of a row's result, sums o over l.
+__device__ __forceinline__ void store_row4(const TreeArgs& a, const Sequence& sq, int head, int row, int entry, f32x4 o, float l) {
+  bf16_bits* out = a.out + (sq.first + row / a.group) * a.out_ts + (int64_t)(head * a.group + row % a.group) * a.out_hs + entry;
+  const float inv = 1.0f / l;
+  const uint32_t x = l == 0.0f ? 0 : f32x2_to_bf16x2(o[0] * inv, o[1] * inv), y = l == 0.0f ? 0 : f32x2_to_bf16x2(o[2] * inv, o[3] * inv);
+  if (a.out_wide) {
+    *reinterpret_cast<u32x2*>(out) = u32x2{x, y};
+  } else {
+    out[0] = (bf16_bits)x;
+    out[1] = (bf16_bits)(x >> 16);
+    out[2] = (bf16_bits)y;
+    out[3] = (bf16_bits)(y >> 16);
+  }
+}
 
 template <int BITS, int W, int QT>
 __global__ void __launch_bounds__(64 * kWaves, QT > 1 ? 1 : 2) k_tree(const TreeArgs a) {
@@ -377,6 +394,9 @@ __global__ void __launch_bounds__(64 * kWaves, QT > 1 ? 1 : 2) k_tree(const Tree
 
     // A constant row has step 0 and code 0: its weight goes in as it is, and its offset with it.
     const float v_step = !kCodes || vs.x == 0.0f ? 1.0f : vs.x;
+    // A step so small that weights times it leave the range: such a token's weight is added to the sum as it is.
+    const bool tiny = kCodes && fabsf(v_step) < 1e-30f;
+    const float v_inv = tiny ? 0.0f : 1.0f / v_step;
     const float v_off = kCodes ? vs.y / v_step - shifted<BITS>() : 0.0f;
     uint32_t p[QT][4][2];
 #pragma unroll
@@ -411,14 +431,19 @@ __global__ void __launch_bounds__(64 * kWaves, QT > 1 ? 1 : 2) k_tree(const Tree
         for (int d = 0; d < kTiles; ++d) o[x][d] *= f;
       }
       const float m = m_run[x] == -INFINITY ? 0.0f : m_run[x];
+      if (__any(tiny)) each<16>([&](auto e) {
+        constexpr int E = decltype(e)::value;
+        l_run[x] += row_bcast<E>(tiny ? 1.0f : 0.0f) * __builtin_amdgcn_exp2f(v[E] - m);
+      });
       each<16>([&](auto e) {
         constexpr int E = decltype(e)::value;
         const float w = __builtin_amdgcn_exp2f(v[E] - m);
-        l_run[x] += w;
-        v[E] = w;
         if constexpr (kCodes) {
           v[E] = w * row_bcast<E>(v_step);
           if (partial && !((vis[x] >> E) & 1)) v[E] = 0.0f;      // (whatever pair the slot holds)
+        } else {
+          l_run[x] += w;
+          v[E] = w;
         }
       });
 #pragma unroll
@@ -429,8 +454,10 @@ __global__ void __launch_bounds__(64 * kWaves, QT > 1 ? 1 : 2) k_tree(const Tree
           constexpr int kAt = BITS == 4 ? (E % 4 == 1 ? 2 : E % 4 == 2 ? 1 : E % 4) : E % 4;     // where pack_weights put it
           const uint32_t u = p[x][E / 4][kAt / 2];
           const float w = __uint_as_float(kAt % 2 ? u & 0xffff0000u : u << 16);
-          const float c = w * row_bcast<E>(v_off);
-          c_run[x] += partial && !((vis[x] >> E) & 1) ? 0.0f : c;
+          const float c = w * row_bcast<E>(v_off), n = w * row_bcast<E>(v_inv);
+          const bool out = partial && !((vis[x] >> E) & 1);
+          c_run[x] += out ? 0.0f : c;
+          l_run[x] += out ? 0.0f : n;
         });
       }
     }
@@ -554,12 +581,8 @@ __global__ void __launch_bounds__(64 * kWaves, QT > 1 ? 1 : 2) k_tree(const Tree
     const int row = row0 + x * 16 + col;
     if (row >= rows) continue;
     if (whole) {
-      const float inv = l_run[x] == 0.0f ? 0.0f : 1.0f / l_run[x];
-      bf16_bits* out = a.out + (sq.first + row / a.group) * a.out_ts + (int64_t)(head * a.group + row % a.group) * a.out_hs;
 #pragma unroll
-      for (int d = 0; d < kTiles; ++d)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) out[d * 16 + g * 4 + r] = l_run[x] == 0.0f ? 0 : f32_to_bf16(o[x][d][r] * inv);
+      for (int d = 0; d < kTiles; ++d) store_row4(a, sq, head, row, d * 16 + g * 4, o[x][d], l_run[x]);
     } else {
       const int64_t at = (((int64_t)b * heads + head) * a.rows + row) * a.chunks + blockIdx.y;
 #pragma unroll
@@ -569,41 +592,79 @@ __global__ void __launch_bounds__(64 * kWaves, QT > 1 ? 1 : 2) k_tree(const Tree
   }
 }
 
-// Joins the chunks of a row: a wavefront a row.
-template <int W>
+// Joins a row's chunks.  WAVES = 1: a wavefront a row, for the few chunks of many rows; 4: a workgroup a row, for up to 256 chunks.  W / 4
+// lanes read a chunk's result as 16-byte vectors, 256 / W chunks at a time, and the first ones are under way before the maxima are.
+template <int W, int WAVES>
 __global__ void __launch_bounds__(256) k_tree_join(const TreeArgs a) {
+  constexpr int kLanes = W / 4, kAt = 64 / kLanes;      // lanes of a chunk, chunks of a wavefront at a time
+  constexpr int kFirst = 4;                             // vectors a lane takes ahead
+  __shared__ float s_f[256];
+  __shared__ float s_red[2][4];
+  __shared__ __attribute__((aligned(16))) float s_o[4][W];
+
   const int b = blockIdx.y;
   const Sequence sq = sequence_of(a, b);
   const int64_t heads = a.cache.heads;
-  const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int rows = sq.count * a.group;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t id = WAVES == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
   const int row = (int)(id / heads), head = (int)(id % heads);
-  if (sq.length <= a.chunk || row >= rows) return;
+  if (sq.length <= a.chunk || row >= sq.count * a.group) return;
   const int chunks = (int)((sq.length + a.chunk - 1) / a.chunk);
-  const int lane = threadIdx.x & 63;
   const int64_t at = (((int64_t)b * heads + head) * a.rows + row) * a.chunks;
+  const int first = (WAVES == 1 ? 0 : wave * kAt) + lane / kLanes;
+  constexpr int kNext = WAVES * kAt;
+  const float* p = a.part + at * W + lane % kLanes * 4;
 
-  float m = -INFINITY;
-  for (int c = lane; c < chunks; c += 64) m = fmaxf(m, a.part_ml[at + c].x);
-  m = wave_max(m);
-  float l = 0.0f;
-  constexpr int kEach = W / 64;
-  float o[kEach];
+  f32x4 v[kFirst];
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) o[i] = 0.0f;
-#pragma unroll 4
-  for (int c = 0; c < chunks; ++c) {
-    const float2 ml = a.part_ml[at + c];
-    const float f = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml.x - m);
-    l += ml.y * f;
-    const float* p = a.part + (at + c) * W + lane * kEach;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) o[i] += f == 0.0f ? 0.0f : p[i] * f;
+  for (int i = 0; i < kFirst; ++i)
+    if (first + i * kNext < chunks) v[i] = *reinterpret_cast<const f32x4*>(p + (int64_t)(first + i * kNext) * W);
+  const int mine = WAVES == 1 ? lane : (int)threadIdx.x;
+  const float2 ml = mine < chunks ? a.part_ml[at + mine] : make_float2(-INFINITY, 0.0f);
+  float m = wave_max(ml.x);
+  if constexpr (WAVES > 1) {
+    if (lane == 0) s_red[0][wave] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(s_red[0][0], s_red[0][1]), fmaxf(s_red[0][2], s_red[0][3]));
   }
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  bf16_bits* out = a.out + (sq.first + row / a.group) * a.out_ts + (int64_t)(head * a.group + row % a.group) * a.out_hs + lane * kEach;
+  const float f = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml.x - m);
+  float l = wave_sum(ml.y * f);
+  if constexpr (WAVES > 1) {
+    if (lane == 0) s_red[1][wave] = l;
+    s_f[threadIdx.x] = f;
+    __syncthreads();
+    l = (s_red[1][0] + s_red[1][1]) + (s_red[1][2] + s_red[1][3]);
+  }
+  auto factor = [&](int c) { return WAVES == 1 ? __shfl(f, c) : s_f[c]; };
+  f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+  auto add = [&](const f32x4& x, float w) {
+    if (w != 0.0f) o += x * w;
+  };
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) out[i] = l == 0.0f ? 0 : f32_to_bf16(o[i] * inv);
+  for (int i = 0; i < kFirst; ++i) {
+    const int c = first + i * kNext;
+    const float w = factor(c & 255);
+    if (c < chunks) add(v[i], w);
+  }
+  for (int c0 = kFirst * kNext; c0 < chunks; c0 += kNext) {
+    const int c = c0 + first;
+    const float w = factor(c & 255);
+    if (c < chunks) add(*reinterpret_cast<const f32x4*>(p + (int64_t)c * W), w);
+  }
+#pragma unroll
+  for (int off = kLanes; off < 64; off *= 2)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) o[r] += __shfl_xor(o[r], off);
+  if constexpr (WAVES > 1) {
+    if (lane < kLanes) *reinterpret_cast<f32x4*>(&s_o[wave][lane * 4]) = o;
+    __syncthreads();
+    if (wave) return;
+    o = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o += *reinterpret_cast<const f32x4*>(&s_o[i][lane % kLanes * 4]);
+  }
+  if (lane >= kLanes) return;
+  store_row4(a, sq, head, row, lane * 4, o, l);
 }
 
 constexpr int64_t kMaxStride = 1ll << 40;
@@ -626,6 +687,7 @@ Plan plan_of(const conqur_tree_call& c) {
   const int64_t steps = (p.context + kStep - 1) / kStep;
   if (groups >= 256) chunks = (p.context + 511) / 512 < 16 ? (p.context + 511) / 512 : 16;
   if (chunks > steps) chunks = steps;
+  if (chunks > kMaxChunks) chunks = kMaxChunks;
   if (chunks < 1) chunks = 1;
   const int64_t each = (steps + chunks - 1) / chunks;
   p.chunk = (each > 0 ? each : 1) * kStep;
@@ -664,8 +726,11 @@ hipError_t launch(const TreeArgs& a, const Plan& p, hipStream_t s) {
     k_tree<BITS, W, 2><<<grid, 64 * kWaves, 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.chunks == 1) return e;
-  const dim3 join((uint32_t)(((int64_t)p.rows * a.cache.heads + 3) / 4), a.batch.sequences);
-  k_tree_join<W><<<join, 256, 0, s>>>(a);
+  const int64_t rows = (int64_t)p.rows * a.cache.heads;
+  if (p.chunks <= 16)
+    k_tree_join<W, 1><<<dim3((uint32_t)((rows + 3) / 4), a.batch.sequences), 256, 0, s>>>(a);
+  else
+    k_tree_join<W, 4><<<dim3((uint32_t)rows, a.batch.sequences), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -694,6 +759,7 @@ extern "C" conqur_status conqur_tree_attention(const conqur_tree_call* c, void* 
   a.out_ts = c->out.token_stride;
   a.out_hs = c->out.head_stride;
   a.q_wide = reinterpret_cast<uintptr_t>(c->q.data) % 16 == 0 && a.q_ts % 8 == 0 && a.q_hs % 8 == 0;
+  a.out_wide = reinterpret_cast<uintptr_t>(c->out.data) % 8 == 0 && a.out_ts % 4 == 0 && a.out_hs % 4 == 0;
   a.mask = c->mask;
   a.tokens = (int64_t)c->tokens;
   a.context = p.context;

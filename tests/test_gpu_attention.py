@@ -681,6 +681,32 @@ def test_on_another_stream_and_in_a_graph(A):
         assert torch.equal(replayed, step(cache, held, pos, start, prefix, table, mask))
 
 
+def test_a_graph_keeps_its_workspace(A):
+    """A larger call on the capturing stream, which takes a larger workspace, leaves a captured call's results alone."""
+    import torch
+    heads, width = 2, 128
+    cache, table = filled_cache(A, [3000, 3000], 64, heads, width, 16, 3)
+    start, prefix, table = i32([0, 1, 2]), i32([2999, 2999]), i32(table)
+    q = randn(4, 2, 8, width)
+    base = A.tree_attention(q, cache, start, prefix, table)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        out = A.tree_attention(q, cache, start, prefix, table)
+    more = randn(5, 128, 64, width)
+    for _ in range(3):
+        with torch.cuda.stream(side):
+            A.tree_attention(more, cache, i32([0, 64, 128]), i32([2936, 2936]), table)
+            out.zero_()
+            graph.replay()
+        torch.cuda.synchronize()
+        held = [torch.full((1 << 22,), 3.0, device="cuda:0") for _ in range(8)]       # takes whatever was given back
+        with torch.cuda.stream(side):
+            graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, base) and all(torch.all(x == 3.0) for x in held)
+
+
 # ------------------------------------------------------------------------------------------------ refusals
 
 def test_refusals(A):
