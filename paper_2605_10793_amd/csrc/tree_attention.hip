@@ -18,127 +18,12 @@
 // The second sum, a scalar a row, takes the weights as they are rounded for the first: so the rounding of a weight is multiplied
 // by the value, as with bf16 values, and not by the code (whose zero may lie far from the values' own).  The sum of the weights that
 // divides the result takes them so too, over step, so that a row with one large weight gets that token's value unharmed.
-#include "../../include/conqur.h"
-
-#include <math.h>
-
-#include "kernels.h"
-
-namespace conqur {
-bool cache_fine(const conqur_cache& c);
-bool batch_fine(const conqur_batch& b);
-}  // namespace conqur
+#include "tree_attention.h"
 
 using namespace conqur;
+using namespace conqur::tree;
 
 namespace {
-
-constexpr int kWaves = 4;
-constexpr int kBlock = 64;                        // keys a wavefront takes at a time
-constexpr int kStep = kBlock * kWaves;            // keys a workgroup takes at a time
-constexpr int kMaxQuery = 64;
-constexpr int kMaxChunks = 256;                   // that one workgroup joins
-
-struct TreeArgs {
-  conqur_cache cache;
-  conqur_batch batch;
-  const bf16_bits* q;
-  bf16_bits* out;
-  int64_t q_ts, q_hs, out_ts, out_hs;
-  const uint64_t* mask;
-  int64_t tokens, context;
-  float* part;               // [sequence][cache head][row][chunk][width] partial results
-  float2* part_ml;           // [sequence][cache head][row][chunk] maxima and sums
-  int64_t chunk;             // keys of a chunk, a multiple of kStep
-  int chunks;                // of the longest context
-  int max_query, group, rows;
-  int row_tiles, q_wide, out_wide;
-  float scale_log2;
-};
-
-struct Sequence {
-  int64_t first, prefix, length;     // first row of q, committed tokens, tokens in sight
-  int count;
-};
-
-__device__ __forceinline__ Sequence sequence_of(const TreeArgs& a, int b) {
-  Sequence s;
-  auto clamp_to = [&](int v) { return v < 0 ? (int64_t)0 : (int64_t)v > a.tokens ? a.tokens : (int64_t)v; };
-  s.first = clamp_to(a.batch.start[b]);
-  const int64_t n = clamp_to(a.batch.start[b + 1]) - s.first;
-  s.prefix = a.batch.prefix[b] < 0 ? 0 : a.batch.prefix[b];
-  s.length = s.prefix + (n < 0 ? 0 : n);
-  if (s.length > a.context) s.length = a.context;
-  s.count = n < 0 ? 0 : n > a.max_query ? a.max_query : (int)n;
-  return s;
-}
-
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-
-__device__ __forceinline__ bf16x8 as_frag(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-  const u32x4 v = {a, b, c, d};
-  return __builtin_bit_cast(bf16x8, v);
-}
-__device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-
-// Over the four lanes l, l + 16, l + 32, l + 48 of a column.
-template <typename Op>
-__device__ __forceinline__ float column_reduce(float v, Op op) {
-  const uint32_t u = __float_as_uint(v);
-  const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-  const uint32_t w = __float_as_uint(op(__uint_as_float(a[0]), __uint_as_float(a[1])));
-  const auto b = __builtin_amdgcn_permlane16_swap(w, w, false, false);
-  return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-__device__ __forceinline__ float column_sum(float v) { return column_reduce(v, [](float a, float b) { return a + b; }); }
-__device__ __forceinline__ float column_max(float v) { return column_reduce(v, [](float a, float b) { return fmaxf(a, b); }); }
-
-// Lane E of every row of 16 to the whole row.
-template <int E>
-__device__ __forceinline__ float row_bcast(float v) {
-  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x150 + E, 0xf, 0xf, true));
-}
-template <typename F, int... I>
-__device__ __forceinline__ void each_of(F&& f, std::integer_sequence<int, I...>) {
-  (f(std::integral_constant<int, I>{}), ...);
-}
-template <int N, typename F>
-__device__ __forceinline__ void each(F&& f) {
-  each_of(f, std::make_integer_sequence<int, N>{});
-}
-
-// How a cache's format meets the operands.
-template <int BITS, int W>
-struct Format {
-  static constexpr int kRow = BITS == 16 ? 2 * W : W * BITS / 8;    // bytes of a key
-  static constexpr int kVRows = BITS == 4 ? W / 2 : W;              // rows of V in a page
-  static constexpr int kVSize = BITS == 16 ? 2 : 1;                 // bytes of a token in such a row
-  static constexpr int kWords = W * BITS / 128;                     // words of a key in each of the four lanes that share it
-  static constexpr int kVTiles = kVRows / 16;                       // tiles of 16 V rows
-  static constexpr int kVWords = 4 * kVSize;                        // words of a lane's 16 tokens in a V row
-};
-
-// Entry of the row that element j of the contraction's operand i holds in quarter g.
-template <int BITS, int W>
-__device__ __forceinline__ int entry_of(int i, int g, int j) {
-  if constexpr (BITS == 16) return (i * 4 + g) * 8 + j;
-  if constexpr (BITS == 8) return W == 128 ? ((i / 2) * 4 + g) * 16 + (i % 2) * 8 + j : g * 16 + i * 8 + j;
-  // 4 bits: bytes in the order 0, 2, 1, 3 within a word; first the low halves' operands, then the high halves'
-  const int byte = (j & 4) | ((j & 1) << 1) | ((j >> 1) & 1);
-  return W == 128 ? (i / 2) * 64 + g * 16 + (i % 2) * 8 + byte : i * 32 + g * 8 + byte;
-}
-
-// Bytes 0 and 1 (2 and 3) of a word as bf16 integers.
-__device__ __forceinline__ uint32_t bytes_to_bf16(uint32_t x, int hi) {
-  const float a = (float)((x >> (hi ? 16 : 0)) & 0xff), b = (float)((x >> (hi ? 24 : 8)) & 0xff);
-  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302);
-}
-// 128 + code for the low (shift 0, 8) or high (4, 12) halves of bytes 0 and 2 (0, 4) or 1 and 3 (8, 12).
-__device__ __forceinline__ uint32_t nibbles_to_bf16(uint32_t x, int shift) { return ((x >> shift) & 0x000f000fu) | 0x43004300u; }
-
-template <int BITS>
-__device__ __forceinline__ constexpr float shifted() { return BITS == 4 ? 128.0f : 0.0f; }      // what an operand holds above the code
 
 template <int BITS, int W>
 struct Keys {        // a lane's share of 64 keys: four tiles of 16
@@ -213,24 +98,6 @@ __device__ __forceinline__ void pack_weights(const float* w, uint32_t* out) {
   out[1] = f32x2_to_bf16x2(w[BITS == 4 ? 1 : 2], w[3]);
 }
 
-// Two halves of a word that hold infinities or NaNs.
-__device__ __forceinline__ bool any_nonfinite(uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
-
-// Four neighbouring entries of a row's result, sums o over l.
-__device__ __forceinline__ void store_row4(const TreeArgs& a, const Sequence& sq, int head, int row, int entry, f32x4 o, float l) {
-  bf16_bits* out = a.out + (sq.first + row / a.group) * a.out_ts + (int64_t)(head * a.group + row % a.group) * a.out_hs + entry;
-  const float inv = 1.0f / l;
-  const uint32_t x = l == 0.0f ? 0 : f32x2_to_bf16x2(o[0] * inv, o[1] * inv), y = l == 0.0f ? 0 : f32x2_to_bf16x2(o[2] * inv, o[3] * inv);
-  if (a.out_wide) {
-    *reinterpret_cast<u32x2*>(out) = u32x2{x, y};
-  } else {
-    out[0] = (bf16_bits)x;
-    out[1] = (bf16_bits)(x >> 16);
-    out[2] = (bf16_bits)y;
-    out[3] = (bf16_bits)(y >> 16);
-  }
-}
-
 template <int BITS, int W, int QT>
 __global__ void __launch_bounds__(64 * kWaves, QT > 1 ? 1 : 2) k_tree(const TreeArgs a) {
   using F = Format<BITS, W>;
@@ -241,16 +108,22 @@ __global__ void __launch_bounds__(64 * kWaves, QT > 1 ? 1 : 2) k_tree(const Tree
   __shared__ __attribute__((aligned(16))) float s_o[2][QT * kTiles][64][4];
   __shared__ float s_ml[2][QT][2][64];
 
-  const int b = blockIdx.z;
   const int head = blockIdx.x / a.row_tiles, row_tile = blockIdx.x % a.row_tiles;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int row0 = row_tile * 16 * QT;
+  Pieces piece;
+  for (bool first = true; piece.next(a, row0, threadIdx.x & 63, first); first = false) {
+  int lane, col, g;
+  auto number = [&] {
+    lane = anew(threadIdx.x & 63);
+    col = lane & 15;
+    g = lane >> 4;
+  };
+  number();
+  const int b = piece.b;
   const Sequence sq = sequence_of(a, b);
-  const int rows = sq.count * a.group, row0 = row_tile * 16 * QT;
-  const int64_t begin = (int64_t)blockIdx.y * a.chunk;
-  if (row0 >= rows || (begin >= sq.length && blockIdx.y > 0)) return;
-  const int64_t end = begin + a.chunk < sq.length ? begin + a.chunk : sq.length;
-
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int col = lane & 15, g = lane >> 4;
+  const int rows = sq.count * a.group;
+  const int64_t begin = (int64_t)piece.first * kBlock, end = (int64_t)piece.last * kBlock < sq.length ? (int64_t)piece.last * kBlock : sq.length;
 
   // Queries: operand i of column `col`, and what the row sees among the new tokens.
   bf16x8 qf[QT][kOps];
@@ -341,12 +214,12 @@ __global__ void __launch_bounds__(64 * kWaves, QT > 1 ? 1 : 2) k_tree(const Tree
     page_v = page_of(kb + v_group);
     fetch_keys(kb, page_k, page_v);
     fetch_values(kb, page_v);
-    next_k = page_of(kb + kStep + k_group);
-    next_v = page_of(kb + kStep + v_group);
+    next_k = page_of(kb + kBlock * kWaves + k_group);
+    next_v = page_of(kb + kBlock * kWaves + v_group);
   }
-  for (; kb < end; kb += kStep) {
-    const bool more = kb + kStep < end;
-    const int32_t after_k = more ? page_of(kb + 2 * kStep + k_group) : -1, after_v = more ? page_of(kb + 2 * kStep + v_group) : -1;
+  for (; kb < end; kb += kBlock * kWaves) {
+    const bool more = kb + kBlock * kWaves < end;
+    const int32_t after_k = more ? page_of(kb + 2 * kBlock * kWaves + k_group) : -1, after_v = more ? page_of(kb + 2 * kBlock * kWaves + v_group) : -1;
 
     f32x4 s[QT][4];
 #pragma unroll
@@ -363,7 +236,7 @@ __global__ void __launch_bounds__(64 * kWaves, QT > 1 ? 1 : 2) k_tree(const Tree
     // Keys that some row does not see: of the new tokens, behind the end, or of no page.
     const bool partial = kb + kBlock > sq.prefix || kb + kBlock > end || __any(page_v < 0);
     const float2 ks_now = ks;
-    if (more) fetch_keys(kb + kStep, next_k, next_v);
+    if (more) fetch_keys(kb + kBlock * kWaves, next_k, next_v);
 
     uint32_t vis[QT];
     if (partial) {
@@ -528,13 +401,14 @@ __global__ void __launch_bounds__(64 * kWaves, QT > 1 ? 1 : 2) k_tree(const Tree
         for (int x = 0; x < QT; ++x) o[x][d] = mfma(vv, as_frag(p[x][2 * m][0], p[x][2 * m][1], p[x][2 * m + 1][0], p[x][2 * m + 1][1]), o[x][d]);
       }
     }
-    if (more) fetch_values(kb + kStep, next_v);
+    if (more) fetch_values(kb + kBlock * kWaves, next_v);
     page_k = next_k;
     page_v = next_v;
     next_k = after_k;
     next_v = after_v;
   }
 
+  number();
   // A row's sums over the lanes that shared its keys; the constant that belongs to every entry of the result.
 #pragma unroll
   for (int x = 0; x < QT; ++x) {
@@ -573,30 +447,30 @@ __global__ void __launch_bounds__(64 * kWaves, QT > 1 ? 1 : 2) k_tree(const Tree
     }
     __syncthreads();
   }
-  if (wave) return;
+  if (wave) continue;
 
-  const bool whole = sq.length <= a.chunk;
 #pragma unroll
   for (int x = 0; x < QT; ++x) {
     const int row = row0 + x * 16 + col;
     if (row >= rows) continue;
-    if (whole) {
+    if (piece.whole) {
 #pragma unroll
       for (int d = 0; d < kTiles; ++d) store_row4(a, sq, head, row, d * 16 + g * 4, o[x][d], l_run[x]);
     } else {
-      const int64_t at = (((int64_t)b * heads + head) * a.rows + row) * a.chunks + blockIdx.y;
+      const int64_t at = part_at(a, head, row_tile, piece.slot, row - row0);
 #pragma unroll
       for (int d = 0; d < kTiles; ++d) *reinterpret_cast<f32x4*>(a.part + at * W + d * 16 + g * 4) = o[x][d];
       if (g == 0) a.part_ml[at] = make_float2(m_run[x], l_run[x]);
     }
   }
+  }
 }
 
-// Joins a row's chunks.  WAVES = 1: a wavefront a row, for the few chunks of many rows; 4: a workgroup a row, for up to 256 chunks.  W / 4
-// lanes read a chunk's result as 16-byte vectors, 256 / W chunks at a time, and the first ones are under way before the maxima are.
+// Joins a row's pieces.  WAVES = 1: a wavefront a row, for up to 64 pieces; 4: a workgroup a row, for up to 256.  W / 4
+// lanes read a piece's result as 16-byte vectors, 256 / W pieces at a time, and the first ones are under way before the maxima are.
 template <int W, int WAVES>
 __global__ void __launch_bounds__(256) k_tree_join(const TreeArgs a) {
-  constexpr int kLanes = W / 4, kAt = 64 / kLanes;      // lanes of a chunk, chunks of a wavefront at a time
+  constexpr int kLanes = W / 4, kAt = 64 / kLanes;      // lanes of a piece, pieces of a wavefront at a time
   constexpr int kFirst = 4;                             // vectors a lane takes ahead
   __shared__ float s_f[256];
   __shared__ float s_red[2][4];
@@ -608,19 +482,26 @@ __global__ void __launch_bounds__(256) k_tree_join(const TreeArgs a) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int64_t id = WAVES == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
   const int row = (int)(id / heads), head = (int)(id % heads);
-  if (sq.length <= a.chunk || row >= sq.count * a.group) return;
-  const int chunks = (int)((sq.length + a.chunk - 1) / a.chunk);
-  const int64_t at = (((int64_t)b * heads + head) * a.rows + row) * a.chunks;
+  if (row >= sq.count * a.group) return;
+  const int row_tile = row / a.tile_rows;
+  const Layout layout(a, row_tile * a.tile_rows, lane);
+  int from = 0, to = 0;
+  layout.range(b, &from, &to);
+  const int p0 = from / layout.each, chunks = (to - 1) / layout.each - p0 + 1;
+  if (chunks <= 1) return;
+  // the first piece may be its workgroup's last, the others are their workgroups' first
+  const int slot0 = 2 * p0 + (from > p0 * layout.each);
+  auto at = [&](int c) { return part_at(a, head, row_tile, c ? 2 * (p0 + c) : slot0, row - row_tile * a.tile_rows); };
   const int first = (WAVES == 1 ? 0 : wave * kAt) + lane / kLanes;
   constexpr int kNext = WAVES * kAt;
-  const float* p = a.part + at * W + lane % kLanes * 4;
+  const int entry = lane % kLanes * 4;
 
   f32x4 v[kFirst];
 #pragma unroll
   for (int i = 0; i < kFirst; ++i)
-    if (first + i * kNext < chunks) v[i] = *reinterpret_cast<const f32x4*>(p + (int64_t)(first + i * kNext) * W);
+    if (first + i * kNext < chunks) v[i] = *reinterpret_cast<const f32x4*>(a.part + at(first + i * kNext) * W + entry);
   const int mine = WAVES == 1 ? lane : (int)threadIdx.x;
-  const float2 ml = mine < chunks ? a.part_ml[at + mine] : make_float2(-INFINITY, 0.0f);
+  const float2 ml = mine < chunks ? a.part_ml[at(mine)] : make_float2(-INFINITY, 0.0f);
   float m = wave_max(ml.x);
   if constexpr (WAVES > 1) {
     if (lane == 0) s_red[0][wave] = m;
@@ -649,7 +530,7 @@ __global__ void __launch_bounds__(256) k_tree_join(const TreeArgs a) {
   for (int c0 = kFirst * kNext; c0 < chunks; c0 += kNext) {
     const int c = c0 + first;
     const float w = factor(c & 255);
-    if (c < chunks) add(*reinterpret_cast<const f32x4*>(p + (int64_t)c * W), w);
+    if (c < chunks) add(*reinterpret_cast<const f32x4*>(a.part + at(c) * W + entry), w);
   }
 #pragma unroll
   for (int off = kLanes; off < 64; off *= 2)
@@ -667,38 +548,87 @@ __global__ void __launch_bounds__(256) k_tree_join(const TreeArgs a) {
   store_row4(a, sq, head, row, lane * 4, o, l);
 }
 
+// Joins the pieces of 16 rows as the workgroups of many rows leave them (their registers' layout): a wavefront takes two of the result's tiles of
+// 16 entries, a lane four entries of one row.
+template <int W>
+__global__ void __launch_bounds__(W * 2) k_tree_join_tiles(const TreeArgs a) {
+  const int b = blockIdx.z, head = blockIdx.y, row0 = blockIdx.x * 16;
+  const Sequence sq = sequence_of(a, b);
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
+  if (row0 >= sq.count * a.group) return;
+  const int row_tile = row0 / a.tile_rows, in_tile = row0 - row_tile * a.tile_rows;
+  const Layout layout(a, row_tile * a.tile_rows, lane);
+  int from = 0, to = 0;
+  layout.range(b, &from, &to);
+  const int p0 = from / layout.each, pieces = (to - 1) / layout.each - p0 + 1;
+  if (pieces <= 1) return;
+  auto at = [&](int c) { return part_at(a, head, row_tile, c ? 2 * (p0 + c) : 2 * p0 + (from > p0 * layout.each), in_tile); };
+
+  float m = -INFINITY;
+#pragma unroll 4
+  for (int c = 0; c < pieces; ++c) m = fmaxf(m, a.part_ml[at(c) + col].x);
+  f32x4 o[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+  float l = 0.0f;
+#pragma unroll 4
+  for (int c = 0; c < pieces; ++c) {
+    const float2 ml = a.part_ml[at(c) + col];
+    const float* const p = a.part + at(c) * W + wave * 512 + lane * 4;
+    const f32x4 v0 = *reinterpret_cast<const f32x4*>(p), v1 = *reinterpret_cast<const f32x4*>(p + 256);
+    const float f = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml.x - m);
+    l += ml.y * f;
+    if (f != 0.0f) {
+      o[0] += v0 * f;
+      o[1] += v1 * f;
+    }
+  }
+  if (row0 + col >= sq.count * a.group) return;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) store_row4(a, sq, head, row0 + col, (wave * 2 + i) * 16 + g * 4, o[i], l);
+}
+
 constexpr int64_t kMaxStride = 1ll << 40;
 
 struct Plan {
-  int qt, row_tiles, rows, chunks;
-  int64_t chunk, context;
+  bool wide;
+  int qt, tile_rows, row_tiles, splits, min_blocks;
+  int64_t context;
 };
 
-// How a call is cut: rows of a cache head into tiles, the context into chunks.
+// How a call is cut: a cache head's rows into tiles, the sequences' blocks into runs.
 Plan plan_of(const conqur_tree_call& c) {
   Plan p;
   const int64_t room = (int64_t)c.batch.table_columns * c.cache.page_tokens;
   p.context = (int64_t)(c.max_context < (uint64_t)room ? c.max_context : (uint64_t)room);
-  p.rows = (int)(c.max_query * (c.q.heads / c.cache.heads));
-  p.qt = p.rows <= 16 ? 1 : 2;
-  p.row_tiles = (p.rows + 16 * p.qt - 1) / (16 * p.qt);
-  const int64_t groups = (int64_t)c.batch.sequences * c.cache.heads * p.row_tiles;
-  int64_t chunks = (1024 + groups - 1) / groups;
-  const int64_t steps = (p.context + kStep - 1) / kStep;
-  if (groups >= 256) chunks = (p.context + 511) / 512 < 16 ? (p.context + 511) / 512 : 16;
-  if (chunks > steps) chunks = steps;
-  if (chunks > kMaxChunks) chunks = kMaxChunks;
-  if (chunks < 1) chunks = 1;
-  const int64_t each = (steps + chunks - 1) / chunks;
-  p.chunk = (each > 0 ? each : 1) * kStep;
-  p.chunks = (int)((p.context + p.chunk - 1) / p.chunk);
-  if (p.chunks < 1) p.chunks = 1;
+  const int rows = (int)(c.max_query * (c.q.heads / c.cache.heads));
+  p.wide = rows > 32;
+  // Rows of a wavefront in sixteens: as few as pad the rows least; 48 rows of bf16 values 128 wide do not fit its registers.
+  p.qt = rows <= 16 ? 1 : 2;
+  if (p.wide) {
+    const int most = c.cache.bits == 16 && c.cache.width == 128 ? 2 : 3;
+    for (int qt = 1, least = 1 << 30; qt <= most; ++qt) {
+      const int padded = (rows + 64 * qt - 1) / (64 * qt) * qt;
+      if (padded <= least) {
+        least = padded;
+        p.qt = qt;
+      }
+    }
+  }
+  p.tile_rows = 16 * p.qt * (p.wide ? kWaves : 1);
+  p.row_tiles = (rows + p.tile_rows - 1) / p.tile_rows;
+  const int64_t groups = (int64_t)c.cache.heads * p.row_tiles, sequences = c.batch.sequences;
+  const int64_t blocks = p.context > kBlock ? (p.context + kBlock - 1) / kBlock : 1;
+  p.min_blocks = kWaves;
+  int64_t splits = kSlots / groups;
+  const int64_t most = (blocks * sequences + p.min_blocks - 1) / p.min_blocks;
+  if (splits > most) splits = most;
+  if (splits > kMaxSplits) splits = kMaxSplits;
+  if (splits < 1) splits = 1;
+  p.splits = blocks <= kWaves || sequences > kMaxScan || sequences * groups >= 4096 ? 0 : (int)splits;
   return p;
 }
 
 uint64_t workspace_of(const conqur_tree_call& c, const Plan& p) {
-  if (p.chunks <= 1) return 0;
-  return (uint64_t)c.batch.sequences * c.cache.heads * p.rows * p.chunks * (c.cache.width + 2) * sizeof(float);
+  return (uint64_t)c.cache.heads * p.row_tiles * 2 * p.splits * p.tile_rows * (c.cache.width + 2) * sizeof(float);
 }
 
 bool call_fine(const conqur_tree_call* c) {
@@ -719,15 +649,22 @@ bool rows_fine(const conqur_heads& h, uint32_t width, uint64_t tokens, bool outp
 
 template <int BITS, int W>
 hipError_t launch(const TreeArgs& a, const Plan& p, hipStream_t s) {
-  const dim3 grid((uint32_t)(a.cache.heads * p.row_tiles), (uint32_t)p.chunks, a.batch.sequences);
-  if (p.qt == 1)
-    k_tree<BITS, W, 1><<<grid, 64 * kWaves, 0, s>>>(a);
-  else
-    k_tree<BITS, W, 2><<<grid, 64 * kWaves, 0, s>>>(a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.chunks == 1) return e;
-  const int64_t rows = (int64_t)p.rows * a.cache.heads;
-  if (p.chunks <= 16)
+  const dim3 grid((uint32_t)(a.cache.heads * p.row_tiles), p.splits ? p.splits : a.batch.sequences);
+  hipError_t e;
+  if (p.wide) {
+    e = launch_wide(a, p.qt, grid, s);
+  } else {
+    if (p.qt == 1)
+      k_tree<BITS, W, 1><<<grid, 64 * kWaves, 0, s>>>(a);
+    else
+      k_tree<BITS, W, 2><<<grid, 64 * kWaves, 0, s>>>(a);
+    e = hipGetLastError();
+  }
+  if (e != hipSuccess || p.splits <= 1) return e;
+  const int64_t rows = (int64_t)a.max_query * a.group * a.cache.heads;
+  if (p.wide)
+    k_tree_join_tiles<W><<<dim3((a.max_query * a.group + 15) / 16, a.cache.heads, a.batch.sequences), W * 2, 0, s>>>(a);
+  else if (p.splits <= 64 && p.splits <= 8 * (int64_t)a.batch.sequences)
     k_tree_join<W, 1><<<dim3((uint32_t)((rows + 3) / 4), a.batch.sequences), 256, 0, s>>>(a);
   else
     k_tree_join<W, 4><<<dim3((uint32_t)rows, a.batch.sequences), 256, 0, s>>>(a);
@@ -763,14 +700,14 @@ extern "C" conqur_status conqur_tree_attention(const conqur_tree_call* c, void* 
   a.mask = c->mask;
   a.tokens = (int64_t)c->tokens;
   a.context = p.context;
-  a.chunk = p.chunk;
-  a.chunks = p.chunks;
+  a.splits = p.splits;
+  a.min_blocks = p.min_blocks;
   a.max_query = (int)c->max_query;
   a.group = (int)(c->q.heads / c->cache.heads);
-  a.rows = p.rows;
+  a.tile_rows = p.tile_rows;
   a.row_tiles = p.row_tiles;
   a.part = static_cast<float*>(c->workspace);
-  a.part_ml = reinterpret_cast<float2*>(a.part + (uint64_t)c->batch.sequences * c->cache.heads * p.rows * p.chunks * c->cache.width);
+  a.part_ml = reinterpret_cast<float2*>(a.part + (uint64_t)c->cache.heads * p.row_tiles * 2 * p.splits * p.tile_rows * c->cache.width);
   a.scale_log2 = c->scale * 1.4426950408889634f;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   hipError_t e;
