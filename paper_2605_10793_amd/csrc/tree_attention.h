@@ -20,6 +20,8 @@ constexpr int kBlock = 64;                        // keys a wavefront takes at a
 constexpr int kMaxQuery = 64;
 constexpr int kMaxSplits = 256;                   // pieces of a sequence that one workgroup joins
 constexpr int kScanChunks = 8;
+constexpr int kRun = 16384;                        // keys after which blocks that were put off are made up for
+constexpr float kRise = 16.0f;                    // by how much (log2) scores may exceed the maximum they are taken against, before it and all results are raised
 constexpr int kSlots = 512;                       // workgroups the device holds: two of 4 wavefronts on each of 256 compute units
 constexpr int kMaxScan = 64 * kScanChunks;        // sequences that a workgroup finds its pieces among
 
@@ -42,27 +44,57 @@ struct TreeArgs {
   float scale_log2;
 };
 
+// The arguments as a kernel reads them, where they lie: each call gives an address that the compiler takes for a new one, so that what a part of a
+// kernel needs of them is read there and not kept in (some hundred) registers from the kernel's beginning.
+typedef const __attribute__((address_space(4))) TreeArgs* Args;
+__device__ __forceinline__ Args kernel_args() {
+  Args p = (Args)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return p;
+}
+
+typedef const __attribute__((address_space(4))) int32_t* Scalars;      // memory that no kernel writes while this one runs
 struct Sequence {
   int64_t first, prefix, length;     // first row of q, committed tokens, tokens in sight
   int count;
 };
 
-__device__ __forceinline__ Sequence sequence_of(const TreeArgs& a, int b) {
+template <typename P>
+__device__ __forceinline__ Sequence sequence_from(Args a, P start, P prefix) {
   Sequence s;
-  auto clamp_to = [&](int v) { return v < 0 ? (int64_t)0 : (int64_t)v > a.tokens ? a.tokens : (int64_t)v; };
-  s.first = clamp_to(a.batch.start[b]);
-  const int64_t n = clamp_to(a.batch.start[b + 1]) - s.first;
-  s.prefix = a.batch.prefix[b] < 0 ? 0 : a.batch.prefix[b];
+  auto clamp_to = [&](int v) { return v < 0 ? (int64_t)0 : (int64_t)v > a->tokens ? a->tokens : (int64_t)v; };
+  s.first = clamp_to(start[0]);
+  const int64_t n = clamp_to(start[1]) - s.first;
+  s.prefix = prefix[0] < 0 ? 0 : prefix[0];
   s.length = s.prefix + (n < 0 ? 0 : n);
-  if (s.length > a.context) s.length = a.context;
-  s.count = n < 0 ? 0 : n > a.max_query ? a.max_query : (int)n;
+  if (s.length > a->context) s.length = a->context;
+  s.count = n < 0 ? 0 : n > a->max_query ? a->max_query : (int)n;
   return s;
+}
+// b the same for a whole wavefront (what follows from it then stays out of the vector registers), or each lane's own.
+__device__ __forceinline__ Sequence sequence_of(Args a, int b) {
+  b = __builtin_amdgcn_readfirstlane(b);
+  return sequence_from(a, (Scalars)(uintptr_t)(a->batch.start + b), (Scalars)(uintptr_t)(a->batch.prefix + b));
+}
+__device__ __forceinline__ Sequence sequence_of_lane(Args a, int b) { return sequence_from(a, a->batch.start + b, a->batch.prefix + b); }
+
+// A value that the compiler takes for a new one: what is made of it is made anew, not kept in registers from one use, far off, to the next.
+__device__ __forceinline__ int anew(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
+// The lane, counted anew: threadIdx.x need not be kept for it.
+__device__ __forceinline__ int lane_anew() {
+  int none = 0;
+  asm volatile("" : "+s"(none));
+  return (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, (uint32_t)none));
 }
 
 // Blocks of a sequence for a row tile that begins at row0: none if it has no such rows, otherwise one at least (which writes zeros if nothing is seen).
-__device__ __forceinline__ int blocks_of(const TreeArgs& a, int b, int row0) {
-  const Sequence s = sequence_of(a, b);
-  if (row0 >= s.count * a.group) return 0;
+__device__ __forceinline__ int blocks_of(Args a, int b, int row0) {
+  const Sequence s = sequence_of_lane(a, b);
+  if (row0 >= s.count * a->group) return 0;
   return s.length > kBlock ? (int)((s.length + kBlock - 1) / kBlock) : 1;
 }
 
@@ -82,26 +114,26 @@ struct Layout {
   int end[kScanChunks];      // last block + 1 of the lane's sequences
   int all;                   // blocks of all
   int each;                  // of a workgroup
-  __device__ __forceinline__ Layout(const TreeArgs& a, int row0, int lane) {
+  __device__ __forceinline__ Layout(Args a, int row0, int lane) {
     all = 0;
 #pragma unroll
     for (int c = 0; c < kScanChunks; ++c) {
       end[c] = all;
-      if (c * 64 < (int)a.batch.sequences) {
+      if (c * 64 < (int)a->batch.sequences) {
         const int b = c * 64 + lane;
-        end[c] = all + wave_scan(b < (int)a.batch.sequences ? blocks_of(a, b, row0) : 0);
+        end[c] = all + wave_scan(b < (int)a->batch.sequences ? blocks_of(a, b, row0) : 0);
         all = __builtin_amdgcn_readlane(end[c], 63);
       }
     }
-    each = (all + a.splits - 1) / a.splits;
-    if (each < a.min_blocks) each = a.min_blocks;
+    each = (all + a->splits - 1) / a->splits;
+    if (each < a->min_blocks) each = a->min_blocks;
   }
   // The sequence that holds block x < all, and where it begins and ends.
-  __device__ __forceinline__ void find(const TreeArgs& a, int x, int* b, int* from, int* to) const {
+  __device__ __forceinline__ void find(Args a, int x, int* b, int* from, int* to) const {
     int before = 0;
 #pragma unroll
     for (int c = 0; c < kScanChunks; ++c) {
-      if (c * 64 < (int)a.batch.sequences) {
+      if (c * 64 < (int)a->batch.sequences) {
         const int last = __builtin_amdgcn_readlane(end[c], 63);
         if (x >= before && x < last) {
           const int i = __popcll(__ballot(end[c] <= x));
@@ -127,9 +159,20 @@ struct Layout {
 };
 
 // Where a row's results of a piece are.
-__device__ __forceinline__ int64_t part_at(const TreeArgs& a, int head, int row_tile, int slot, int row_in_tile) {
-  return (((int64_t)head * a.row_tiles + row_tile) * 2 * a.splits + slot) * a.tile_rows + row_in_tile;
+__device__ __forceinline__ int64_t part_at(Args a, int head, int row_tile, int slot, int row_in_tile) {
+  return (((int64_t)head * a->row_tiles + row_tile) * 2 * a->splits + slot) * a->tile_rows + row_in_tile;
 }
+
+// Pages of a block's four groups of 16 keys, -1 where there is none; the same for a whole wavefront.
+struct Pages {
+  int32_t at[4];
+  __device__ __forceinline__ bool missing() const { return (at[0] | at[1] | at[2] | at[3]) < 0; }
+  __device__ __forceinline__ int32_t pick(int u) const {
+    const int32_t a0 = at[0], a1 = at[1], a2 = at[2], a3 = at[3];
+    const int32_t lo = u & 1 ? a1 : a0, hi = u & 1 ? a3 : a2;
+    return u & 2 ? hi : lo;
+  }
+};
 
 // What a workgroup has to do, piece by piece: blocks [first, last) of sequence b.
 struct Pieces {
@@ -137,8 +180,8 @@ struct Pieces {
   int b, first, last, slot;
   bool whole;
   // False: nothing left.  Called by whole wavefronts, with the same results in all of them.
-  __device__ __forceinline__ bool next(const TreeArgs& a, int row0, int lane, bool begin) {
-    if (a.splits == 0) {
+  __device__ __forceinline__ bool next(Args a, int row0, bool begin) {
+    if (a->splits == 0) {
       if (!begin) return false;
       b = blockIdx.y;
       first = 0;
@@ -146,7 +189,7 @@ struct Pieces {
       whole = true;
       return last > 0;
     }
-    const Layout l(a, row0, lane);
+    const Layout l(a, row0, lane_anew());
     const int start = (int)blockIdx.y * l.each;
     if (begin) {
       x = start;
@@ -164,7 +207,6 @@ struct Pieces {
   }
 };
 
-typedef const __attribute__((address_space(4))) int32_t* Scalars;      // memory that no kernel writes while this one runs
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
@@ -173,12 +215,6 @@ __device__ __forceinline__ bf16x8 as_frag(uint32_t a, uint32_t b, uint32_t c, ui
   return __builtin_bit_cast(bf16x8, v);
 }
 __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-
-// A value that the compiler takes for a new one: what is made of it is made anew, not kept in registers from one use, far off, to the next.
-__device__ __forceinline__ int anew(int v) {
-  asm volatile("" : "+v"(v));
-  return v;
-}
 
 // Over the four lanes l, l + 16, l + 32, l + 48 of a column.
 template <typename Op>
@@ -238,15 +274,25 @@ __device__ __forceinline__ uint32_t nibbles_to_bf16(uint32_t x, int shift) { ret
 template <int BITS>
 __device__ __forceinline__ constexpr float shifted() { return BITS == 4 ? 128.0f : 0.0f; }      // what an operand holds above the code
 
+// Takes the running maximum m to where the highest of new scores, `top` above it, is (none: -inf): what was and what is new fall by the returned amount.
+__device__ __forceinline__ float raise(float& m, float top) {
+  const bool unset = m == -INFINITY;
+  const float by = unset ? (top == -INFINITY ? 0.0f : top) : fmaxf(top, 0.0f);
+  m = unset ? top : m + by;
+  return by;
+}
+// The factor on sums over the scores before that; before the first of them they are 0 and `by` may be anything.
+__device__ __forceinline__ float m_factor(float by) { return __builtin_amdgcn_exp2f(-fmaxf(by, 0.0f)); }
+
 // Two halves of a word that hold infinities or NaNs.
 __device__ __forceinline__ bool any_nonfinite(uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
 
 // Four neighbouring entries of a row's result, sums o over l.
-__device__ __forceinline__ void store_row4(const TreeArgs& a, const Sequence& sq, int head, int row, int entry, f32x4 o, float l) {
-  bf16_bits* out = a.out + (sq.first + row / a.group) * a.out_ts + (int64_t)(head * a.group + row % a.group) * a.out_hs + entry;
+__device__ __forceinline__ void store_row4(Args a, const Sequence& sq, int head, int row, int entry, f32x4 o, float l) {
+  bf16_bits* out = a->out + (sq.first + row / a->group) * a->out_ts + (int64_t)(head * a->group + row % a->group) * a->out_hs + entry;
   const float inv = 1.0f / l;
   const uint32_t x = l == 0.0f ? 0 : f32x2_to_bf16x2(o[0] * inv, o[1] * inv), y = l == 0.0f ? 0 : f32x2_to_bf16x2(o[2] * inv, o[3] * inv);
-  if (a.out_wide) {
+  if (a->out_wide) {
     *reinterpret_cast<u32x2*>(out) = u32x2{x, y};
   } else {
     out[0] = (bf16_bits)x;

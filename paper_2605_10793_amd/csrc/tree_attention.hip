@@ -34,21 +34,31 @@ struct Values {      // a lane's 16 tokens of its V rows
   uint32_t w[Format<BITS, W>::kVTiles][Format<BITS, W>::kVWords];
 };
 
-template <int BITS, int W>
-__device__ __forceinline__ void load_keys(Keys<BITS, W>& k, const unsigned char* p) {    // p: row of the lane's first key
+// 16 bytes (8) from where `from` and a uniform offset, the same for all lanes, and a lane's offset point to.
+__device__ __forceinline__ u32x4 load_b128(const unsigned char* from, int lane_offset, int offset) {
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(from), 0, 0x7fffffff, 0x00020000);
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, lane_offset, offset, 0));
+}
+__device__ __forceinline__ u32x2 load_b64(const unsigned char* from, int lane_offset, int offset) {
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(from), 0, 0x7fffffff, 0x00020000);
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, lane_offset, offset, 0));
+}
+
+// A lane's share of 64 keys: tile t's keys are 4 t further on.  at(bytes): 16 bytes (8) that far behind the lane's first key.
+template <int BITS, int W, typename At16, typename At8>
+__device__ __forceinline__ void load_keys(Keys<BITS, W>& k, At16 at16, At8 at8) {
   using F = Format<BITS, W>;
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
-    const unsigned char* r = p + t * 4 * F::kRow;
     if constexpr (F::kWords >= 4) {
 #pragma unroll
       for (int i = 0; i < F::kWords / 4; ++i) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(r + i * 64);
+        const u32x4 x = at16(t * 4 * F::kRow + i * 64);
 #pragma unroll
         for (int j = 0; j < 4; ++j) k.w[t][4 * i + j] = x[j];
       }
     } else {
-      const u32x2 x = *reinterpret_cast<const u32x2*>(r);
+      const u32x2 x = at8(t * 4 * F::kRow);
       k.w[t][0] = x[0];
       k.w[t][1] = x[1];
     }
@@ -66,14 +76,15 @@ __device__ __forceinline__ bf16x8 key_operand(const Keys<BITS, W>& k, int t, int
   const uint32_t a = k.w[t][o], b = k.w[t][o + 1];
   return as_frag(nibbles_to_bf16(a, s), nibbles_to_bf16(a, s + 8), nibbles_to_bf16(b, s), nibbles_to_bf16(b, s + 8));
 }
-template <int BITS, int W>
-__device__ __forceinline__ void load_values(Values<BITS, W>& v, const unsigned char* p, int pitch) {   // p: the lane's row of the first tile
+// at(tile, bytes): 16 bytes that far behind the lane's first token, in its V row of that tile.
+template <int BITS, int W, typename At>
+__device__ __forceinline__ void load_values(Values<BITS, W>& v, At at) {
   using F = Format<BITS, W>;
 #pragma unroll
   for (int t = 0; t < F::kVTiles; ++t)
 #pragma unroll
     for (int i = 0; i < F::kVSize; ++i) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(p + (int64_t)t * 16 * pitch + i * 16);
+      const u32x4 x = at(t, i * 16);
 #pragma unroll
       for (int j = 0; j < 4; ++j) v.w[t][4 * i + j] = x[j];
     }
@@ -98,378 +109,482 @@ __device__ __forceinline__ void pack_weights(const float* w, uint32_t* out) {
   out[1] = f32x2_to_bf16x2(w[BITS == 4 ? 1 : 2], w[3]);
 }
 
-template <int BITS, int W, int QT>
-__global__ void __launch_bounds__(64 * kWaves, QT > 1 ? 1 : 2) k_tree(const TreeArgs a) {
+// ONE_PAGE: pages of 64 tokens or more, so that a block lies in one and its address is the same for all lanes but for an offset.  (Both forms in one
+// kernel take 60 registers more than either: 16-bit values 128 wide then spill, 215 -> 369 us for the batch of the figures below.)
+template <int BITS, int W, int QT, bool ONE_PAGE>
+__global__ void __launch_bounds__(64 * kWaves, 2) k_tree(const TreeArgs) {
+  Args a = kernel_args();
   using F = Format<BITS, W>;
   constexpr int kOps = W / 32;            // operands of the first product
   constexpr int kTiles = W / 16;          // tiles of the result
   constexpr bool kCodes = BITS != 16;
+  constexpr int kStep = kBlock * kWaves;
+  constexpr int kParts = QT > 1 || !kCodes ? 2 : 1, kT = 4 / kParts;      // parts of a block, key tiles of a part
+  constexpr bool kThrough = QT == 1;      // the loop over committed tokens also fetches the first block behind them (with QT = 2 that takes registers which are not there)
   // The wavefronts' results meet here at the end: two wavefronts' at a time.
   __shared__ __attribute__((aligned(16))) float s_o[2][QT * kTiles][64][4];
   __shared__ float s_ml[2][QT][2][64];
 
-  const int head = blockIdx.x / a.row_tiles, row_tile = blockIdx.x % a.row_tiles;
+  const int head = blockIdx.x / a->row_tiles, row_tile = blockIdx.x % a->row_tiles;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int row0 = row_tile * 16 * QT;
+  const bf16x8 ones = as_frag(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);      // a row of the sums of the weights as they are rounded
   Pieces piece;
-  for (bool first = true; piece.next(a, row0, threadIdx.x & 63, first); first = false) {
-  int lane, col, g;
-  auto number = [&] {
-    lane = anew(threadIdx.x & 63);
-    col = lane & 15;
-    g = lane >> 4;
-  };
-  number();
-  const int b = piece.b;
-  const Sequence sq = sequence_of(a, b);
-  const int rows = sq.count * a.group;
-  const int64_t begin = (int64_t)piece.first * kBlock, end = (int64_t)piece.last * kBlock < sq.length ? (int64_t)piece.last * kBlock : sq.length;
+  for (bool first = true; piece.next(a, row0, first); first = false) {
+    int lane, col, g;
+    auto number = [&] {
+      a = kernel_args();
+      lane = lane_anew();
+      col = lane & 15;
+      g = lane >> 4;
+    };
+    number();
+    const int b = piece.b;
+    const Sequence sq = sequence_of(a, b);
+    const int rows = sq.count * a->group;
+    const int64_t begin = (int64_t)piece.first * kBlock, end = (int64_t)piece.last * kBlock < sq.length ? (int64_t)piece.last * kBlock : sq.length;
 
-  // Queries: operand i of column `col`, and what the row sees among the new tokens.
-  bf16x8 qf[QT][kOps];
-  float q_sum[QT];
-  uint64_t seen[QT];
+    // Queries: operand i of column `col`, in the order in which the keys' operands have the entries.
+    bf16x8 qf[QT][kOps];
+    float q_sum[QT];
 #pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    const int row = row0 + t * 16 + col;
-    const bool here = row < rows;
-    const int node = here ? row / a.group : 0;
-    const bf16_bits* p = a.q + (sq.first + node) * a.q_ts + (int64_t)(head * a.group + (here ? row % a.group : 0)) * a.q_hs;
-    float sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kOps; ++i) {
-      bf16_bits e[8];
-      const int base = entry_of<BITS, W>(i, g, 0);
-      if (a.q_wide) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(p + base);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) e[j] = (bf16_bits)(x[j / 2] >> (j % 2 * 16));
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) e[j] = p[base + j];
-      }
-      uint32_t u[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int x = entry_of<BITS, W>(i, g, 2 * j) - base, y = entry_of<BITS, W>(i, g, 2 * j + 1) - base;
-        u[j] = here ? e[x] | (uint32_t)e[y] << 16 : 0;
-        if (kCodes && here) sum += bf16_to_f32(e[x]) + bf16_to_f32(e[y]);
-      }
-      qf[t][i] = as_frag(u[0], u[1], u[2], u[3]);
-    }
-    q_sum[t] = kCodes ? column_sum(sum) : 0.0f;
-    uint64_t m = 0;
-    if (here) m = a.mask ? a.mask[sq.first + node] : (2ull << node) - 1;
-    if (sq.count < 64) m &= (1ull << sq.count) - 1;
-    seen[t] = m;
-  }
-
-  f32x4 o[QT][kTiles];
-  float m_run[QT], l_run[QT], c_run[QT];
-#pragma unroll
-  for (int t = 0; t < QT; ++t) {
-#pragma unroll
-    for (int d = 0; d < kTiles; ++d) o[t][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    m_run[t] = -INFINITY;
-    l_run[t] = c_run[t] = 0.0f;
-  }
-
-  const int page_tokens = (int)a.cache.page_tokens;
-  const int page_shift = 31 - __builtin_clz(page_tokens);
-  const int32_t* table = a.batch.table + (int64_t)b * a.batch.table_stride;
-  const int64_t heads = a.cache.heads;
-  // Page of a group of 16 tokens from `pos` on, -1 where there is none; reads stay in the pool either way.
-  auto page_of = [&](int64_t pos) {
-    if (pos >= end) return -1;
-    const int32_t p = table[pos >> page_shift];
-    return p >= 0 && (uint64_t)p < a.cache.pages ? p : -1;
-  };
-  const unsigned char* kp = static_cast<const unsigned char*>(a.cache.k);
-  const unsigned char* vp = static_cast<const unsigned char*>(a.cache.v);
-  const int k_group = (col >> 2) * 16, v_group = g * 16;      // first of the 16 keys that the lane's A rows (its scores and V) come from
-  const int v_pitch = page_tokens * F::kVSize;
-
-  Keys<BITS, W> kf;
-  Values<BITS, W> vf;
-  float2 ks, vs;                      // the pair of key `lane` of the block
-  int32_t page_k = 0, page_v = 0;     // of the block that the operands hold
-  auto fetch_keys = [&](int64_t kb, int32_t pk, int32_t pv) {
-    const int64_t slot = ((kb + k_group) & (page_tokens - 1)) + (col & 3);
-    load_keys<BITS, W>(kf, kp + (((int64_t)(pk < 0 ? 0 : pk) * heads + head) * page_tokens + slot) * F::kRow + g * (F::kWords >= 4 ? 16 : 8));
-    if constexpr (kCodes) {
-      const int64_t at = ((int64_t)(pv < 0 ? 0 : pv) * heads + head) * page_tokens + ((kb + lane) & (page_tokens - 1));
-      ks = reinterpret_cast<const float2*>(a.cache.k_scale)[at];
-    }
-  };
-  auto fetch_values = [&](int64_t kb, int32_t pv) {
-    const int64_t base = ((int64_t)(pv < 0 ? 0 : pv) * heads + head);
-    load_values<BITS, W>(vf, vp + (base * F::kVRows + col) * v_pitch + ((kb + v_group) & (page_tokens - 1)) * F::kVSize, v_pitch);
-    if constexpr (kCodes) vs = reinterpret_cast<const float2*>(a.cache.v_scale)[base * page_tokens + ((kb + lane) & (page_tokens - 1))];
-  };
-
-  int64_t kb = begin + wave * kBlock;
-  int32_t next_k = -1, next_v = -1;
-  if (kb < end) {
-    page_k = page_of(kb + k_group);
-    page_v = page_of(kb + v_group);
-    fetch_keys(kb, page_k, page_v);
-    fetch_values(kb, page_v);
-    next_k = page_of(kb + kBlock * kWaves + k_group);
-    next_v = page_of(kb + kBlock * kWaves + v_group);
-  }
-  for (; kb < end; kb += kBlock * kWaves) {
-    const bool more = kb + kBlock * kWaves < end;
-    const int32_t after_k = more ? page_of(kb + 2 * kBlock * kWaves + k_group) : -1, after_v = more ? page_of(kb + 2 * kBlock * kWaves + v_group) : -1;
-
-    f32x4 s[QT][4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-#pragma unroll
-      for (int x = 0; x < QT; ++x) s[x][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int t = 0; t < QT; ++t) {
+      const int row = row0 + t * 16 + col;
+      const bool here = row < rows;
+      const bf16_bits* p = a->q + (sq.first + (here ? row / a->group : 0)) * a->q_ts + (int64_t)(head * a->group + (here ? row % a->group : 0)) * a->q_hs;
+      float sum = 0.0f;
 #pragma unroll
       for (int i = 0; i < kOps; ++i) {
-        const bf16x8 kk = key_operand<BITS, W>(kf, t, i);
+        bf16_bits e[8];
+        const int base = entry_of<BITS, W>(i, g, 0);
+        if (a->q_wide) {
+          const u32x4 x = *reinterpret_cast<const u32x4*>(p + base);
 #pragma unroll
-        for (int x = 0; x < QT; ++x) s[x][t] = mfma(kk, qf[x][i], s[x][t]);
+          for (int j = 0; j < 8; ++j) e[j] = (bf16_bits)(x[j / 2] >> (j % 2 * 16));
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) e[j] = p[base + j];
+        }
+        uint32_t u[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int x = entry_of<BITS, W>(i, g, 2 * j) - base, y = entry_of<BITS, W>(i, g, 2 * j + 1) - base;
+          u[j] = here ? e[x] | (uint32_t)e[y] << 16 : 0;
+          if (kCodes && here) sum += bf16_to_f32(e[x]) + bf16_to_f32(e[y]);
+        }
+        qf[t][i] = as_frag(u[0], u[1], u[2], u[3]);
       }
-    }
-    // Keys that some row does not see: of the new tokens, behind the end, or of no page.
-    const bool partial = kb + kBlock > sq.prefix || kb + kBlock > end || __any(page_v < 0);
-    const float2 ks_now = ks;
-    if (more) fetch_keys(kb + kBlock * kWaves, next_k, next_v);
-
-    uint32_t vis[QT];
-    if (partial) {
-      const int64_t pos = kb + v_group;
-      uint32_t exists = 0;
-      if (page_v >= 0 && pos < end) exists = end - pos >= 16 ? 0xffffu : (1u << (int)(end - pos)) - 1;
-      const int64_t j0 = pos - sq.prefix;
-#pragma unroll
-      for (int x = 0; x < QT; ++x) {
-        uint32_t v;
-        if (j0 >= 0)
-          v = j0 < 64 ? (uint32_t)(seen[x] >> j0) : 0;
-        else
-          v = j0 > -16 ? (uint32_t)(seen[x] << -j0) | ((1u << -j0) - 1) : 0xffffu;
-        vis[x] = v & exists;
-      }
-      if constexpr (!kCodes) {
-        // Slots that hold no token yet hold anything: zeros instead, for 0 * NaN is NaN.
-#pragma unroll
-        for (int d = 0; d < F::kVTiles; ++d)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const uint32_t keep = ((exists >> (2 * i)) & 1 ? 0xffffu : 0u) | ((exists >> (2 * i + 1)) & 1 ? 0xffff0000u : 0u);
-            vf.w[d][i] &= keep;
-          }
-      }
+      q_sum[t] = kCodes ? column_sum(sum) : 0.0f;
     }
 
-    // A constant row has step 0 and code 0: its weight goes in as it is, and its offset with it.
-    const float v_step = !kCodes || vs.x == 0.0f ? 1.0f : vs.x;
-    // A step so small that weights times it leave the range: such a token's weight is added to the sum as it is.
-    const bool tiny = kCodes && fabsf(v_step) < 1e-30f;
-    const float v_inv = tiny ? 0.0f : 1.0f / v_step;
-    const float v_off = kCodes ? vs.y / v_step - shifted<BITS>() : 0.0f;
-    uint32_t p[QT][4][2];
+    f32x4 o[QT][kTiles], l_acc[kCodes ? 1 : QT];
+    float m[QT], l_run[kCodes ? QT : 1], c_run[kCodes ? QT : 1];      // maxima as in raise(), sums of weights, what belongs to every entry of a row
 #pragma unroll
-    for (int x = 0; x < QT; ++x) {
-      float v[16];
-      float k_off = 0.0f;
-      if constexpr (kCodes) k_off = (ks_now.y - shifted<BITS>() * ks_now.x) * a.scale_log2;
-      const float k_step = kCodes ? ks_now.x * a.scale_log2 : 0.0f;
-      each<16>([&](auto e) {
-        constexpr int E = decltype(e)::value;
-        const float acc = s[x][E / 4][E % 4];
-        if constexpr (kCodes)
-          v[E] = row_bcast<E>(k_step) * acc + row_bcast<E>(k_off) * q_sum[x];
-        else
-          v[E] = acc * a.scale_log2;
-      });
-      if (partial) {
+    for (int t = 0; t < QT; ++t) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) v[e] = (vis[x] >> e) & 1 ? v[e] : -INFINITY;
+      for (int d = 0; d < kTiles; ++d) o[t][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      if constexpr (kCodes)
+        l_run[t] = c_run[t] = 0.0f;
+      else
+        l_acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      m[t] = -INFINITY;
+    }
+
+    const int page_tokens = (int)a->cache.page_tokens;
+    const int page_shift = 31 - __builtin_clz(page_tokens);
+    const Scalars table = (Scalars)(uintptr_t)(a->batch.table + (int64_t)b * a->batch.table_stride);
+    const int64_t heads = a->cache.heads;
+    const uint32_t pages = (uint32_t)a->cache.pages;
+    const float* const k_scale = a->cache.k_scale;
+    const float* const v_scale = a->cache.v_scale;
+    const float scale = a->scale_log2;
+    auto pages_of = [&](int64_t kb) {
+      Pages p;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int64_t pos = kb + 16 * u;
+        int32_t x = ONE_PAGE && u ? p.at[0] : -1;
+        if (!(ONE_PAGE && u) && pos < end) x = table[pos >> page_shift];
+        p.at[u] = x >= 0 && (uint32_t)x < pages ? x : -1;
       }
-      float top = v[0];
-#pragma unroll
-      for (int e = 1; e < 16; ++e) top = fmaxf(top, v[e]);
-      top = column_max(top);
-      if (__any(top > m_run[x])) {
-        const float m_new = fmaxf(m_run[x], top);
-        const float f = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_run[x] - m_new);
-        m_run[x] = m_new;
+      return p;
+    };
+    const unsigned char* kp = static_cast<const unsigned char*>(a->cache.k);
+    const unsigned char* vp = static_cast<const unsigned char*>(a->cache.v);
+    const int v_pitch = page_tokens * F::kVSize;
+    auto page_at = [&](int32_t p) { return (int64_t)(p < 0 ? 0 : p) * (ONE_PAGE ? heads : kernel_args()->cache.heads) + head; };      // where there is none, reads go to page 0 and are not used
+
+    Keys<BITS, W> kf;
+    Values<BITS, W> vf;
+    float2 ks, vs;                      // the pair of key `lane` of the block
+    auto fetch_keys = [&](int64_t kb, const Pages& p) {
+      const int me = lane_anew(), c = me & 15, part = (me >> 4) * (F::kWords >= 4 ? 16 : 8);
+      if constexpr (ONE_PAGE) {
+        const int64_t at = page_at(p.at[0]) * page_tokens + (kb & (page_tokens - 1));
+        const unsigned char* from = kp + at * F::kRow;
+        const int offset = ((c >> 2) * 16 + (c & 3)) * F::kRow + part;
+        load_keys<BITS, W>(kf, [&](int bytes) { return load_b128(from, offset + bytes, 0); }, [&](int bytes) { return load_b64(from, offset + bytes, 0); });
+        if constexpr (kCodes) ks = __builtin_bit_cast(float2, load_b64(reinterpret_cast<const unsigned char*>(k_scale + 2 * at), me * 8, 0));
+      } else {
+        const unsigned char* from = static_cast<const unsigned char*>(kernel_args()->cache.k) + (page_at(p.pick(c >> 2)) * page_tokens + ((kb + (c >> 2) * 16) & (page_tokens - 1)) + (c & 3)) * F::kRow + part;
+        load_keys<BITS, W>(kf, [&](int bytes) { return *reinterpret_cast<const u32x4*>(from + bytes); },
+                           [&](int bytes) { return *reinterpret_cast<const u32x2*>(from + bytes); });
+        if constexpr (kCodes) ks = reinterpret_cast<const float2*>(kernel_args()->cache.k_scale)[page_at(p.pick(me >> 4)) * page_tokens + ((kb + me) & (page_tokens - 1))];
+      }
+    };
+    auto fetch_values = [&](int64_t kb, const Pages& p) {
+      const int me = lane_anew(), c = me & 15, quarter = me >> 4;
+      if constexpr (ONE_PAGE) {
+        const int slot = (int)(kb & (page_tokens - 1));
+        const unsigned char* from = vp + page_at(p.at[0]) * F::kVRows * v_pitch + slot * F::kVSize;
+        const int offset = c * v_pitch + quarter * 16 * F::kVSize;
+        load_values<BITS, W>(vf, [&](int t, int bytes) { return load_b128(from, offset + bytes, t * 16 * v_pitch); });
+        if constexpr (kCodes) vs = __builtin_bit_cast(float2, load_b64(reinterpret_cast<const unsigned char*>(v_scale + 2 * (page_at(p.at[0]) * page_tokens + slot)), me * 8, 0));
+      } else {
+        const int64_t page = page_at(p.pick(quarter));
+        const unsigned char* from = static_cast<const unsigned char*>(kernel_args()->cache.v) + (page * F::kVRows + c) * v_pitch + ((kb + quarter * 16) & (page_tokens - 1)) * F::kVSize;
+        load_values<BITS, W>(vf, [&](int t, int bytes) {
+          if (t > 0 && bytes == 0) from += 16 * v_pitch;      // (one pointer, not one a tile)
+          return *reinterpret_cast<const u32x4*>(from + bytes);
+        });
+        if constexpr (kCodes) vs = reinterpret_cast<const float2*>(kernel_args()->cache.v_scale)[page * page_tokens + ((kb + me) & (page_tokens - 1))];
+      }
+    };
+    // What the scores and the values have beside step times code, from a pair; see the top.  A constant row has step 0 and code 0: its weight goes
+    // in as it is, and its offset with it.  A step so small that weights times it leave the range: its offset is added by the weight itself.
+    auto step_of = [](float2 x) { return x.x == 0.0f ? 1.0f : x.x; };
+    auto is_tiny = [&](float2 x) { return fabsf(step_of(x)) < 1e-30f; };
+    auto off_of = [&](float2 x) { return is_tiny(x) ? 0.0f : x.y / step_of(x) - shifted<BITS>(); };
+    auto place = [](int e) { return BITS == 4 ? (e % 4 == 1 ? 2 : e % 4 == 2 ? 1 : e % 4) : e % 4; };      // where pack_weights puts weight e of four
+
+    // What is new falls to where the maximum was raised by `by`, and what was with it.
+    auto lower = [&](int x, float by) {
+      const float f = m_factor(by);
+      if constexpr (kCodes) {
         l_run[x] *= f;
         c_run[x] *= f;
-#pragma unroll
-        for (int d = 0; d < kTiles; ++d) o[x][d] *= f;
+      } else {
+        l_acc[x] *= f;
       }
-      const float m = m_run[x] == -INFINITY ? 0.0f : m_run[x];
-      if (__any(tiny)) each<16>([&](auto e) {
-        constexpr int E = decltype(e)::value;
-        l_run[x] += row_bcast<E>(tiny ? 1.0f : 0.0f) * __builtin_amdgcn_exp2f(v[E] - m);
-      });
-      each<16>([&](auto e) {
-        constexpr int E = decltype(e)::value;
-        const float w = __builtin_amdgcn_exp2f(v[E] - m);
-        if constexpr (kCodes) {
-          v[E] = w * row_bcast<E>(v_step);
-          if (partial && !((vis[x] >> E) & 1)) v[E] = 0.0f;      // (whatever pair the slot holds)
-        } else {
-          l_run[x] += w;
-          v[E] = w;
-        }
-      });
 #pragma unroll
-      for (int t = 0; t < 4; ++t) pack_weights<BITS>(v + 4 * t, p[x][t]);
-      if constexpr (kCodes) {
-        each<16>([&](auto e) {
-          constexpr int E = decltype(e)::value;
-          constexpr int kAt = BITS == 4 ? (E % 4 == 1 ? 2 : E % 4 == 2 ? 1 : E % 4) : E % 4;     // where pack_weights put it
-          const uint32_t u = p[x][E / 4][kAt / 2];
-          const float w = __uint_as_float(kAt % 2 ? u & 0xffff0000u : u << 16);
-          const float c = w * row_bcast<E>(v_off), n = w * row_bcast<E>(v_inv);
-          const bool out = partial && !((vis[x] >> E) & 1);
-          c_run[x] += out ? 0.0f : c;
-          l_run[x] += out ? 0.0f : n;
-        });
-      }
-    }
+      for (int d = 0; d < kTiles; ++d) o[x][d] *= f;
+    };
 
-    if constexpr (!kCodes) {
-      // An infinity or a NaN among the values of new tokens is met by the rows that see it only.
-      if (partial) {
+    const int64_t old_end = sq.prefix < end ? sq.prefix : end;
+    const int64_t plain_end = old_end > begin ? begin + (old_end - begin) / kBlock * kBlock : begin;
+    for (int64_t run = begin; run < end; run += kRun) {
+      const int64_t run_end = run + kRun < end ? run + kRun : end, plain = plain_end < run_end ? plain_end : run_end;
+      uint64_t later = 0;               // blocks of the wavefront without a page for some of their tokens
+      int64_t kb = run + wave * kBlock;
+      const bool started = kb < plain;
+      // First the blocks of committed tokens, nearly all.
+      if (started) {
+        Pages ahead = pages_of(kb);
+        fetch_keys(kb, ahead);
+        fetch_values(kb, ahead);
+        bool hole = ahead.missing();
+        ahead = pages_of(kb + kStep);
+        uint64_t bit = 1;
+        for (; kb < plain; kb += kStep, bit <<= 1) {
+          const bool more = kb + kStep < (kThrough ? run_end : plain);
+          const float k_step = kCodes ? ks.x * scale : scale, k_off = kCodes ? (ks.y - shifted<BITS>() * ks.x) * scale : 0.0f;
+          // A block in parts: what of its scores is in registers at a time.
+          each<kParts>([&](auto part) {
+            constexpr int T = decltype(part)::value * kT, E0 = T * 4;          // first key tile, first of the lane's keys
+            f32x4 s[QT][kT];
+#pragma unroll
+            for (int t = 0; t < kT; ++t) {
+#pragma unroll
+              for (int x = 0; x < QT; ++x) s[x][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+              for (int i = 0; i < kOps; ++i) {
+                const bf16x8 kk = key_operand<BITS, W>(kf, T + t, i);
+#pragma unroll
+                for (int x = 0; x < QT; ++x) s[x][t] = mfma(kk, qf[x][i], s[x][t]);
+              }
+              __builtin_amdgcn_sched_barrier(0);      // (operands made ahead of their use fill the registers)
+            }
+            if (T + kT == 4 && more) fetch_keys(kb + kStep, ahead);
+            if (hole) return;
+            float base[QT], top[QT];
+#pragma unroll
+            for (int x = 0; x < QT; ++x) {
+              base[x] = m[x] == -INFINITY ? 0.0f : m[x];
+              top[x] = -INFINITY;
+            }
+            each<4 * kT>([&](auto e) {
+              constexpr int E = decltype(e)::value;
+              const float step = kCodes ? row_bcast<E0 + E>(k_step) : k_step, off = kCodes ? row_bcast<E0 + E>(k_off) : 0.0f;
+#pragma unroll
+              for (int x = 0; x < QT; ++x) {
+                const float y = fmaf(s[x][E / 4][E % 4], step, kCodes ? fmaf(off, q_sum[x], -base[x]) : -base[x]);
+                s[x][E / 4][E % 4] = y;
+                top[x] = fmaxf(top[x], y);
+              }
+            });
+#pragma unroll
+            for (int x = 0; x < QT; ++x) {
+              if (__any(top[x] > (m[x] == -INFINITY ? -INFINITY : kRise))) {
+                const float by = raise(m[x], column_max(top[x]));
+#pragma unroll
+                for (int t = 0; t < kT; ++t) s[x][t] -= by;
+                lower(x, by);
+              }
+            }
+            uint32_t p[QT][kT][2];
+            const float v_step = kCodes ? step_of(vs) : 1.0f, v_off = kCodes ? off_of(vs) : 0.0f;
+#pragma unroll
+            for (int x = 0; x < QT; ++x) {
+              float w[4 * kT];
+#pragma unroll
+              for (int e = 0; e < 4 * kT; ++e) {
+                w[e] = __builtin_amdgcn_exp2f(s[x][e / 4][e % 4]);
+                if constexpr (kCodes) l_run[x] += w[e];
+              }
+              if constexpr (kCodes) {
+                if (__any(is_tiny(vs))) {
+                  const float alone = is_tiny(vs) ? vs.y : 0.0f;
+                  each<4 * kT>([&](auto e) { c_run[x] += w[decltype(e)::value] * row_bcast<E0 + decltype(e)::value>(alone); });
+                }
+                each<4 * kT>([&](auto e) { w[decltype(e)::value] *= row_bcast<E0 + decltype(e)::value>(v_step); });
+              }
+#pragma unroll
+              for (int t = 0; t < kT; ++t) pack_weights<BITS>(w + 4 * t, p[x][t]);
+              if constexpr (kCodes) each<4 * kT>([&](auto e) {
+                constexpr int E = decltype(e)::value;
+                const uint32_t u = p[x][E / 4][place(E) / 2];
+                c_run[x] += __uint_as_float(place(E) % 2 ? u & 0xffff0000u : u << 16) * row_bcast<E0 + E>(v_off);
+              });
+            }
+#pragma unroll
+            for (int h = 0; h < kT / 2; ++h) {
+              bf16x8 pf[QT];
+#pragma unroll
+              for (int x = 0; x < QT; ++x) pf[x] = as_frag(p[x][2 * h][0], p[x][2 * h][1], p[x][2 * h + 1][0], p[x][2 * h + 1][1]);
+#pragma unroll
+              for (int d = 0; d < kTiles; ++d) {
+                const bf16x8 vv = value_operand<BITS, W>(vf, d, T / 2 + h);
+#pragma unroll
+                for (int x = 0; x < QT; ++x) o[x][d] = mfma(vv, pf[x], o[x][d]);
+                if (d % 2) __builtin_amdgcn_sched_barrier(0);
+              }
+              if constexpr (!kCodes) {
+#pragma unroll
+                for (int x = 0; x < QT; ++x) l_acc[x] = mfma(ones, pf[x], l_acc[x]);
+              }
+            }
+          });
+          if (hole) later |= bit;
+          if (more) fetch_values(kb + kStep, ahead);
+          hole = ahead.missing();
+          ahead = pages_of(kb + 2 * kStep);
+        }
+      }
+
+      // Then what was put off, and the blocks of new tokens: one at a time, with every case.
+      number();
+      for (bool fetched = kThrough && started && kb < run_end; later || kb < run_end; fetched = false) {
+        int64_t at = kb;
+        if (later && !fetched) {
+          at = run + wave * kBlock + (int64_t)__builtin_ctzll(later) * kStep;
+          later &= later - 1;
+        } else {
+          kb += kStep;
+        }
+        const Pages p = pages_of(at);
+        if (!fetched) {
+          fetch_keys(at, p);
+          fetch_values(at, p);
+        }
+        const int64_t pos = at + g * 16, j0 = pos - sq.prefix;
+        uint32_t exists = 0;
+        if (pos < end && p.pick(g) >= 0) exists = end - pos >= 16 ? 0xffffu : (1u << (int)(end - pos)) - 1;
         bool odd = false;
+        if constexpr (!kCodes) {
+          // Slots that hold no token hold anything: zeros instead, for 0 * NaN is NaN.  Infinities and NaNs of new tokens are looked after below.
 #pragma unroll
-        for (int d = 0; d < F::kVTiles; ++d)
+          for (int d = 0; d < F::kVTiles; ++d)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) odd = odd || any_nonfinite(vf.w[d][i]);
-        if (__any(odd)) {
-          // One token at a time: its weight alone, then the product with its values alone, in the rows that see it.
-          for (int e = 0; e < kBlock; ++e) {
-            const int eg = e >> 4, bit = e & 15;
-            bool bad = false;
+            for (int i = 0; i < 8; ++i) {
+              vf.w[d][i] &= ((exists >> (2 * i)) & 1 ? 0xffffu : 0u) | ((exists >> (2 * i + 1)) & 1 ? 0xffff0000u : 0u);
+              odd = odd || any_nonfinite(vf.w[d][i]);
+            }
+          odd = __any(odd);
+        }
+        const float k_step = kCodes ? ks.x * scale : scale, k_off = kCodes ? (ks.y - shifted<BITS>() * ks.x) * scale : 0.0f;
+        const float v_step = kCodes ? step_of(vs) : 1.0f, v_off = kCodes ? off_of(vs) : 0.0f, alone = kCodes && is_tiny(vs) ? vs.y : 0.0f;
+#pragma unroll
+        for (int x = 0; x < QT; ++x) {
+          const int row = row0 + x * 16 + col, node = row / a->group;
+          uint64_t seen = 0;
+          if (row < rows) seen = a->mask ? a->mask[sq.first + node] : (2ull << node) - 1;
+          if (sq.count < 64) seen &= (1ull << sq.count) - 1;
+          uint32_t vis;
+          if (j0 >= 0)
+            vis = j0 < 64 ? (uint32_t)(seen >> j0) : 0;
+          else
+            vis = j0 > -16 ? (uint32_t)(seen << -j0) | ((1u << -j0) - 1) : 0xffffu;
+          vis &= exists;
+          if (x) {                      // the operands made anew for the next 16 rows, not kept
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+              for (int i = 0; i < F::kWords; ++i) kf.w[t][i] = anew(kf.w[t][i]);
 #pragma unroll
             for (int d = 0; d < F::kVTiles; ++d)
 #pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const uint32_t h = bit & 1 ? vf.w[d][i] >> 16 : vf.w[d][i] & 0xffffu;
-                bad = bad || (g == eg && (bit >> 1) == i && (h & 0x7f80u) == 0x7f80u);
-              }
-            if (!__any(bad)) continue;
+              for (int i = 0; i < F::kVWords; ++i) vf.w[d][i] = anew(vf.w[d][i]);
+          }
+          float w[16];
+          float top = -INFINITY;
+          const float base = m[x] == -INFINITY ? 0.0f : m[x];
 #pragma unroll
-            for (int d = 0; d < kTiles; ++d) {
-              // value of this token in the result's entries d * 16 + 4 g + r, which lane (4 g + r) of quarter eg holds
-              uint32_t word = 0;
+          for (int t = 0; t < 4; ++t) {
+            f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-              for (int i = 0; i < 8; ++i) word = (bit >> 1) == i ? vf.w[d][i] : word;
-              const uint32_t h = bit & 1 ? word >> 16 : word & 0xffffu;
+            for (int i = 0; i < kOps; ++i) s = mfma(key_operand<BITS, W>(kf, t, i), qf[x][i], s);
 #pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                const uint32_t y = (uint32_t)__shfl((int)h, eg * 16 + g * 4 + r);
-                const bool inf_or_nan = (y & 0x7f80u) == 0x7f80u;
+            for (int r = 0; r < 4; ++r) w[4 * t + r] = s[r];
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          each<16>([&](auto e) {
+            constexpr int E = decltype(e)::value;
+            float y = w[E] * (kCodes ? row_bcast<E>(k_step) : k_step);
+            if constexpr (kCodes) y += row_bcast<E>(k_off) * q_sum[x];
+            w[E] = (vis >> E) & 1 ? y - base : -INFINITY;
+            top = fmaxf(top, w[E]);
+          });
+          const float by = raise(m[x], column_max(top));
+          lower(x, by);
+          uint32_t q[4][2];
+          each<16>([&](auto e) {
+            constexpr int E = decltype(e)::value;
+            w[E] = __builtin_amdgcn_exp2f(w[E] - by);
+            if constexpr (kCodes) {      // (whatever pair the slot holds)
+              l_run[x] += w[E];
+              const float add = w[E] * row_bcast<E>(alone), y = w[E] * row_bcast<E>(v_step);
+              c_run[x] += (vis >> E) & 1 ? add : 0.0f;
+              w[E] = (vis >> E) & 1 ? y : 0.0f;
+            }
+          });
 #pragma unroll
-                for (int x = 0; x < QT; ++x) {
-                  uint32_t pw = 0;
+          for (int t = 0; t < 4; ++t) pack_weights<BITS>(w + 4 * t, q[t]);
+          if constexpr (kCodes) each<16>([&](auto e) {
+            constexpr int E = decltype(e)::value;
+            const uint32_t u = q[E / 4][place(E) / 2];
+            const float add = __uint_as_float(place(E) % 2 ? u & 0xffff0000u : u << 16) * row_bcast<E>(v_off);
+            c_run[x] += (vis >> E) & 1 ? add : 0.0f;
+          });
+          if (!kCodes && odd) {
+            // One token at a time, its values to the rows that see it.
+            for (int e = 0; e < kBlock; ++e) {
+              const int eg = e >> 4, bit = e & 15;
+              uint32_t pw = 0;
 #pragma unroll
-                  for (int i = 0; i < 8; ++i) pw = (bit >> 1) == i ? p[x][i / 2][i % 2] : pw;
-                  const uint32_t ph = (uint32_t)__shfl((int)(bit & 1 ? pw >> 16 : pw & 0xffffu), eg * 16 + col);
-                  const uint32_t vb = (uint32_t)__shfl((int)vis[x], eg * 16 + col);
-                  if (inf_or_nan && ((vb >> bit) & 1)) o[x][d][r] += bf16_to_f32((bf16_bits)ph) * bf16_to_f32((bf16_bits)y);
+              for (int i = 0; i < 8; ++i) pw = (bit >> 1) == i ? q[i / 2][i % 2] : pw;
+              const float one = bf16_to_f32((bf16_bits)__shfl((int)(bit & 1 ? pw >> 16 : pw & 0xffffu), eg * 16 + col));
+              const bool sees = (__shfl((int)vis, eg * 16 + col) >> bit) & 1;
+#pragma unroll
+              for (int d = 0; d < kTiles; ++d) {
+                // its values in the result's entries d * 16 + 4 g + r, which lane 4 g + r of quarter eg holds
+                uint32_t word = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) word = (bit >> 1) == i ? vf.w[d % F::kVTiles][i % F::kVWords] : word;
+                const uint32_t h = bit & 1 ? word >> 16 : word & 0xffffu;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                  const uint32_t y = (uint32_t)__shfl((int)h, eg * 16 + g * 4 + r);
+                  if (sees && (y & 0x7f80u) == 0x7f80u) o[x][d][r] += one * bf16_to_f32((bf16_bits)y);
                 }
               }
             }
           }
 #pragma unroll
-          for (int d = 0; d < F::kVTiles; ++d)
+          for (int h = 0; h < 2; ++h) {
+            const bf16x8 pf = as_frag(q[2 * h][0], q[2 * h][1], q[2 * h + 1][0], q[2 * h + 1][1]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              uint32_t y = vf.w[d][i];
-              if ((y & 0x7f80u) == 0x7f80u) y &= 0xffff0000u;
-              if ((y & 0x7f800000u) == 0x7f800000u) y &= 0x0000ffffu;
-              vf.w[d][i] = y;
+            for (int d = 0; d < kTiles; ++d) {
+              u32x4 z = __builtin_bit_cast(u32x4, value_operand<BITS, W>(vf, d, h));
+              if (!kCodes && odd) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  if ((z[j] & 0x7f80u) == 0x7f80u) z[j] &= 0xffff0000u;
+                  if ((z[j] & 0x7f800000u) == 0x7f800000u) z[j] &= 0x0000ffffu;
+                }
+              }
+              o[x][d] = mfma(__builtin_bit_cast(bf16x8, z), pf, o[x][d]);
+              if (d % 2) __builtin_amdgcn_sched_barrier(0);
             }
+            if constexpr (!kCodes) l_acc[x] = mfma(ones, pf, l_acc[x]);
+          }
         }
       }
     }
 
+    // A row's sums over the lanes that shared its keys, and the constant that belongs to every entry of its result.
+    number();
+    float l[QT];
 #pragma unroll
-    for (int m = 0; m < 2; ++m) {
+    for (int x = 0; x < QT; ++x) {
+      l[x] = kCodes ? column_sum(l_run[kCodes ? x : 0]) : l_acc[kCodes ? 0 : x][0];
+      if constexpr (kCodes) {
+        const float c = column_sum(c_run[x]);
 #pragma unroll
-      for (int d = 0; d < kTiles; ++d) {
-        const bf16x8 vv = value_operand<BITS, W>(vf, d, m);
-#pragma unroll
-        for (int x = 0; x < QT; ++x) o[x][d] = mfma(vv, as_frag(p[x][2 * m][0], p[x][2 * m][1], p[x][2 * m + 1][0], p[x][2 * m + 1][1]), o[x][d]);
+        for (int d = 0; d < kTiles; ++d) o[x][d] += c;
       }
     }
-    if (more) fetch_values(kb + kBlock * kWaves, next_v);
-    page_k = next_k;
-    page_v = next_v;
-    next_k = after_k;
-    next_v = after_v;
-  }
-
-  number();
-  // A row's sums over the lanes that shared its keys; the constant that belongs to every entry of the result.
+    // Wavefronts 2 and 3 into 0 and 1, then 1 into 0.
 #pragma unroll
-  for (int x = 0; x < QT; ++x) {
-    l_run[x] = column_sum(l_run[x]);
-    if constexpr (kCodes) {
-      const float c = column_sum(c_run[x]);
+    for (int half = kWaves / 2; half > 0; half /= 2) {
+      if (wave >= half && wave < 2 * half) {
 #pragma unroll
-      for (int d = 0; d < kTiles; ++d) o[x][d] += c;
-    }
-  }
-  // Wavefronts 2 and 3 into 0 and 1, then 1 into 0.
+        for (int x = 0; x < QT; ++x) {
 #pragma unroll
-  for (int half = kWaves / 2; half > 0; half /= 2) {
-    if (wave >= half && wave < 2 * half) {
-#pragma unroll
-      for (int x = 0; x < QT; ++x) {
-#pragma unroll
-        for (int d = 0; d < kTiles; ++d) *reinterpret_cast<f32x4*>(s_o[wave - half][x * kTiles + d][lane]) = o[x][d];
-        s_ml[wave - half][x][0][lane] = m_run[x];
-        s_ml[wave - half][x][1][lane] = l_run[x];
+          for (int d = 0; d < kTiles; ++d) *reinterpret_cast<f32x4*>(s_o[wave - half][x * kTiles + d][lane]) = o[x][d];
+          s_ml[wave - half][x][0][lane] = m[x];
+          s_ml[wave - half][x][1][lane] = l[x];
+        }
       }
-    }
-    __syncthreads();
-    if (wave < half) {
+      __syncthreads();
+      if (wave < half) {
 #pragma unroll
-      for (int x = 0; x < QT; ++x) {
-        const float m2 = s_ml[wave][x][0][lane], l2 = s_ml[wave][x][1][lane];
-        const float m_new = fmaxf(m_run[x], m2);
-        const float f1 = m_run[x] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run[x] - m_new);
-        const float f2 = m2 == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m2 - m_new);
-        m_run[x] = m_new;
-        l_run[x] = l_run[x] * f1 + l2 * f2;
+        for (int x = 0; x < QT; ++x) {
+          const float m2 = s_ml[wave][x][0][lane], l2 = s_ml[wave][x][1][lane];
+          const float m_new = fmaxf(m[x], m2);
+          const float f1 = m[x] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[x] - m_new);
+          const float f2 = m2 == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m2 - m_new);
+          m[x] = m_new;
+          l[x] = l[x] * f1 + l2 * f2;
 #pragma unroll
-        for (int d = 0; d < kTiles; ++d) o[x][d] = o[x][d] * f1 + *reinterpret_cast<const f32x4*>(s_o[wave][x * kTiles + d][lane]) * f2;
+          for (int d = 0; d < kTiles; ++d) o[x][d] = o[x][d] * f1 + *reinterpret_cast<const f32x4*>(s_o[wave][x * kTiles + d][lane]) * f2;
+        }
       }
+      __syncthreads();
     }
-    __syncthreads();
-  }
-  if (wave) continue;
+    if (wave) continue;
 
 #pragma unroll
-  for (int x = 0; x < QT; ++x) {
-    const int row = row0 + x * 16 + col;
-    if (row >= rows) continue;
-    if (piece.whole) {
+    for (int x = 0; x < QT; ++x) {
+      const int row = row0 + x * 16 + col;
+      if (row >= rows) continue;
+      if (piece.whole) {
 #pragma unroll
-      for (int d = 0; d < kTiles; ++d) store_row4(a, sq, head, row, d * 16 + g * 4, o[x][d], l_run[x]);
-    } else {
-      const int64_t at = part_at(a, head, row_tile, piece.slot, row - row0);
+        for (int d = 0; d < kTiles; ++d) store_row4(a, sq, head, row, d * 16 + g * 4, o[x][d], l[x]);
+      } else {
+        const int64_t at = part_at(a, head, row_tile, piece.slot, row - row0);
 #pragma unroll
-      for (int d = 0; d < kTiles; ++d) *reinterpret_cast<f32x4*>(a.part + at * W + d * 16 + g * 4) = o[x][d];
-      if (g == 0) a.part_ml[at] = make_float2(m_run[x], l_run[x]);
+        for (int d = 0; d < kTiles; ++d) *reinterpret_cast<f32x4*>(a->part + at * W + d * 16 + g * 4) = o[x][d];
+        if (g == 0) a->part_ml[at] = make_float2(m[x], l[x]);
+      }
     }
-  }
   }
 }
 
 // Joins a row's pieces.  WAVES = 1: a wavefront a row, for up to 64 pieces; 4: a workgroup a row, for up to 256.  W / 4
 // lanes read a piece's result as 16-byte vectors, 256 / W pieces at a time, and the first ones are under way before the maxima are.
 template <int W, int WAVES>
-__global__ void __launch_bounds__(256) k_tree_join(const TreeArgs a) {
+__global__ void __launch_bounds__(256) k_tree_join(const TreeArgs) {
+  const Args a = kernel_args();
   constexpr int kLanes = W / 4, kAt = 64 / kLanes;      // lanes of a piece, pieces of a wavefront at a time
   constexpr int kFirst = 4;                             // vectors a lane takes ahead
   __shared__ float s_f[256];
@@ -478,20 +593,20 @@ __global__ void __launch_bounds__(256) k_tree_join(const TreeArgs a) {
 
   const int b = blockIdx.y;
   const Sequence sq = sequence_of(a, b);
-  const int64_t heads = a.cache.heads;
+  const int64_t heads = a->cache.heads;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int64_t id = WAVES == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
   const int row = (int)(id / heads), head = (int)(id % heads);
-  if (row >= sq.count * a.group) return;
-  const int row_tile = row / a.tile_rows;
-  const Layout layout(a, row_tile * a.tile_rows, lane);
+  if (row >= sq.count * a->group) return;
+  const int row_tile = row / a->tile_rows;
+  const Layout layout(a, row_tile * a->tile_rows, lane);
   int from = 0, to = 0;
   layout.range(b, &from, &to);
   const int p0 = from / layout.each, chunks = (to - 1) / layout.each - p0 + 1;
   if (chunks <= 1) return;
   // the first piece may be its workgroup's last, the others are their workgroups' first
   const int slot0 = 2 * p0 + (from > p0 * layout.each);
-  auto at = [&](int c) { return part_at(a, head, row_tile, c ? 2 * (p0 + c) : slot0, row - row_tile * a.tile_rows); };
+  auto at = [&](int c) { return part_at(a, head, row_tile, c ? 2 * (p0 + c) : slot0, row - row_tile * a->tile_rows); };
   const int first = (WAVES == 1 ? 0 : wave * kAt) + lane / kLanes;
   constexpr int kNext = WAVES * kAt;
   const int entry = lane % kLanes * 4;
@@ -499,9 +614,9 @@ __global__ void __launch_bounds__(256) k_tree_join(const TreeArgs a) {
   f32x4 v[kFirst];
 #pragma unroll
   for (int i = 0; i < kFirst; ++i)
-    if (first + i * kNext < chunks) v[i] = *reinterpret_cast<const f32x4*>(a.part + at(first + i * kNext) * W + entry);
+    if (first + i * kNext < chunks) v[i] = *reinterpret_cast<const f32x4*>(a->part + at(first + i * kNext) * W + entry);
   const int mine = WAVES == 1 ? lane : (int)threadIdx.x;
-  const float2 ml = mine < chunks ? a.part_ml[at(mine)] : make_float2(-INFINITY, 0.0f);
+  const float2 ml = mine < chunks ? a->part_ml[at(mine)] : make_float2(-INFINITY, 0.0f);
   float m = wave_max(ml.x);
   if constexpr (WAVES > 1) {
     if (lane == 0) s_red[0][wave] = m;
@@ -530,7 +645,7 @@ __global__ void __launch_bounds__(256) k_tree_join(const TreeArgs a) {
   for (int c0 = kFirst * kNext; c0 < chunks; c0 += kNext) {
     const int c = c0 + first;
     const float w = factor(c & 255);
-    if (c < chunks) add(*reinterpret_cast<const f32x4*>(a.part + at(c) * W + entry), w);
+    if (c < chunks) add(*reinterpret_cast<const f32x4*>(a->part + at(c) * W + entry), w);
   }
 #pragma unroll
   for (int off = kLanes; off < 64; off *= 2)
@@ -551,13 +666,14 @@ __global__ void __launch_bounds__(256) k_tree_join(const TreeArgs a) {
 // Joins the pieces of 16 rows as the workgroups of many rows leave them (their registers' layout): a wavefront takes two of the result's tiles of
 // 16 entries, a lane four entries of one row.
 template <int W>
-__global__ void __launch_bounds__(W * 2) k_tree_join_tiles(const TreeArgs a) {
+__global__ void __launch_bounds__(W * 2) k_tree_join_tiles(const TreeArgs) {
+  const Args a = kernel_args();
   const int b = blockIdx.z, head = blockIdx.y, row0 = blockIdx.x * 16;
   const Sequence sq = sequence_of(a, b);
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
-  if (row0 >= sq.count * a.group) return;
-  const int row_tile = row0 / a.tile_rows, in_tile = row0 - row_tile * a.tile_rows;
-  const Layout layout(a, row_tile * a.tile_rows, lane);
+  if (row0 >= sq.count * a->group) return;
+  const int row_tile = row0 / a->tile_rows, in_tile = row0 - row_tile * a->tile_rows;
+  const Layout layout(a, row_tile * a->tile_rows, lane);
   int from = 0, to = 0;
   layout.range(b, &from, &to);
   const int p0 = from / layout.each, pieces = (to - 1) / layout.each - p0 + 1;
@@ -566,13 +682,13 @@ __global__ void __launch_bounds__(W * 2) k_tree_join_tiles(const TreeArgs a) {
 
   float m = -INFINITY;
 #pragma unroll 4
-  for (int c = 0; c < pieces; ++c) m = fmaxf(m, a.part_ml[at(c) + col].x);
+  for (int c = 0; c < pieces; ++c) m = fmaxf(m, a->part_ml[at(c) + col].x);
   f32x4 o[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
   float l = 0.0f;
 #pragma unroll 4
   for (int c = 0; c < pieces; ++c) {
-    const float2 ml = a.part_ml[at(c) + col];
-    const float* const p = a.part + at(c) * W + wave * 512 + lane * 4;
+    const float2 ml = a->part_ml[at(c) + col];
+    const float* const p = a->part + at(c) * W + wave * 512 + lane * 4;
     const f32x4 v0 = *reinterpret_cast<const f32x4*>(p), v1 = *reinterpret_cast<const f32x4*>(p + 256);
     const float f = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml.x - m);
     l += ml.y * f;
@@ -581,7 +697,7 @@ __global__ void __launch_bounds__(W * 2) k_tree_join_tiles(const TreeArgs a) {
       o[1] += v1 * f;
     }
   }
-  if (row0 + col >= sq.count * a.group) return;
+  if (row0 + col >= sq.count * a->group) return;
 #pragma unroll
   for (int i = 0; i < 2; ++i) store_row4(a, sq, head, row0 + col, (wave * 2 + i) * 16 + g * 4, o[i], l);
 }
@@ -600,7 +716,8 @@ Plan plan_of(const conqur_tree_call& c) {
   const int64_t room = (int64_t)c.batch.table_columns * c.cache.page_tokens;
   p.context = (int64_t)(c.max_context < (uint64_t)room ? c.max_context : (uint64_t)room);
   const int rows = (int)(c.max_query * (c.q.heads / c.cache.heads));
-  p.wide = rows > 32;
+  // 17 to 32 rows: of codes, a wavefront's registers hold 64 keys and values and two tiles of results; bf16 values are laid out in LDS.
+  p.wide = rows > (c.cache.bits == 16 ? 16 : 32);
   // Rows of a wavefront in sixteens: as few as pad the rows least; 48 rows of bf16 values 128 wide do not fit its registers.
   p.qt = rows <= 16 ? 1 : 2;
   if (p.wide) {
@@ -654,10 +771,16 @@ hipError_t launch(const TreeArgs& a, const Plan& p, hipStream_t s) {
   if (p.wide) {
     e = launch_wide(a, p.qt, grid, s);
   } else {
-    if (p.qt == 1)
-      k_tree<BITS, W, 1><<<grid, 64 * kWaves, 0, s>>>(a);
+    constexpr int kMostTiles = BITS == 16 ? 1 : 2;
+    const bool one_page = a.cache.page_tokens >= (uint32_t)kBlock;
+    if (p.qt == 1 && one_page)
+      k_tree<BITS, W, 1, true><<<grid, 64 * kWaves, 0, s>>>(a);
+    else if (p.qt == 1)
+      k_tree<BITS, W, 1, false><<<grid, 64 * kWaves, 0, s>>>(a);
+    else if (one_page)
+      k_tree<BITS, W, kMostTiles, true><<<grid, 64 * kWaves, 0, s>>>(a);
     else
-      k_tree<BITS, W, 2><<<grid, 64 * kWaves, 0, s>>>(a);
+      k_tree<BITS, W, kMostTiles, false><<<grid, 64 * kWaves, 0, s>>>(a);
     e = hipGetLastError();
   }
   if (e != hipSuccess || p.splits <= 1) return e;

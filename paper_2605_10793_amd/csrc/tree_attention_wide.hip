@@ -14,8 +14,6 @@ namespace tree {
 
 namespace {
 
-constexpr float kRise = 16.0f;            // by how much (log2) scores may exceed the maximum they are taken against
-constexpr int kRun = 16384;            // keys after which blocks that were put off are made up for
 constexpr int kDepth = 4;                  // blocks whose steps and zeros are in LDS
 
 template <int BITS, int W>
@@ -75,16 +73,6 @@ __device__ __forceinline__ int key_at(int t, int i, int c) {
 }
 __device__ __forceinline__ int value_at(int d, int c) { return d * kBlock * 2 + ((c ^ ((d >> 1) & 7)) << 4); }
 
-// Takes the running maximum m to where the highest of new scores, `top` above it, is (none: -inf): what was and what is new fall by the returned amount.
-__device__ __forceinline__ float raise(float& m, float top) {
-  const bool unset = m == -INFINITY;
-  const float by = unset ? (top == -INFINITY ? 0.0f : top) : fmaxf(top, 0.0f);
-  m = unset ? top : m + by;
-  return by;
-}
-// The factor on sums over the scores before that; before the first of them they are 0 and `by` may be anything.
-__device__ __forceinline__ float m_factor(float by) { return __builtin_amdgcn_exp2f(-fmaxf(by, 0.0f)); }
-
 // Four codes (bytes of x) less z, as bf16.
 __device__ __forceinline__ u32x2 less_zero(uint32_t x, float z) {
   return u32x2{f32x2_to_bf16x2((float)(x & 0xff) - z, (float)((x >> 8) & 0xff) - z), f32x2_to_bf16x2((float)((x >> 16) & 0xff) - z, (float)(x >> 24) - z)};
@@ -95,7 +83,8 @@ __device__ __forceinline__ u32x2 less_zeros(uint32_t x, f32x4 z) {
 }
 
 template <int BITS, int W, int QT>
-__global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs a) {
+__global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs) {
+  Args a = kernel_args();
   using F = Format<BITS, W>;
   using D = Wide<BITS, W>;
   constexpr int kOps = W / 32, kTiles = W / 16;
@@ -108,22 +97,23 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs a) 
   int* const s_flag = reinterpret_cast<int*>(shared + D::kFlagAt);          // of a pair's slot: K's tokens, V's tokens have rests
   uint16_t* const s_later = reinterpret_cast<uint16_t*>(s_flag + 2 * kDepth);
 
-  const int head = blockIdx.x / a.row_tiles, row_tile = blockIdx.x % a.row_tiles;
+  const int head = blockIdx.x / a->row_tiles, row_tile = blockIdx.x % a->row_tiles;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int row0 = (row_tile * kWaves + wave) * 16 * QT;
   Pieces piece;
-  for (bool first = true; piece.next(a, row_tile * 64 * QT, threadIdx.x & 63, first); first = false) {
+  for (bool first = true; piece.next(a, row_tile * 64 * QT, first); first = false) {
   int tid, lane, col, g;
   auto number = [&] {
-    tid = anew(threadIdx.x);
-    lane = tid & 63;
+    a = kernel_args();
+    lane = lane_anew();
+    tid = wave * 64 + lane;
     col = lane & 15;
     g = lane >> 4;
   };
   number();
   const int b = piece.b;
   const Sequence sq = sequence_of(a, b);
-  const int rows = sq.count * a.group;
+  const int rows = sq.count * a->group;
   const bool idle = row0 >= rows;        // still loads and meets the barriers
   const int64_t piece_end = (int64_t)piece.last * kBlock < sq.length ? (int64_t)piece.last * kBlock : sq.length;
 
@@ -132,24 +122,24 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs a) 
   for (int t = 0; t < QT; ++t) {
     const int row = row0 + t * 16 + col;
     const bool here = row < rows;
-    const bf16_bits* p = a.q + (sq.first + (here ? row / a.group : 0)) * a.q_ts + (int64_t)(head * a.group + (here ? row % a.group : 0)) * a.q_hs;
+    const bf16_bits* p = a->q + (sq.first + (here ? row / a->group : 0)) * a->q_ts + (int64_t)(head * a->group + (here ? row % a->group : 0)) * a->q_hs;
 #pragma unroll
     for (int i = 0; i < kOps; ++i) {
       const int base = (i * 4 + g) * 8;
       u32x4 x = {0, 0, 0, 0};
       if (here) {
-        if (a.q_wide) {
+        if (a->q_wide) {
           x = *reinterpret_cast<const u32x4*>(p + base);
         } else {
 #pragma unroll
           for (int j = 0; j < 4; ++j) x[j] = p[base + 2 * j] | (uint32_t)p[base + 2 * j + 1] << 16;
         }
       }
-      if (a.scale_log2 < 0.0f) x ^= 0x80008000u;          // the maxima below are taken before the scale
+      if (a->scale_log2 < 0.0f) x ^= 0x80008000u;          // the maxima below are taken before the scale
       qf[t][i] = __builtin_bit_cast(bf16x8, x);
     }
   }
-  const float scale = fabsf(a.scale_log2);
+  const float scale = fabsf(a->scale_log2);
   const bf16x8 ones = as_frag(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);      // a row of the sums of the weights as they are rounded
 
   // m is what scores are taken against: the running maximum, or up to kRise less, since every rise multiplies all results; -inf before the first
@@ -167,19 +157,18 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs a) 
     m[t] = -INFINITY;
   }
 
-  const int page_tokens = (int)a.cache.page_tokens;
+  const int page_tokens = (int)a->cache.page_tokens;
   const int page_shift = 31 - __builtin_clz(page_tokens);
   // (read by the scalar unit: a vector load would be waited for together with the keys that are under way)
-  const Scalars table = (Scalars)(uintptr_t)(a.batch.table + (int64_t)b * a.batch.table_stride);
-  const int64_t heads = a.cache.heads;
-  const unsigned char* kp = static_cast<const unsigned char*>(a.cache.k);
-  const unsigned char* vp = static_cast<const unsigned char*>(a.cache.v);
+  const Scalars table = (Scalars)(uintptr_t)(a->batch.table + (int64_t)b * a->batch.table_stride);
+  const int64_t heads = a->cache.heads;
+  const uint32_t pages = (uint32_t)a->cache.pages;
+  const float* const k_scale = a->cache.k_scale;
+  const float* const v_scale = a->cache.v_scale;
+  const unsigned char* kp = static_cast<const unsigned char*>(a->cache.k);
+  const unsigned char* vp = static_cast<const unsigned char*>(a->cache.v);
 
   int64_t end = piece_end;               // of the run that is worked on
-  // Pages of a block's four groups of 16 keys, -1 where there is none.
-  struct Pages {
-    int32_t at[4];
-  };
   auto pages_of = [&](int64_t kb) {
     Pages p;
 #pragma unroll
@@ -187,14 +176,9 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs a) 
       const int64_t pos = kb + 16 * u;
       int32_t x = -1;
       if (pos < end) x = table[pos >> page_shift];
-      p.at[u] = x >= 0 && (uint64_t)x < a.cache.pages ? x : -1;
+      p.at[u] = x >= 0 && (uint32_t)x < pages ? x : -1;
     }
     return p;
-  };
-  auto pick = [](Pages p, int u) {
-    const int32_t a0 = p.at[0], a1 = p.at[1], a2 = p.at[2], a3 = p.at[3];
-    const int32_t lo = u & 1 ? a1 : a0, hi = u & 1 ? a3 : a2;
-    return u & 2 ? hi : lo;
   };
 
   const int64_t k_page = heads * page_tokens * F::kRow, v_page = heads * F::kVRows * page_tokens * F::kVSize;
@@ -203,14 +187,14 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs a) 
   auto page_or_0 = [](int32_t p) { return (int64_t)(p < 0 ? 0 : p); };
   // Bytes at to at + 16 of key `key` of the block from kb on, and of tokens key to key + kVKeys - 1 of V row d.
   auto key_source = [&](int64_t kb, const Pages& p, int key, int at) {
-    return kp + page_or_0(pick(p, key >> 4)) * k_page + k_head + ((kb + key) & (page_tokens - 1)) * F::kRow + at;
+    return kp + page_or_0(p.pick(key >> 4)) * k_page + k_head + ((kb + key) & (page_tokens - 1)) * F::kRow + at;
   };
   auto value_source = [&](int64_t kb, const Pages& p, int d, int key) {
-    return vp + page_or_0(pick(p, key >> 4)) * v_page + v_head + ((kb + key) & (page_tokens - 1)) * F::kVSize + d * page_tokens * F::kVSize;
+    return vp + page_or_0(p.pick(key >> 4)) * v_page + v_head + ((kb + key) & (page_tokens - 1)) * F::kVSize + d * page_tokens * F::kVSize;
   };
   // Runs over the thread's units: keys(unit, u), values(unit, u).
   auto units = [&](auto keys, auto values) {
-    const int first = anew(tid);         // (what a unit's place gives is made here, not kept in registers)
+    const int first = wave * 64 + lane_anew();         // (what a unit's place gives is made here, not kept in registers)
     if constexpr (D::kApart) {
       if (wave < 2)
         keys(first, 0);
@@ -227,9 +211,9 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs a) 
   auto send = [&](int64_t kb, int block, const Pages& p) {
     if constexpr (kCodes) {
       if (wave == 0) {       // the pairs, two tokens a lane: keys' to lanes 0 to 31, values' to the others
-        const int half = anew(lane) & 31, token = half * 2;
-        const int64_t at = (page_or_0(pick(p, token >> 4)) * heads + head) * page_tokens + ((kb + token) & (page_tokens - 1));
-        to_lds(reinterpret_cast<const unsigned char*>((anew(lane) < 32 ? a.cache.k_scale : a.cache.v_scale) + 2 * at), s_raw(block) + 2 * D::kKAll * 16);
+        const int me = lane_anew(), half = me & 31, token = half * 2;
+        const int64_t at = (page_or_0(p.pick(token >> 4)) * heads + head) * page_tokens + ((kb + token) & (page_tokens - 1));
+        to_lds(reinterpret_cast<const unsigned char*>((me < 32 ? k_scale : v_scale) + 2 * at), s_raw(block) + 2 * D::kKAll * 16);
       }
     }
     const int w64 = D::kApart ? (wave & 1) * 64 : wave * 64;
@@ -361,15 +345,14 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs a) 
   const int blocks = old_end > begin ? (int)((old_end - begin) / kBlock) : 0;
   const int all_blocks = (int)((end - begin + kBlock - 1) / kBlock);
   constexpr int kAhead = kCodes ? 2 : 1;
-  auto missing = [](const Pages& p) { return (p.at[0] | p.at[1] | p.at[2] | p.at[3]) < 0 ? 1u : 0u; };
   int later = 0;
   if (blocks > 0) {
     Pages ahead = pages_of(begin);       // of the block that is sent for next
-    uint32_t holes = missing(ahead);     // bit j: block n + j has no page for some of its tokens
+    uint32_t holes = ahead.missing();     // bit j: block n + j has no page for some of its tokens
     send(begin, 0, ahead);
     if constexpr (kCodes) {
       ahead = pages_of(begin + kBlock);
-      holes |= missing(ahead) << 1;
+      holes |= (uint32_t)ahead.missing() << 1;
       wait_loads<0>();
       lay_pairs(0);
       if (blocks > 1) send(begin + kBlock, 1, ahead);
@@ -380,7 +363,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs a) 
     for (int n = 0; n < blocks; ++n) {
       const int64_t kb = begin + (int64_t)n * kBlock;
       const bool more = n + kAhead < blocks;
-      holes |= missing(ahead) << kAhead;
+      holes |= (uint32_t)ahead.missing() << kAhead;
       if constexpr (kCodes) {
         // all but what was sent for last, the units of block n + 1: its pairs were sent for before them
         if (n + 1 < blocks) {
@@ -501,10 +484,10 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs a) 
     if (tid == 0) s_flag[1] = 0;
     if constexpr (kCodes) {
       if (wave < 2) {
-        const int32_t page = pick(p, g);
+        const int32_t page = p.pick(g);
         const int64_t at = (page_or_0(page) * heads + head) * page_tokens + ((kb + lane) & (page_tokens - 1));
         float2 x = make_float2(0.0f, 0.0f);
-        if (page >= 0 && kb + lane < end) x = reinterpret_cast<const float2*>(wave ? a.cache.v_scale : a.cache.k_scale)[at];
+        if (page >= 0 && kb + lane < end) x = reinterpret_cast<const float2*>(wave ? v_scale : k_scale)[at];
         lay_pair(0, wave, x);
       }
     }
@@ -515,7 +498,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs a) 
             if constexpr (BITS == 16) {
               // slots that hold no token hold anything; infinities and NaNs of new tokens are looked after below
               const int part = unit % D::kVParts;
-              const int64_t left = pick(p, part >> 1) < 0 ? 0 : end - kb - part * 8;
+              const int64_t left = p.pick(part >> 1) < 0 ? 0 : end - kb - part * 8;
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
                 x[j] &= (left > 2 * j ? 0xffffu : 0u) | (left > 2 * j + 1 ? 0xffff0000u : 0u);
@@ -539,12 +522,12 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs a) 
     }
     const int64_t pos = kb + g * 16, j0 = pos - sq.prefix;
     uint32_t exists = 0;
-    if (pos < end && pick(p, g) >= 0) exists = end - pos >= 16 ? 0xffffu : (1u << (int)(end - pos)) - 1;
+    if (pos < end && p.pick(g) >= 0) exists = end - pos >= 16 ? 0xffffu : (1u << (int)(end - pos)) - 1;
 #pragma unroll
     for (int x = 0; x < QT; ++x) {
-      const int row = row0 + x * 16 + col, node = row / a.group;
+      const int row = row0 + x * 16 + col, node = row / a->group;
       uint64_t seen = 0;
-      if (row < rows) seen = a.mask ? a.mask[sq.first + node] : (2ull << node) - 1;
+      if (row < rows) seen = a->mask ? a->mask[sq.first + node] : (2ull << node) - 1;
       if (sq.count < 64) seen &= (1ull << sq.count) - 1;
       uint32_t vis;
       if (j0 >= 0)
@@ -652,7 +635,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs a) 
     const int row = row0 + x * 16 + col;
     const float l = kCodes ? column_sum(l_run[kCodes ? x : 0]) : l_acc[kCodes ? 0 : x][0];
     if (!piece.whole) {      // as the registers have it, 16 rows a tile: whole lines of memory
-      float* const to = a.part + part_at(a, head, row_tile, piece.slot, row0 + x * 16 - row_tile * 64 * QT) * W + lane * 4;
+      float* const to = a->part + part_at(a, head, row_tile, piece.slot, row0 + x * 16 - row_tile * 64 * QT) * W + lane * 4;
 #pragma unroll
       for (int d = 0; d < kTiles; ++d) *reinterpret_cast<f32x4*>(to + d * 256) = o[x][d];
     }
@@ -661,7 +644,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs a) 
 #pragma unroll
       for (int d = 0; d < kTiles; ++d) store_row4(a, sq, head, row, d * 16 + g * 4, o[x][d], l);
     } else {
-      if (g == 0) a.part_ml[part_at(a, head, row_tile, piece.slot, row - row_tile * 64 * QT)] = make_float2(m[x], l);
+      if (g == 0) a->part_ml[part_at(a, head, row_tile, piece.slot, row - row_tile * 64 * QT)] = make_float2(m[x], l);
     }
   }
   }
