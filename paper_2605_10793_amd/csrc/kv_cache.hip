@@ -123,15 +123,15 @@ __global__ void __launch_bounds__(kThreads) k_append(const AppendArgs a) {
   // touches at most n / 64 + 2 blocks of slots).
   const int64_t id = blockIdx.x;
   const int head = blockIdx.y;
+  // The last sequence whose first block is not behind this one, each lane of a wavefront asking for one: one read for up to 64 sequences, three
+  // for the most, where halving takes six and sixteen, each behind the other.
+  const int sequences = (int)a.batch.sequences;
   int b = 0;
-  for (int lo = 0, hi = (int)a.batch.sequences - 1; lo <= hi;) {
-    const int mid = (lo + hi) / 2;
-    if (clamp_to(a.batch.start[mid], a.tokens) / kBlock + 2 * (int64_t)mid <= id) {
-      b = mid;
-      lo = mid + 1;
-    } else {
-      hi = mid - 1;
-    }
+  for (int step = sequences <= 64 ? 1 : sequences <= 4096 ? 64 : 4096; step; step = step == 1 ? 0 : step / 64) {
+    const int64_t x = b + (int64_t)(threadIdx.x & 63) * step;
+    const bool begun = x < sequences && clamp_to(a.batch.start[x], a.tokens) / kBlock + 2 * x <= id;
+    const int n = __popcll(__ballot(begun));
+    b += n ? (n - 1) * step : 0;
   }
   const int64_t first = clamp_to(a.batch.start[b], a.tokens);
   const int64_t count = clamp_to(a.batch.start[b + 1], a.tokens) - first;
@@ -146,17 +146,20 @@ __global__ void __launch_bounds__(kThreads) k_append(const AppendArgs a) {
   const int64_t heads = a.cache.heads;
 
   const int lane = threadIdx.x % kLanes, row0 = threadIdx.x / kLanes;
+  for (int r = row0; r < kBlock; r += kRows) {
+    const int64_t pos = base + r;
+    if (pos < prefix || pos >= end) continue;
+    const int32_t page = table[pos / page_tokens];
+    if (page < 0 || (uint64_t)page >= a.cache.pages) continue;
+    const int64_t token = first + pos - prefix;
+    const int64_t at = ((int64_t)page * heads + head) * page_tokens + pos % page_tokens;
+    uint32_t rows[2][8];
 #pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    for (int r = row0; r < kBlock; r += kRows) {
-      const int64_t pos = base + r;
-      if (pos < prefix || pos >= end) continue;
-      const int32_t page = table[pos / page_tokens];
-      if (page < 0 || (uint64_t)page >= a.cache.pages) continue;
-      const int64_t token = first + pos - prefix;
-      const int64_t at = ((int64_t)page * heads + head) * page_tokens + pos % page_tokens;
-      uint32_t u[8];
-      load16(a.in[which] + token * a.in_ts[which] + head * a.in_hs[which] + 8 * lane, W / 2, a.wide[which], u);
+    for (int which = 0; which < 2; ++which)
+      load16(a.in[which] + token * a.in_ts[which] + head * a.in_hs[which] + 8 * lane, W / 2, a.wide[which], rows[which]);
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      const uint32_t* u = rows[which];
       if constexpr (BITS == 16) {
         if (which == 0) {
           store16(static_cast<bf16_bits*>(a.cache.k) + at * W + 8 * lane, W / 2, true, u);

@@ -29,6 +29,7 @@ namespace {
 
 constexpr int kWaves = 4;            // wavefronts of a workgroup
 constexpr int kMaxWidth = 512;
+constexpr int kGradVector = 4;       // (8 bf16 entries a lane take 190 registers with the next rows under way, half the wavefronts: 60.8 us for the 58.9 below)
 constexpr int kGradGroups = 1024;    // workgroups of the gradient's launch: four of 4 wavefronts on each of 256 compute units
 
 struct View {                        // [token][head][width], entries next to each other
@@ -173,58 +174,67 @@ __device__ __forceinline__ void rotate_unit(float* x, const float* cs, const flo
   }
 }
 
+// The angles of a token's pairs, at `place`: whole turns are dropped in 64 bits.  The place is one wavefront's own, whose LDS accesses stay in order:
+// no barrier (which would also wait for the rows that are being written), only that the compiler keeps that order.
+__device__ __forceinline__ void put_angles(const RotaryArgs& a, int64_t position, double first_turns, int lane, float2* place) {
+  const double pos = (double)position;
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  for (int p = lane; p < a.part / 2; p += 64) {
+    const double t = pos * (p == lane ? first_turns : a.turns[p]);
+    float sn, cs;
+    sincospif(2.0f * (float)(t - floor(t)), &sn, &cs);
+    place[p] = make_float2(cs * a.magnitude, (a.transposed ? -sn : sn) * a.magnitude);
+  }
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+template <int V, int U, bool INTERLEAVED>
+__device__ __forceinline__ void take_angles(const Units<V, U, INTERLEAVED>& unit, const float2* place, float (*cs)[V], float (*sn)[V]) {
+#pragma unroll
+  for (int i = 0; i < U; ++i)
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const float2 x = unit.pair[i] >= 0 ? place[unit.pair[i] + j] : make_float2(1.0f, 0.0f);
+      cs[i][j] = x.x;
+      sn[i][j] = x.y;
+    }
+}
+
+// A wavefront's task: steps [first, end) of a token.
+struct Task {
+  int64_t token;
+  int first, end;
+  __device__ __forceinline__ Task(const RotaryArgs& a, int64_t task) {
+    token = task / a.chunks;
+    first = (int)(task - token * a.chunks) * a.chunk_steps;
+    end = min(first + a.chunk_steps, a.steps[0] + a.steps[1]);
+  }
+};
+
 template <typename T, int V, int U, bool INTERLEAVED, Mode MODE>
 __global__ void __launch_bounds__(64 * kWaves) k_rotary(const RotaryArgs a) {
   __shared__ float2 s_angle[kWaves][kMaxWidth / 2];
-  __shared__ float s_sum[MODE == kGrad ? kWaves : 1][MODE == kGrad ? kMaxWidth : 1];
 
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int lanes = a.lanes, rows = 64 / lanes, row = lane / lanes;
   const Units<V, U, INTERLEAVED> unit(lane % lanes, lanes, a.width, a.part);
-  float dw[2][U][2 * V];
-  if constexpr (MODE == kGrad) {
-#pragma unroll
-    for (int i = 0; i < 2 * U * 2 * V; ++i) (&dw[0][0][0])[i] = 0.0f;
-  }
-
-  // Every wavefront of the workgroup makes the same number of turns: the barriers below are met by all of them.
+  const double turns = lane < a.part / 2 ? a.turns[lane] : 0.0;
   const int64_t stride = (int64_t)gridDim.x * kWaves;
-  for (int64_t base = (int64_t)blockIdx.x * kWaves; base < a.tasks; base += stride) {
-    const int64_t task = base + wave;
-    const bool live = task < a.tasks;
-    const int64_t token = live ? task / a.chunks : 0;
-    const int first_step = live ? (int)(task - token * a.chunks) * a.chunk_steps : 0;
-    const int all_steps = a.steps[0] + a.steps[1];
-    const int end_step = live ? min(first_step + a.chunk_steps, all_steps) : 0;
-
-    if (live) {
-      const double pos = (double)a.positions[token];
-      for (int p = lane; p < a.part / 2; p += 64) {
-        const double t = pos * a.turns[p];
-        float sn, cs;
-        sincospif(2.0f * (float)(t - floor(t)), &sn, &cs);
-        s_angle[wave][p] = make_float2(cs * a.magnitude, (a.transposed ? -sn : sn) * a.magnitude);
-      }
-    }
-    __syncthreads();
+  for (int64_t at = (int64_t)blockIdx.x * kWaves + wave; at < a.tasks; at += stride) {
+    const Task task(a, at);
+    put_angles(a, a.positions[task.token], turns, lane, s_angle[wave]);
     float cs[U][V], sn[U][V];
-#pragma unroll
-    for (int i = 0; i < U; ++i)
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const float2 x = unit.pair[i] >= 0 ? s_angle[wave][unit.pair[i] + j] : make_float2(1.0f, 0.0f);
-        cs[i][j] = x.x;
-        sn[i][j] = x.y;
-      }
-    __syncthreads();
+    take_angles(unit, s_angle[wave], cs, sn);
 
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
-      const int lo = which ? max(first_step - a.steps[0], 0) : first_step;
-      const int hi = which ? end_step - a.steps[0] : min(end_step, a.steps[0]);
+      const int lo = which ? max(task.first - a.steps[0], 0) : task.first;
+      const int hi = which ? task.end - a.steps[0] : min(task.end, a.steps[0]);
       if (lo >= hi) continue;
       float w[U][2 * V];
-      if constexpr (MODE != kRotary) {
+      if constexpr (MODE == kNorm) {
         const T* pw = static_cast<const T*>(a.w[which]);
 #pragma unroll
         for (int i = 0; i < U; ++i)
@@ -233,69 +243,38 @@ __global__ void __launch_bounds__(64 * kWaves) k_rotary(const RotaryArgs a) {
             load_vec<V>(pw + unit.b[i], w[i] + V);
           }
       }
-      const T* pin = static_cast<const T*>(a.in[which].p) + token * a.in[which].ts;
-      T* pout = const_cast<T*>(static_cast<const T*>(a.out[which].p)) + token * a.out[which].ts;
-      const T* pgrad = MODE == kGrad ? static_cast<const T*>(a.grad[which].p) + token * a.grad[which].ts : nullptr;
+      const T* pin = static_cast<const T*>(a.in[which].p) + task.token * a.in[which].ts;
+      T* pout = const_cast<T*>(static_cast<const T*>(a.out[which].p)) + task.token * a.out[which].ts;
       for (int step = lo; step < hi; ++step) {
         const int head = step * rows + row;
         const bool here = head < a.heads[which];
-        float x[U][2 * V], g[U][2 * V];
+        float x[U][2 * V];
 #pragma unroll
         for (int i = 0; i < U; ++i)
           if (here && unit.pair[i] > -2) {
             const T* p = pin + head * a.in[which].hs;
             load_vec<V>(p + unit.a[i], x[i]);
             load_vec<V>(p + unit.b[i], x[i] + V);
-            if constexpr (MODE == kGrad) {
-              const T* q = pgrad + head * a.grad[which].hs;
-              load_vec<V>(q + unit.a[i], g[i]);
-              load_vec<V>(q + unit.b[i], g[i] + V);
-            }
           } else {
 #pragma unroll
-            for (int j = 0; j < 2 * V; ++j) x[i][j] = g[i][j] = 0.0f;
+            for (int j = 0; j < 2 * V; ++j) x[i][j] = 0.0f;
           }
 
-        float rstd = 1.0f;
-        if constexpr (MODE != kRotary) {
+        if constexpr (MODE == kNorm) {
           float s = 0.0f;
 #pragma unroll
           for (int i = 0; i < U; ++i)
 #pragma unroll
             for (int j = 0; j < 2 * V; ++j) s += x[i][j] * x[i][j];
-          rstd = 1.0f / sqrtf(group_sum(s, lanes) * a.inv_width + a.eps);
-        }
-        if constexpr (MODE == kNorm) {
+          const float rstd = 1.0f / sqrtf(group_sum(s, lanes) * a.inv_width + a.eps);
 #pragma unroll
           for (int i = 0; i < U; ++i)
 #pragma unroll
             for (int j = 0; j < 2 * V; ++j) x[i][j] = x[i][j] * rstd * w[i][j];
         }
-        if constexpr (MODE != kGrad) {
 #pragma unroll
-          for (int i = 0; i < U; ++i)
-            if (unit.pair[i] >= 0) rotate_unit<V, INTERLEAVED>(x[i], cs[i], sn[i]);
-        } else {
-          float s = 0.0f;
-#pragma unroll
-          for (int i = 0; i < U; ++i) {
-            if (unit.pair[i] >= 0) rotate_unit<V, INTERLEAVED>(g[i], cs[i], sn[i]);
-            if (here && unit.pair[i] > -2) {     // (a lane without a row has nothing to add, whatever its 1 / sqrt(eps))
-#pragma unroll
-              for (int j = 0; j < 2 * V; ++j) {
-                x[i][j] *= rstd;                 // x^
-                dw[which][i][j] += g[i][j] * x[i][j];
-                g[i][j] *= w[i][j];
-                s += g[i][j] * x[i][j];
-              }
-            }
-          }
-          s = group_sum(s, lanes) * a.inv_width;
-#pragma unroll
-          for (int i = 0; i < U; ++i)
-#pragma unroll
-            for (int j = 0; j < 2 * V; ++j) x[i][j] = rstd * (g[i][j] - x[i][j] * s);
-        }
+        for (int i = 0; i < U; ++i)
+          if (unit.pair[i] >= 0) rotate_unit<V, INTERLEAVED>(x[i], cs[i], sn[i]);
 #pragma unroll
         for (int i = 0; i < U; ++i)
           if (here && unit.pair[i] > -2) {
@@ -306,27 +285,166 @@ __global__ void __launch_bounds__(64 * kWaves) k_rotary(const RotaryArgs a) {
       }
     }
   }
+}
 
-  if constexpr (MODE == kGrad) {
+// V entries as they are in memory.
+template <typename T, int V>
+struct alignas(V * sizeof(T)) Packed {
+  T e[V];
+  __device__ __forceinline__ void load(const T* p) { *this = *reinterpret_cast<const Packed*>(p); }
+  __device__ __forceinline__ void unpack(float* v) const {
 #pragma unroll
-    for (int which = 0; which < 2; ++which) {
+    for (int i = 0; i < V; ++i) v[i] = load1(e + i);
+  }
+};
+
+template <typename T>
+struct Packed<T, 1> {
+  float e;
+  __device__ __forceinline__ void load(const T* p) { e = load1(p); }
+  __device__ __forceinline__ void unpack(float* v) const { *v = e; }
+};
+
+// As above, with the rows of the next step, of the next token after a token's last, under way while one is computed.
+template <typename T, int V, int U, bool INTERLEAVED>
+__global__ void __launch_bounds__(64 * kWaves, V == 1 ? 2 : 4) k_norm_gradient(const RotaryArgs a) {
+  __shared__ float2 s_angle[kWaves][kMaxWidth / 2];
+  __shared__ float s_sum[kWaves][kMaxWidth];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int lanes = a.lanes, rows = 64 / lanes, row = lane / lanes;
+  const Units<V, U, INTERLEAVED> unit(lane % lanes, lanes, a.width, a.part);
+  const double turns = lane < a.part / 2 ? a.turns[lane] : 0.0;
+  float dw[2][U][2 * V];
+  Packed<T, V> w[2][U][2];
+#pragma unroll
+  for (int which = 0; which < 2; ++which)
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+#pragma unroll
+      for (int j = 0; j < 2 * V; ++j) dw[which][i][j] = 0.0f;
+      if (a.heads[which] && unit.pair[i] > -2) {
+        const T* p = static_cast<const T*>(a.w[which]);
+        w[which][i][0].load(p + unit.a[i]);
+        w[which][i][1].load(p + unit.b[i]);
+      }
+    }
+
+  Packed<T, V> xs[U][2], gs[U][2];
+  auto fetch = [&](int64_t token, int step) {
+    const int which = step >= a.steps[0];
+    const int head = (which ? step - a.steps[0] : step) * rows + row;
+    if (head < (which ? a.heads[1] : a.heads[0])) {
+      const View in = which ? a.in[1] : a.in[0], grad = which ? a.grad[1] : a.grad[0];
+      const T* p = static_cast<const T*>(in.p) + token * in.ts + head * in.hs;
+      const T* q = static_cast<const T*>(grad.p) + token * grad.ts + head * grad.hs;
 #pragma unroll
       for (int i = 0; i < U; ++i)
-#pragma unroll
-        for (int j = 0; j < 2 * V; ++j) {
-          float v = dw[which][i][j];
-          for (int o = lanes; o < 64; o <<= 1) v += __shfl_xor(v, o);
-          if (row == 0 && unit.pair[i] > -2) s_sum[wave][(j < V ? unit.a[i] : unit.b[i] - V) + j] = v;
+        if (unit.pair[i] > -2) {
+          xs[i][0].load(p + unit.a[i]);
+          xs[i][1].load(p + unit.b[i]);
+          gs[i][0].load(q + unit.a[i]);
+          gs[i][1].load(q + unit.b[i]);
         }
-      __syncthreads();
-      for (int c = threadIdx.x; c < a.width; c += 64 * kWaves) {
-        float v = 0.0f;
-#pragma unroll
-        for (int i = 0; i < kWaves; ++i) v += s_sum[i][c];
-        a.part_sums[((int64_t)blockIdx.x * 2 + which) * a.width + c] = v;
-      }
-      __syncthreads();
     }
+  };
+
+  const int64_t stride = (int64_t)gridDim.x * kWaves;
+  int64_t at = (int64_t)blockIdx.x * kWaves + wave;
+  int64_t position = 0;
+  if (at < a.tasks) {
+    const Task task(a, at);
+    position = a.positions[task.token];
+    fetch(task.token, task.first);
+  }
+  for (; at < a.tasks; at += stride) {
+    const Task task(a, at), then(a, at + stride < a.tasks ? at + stride : at);
+    put_angles(a, position, turns, lane, s_angle[wave]);
+    position = a.positions[then.token];
+    float cs[U][V], sn[U][V];
+    take_angles(unit, s_angle[wave], cs, sn);
+
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      const int before = which ? a.steps[0] : 0;
+      const int lo = max(task.first, before), hi = which ? task.end : min(task.end, a.steps[0]);
+      T* pout = const_cast<T*>(static_cast<const T*>(a.out[which].p)) + task.token * a.out[which].ts;
+      for (int step = lo; step < hi; ++step) {
+        const int head = (step - before) * rows + row;
+        const bool here = head < a.heads[which];
+        float x[U][2 * V], g[U][2 * V];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            xs[i][h].unpack(x[i] + h * V);
+            gs[i][h].unpack(g[i] + h * V);
+          }
+          if (!here || unit.pair[i] < -1) {      // (nothing to add, whatever its 1 / sqrt(eps))
+#pragma unroll
+            for (int j = 0; j < 2 * V; ++j) x[i][j] = g[i][j] = 0.0f;
+          }
+        }
+        if (step + 1 < task.end)
+          fetch(task.token, step + 1);
+        else if (at + stride < a.tasks)
+          fetch(then.token, then.first);
+
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+#pragma unroll
+          for (int j = 0; j < 2 * V; ++j) s += x[i][j] * x[i][j];
+        const float rstd = 1.0f / sqrtf(group_sum(s, lanes) * a.inv_width + a.eps);
+        s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          if (unit.pair[i] >= 0) rotate_unit<V, INTERLEAVED>(g[i], cs[i], sn[i]);
+          if (here && unit.pair[i] > -2) {
+            float ws[2 * V];
+            w[which][i][0].unpack(ws);
+            w[which][i][1].unpack(ws + V);
+#pragma unroll
+            for (int j = 0; j < 2 * V; ++j) {
+              x[i][j] *= rstd;                 // x^
+              dw[which][i][j] += g[i][j] * x[i][j];
+              g[i][j] *= ws[j];
+              s += g[i][j] * x[i][j];
+            }
+          }
+        }
+        s = group_sum(s, lanes) * a.inv_width;
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+          if (here && unit.pair[i] > -2) {
+#pragma unroll
+            for (int j = 0; j < 2 * V; ++j) x[i][j] = rstd * (g[i][j] - x[i][j] * s);
+            T* p = pout + head * a.out[which].hs;
+            store_vec<V>(p + unit.a[i], x[i]);
+            store_vec<V>(p + unit.b[i], x[i] + V);
+          }
+      }
+    }
+  }
+
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+      for (int j = 0; j < 2 * V; ++j) {
+        float v = dw[which][i][j];
+        for (int o = lanes; o < 64; o <<= 1) v += __shfl_xor(v, o);
+        if (row == 0 && unit.pair[i] > -2) s_sum[wave][(j < V ? unit.a[i] : unit.b[i] - V) + j] = v;
+      }
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.width; c += 64 * kWaves) {
+      float v = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) v += s_sum[i][c];
+      a.part_sums[((int64_t)blockIdx.x * 2 + which) * a.width + c] = v;
+    }
+    __syncthreads();
   }
 }
 
@@ -354,10 +472,16 @@ __global__ void __launch_bounds__(1024) k_weight_sums(const float* __restrict__ 
 
 template <typename T, int V, int U, Mode MODE>
 hipError_t launch_layout(const RotaryArgs& a, int layout, int groups, hipStream_t s) {
-  if (layout)
+  if constexpr (MODE == kGrad) {
+    if (layout)
+      k_norm_gradient<T, V, U, true><<<groups, 64 * kWaves, 0, s>>>(a);
+    else
+      k_norm_gradient<T, V, U, false><<<groups, 64 * kWaves, 0, s>>>(a);
+  } else if (layout) {
     k_rotary<T, V, U, true, MODE><<<groups, 64 * kWaves, 0, s>>>(a);
-  else
+  } else {
     k_rotary<T, V, U, false, MODE><<<groups, 64 * kWaves, 0, s>>>(a);
+  }
   return hipGetLastError();
 }
 
@@ -368,7 +492,7 @@ bool aligned(const View& v, int64_t elems, int esz, int heads) {
 
 // Vector length: the longest whose units cut both the rotated and the copied part, and at whose alignment every row starts.
 int vector_length(const RotaryArgs& a, int esz, Mode mode) {
-  for (int v = 16 / esz; v > 1; v = v == 8 ? 4 : 1) {
+  for (int v = mode == kGrad ? kGradVector : 16 / esz; v > 1; v = v == 8 ? 4 : 1) {
     if (a.part % (2 * v) || (a.width - a.part) % (2 * v)) continue;
     bool ok = true;
     for (int i = 0; i < 2; ++i) {
@@ -405,7 +529,9 @@ hipError_t launch(RotaryArgs& a, bool f32, int layout, int* groups_out, hipStrea
     if (v == 4) return launch_layout<float, 4, 1, MODE>(a, layout, (int)groups, s);
     return launch_layout<float, 1, 4, MODE>(a, layout, (int)groups, s);
   }
-  if (v == 8) return launch_layout<bf16_bits, 8, 1, MODE>(a, layout, (int)groups, s);
+  if constexpr (MODE != kGrad) {
+    if (v == 8) return launch_layout<bf16_bits, 8, 1, MODE>(a, layout, (int)groups, s);
+  }
   if (v == 4) return launch_layout<bf16_bits, 4, 1, MODE>(a, layout, (int)groups, s);
   return launch_layout<bf16_bits, 1, 4, MODE>(a, layout, (int)groups, s);
 }
