@@ -126,17 +126,24 @@ __global__ void __launch_bounds__(kThreads) k_append(const AppendArgs a) {
   // The last sequence whose first block is not behind this one, each lane of a wavefront asking for one: one read for up to 64 sequences, three
   // for the most, where halving takes six and sixteen, each behind the other.
   const int sequences = (int)a.batch.sequences;
-  int b = 0;
+  int b = 0, from = 0, to = 0, before = 0;      // the sequence, its tokens, its prefix
   for (int step = sequences <= 64 ? 1 : sequences <= 4096 ? 64 : 4096; step; step = step == 1 ? 0 : step / 64) {
     const int64_t x = b + (int64_t)(threadIdx.x & 63) * step;
-    const bool begun = x < sequences && clamp_to(a.batch.start[x], a.tokens) / kBlock + 2 * x <= id;
-    const int n = __popcll(__ballot(begun));
-    b += n ? (n - 1) * step : 0;
+    if (x < sequences) {
+      from = clamp_to(a.batch.start[x], a.tokens);
+      to = clamp_to(a.batch.start[x + 1], a.tokens);
+      before = a.batch.prefix[x];
+    }
+    const int n = max(__popcll(__ballot(x < sequences && from / kBlock + 2 * x <= id)), 1) - 1;
+    b += n * step;
+    if (step == 1) {
+      from = __builtin_amdgcn_readlane(from, n);
+      to = __builtin_amdgcn_readlane(to, n);
+      before = __builtin_amdgcn_readlane(before, n);
+    }
   }
-  const int64_t first = clamp_to(a.batch.start[b], a.tokens);
-  const int64_t count = clamp_to(a.batch.start[b + 1], a.tokens) - first;
-  const int64_t prefix = a.batch.prefix[b] < 0 ? 0 : a.batch.prefix[b];
-  const int page_tokens = (int)a.cache.page_tokens;
+  const int64_t first = from, count = (int64_t)to - from, prefix = before < 0 ? 0 : before;
+  const int page_tokens = (int)a.cache.page_tokens, page_shift = 31 - __builtin_clz(page_tokens);
   const int64_t room = (int64_t)a.batch.table_columns * page_tokens;
   const int64_t end = prefix + count < room ? prefix + count : room;
   const int64_t k = id - (first / kBlock + 2 * (int64_t)b);
@@ -149,10 +156,10 @@ __global__ void __launch_bounds__(kThreads) k_append(const AppendArgs a) {
   for (int r = row0; r < kBlock; r += kRows) {
     const int64_t pos = base + r;
     if (pos < prefix || pos >= end) continue;
-    const int32_t page = table[pos / page_tokens];
+    const int32_t page = table[pos >> page_shift];
     if (page < 0 || (uint64_t)page >= a.cache.pages) continue;
     const int64_t token = first + pos - prefix;
-    const int64_t at = ((int64_t)page * heads + head) * page_tokens + pos % page_tokens;
+    const int64_t at = ((int64_t)page * heads + head) * page_tokens + (pos & (page_tokens - 1));
     uint32_t rows[2][8];
 #pragma unroll
     for (int which = 0; which < 2; ++which)
@@ -208,10 +215,10 @@ __global__ void __launch_bounds__(kThreads) k_append(const AppendArgs a) {
     const int d = u / (kBlock / 16), group = u % (kBlock / 16);
     const int64_t pos = base + group * 16;
     if (pos + 16 <= prefix || pos >= end) continue;
-    const int32_t page = table[pos / page_tokens];
+    const int32_t page = table[pos >> page_shift];
     if (page < 0 || (uint64_t)page >= a.cache.pages) continue;
     unsigned char* out = static_cast<unsigned char*>(a.cache.v) +
-                         ((((int64_t)page * heads + head) * kOut + d) * page_tokens + pos % page_tokens) * kSize;
+                         ((((int64_t)page * heads + head) * kOut + d) * page_tokens + (pos & (page_tokens - 1))) * kSize;
     const unsigned char* s = s_v + group * 16 * kPitch + d * kSize;
     if (pos >= prefix && pos + 16 <= end) {
       uint32_t w[4 * kSize];
