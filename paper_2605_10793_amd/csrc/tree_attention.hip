@@ -250,11 +250,10 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree(const TreeArgs) {
         if constexpr (kCodes) vs = reinterpret_cast<const float2*>(kernel_args()->cache.v_scale)[page * page_tokens + ((kb + me) & (page_tokens - 1))];
       }
     };
-    // What the scores and the values have beside step times code, from a pair; see the top.  A constant row has step 0 and code 0: its weight goes
-    // in as it is, and its offset with it.  A step so small that weights times it leave the range: its offset is added by the weight itself.
-    auto step_of = [](float2 x) { return x.x == 0.0f ? 1.0f : x.x; };
-    auto is_tiny = [&](float2 x) { return fabsf(step_of(x)) < 1e-30f; };
-    auto off_of = [&](float2 x) { return is_tiny(x) ? 0.0f : x.y / step_of(x) - shifted<BITS>(); };
+    // What the scores and the values have beside step times code, from a pair; see the top.  With a step of 0 (a constant row) or one so small that
+    // weights times it leave the range, the offset is added by the weight itself.
+    auto is_tiny = [&](float2 x) { return fabsf(x.x) < 1e-30f; };
+    auto off_of = [&](float2 x) { return is_tiny(x) ? 0.0f : x.y / x.x - shifted<BITS>(); };
     auto place = [](int e) { return BITS == 4 ? (e % 4 == 1 ? 2 : e % 4 == 2 ? 1 : e % 4) : e % 4; };      // where pack_weights puts weight e of four
 
     // What is new falls to where the maximum was raised by `by`, and what was with it.
@@ -332,7 +331,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree(const TreeArgs) {
               }
             }
             uint32_t p[QT][kT][2];
-            const float v_step = kCodes ? step_of(vs) : 1.0f, v_off = kCodes ? off_of(vs) : 0.0f;
+            const float v_step = kCodes ? vs.x : 1.0f, v_off = kCodes ? off_of(vs) : 0.0f;
 #pragma unroll
             for (int x = 0; x < QT; ++x) {
               float w[4 * kT];
@@ -412,7 +411,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree(const TreeArgs) {
           odd = __any(odd);
         }
         const float k_step = kCodes ? ks.x * scale : scale, k_off = kCodes ? (ks.y - shifted<BITS>() * ks.x) * scale : 0.0f;
-        const float v_step = kCodes ? step_of(vs) : 1.0f, v_off = kCodes ? off_of(vs) : 0.0f, alone = kCodes && is_tiny(vs) ? vs.y : 0.0f;
+        const float v_step = kCodes ? vs.x : 1.0f, v_off = kCodes ? off_of(vs) : 0.0f, alone = kCodes && is_tiny(vs) ? vs.y : 0.0f;
 #pragma unroll
         for (int x = 0; x < QT; ++x) {
           const int row = row0 + x * 16 + col, node = row / a->group;

@@ -262,16 +262,15 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs) {
             });
     }
   };
-  // Steps, zeros and rests of a block's tokens.  A constant row's offset becomes its step, its code 1 (0 less a zero of -1); a pair that is not finite
-  // goes into the step alone, so that it meets the rows that see it and no others.
+  // Steps, zeros and rests of a block's tokens.  A pair that is not finite goes into the step alone, so that it meets the rows that see it and no
+  // others.
   auto lay_pair = [&](int block, int which, float2 x) {
     float step = x.x, zero = rintf(fminf(fmaxf(-x.y / x.x, 0.0f), (float)((1 << (BITS == 16 ? 8 : BITS)) - 1)));
     float rest = fmaf(step, zero, x.y);
     if (fabsf(rest) <= 0x1p-20f * fabsf(x.y)) rest = 0.0f;        // the rounding of offset = -step * zero
     if (step == 0.0f) {
-      step = x.y;
-      zero = -1.0f;
-      rest = 0.0f;
+      zero = 0.0f;
+      rest = x.y;
     }
     if (!(fabsf(x.x) < INFINITY) || !(fabsf(x.y) < INFINITY)) {
       step = NAN;
