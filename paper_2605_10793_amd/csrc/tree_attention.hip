@@ -739,7 +739,8 @@ Plan plan_of(const conqur_tree_call& c) {
   if (splits > most) splits = most;
   if (splits > kMaxSplits) splits = kMaxSplits;
   if (splits < 1) splits = 1;
-  p.splits = blocks <= kWaves || sequences > kMaxScan || sequences * groups >= 4096 ? 0 : (int)splits;
+  // (blocks are counted in 31 bits)
+  p.splits = blocks <= kWaves || sequences > kMaxScan || sequences * groups >= 4096 || blocks * sequences >= 1ll << 31 ? 0 : (int)splits;
   return p;
 }
 
