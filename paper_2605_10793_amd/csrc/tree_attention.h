@@ -92,8 +92,7 @@ __device__ __forceinline__ int lane_anew() {
 }
 
 // Blocks of a sequence for a row tile that begins at row0: none if it has no such rows, otherwise one at least (which writes zeros if nothing is seen).
-__device__ __forceinline__ int blocks_of(Args a, int b, int row0) {
-  const Sequence s = sequence_of_lane(a, b);
+__device__ __forceinline__ int blocks_in(Args a, const Sequence& s, int row0) {
   if (row0 >= s.count * a->group) return 0;
   return s.length > kBlock ? (int)((s.length + kBlock - 1) / kBlock) : 1;
 }
@@ -121,7 +120,7 @@ struct Layout {
       end[c] = all;
       if (c * 64 < (int)a->batch.sequences) {
         const int b = c * 64 + lane;
-        end[c] = all + wave_scan(b < (int)a->batch.sequences ? blocks_of(a, b, row0) : 0);
+        end[c] = all + wave_scan(b < (int)a->batch.sequences ? blocks_in(a, sequence_of_lane(a, b), row0) : 0);
         all = __builtin_amdgcn_readlane(end[c], 63);
       }
     }
@@ -185,24 +184,36 @@ struct Pieces {
       if (!begin) return false;
       b = blockIdx.y;
       first = 0;
-      last = blocks_of(a, b, row0);
+      last = blocks_in(a, sequence_of(a, b), row0);
       whole = true;
       return last > 0;
     }
-    const Layout l(a, row0, lane_anew());
-    const int start = (int)blockIdx.y * l.each;
     if (begin) {
-      x = start;
+      const Layout l(a, row0, lane_anew());
+      x = (int)blockIdx.y * l.each;
       stop = l.all - x < l.each ? l.all : x + l.each;
+      if (x >= stop) return false;
+      int from = 0, to = 0;
+      l.find(a, x, &b, &from, &to);
+      first = x - from;
+      last = (to < stop ? to : stop) - from;
+      whole = first == 0 && from + last == to;
+      slot = 2 * (int)blockIdx.y;
+      x = from + last;
+      return true;
     }
+    // What follows begins with the next sequence that has blocks.
     if (x >= stop) return false;
-    int from = 0, to = 0;
-    l.find(a, x, &b, &from, &to);
-    first = x - from;
-    last = (to < stop ? to : stop) - from;
-    whole = first == 0 && from + last == to;
-    slot = 2 * (int)blockIdx.y + (x > start);
-    x = from + last;
+    int n = 0;
+    while (n == 0) {
+      if (++b >= (int)a->batch.sequences) return false;
+      n = blocks_in(a, sequence_of(a, b), row0);
+    }
+    first = 0;
+    last = n < stop - x ? n : stop - x;
+    whole = last == n;
+    slot = 2 * (int)blockIdx.y + 1;
+    x += last;
     return true;
   }
 };

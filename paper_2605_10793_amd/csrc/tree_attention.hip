@@ -739,8 +739,12 @@ Plan plan_of(const conqur_tree_call& c) {
   if (splits > most) splits = most;
   if (splits > kMaxSplits) splits = kMaxSplits;
   if (splits < 1) splits = 1;
-  // (blocks are counted in 31 bits)
-  p.splits = blocks <= kWaves || sequences > kMaxScan || sequences * groups >= 4096 || blocks * sequences >= 1ll << 31 ? 0 : (int)splits;
+  // A workgroup for each sequence, which needs no join and finds its work at once, where the sequences are short (one of 200 tokens: 12.1 us for 13.8
+  // in runs; 64 of 200 to 250: 18.4 for 23.5) or where there are many and none is so long that it would be waited for (256 of 500 to 8000
+  // tokens in 4 bits, 8 heads: 260 us for 294; 512 of 500 to 2000: 166 for 244; but 64 of 501 to 8190 in 16 bits: 230 for 209).  More sequences than a
+  // wavefront can look through, or more blocks than 31 bits count, take that way too.
+  const bool short_ones = blocks <= kWaves, many = sequences * groups >= 2048 && blocks <= 256;
+  p.splits = short_ones || many || sequences > kMaxScan || blocks * sequences >= 1ll << 31 ? 0 : (int)splits;
   return p;
 }
 
@@ -787,6 +791,8 @@ hipError_t launch(const TreeArgs& a, const Plan& p, hipStream_t s) {
   const int64_t rows = (int64_t)a.max_query * a.group * a.cache.heads;
   if (p.wide)
     k_tree_join_tiles<W><<<dim3((a.max_query * a.group + 15) / 16, a.cache.heads, a.batch.sequences), W * 2, 0, s>>>(a);
+  // A wavefront a row, or four where there are few rows and they have many pieces (one sequence of 30000 tokens: 33.3 us with four, 40.5 with one;
+  // 16 of 2000 to 9000 tokens, 16 rows a head: 39.8 with one, 42.6 with four).
   else if (p.splits <= 64 && p.splits <= 8 * (int64_t)a.batch.sequences)
     k_tree_join<W, 1><<<dim3((uint32_t)((rows + 3) / 4), a.batch.sequences), 256, 0, s>>>(a);
   else
