@@ -739,12 +739,14 @@ Plan plan_of(const conqur_tree_call& c) {
   if (splits > most) splits = most;
   if (splits > kMaxSplits) splits = kMaxSplits;
   if (splits < 1) splits = 1;
-  // A workgroup for each sequence, which needs no join and finds its work at once, where the sequences are short (one of 200 tokens: 12.1 us for 13.8
-  // in runs; 64 of 200 to 250: 18.4 for 23.5) or where there are many and none is so long that it would be waited for (256 of 500 to 8000
-  // tokens in 4 bits, 8 heads: 260 us for 294; 512 of 500 to 2000: 166 for 244; but 64 of 501 to 8190 in 16 bits: 230 for 209).  More sequences than a
-  // wavefront can look through, or more blocks than 31 bits count, take that way too.
-  const bool short_ones = blocks <= kWaves, many = sequences * groups >= 2048 && blocks <= 256;
-  p.splits = short_ones || many || sequences > kMaxScan || blocks * sequences >= 1ll << 31 ? 0 : (int)splits;
+  // A workgroup for each sequence, which needs no join and finds its work at once, where no sequence is so long that it would be waited for: up to 4
+  // blocks (one of 200 tokens: 12.1 us for 13.8 in runs); up to 32 if they fill the device (8 heads, 64 sequences of 20 to 1000 tokens in 4 bits
+  // 18.4 us for 36.8, of 600 to 2000 in 16 bits 76.5 for 78.9); up to 128 if they do so four times (256 of 500 to 4000 in 8 bits 240 for 279, of
+  // 500 to 8000 in 16 bits 811 for 772).  Longer ones gain from runs: 128 of 500 to 15000 in 16 bits 716 us for 831, 64 of 501 to 8190 209 for 230.
+  // More sequences than a wavefront can look through, or more blocks than 31 bits count, take that way too.
+  const int64_t workgroups = sequences * groups;
+  const bool alone = blocks <= kWaves || (blocks <= 32 && workgroups >= kSlots) || (blocks <= 128 && workgroups >= 4 * kSlots);
+  p.splits = alone || sequences > kMaxScan || blocks * sequences >= 1ll << 31 ? 0 : (int)splits;
   return p;
 }
 
