@@ -15,8 +15,15 @@
 //     the lanes that need it through LDS.  A table of angles in memory would add 4 part bytes a token to the traffic and a bound on
 //     the positions.
 //   * Few tokens: the heads of a token are dealt to several wavefronts.
+//   * The gradient keeps the next step's rows under way while it computes one (79 -> 59 us together with the next point), which the other
+//     two, with more wavefronts a compute unit, do not need.  No barrier: a wavefront's angles are its own.
 //   * The weights' gradients are summed per lane over the rows it meets, then over the lanes, the wavefronts and, by a second
 //     launch, the workgroups, in a fixed order: no atomics, the same bits in every run.
+//
+// Measured, calls one behind the other: rotary of 4096 tokens of 32 + 8 heads of 128 in bf16 15.1 us (5.6 TB/s read and written), transposed of 1999
+// tokens of 32 + 32 heads of 80 in fp32 17.5 us (4.7 TB/s); norms and rotary of 8192 tokens of 32 + 8 heads of 128 in bf16 36 us (4.7 TB/s), their
+// gradients 59 us (4.3 TB/s; 49 and 4.6 in the two launches, and what lies between).  A token, or 64: 10 to 11 us a call, of which the kernel
+// is 3.2 and 4.6; the rest is the caller's.
 #include "../../include/conqur.h"
 
 #include <math.h>
@@ -305,7 +312,8 @@ struct Packed<T, 1> {
   __device__ __forceinline__ void unpack(float* v) const { *v = e; }
 };
 
-// As above, with the rows of the next step, of the next token after a token's last, under way while one is computed.
+// The gradients: as above, with the rows of the next step, of the next token after a token's last, under way while one is computed.  8 products and sums an
+// element and three rows' traffic: bound by HBM.
 template <typename T, int V, int U, bool INTERLEAVED>
 __global__ void __launch_bounds__(64 * kWaves, V == 1 ? 2 : 4) k_norm_gradient(const RotaryArgs a) {
   __shared__ float2 s_angle[kWaves][kMaxWidth / 2];

