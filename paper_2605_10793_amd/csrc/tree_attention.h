@@ -39,6 +39,7 @@ struct TreeArgs {
   float* part;               // [cache head][row tile][workgroup][slot][row][width] sums
   float2* part_ml;           // [cache head][row tile][workgroup][slot][row] maxima, sums of weights
   int splits, min_blocks;
+  int tail;                  // blocks that a sequence's end, its new tokens, counts for beside its own
   int max_query, group, tile_rows, row_tiles;
   int q_wide, out_wide;
   float scale_log2;
@@ -94,7 +95,7 @@ __device__ __forceinline__ int lane_anew() {
 // Blocks of a sequence for a row tile that begins at row0: none if it has no such rows, otherwise one at least (which writes zeros if nothing is seen).
 __device__ __forceinline__ int blocks_in(Args a, const Sequence& s, int row0) {
   if (row0 >= s.count * a->group) return 0;
-  return s.length > kBlock ? (int)((s.length + kBlock - 1) / kBlock) : 1;
+  return (s.length > kBlock ? (int)((s.length + kBlock - 1) / kBlock) : 1) + a->tail;
 }
 
 // Sum over the lanes up to a lane.

@@ -712,7 +712,7 @@ constexpr int64_t kMaxStride = 1ll << 40;
 
 struct Plan {
   bool wide;
-  int qt, tile_rows, row_tiles, splits, min_blocks;
+  int qt, tile_rows, row_tiles, splits, min_blocks, tail;
   int64_t context;
 };
 
@@ -755,6 +755,10 @@ Plan plan_of(const conqur_tree_call& c) {
   // More sequences than a wavefront can look through, or more blocks than 31 bits count, take that way too.
   const int64_t workgroups = sequences * groups;
   const bool alone = blocks <= kWaves || (blocks <= 32 && workgroups >= kSlots) || (blocks <= 128 && workgroups >= 4 * kSlots);
+  // The new tokens, with their masks, take a workgroup as long as some four blocks of committed ones, so they count for as many, where a run is long
+  // enough to be cut (48 tokens of 8 sequences of 4096, 8 bits: 70 us for 77; 20 of 16 of 3000 to 6000, 4 bits, 80 rows a head: 87 for 96; one of 64 of
+  // 501 to 8190, 4 bits: 87 for 92).  Few rows of bf16 values wait for memory, not for them (215 us either way).
+  p.tail = p.wide || (c.cache.bits != 16 && blocks * sequences >= 8 * splits) ? 4 : 0;
   p.splits = alone || sequences > kMaxScan || blocks * sequences >= 1ll << 31 ? 0 : (int)splits;
   return p;
 }
@@ -842,6 +846,7 @@ extern "C" conqur_status conqur_tree_attention(const conqur_tree_call* c, void* 
   a.context = p.context;
   a.splits = p.splits;
   a.min_blocks = p.min_blocks;
+  a.tail = p.splits ? p.tail : 0;
   a.max_query = (int)c->max_query;
   a.group = (int)(c->q.heads / c->cache.heads);
   a.tile_rows = p.tile_rows;

@@ -19,6 +19,8 @@ namespace tree {
 
 namespace {
 
+constexpr int kRing = 4;                   // operands on their way from LDS ahead of the products that take them (8 sequences of 16384 tokens: 181 us for 190 as the compiler has it)
+constexpr int kArithmetic = 0x6;           // what may pass the fences between products: vector and scalar arithmetic
 constexpr int kDepth = 4;                  // blocks whose steps and zeros are in LDS
 
 template <int BITS, int W>
@@ -401,21 +403,33 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs) {
       }
       const bool work = !idle && !put_off;
 
+      // The operands of a block in the order of their use: of each half those of the keys, then those of the values.  kRing of them are on their way
+      // from LDS ahead of the products that take them.
+      constexpr int kOfKeys = 2 * kOps, kOfHalf = kOfKeys + kTiles;
+      bf16x8 ring[kRing];
+      auto operand = [&](auto index) {
+        constexpr int N = decltype(index)::value, H = N / kOfHalf, J = N % kOfHalf;
+        if constexpr (H < 2) {
+          if constexpr (J < kOfKeys)
+            ring[N % kRing] = *reinterpret_cast<const bf16x8*>(sk + key_at<W>(2 * H + J / kOps, col, J % kOps * 4 + g));
+          else
+            ring[N % kRing] = *reinterpret_cast<const bf16x8*>(sv + value_at((J - kOfKeys) * 16 + col, g * 2 + H));
+        }
+      };
+
       // A half: the 32 keys 16 g + 8 H to 16 g + 8 H + 7 of the quarters.
       auto half = [&](auto h) {
         constexpr int H = decltype(h)::value;
         f32x4 s[QT][2];
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int x = 0; x < QT; ++x) s[x][0] = s[x][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        each<kOfKeys>([&](auto j) {
+          constexpr int J = decltype(j)::value, N = H * kOfHalf + J;
 #pragma unroll
-          for (int x = 0; x < QT; ++x) s[x][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-          for (int i = 0; i < kOps; ++i) {
-            const bf16x8 kk = *reinterpret_cast<const bf16x8*>(sk + key_at<W>(2 * H + t, col, i * 4 + g));
-#pragma unroll
-            for (int x = 0; x < QT; ++x) s[x][t] = mfma(kk, qf[x][i], s[x][t]);
-          }
-        }
+          for (int x = 0; x < QT; ++x) s[x][J / kOps] = mfma(ring[N % kRing], qf[x][J % kOps], s[x][J / kOps]);
+          operand(std::integral_constant<int, N + kRing>{});
+          __builtin_amdgcn_sched_barrier(kArithmetic);
+        });
         float ks[8];
         float v_step = 1.0f;
         if constexpr (kCodes) {
@@ -454,18 +468,20 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs) {
           if constexpr (kCodes) each<8>([&](auto e) { y[decltype(e)::value] *= row_bcast<8 * H + decltype(e)::value>(v_step); });
           pf[x] = as_frag(f32x2_to_bf16x2(y[0], y[1]), f32x2_to_bf16x2(y[2], y[3]), f32x2_to_bf16x2(y[4], y[5]), f32x2_to_bf16x2(y[6], y[7]));
         }
+        each<kTiles>([&](auto d) {
+          constexpr int D = decltype(d)::value, N = H * kOfHalf + kOfKeys + D;
 #pragma unroll
-        for (int d = 0; d < kTiles; ++d) {
-          const bf16x8 z = *reinterpret_cast<const bf16x8*>(sv + value_at(d * 16 + col, g * 2 + H));
-#pragma unroll
-          for (int x = 0; x < QT; ++x) o[x][d] = mfma(z, pf[x], o[x][d]);
-        }
+          for (int x = 0; x < QT; ++x) o[x][D] = mfma(ring[N % kRing], pf[x], o[x][D]);
+          operand(std::integral_constant<int, N + kRing>{});
+          __builtin_amdgcn_sched_barrier(kArithmetic);
+        });
         if constexpr (!kCodes) {
 #pragma unroll
           for (int x = 0; x < QT; ++x) l_acc[x] = mfma(ones, pf[x], l_acc[x]);
         }
       };
       if (work) {
+        each<kRing>(operand);
         half(std::integral_constant<int, 0>{});
         half(std::integral_constant<int, 1>{});
       }
