@@ -21,7 +21,7 @@
 //
 // The kernel below is for few rows, bound by HBM: each of a workgroup's four wavefronts takes 64 keys at a time by itself, from memory straight into
 // operands, and has the next 64 under way; their results meet in LDS at the end.  Measured, 32 query and 8 cache heads of 128: a
-// token of 64 sequences of 501 to 8190 tokens, 16 bits, 204 to 210 us (5.4 to 5.6 TB/s); in 8 bits 129 us (4.7 TB/s), in 4 bits 92 us (3.5 TB/s, as
+// token of 64 sequences of 501 to 8190 tokens, 16 bits, 204 to 210 us (5.4 to 5.6 TB/s); in 8 bits 122 us (5.0 TB/s), in 4 bits 86 us (3.7 TB/s, as
 // much work as in 16 bits for a third of the bytes); 5 tokens of 2 sequences of 131000 tokens, 4 bits, 20 rows a cache head, 86 us (3.4
 // TB/s): there the conversions, exponentials and the two products of a wavefront, two wavefronts a SIMD, are what takes the time.  One token of one
 // sequence of 777 tokens 13.8 us, two launches of a chain of dependent reads.
@@ -723,8 +723,8 @@ Plan plan_of(const conqur_tree_call& c) {
   p.context = (int64_t)(c.max_context < (uint64_t)room ? c.max_context : (uint64_t)room);
   const int rows = (int)(c.max_query * (c.q.heads / c.cache.heads));
   // 17 to 32 rows: of codes, a wavefront's registers hold 64 keys and values and two tiles of results (16 sequences of 3000 to 6000 tokens, 32
-  // rows a head, 4 bits: 48 us, laid out in LDS 78; 8 bits, 20 rows: 47 for 62); of bf16 they do not, and LDS is quicker (8 sequences of 4000
-  // to 9000, 20 rows: 66 us for 70, 16 of 3000 to 6000, 32 rows: 77 for 90).
+  // rows a head, 4 bits: 48 us, laid out in LDS 78; 8 of 4000 to 9000, 20 rows, 8 bits: 47 for 62); of bf16 they do not, and LDS is quicker (the
+  // same two 77 us for 90 and 66 for 70).  All before new tokens counted for more, which took each of these a tenth down.
   p.wide = rows > (c.cache.bits == 16 ? 16 : 32);
   // Rows of a wavefront in sixteens: as few as pad the rows least; 48 rows of bf16 values 128 wide do not fit its registers.
   p.qt = rows <= 16 ? 1 : 2;
