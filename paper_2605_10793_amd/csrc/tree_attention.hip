@@ -261,6 +261,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree(const TreeArgs) {
     // weights times it leave the range, the offset is added by the weight itself.
     auto is_tiny = [&](float2 x) { return fabsf(x.x) < 1e-30f; };
     auto off_of = [&](float2 x) { return is_tiny(x) ? 0.0f : x.y / x.x - shifted<BITS>(); };
+    auto inv_of = [&](float2 x) { return is_tiny(x) ? 0.0f : __builtin_amdgcn_rcpf(x.x); };
     auto place = [](int e) { return BITS == 4 ? (e % 4 == 1 ? 2 : e % 4 == 2 ? 1 : e % 4) : e % 4; };      // where pack_weights puts weight e of four
 
     // What is new falls to where the maximum was raised by `by`, and what was with it.
@@ -338,19 +339,21 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree(const TreeArgs) {
               }
             }
             uint32_t p[QT][kT][2];
-            const float v_step = kCodes ? vs.x : 1.0f, v_off = kCodes ? off_of(vs) : 0.0f;
+            const float v_step = kCodes ? vs.x : 1.0f, v_off = kCodes ? off_of(vs) : 0.0f, v_inv = kCodes ? inv_of(vs) : 0.0f;
 #pragma unroll
             for (int x = 0; x < QT; ++x) {
               float w[4 * kT];
 #pragma unroll
               for (int e = 0; e < 4 * kT; ++e) {
                 w[e] = __builtin_amdgcn_exp2f(s[x][e / 4][e % 4]);
-                if constexpr (kCodes) l_run[x] += w[e];
               }
               if constexpr (kCodes) {
                 if (__any(is_tiny(vs))) {
-                  const float alone = is_tiny(vs) ? vs.y : 0.0f;
-                  each<4 * kT>([&](auto e) { c_run[x] += w[decltype(e)::value] * row_bcast<E0 + decltype(e)::value>(alone); });
+                  const float alone = is_tiny(vs) ? vs.y : 0.0f, one = is_tiny(vs) ? 1.0f : 0.0f;
+                  each<4 * kT>([&](auto e) {
+                    c_run[x] += w[decltype(e)::value] * row_bcast<E0 + decltype(e)::value>(alone);
+                    l_run[x] += w[decltype(e)::value] * row_bcast<E0 + decltype(e)::value>(one);
+                  });
                 }
                 each<4 * kT>([&](auto e) { w[decltype(e)::value] *= row_bcast<E0 + decltype(e)::value>(v_step); });
               }
@@ -359,7 +362,9 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree(const TreeArgs) {
               if constexpr (kCodes) each<4 * kT>([&](auto e) {
                 constexpr int E = decltype(e)::value;
                 const uint32_t u = p[x][E / 4][place(E) / 2];
-                c_run[x] += __uint_as_float(place(E) % 2 ? u & 0xffff0000u : u << 16) * row_bcast<E0 + E>(v_off);
+                const float rounded = __uint_as_float(place(E) % 2 ? u & 0xffff0000u : u << 16);
+                c_run[x] += rounded * row_bcast<E0 + E>(v_off);
+                l_run[x] += rounded * row_bcast<E0 + E>(v_inv);
               });
             }
 #pragma unroll
@@ -418,7 +423,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree(const TreeArgs) {
           odd = __any(odd);
         }
         const float k_step = kCodes ? ks.x * scale : scale, k_off = kCodes ? (ks.y - shifted<BITS>() * ks.x) * scale : 0.0f;
-        const float v_step = kCodes ? vs.x : 1.0f, v_off = kCodes ? off_of(vs) : 0.0f, alone = kCodes && is_tiny(vs) ? vs.y : 0.0f;
+        const float v_step = kCodes ? vs.x : 1.0f, v_off = kCodes ? off_of(vs) : 0.0f, v_inv = kCodes ? inv_of(vs) : 0.0f;
 #pragma unroll
         for (int x = 0; x < QT; ++x) {
           const int row = row0 + x * 16 + col, node = row / a->group;
@@ -463,23 +468,33 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree(const TreeArgs) {
           const float by = raise(m[x], column_max(top));
           lower(x, by);
           uint32_t q[4][2];
-          each<16>([&](auto e) {
-            constexpr int E = decltype(e)::value;
-            w[E] = __builtin_amdgcn_exp2f(w[E] - by);
-            if constexpr (kCodes) {      // (whatever pair the slot holds)
-              l_run[x] += w[E];
-              const float add = w[E] * row_bcast<E>(alone), y = w[E] * row_bcast<E>(v_step);
-              c_run[x] += (vis >> E) & 1 ? add : 0.0f;
-              w[E] = (vis >> E) & 1 ? y : 0.0f;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) w[e] = __builtin_amdgcn_exp2f(w[e] - by);
+          if constexpr (kCodes) {        // (whatever pair the slot holds)
+            if (__any(is_tiny(vs))) {
+              const float alone = is_tiny(vs) ? vs.y : 0.0f, one = is_tiny(vs) ? 1.0f : 0.0f;
+              each<16>([&](auto e) {
+                constexpr int E = decltype(e)::value;
+                const float add = w[E] * row_bcast<E>(alone);
+                c_run[x] += (vis >> E) & 1 ? add : 0.0f;
+                l_run[x] += w[E] * row_bcast<E>(one);
+              });
             }
-          });
+            each<16>([&](auto e) {
+              constexpr int E = decltype(e)::value;
+              const float y = w[E] * row_bcast<E>(v_step);
+              w[E] = (vis >> E) & 1 ? y : 0.0f;
+            });
+          }
 #pragma unroll
           for (int t = 0; t < 4; ++t) pack_weights<BITS>(w + 4 * t, q[t]);
           if constexpr (kCodes) each<16>([&](auto e) {
             constexpr int E = decltype(e)::value;
             const uint32_t u = q[E / 4][place(E) / 2];
-            const float add = __uint_as_float(place(E) % 2 ? u & 0xffff0000u : u << 16) * row_bcast<E>(v_off);
+            const float rounded = __uint_as_float(place(E) % 2 ? u & 0xffff0000u : u << 16);
+            const float add = rounded * row_bcast<E>(v_off), weight = rounded * row_bcast<E>(v_inv);
             c_run[x] += (vis >> E) & 1 ? add : 0.0f;
+            l_run[x] += (vis >> E) & 1 ? weight : 0.0f;
           });
           if (!kCodes && odd) {
             // One token at a time, its values to the rows that see it.

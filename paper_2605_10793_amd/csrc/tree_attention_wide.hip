@@ -22,6 +22,7 @@ namespace {
 
 constexpr int kRing = 4;                   // operands on their way from LDS ahead of the products that take them (8 sequences of 16384 tokens: 181 us for 190 as the compiler has it)
 constexpr int kArithmetic = 0x6;           // what may pass the fences between products: vector and scalar arithmetic
+constexpr float kTiny = 1e-30f;            // steps below it are not divided by
 constexpr int kDepth = 4;                  // blocks whose steps and zeros are in LDS
 
 template <int BITS, int W>
@@ -288,7 +289,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs) {
     to[0] = step;
     to[kBlock] = zero;
     to[2 * kBlock] = rest;
-    const bool any = __any(rest != 0.0f);
+    const bool any = __any(rest != 0.0f || (which && fabsf(step) < kTiny));
     if (lane == 0) s_flag[2 * (block & (kDepth - 1)) + which] = any;
   };
   // From what was sent for, by the wavefront that did.
@@ -432,10 +433,11 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs) {
           __builtin_amdgcn_sched_barrier(kArithmetic);
         });
         float ks[8];
-        float v_step = 1.0f;
+        float v_step = 1.0f, v_inv = 1.0f;
         if constexpr (kCodes) {
           const float k_step = s_pair(n)[lane] * scale;
           v_step = s_pair(n)[3 * kBlock + lane];
+          v_inv = __builtin_amdgcn_rcpf(v_step);
           each<8>([&](auto e) { ks[decltype(e)::value] = row_bcast<8 * H + decltype(e)::value>(k_step); });
         }
 #pragma unroll
@@ -464,10 +466,15 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             y[e] = __builtin_amdgcn_exp2f(s[x][e / 4][e % 4]);
-            if (kCodes) l_run[kCodes ? x : 0] += y[e];
           }
           if constexpr (kCodes) each<8>([&](auto e) { y[decltype(e)::value] *= row_bcast<8 * H + decltype(e)::value>(v_step); });
-          pf[x] = as_frag(f32x2_to_bf16x2(y[0], y[1]), f32x2_to_bf16x2(y[2], y[3]), f32x2_to_bf16x2(y[4], y[5]), f32x2_to_bf16x2(y[6], y[7]));
+          const uint32_t w[4] = {f32x2_to_bf16x2(y[0], y[1]), f32x2_to_bf16x2(y[2], y[3]), f32x2_to_bf16x2(y[4], y[5]), f32x2_to_bf16x2(y[6], y[7])};
+          pf[x] = as_frag(w[0], w[1], w[2], w[3]);
+          // The weights that the sum is divided by, as they are rounded.
+          if constexpr (kCodes) each<8>([&](auto at) {
+            constexpr int e = decltype(at)::value;
+            l_run[x] += __uint_as_float(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16) * row_bcast<8 * H + e>(v_inv);
+          });
         }
         each<kTiles>([&](auto d) {
           constexpr int D = decltype(d)::value, N = H * kOfHalf + kOfKeys + D;
@@ -533,13 +540,19 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs) {
     const unsigned char* const sk = s_k(0);
     const unsigned char* const sv = s_v(0);
     const bool odd = !kCodes && s_flag[1];
-    float k_step = scale, v_step = 1.0f, k_rest = 0.0f, v_rest = 0.0f;
+    float k_step = scale, v_step = 1.0f, k_rest = 0.0f, v_rest = 0.0f, v_inv = 1.0f, v_one = 0.0f;      // v_one: the weight goes in as it is
     if constexpr (kCodes) {
       const float* const pair = s_pair(0) + lane;
       k_step *= pair[0];
       k_rest = pair[2 * kBlock] * scale;
       v_step = pair[3 * kBlock];
       v_rest = pair[5 * kBlock];
+      if (fabsf(v_step) < kTiny) {
+        v_inv = 0.0f;
+        v_one = 1.0f;
+      } else {
+        v_inv = __builtin_amdgcn_rcpf(v_step);
+      }
     }
     const int64_t pos = kb + g * 16, j0 = pos - sq.prefix;
     uint32_t exists = 0;
@@ -596,7 +609,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs) {
           constexpr int e = decltype(at)::value;
           y[e] = __builtin_amdgcn_exp2f(s[e / 4][e % 4] - by);
           if constexpr (kCodes) {
-            l_run[x] += y[e];
+            l_run[x] += y[e] * row_bcast<e>(v_one);
             const float add = y[e] * row_bcast<e>(v_rest), w = y[e] * row_bcast<e>(v_step);      // (whatever pair the slot holds)
             c += (see >> e) & 1 ? add : 0.0f;
             y[e] = (see >> e) & 1 ? w : 0.0f;
@@ -607,6 +620,11 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs) {
         for (int d = 0; d < kTiles; ++d) o[x][d] = o[x][d] * f + c;
         const uint32_t w[4] = {f32x2_to_bf16x2(y[0], y[1]), f32x2_to_bf16x2(y[2], y[3]), f32x2_to_bf16x2(y[4], y[5]), f32x2_to_bf16x2(y[6], y[7])};
         const bf16x8 pf = as_frag(w[0], w[1], w[2], w[3]);
+        if constexpr (kCodes) each<8>([&](auto at) {
+          constexpr int e = decltype(at)::value;
+          const float weight = __uint_as_float(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16) * row_bcast<e>(v_inv);
+          l_run[x] += (see >> e) & 1 ? weight : 0.0f;
+        });
 #pragma unroll
         for (int d = 0; d < kTiles; ++d) {
           u32x4 z = *reinterpret_cast<const u32x4*>(sv + value_at(d * 16 + col, g * 2 + H));
@@ -643,6 +661,8 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs) {
           k_rest = row_rotated<8>(k_rest);
           v_step = row_rotated<8>(v_step);
           v_rest = row_rotated<8>(v_rest);
+          v_inv = row_rotated<8>(v_inv);
+          v_one = row_rotated<8>(v_one);
         }
       }
     }

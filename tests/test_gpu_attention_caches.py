@@ -145,6 +145,23 @@ def test_more_sequences_than_are_searched(A, bits, count, group):
     within(few, want[start[70]:start[80]], size[start[70]:start[80]])
 
 
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("count,group", [(1, 1), (1, 20), (40, 1)])
+def test_runs_over_many_sequences(A, bits, count, group):
+    """So many heads that a workgroup's run spans several sequences, empty ones among them, and one sequence several runs."""
+    import torch
+    heads, width, page = 32 if group == 1 else 16, 64, 32
+    prefix = [70, 0, 0, 3000, 5, 64, 0, 1, 130, 63, 0, 0, 900, 10, 40]
+    counts = [count, 0, count, count, 1, 0, 0, 1, count, 1, 0, 0, 1, 0, 1]
+    cache, table = filled_cache(A, [p + n for p, n in zip(prefix, counts)], page, heads, width, bits, 13)
+    start = [0] + [int(x) for x in np.cumsum(counts)]
+    q = randn(14, start[-1], heads * group, width)
+    want, size = attend64(q, cache, start, prefix, table, None, 0.125)
+    got = A.tree_attention(q, cache, i32(start), i32(prefix), i32(table), max_query=count)
+    within(got, want, size)
+    assert torch.equal(got, A.tree_attention(q, cache, i32(start), i32(prefix), i32(table), max_query=count))
+
+
 @pytest.mark.parametrize("sequences", [1, 64, 65, 4097])
 def test_append_finds_every_sequence(A, sequences):
     import torch
