@@ -21,8 +21,8 @@
 //
 // The kernel below is for few rows, bound by HBM: each of a workgroup's four wavefronts takes 64 keys at a time by itself, from memory straight into
 // operands, and has the next 64 under way; their results meet in LDS at the end.  Measured, 32 query and 8 cache heads of 128: a
-// token of 64 sequences of 501 to 8190 tokens, 16 bits, 204 to 210 us (5.4 to 5.6 TB/s); in 8 bits 122 us (5.0 TB/s), in 4 bits 86 us (3.7 TB/s, as
-// much work as in 16 bits for a third of the bytes); 5 tokens of 2 sequences of 131000 tokens, 4 bits, 20 rows a cache head, 86 us (3.4
+// token of 64 sequences of 501 to 8190 tokens, 16 bits, 204 to 210 us (5.4 to 5.6 TB/s); in 8 bits 122 us (5.0 TB/s), in 4 bits 87 us (3.7 TB/s, as
+// much work as in 16 bits for a third of the bytes); 5 tokens of 2 sequences of 131000 tokens, 4 bits, 20 rows a cache head, 89 us (3.3
 // TB/s): there the conversions, exponentials and the two products of a wavefront, two wavefronts a SIMD, are what takes the time.  One token of one
 // sequence of 777 tokens 13.8 us, two launches of a chain of dependent reads.
 #include "tree_attention.h"

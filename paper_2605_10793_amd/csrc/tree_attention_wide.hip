@@ -8,8 +8,8 @@
 // value; where that lies outside the range (a row without a sign change) or between two codes, the rest, value - step (c - zero), is
 // added to the scores and the results of the block apart.
 //
-// Measured: 48 tokens of 8 sequences of 1000 to 16000 tokens, 32 query and 8 cache heads of 128, 8 bits (192 rows a cache head, one tile): 111 us, 480
-// TFLOP/s with the join; of 16384 tokens each 168 us, 613 TFLOP/s.  What bounds it: of a wavefront's time 30 % are vector instructions (a score's
+// Measured: 48 tokens of 8 sequences of 1000 to 16000 tokens, 32 query and 8 cache heads of 128, 8 bits (192 rows a cache head, one tile): 117 us, 456
+// TFLOP/s with the join (111 with the sums of the weights as they are before they are rounded, and results a third less exact).  What bounds it: of a wavefront's time 31 % are vector instructions (a score's
 // exponential, factors and packing, a code's conversion), twice that with the two wavefronts of a SIMD; a quarter waits to issue, a third
 // for LDS, memory and the barrier of every 64 keys.  What a call takes beside its 64 keys a turn, some 35 us, is mostly the partial results:
 // 53 MiB written, and read again by the join (14 us).
