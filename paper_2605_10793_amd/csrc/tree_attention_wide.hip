@@ -604,27 +604,33 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs) {
           l_run[x] *= f;
         else
           l_acc[x] *= f;
+        // Each weight reaches the sum that divides and the rest of its value (c) as the product takes it: rounded, over the step.
         float y[8], c = 0.0f;
         each<8>([&](auto at) {
           constexpr int e = decltype(at)::value;
           y[e] = __builtin_amdgcn_exp2f(s[e / 4][e % 4] - by);
           if constexpr (kCodes) {
-            l_run[x] += y[e] * row_bcast<e>(v_one);
-            const float add = y[e] * row_bcast<e>(v_rest), w = y[e] * row_bcast<e>(v_step);      // (whatever pair the slot holds)
+            const float one = y[e] * row_bcast<e>(v_one);
+            const float add = one * row_bcast<e>(v_rest), w = y[e] * row_bcast<e>(v_step);      // (whatever pair the slot holds)
+            l_run[x] += one;
             c += (see >> e) & 1 ? add : 0.0f;
             y[e] = (see >> e) & 1 ? w : 0.0f;
           }
         });
-        if constexpr (kCodes) c = column_sum(c);
-#pragma unroll
-        for (int d = 0; d < kTiles; ++d) o[x][d] = o[x][d] * f + c;
         const uint32_t w[4] = {f32x2_to_bf16x2(y[0], y[1]), f32x2_to_bf16x2(y[2], y[3]), f32x2_to_bf16x2(y[4], y[5]), f32x2_to_bf16x2(y[6], y[7])};
         const bf16x8 pf = as_frag(w[0], w[1], w[2], w[3]);
-        if constexpr (kCodes) each<8>([&](auto at) {
-          constexpr int e = decltype(at)::value;
-          const float weight = __uint_as_float(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16) * row_bcast<e>(v_inv);
-          l_run[x] += (see >> e) & 1 ? weight : 0.0f;
-        });
+        if constexpr (kCodes) {
+          each<8>([&](auto at) {
+            constexpr int e = decltype(at)::value;
+            const float weight = __uint_as_float(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16) * row_bcast<e>(v_inv);
+            const float add = weight * row_bcast<e>(v_rest);
+            l_run[x] += (see >> e) & 1 ? weight : 0.0f;
+            c += (see >> e) & 1 ? add : 0.0f;
+          });
+          c = column_sum(c);
+        }
+#pragma unroll
+        for (int d = 0; d < kTiles; ++d) o[x][d] = o[x][d] * f + c;
 #pragma unroll
         for (int d = 0; d < kTiles; ++d) {
           u32x4 z = *reinterpret_cast<const u32x4*>(sv + value_at(d * 16 + col, g * 2 + H));
