@@ -15,6 +15,7 @@ from __future__ import annotations
 
 import ctypes
 import struct
+import threading
 from typing import Optional, Tuple
 
 import torch
@@ -147,8 +148,7 @@ def qk_norm_rotary_backward(plan: Rotary, q, k, q_weight, k_weight, positions, q
 class KVCache:
     """A pool of pages.  bits 16: k [pages, heads, page_tokens, width] and v [pages, heads, width, page_tokens] in bf16; bits 8: uint8 codes in
     the same layout; bits 4: two codes a byte, width/2 bytes in place of width.  Codes have k_scale and v_scale [pages, heads, page_tokens,
-    2] in fp32, (step, offset) of every token.  page_tokens: a power of two, 16 to 256; width 64 or 128.  `empty` allocates one.
-    The workspace that tree_attention needs is kept here, one for each stream it is called on."""
+    2] in fp32, (step, offset) of every token.  page_tokens: a power of two, 16 to 256; width 64 or 128.  `empty` allocates one."""
 
     def __init__(self, k, v, k_scale=None, v_scale=None, bits: int = 16):
         if bits not in (16, 8, 4):
@@ -170,7 +170,6 @@ class KVCache:
         self.width = n * 2 if bits == 4 else n
         self._fields = (k.data_ptr(), v.data_ptr(), 0 if k_scale is None else k_scale.data_ptr(), 0 if v_scale is None else v_scale.data_ptr(),
                         pages, heads, self.width, page_tokens, bits)
-        self._workspace = {}
 
     @classmethod
     def empty(cls, pages: int, heads: int, page_tokens: int, width: int, bits: int = 16, device: str = "cuda:0") -> "KVCache":
@@ -206,6 +205,17 @@ def append(cache: KVCache, k, v, start, prefix, table, values: bool = False, k_v
     return (k_values, v_values) if values else None
 
 
+class _Kept(threading.local):
+    """The workspaces of tree_attention, each thread its own, by device and stream.  A call's launches meet in it: the calls of one thread on one
+    stream come one behind the other, whatever their caches, those of two threads may be enqueued between each other's launches."""
+
+    def __init__(self):
+        self.rooms = {}
+
+
+_kept = _Kept()
+
+
 def tree_attention(q, cache: KVCache, start, prefix, table, mask=None, max_query: int = 64, max_context: Optional[int] = None,
                    scale: Optional[float] = None, out=None):
     """Attention of new tokens q (bf16 [tokens, heads, width]; packed as in `append`, which has put their keys and values into the cache) over
@@ -224,18 +234,20 @@ def tree_attention(q, cache: KVCache, start, prefix, table, mask=None, max_query
               table.shape[1] * cache.page_tokens if max_context is None else max_context)
     tail = (max_query, width ** -0.5 if scale is None else scale)
     lib = binding.load()
-    stream = torch._C._cuda_getCurrentRawStream(q.get_device())
+    index = q.get_device()
+    at = index, torch._C._cuda_getCurrentRawStream(index)
     # (a graph keeps the room it was captured with: it takes its own, from its memory pool)
     capturing = torch._C._cuda_isCurrentStreamCapturing()
-    have = _NOTHING if capturing else cache._workspace.get(stream, _NOTHING)
+    rooms = _kept.rooms
+    have = _NOTHING if capturing else rooms.get(at, _NOTHING)
     status = _run(lib.conqur_tree_attention, q, _TREE.pack(*fields, *have[1:], *tail))
-    if status == binding.EINVAL:       # perhaps for want of room alone: one that is large enough stays with the cache
+    if status == binding.EINVAL:       # perhaps for want of room alone: one that is large enough stays
         size = lib.conqur_tree_attention_workspace(_TREE.pack(*fields, 0, 0, *tail))
         if size > have[2]:
             room = torch.empty(size, dtype=torch.uint8, device=q.device)
             have = (room, room.data_ptr(), size)
             if not capturing:
-                cache._workspace[stream] = have
+                rooms[at] = have
             status = _run(lib.conqur_tree_attention, q, _TREE.pack(*fields, *have[1:], *tail))
     _check(status, "conqur_tree_attention")
     return out
