@@ -9,7 +9,8 @@ the stream (the current one of the tensors' device).  Nothing synchronises, noth
   KVCache, append                     a paged cache of keys and values in bf16 or in 8- or 4-bit zero-point codes
   tree_attention                      attention of new tokens (a tree of drafted ones, a chain, a single one) over the cache
 
-Rows are [tokens, heads, width] tensors of any token and head stride, e.g. slices of a fused projection's output.
+Rows are [tokens, heads, width] tensors of any token and head stride, e.g. slices of a fused projection's output.  All tensors of a call, its
+plan and its cache lie on one device.
 """
 from __future__ import annotations
 
@@ -43,17 +44,26 @@ def _check(status: int, what: str) -> None:
 # as few attribute reads as the checks need, and the stream is asked for by device index (a pass of `rotary` 15.1 -> 10 us, of which the
 # launch is 3.7).
 
-def _rows(x, name: str, dtype, tokens: int, heads: int, width: int) -> Tuple[int, int, int, int]:
+def _rows(x, name: str, dtype, device: int, tokens: int, heads: int, width: int) -> Tuple[int, int, int, int]:
     shape, stride = x.shape, x.stride()
-    if len(shape) != 3 or shape[0] != tokens or shape[1] != heads or shape[2] != width or stride[2] != 1 or x.dtype is not dtype or not x.is_cuda:
+    if len(shape) != 3 or shape[0] != tokens or shape[1] != heads or shape[2] != width or stride[2] != 1 or x.dtype is not dtype:
         raise ValueError(f"{name} must be a [{tokens}, {heads}, {width}] device tensor of {dtype} with unit stride along the width")
+    if x.get_device() != device or device < 0:
+        _elsewhere(x, name, device)
     return x.data_ptr(), stride[0], stride[1], heads
 
 
-def _vector(x, name: str, dtype, n: int) -> int:
-    if x.dtype is not dtype or x.shape != (n,) or not x.is_cuda or not x.is_contiguous():
+def _vector(x, name: str, dtype, device: int, n: int) -> int:
+    if x.dtype is not dtype or x.shape != (n,) or not x.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} device tensor of {n} entries")
+    if x.get_device() != device or device < 0:
+        _elsewhere(x, name, device)
     return x.data_ptr()
+
+
+def _elsewhere(x, name: str, device: int):
+    """A kernel takes addresses as they are: what lies on the host or on another GPU must not get that far."""
+    raise ValueError(f"{name} lies on {x.device}, where a tensor on " + ("a GPU" if device < 0 else f"cuda:{device}") + " is needed")
 
 
 def _run(call, x, *args) -> int:
@@ -75,7 +85,7 @@ class Rotary:
     (conqur_rotary_scaling in the header says what `low` and `high` are)."""
 
     def __init__(self, part: int, theta: float = 10000.0, interleaved: bool = False, scaling: str = "none", factor: float = 1.0, low: float = 1.0,
-                 high: float = 4.0, context: float = 8192.0, device: str = "cuda:0"):
+                 high: float = 4.0, context: float = 8192.0, device: str = "cuda"):
         if scaling not in SCALINGS:
             raise ValueError(f"scaling must be one of {sorted(SCALINGS)}")
         turns = torch.empty(max(part // 2, 1), dtype=torch.float64)
@@ -94,15 +104,18 @@ def _rotary_call(plan, q, k, positions, q_out, k_out, q_grad=None, k_grad=None, 
         raise ValueError("queries and keys must be [tokens, heads, width]")
     tokens, heads, width = q.shape
     k_heads = 0 if k is None else k.shape[1]
-    same = (dtype, tokens, heads, width)
-    k_same = (dtype, tokens, k_heads, width)
+    device = q.get_device()
+    if plan.turns.get_device() != device:
+        _elsewhere(plan.turns, "the plan", device)
+    same = (dtype, device, tokens, heads, width)
+    k_same = (dtype, device, tokens, k_heads, width)
     return _ROTARY.pack(*_rows(q, "q", *same), *(_ABSENT if k is None else _rows(k, "k", *k_same)),
                         *_rows(q_out, "the result of q", *same), *(_ABSENT if k is None else _rows(k_out, "the result of k", *k_same)),
                         *(_ABSENT if q_grad is None else _rows(q_grad, "the gradient of q", *same)),
                         *(_ABSENT if k_grad is None else _rows(k_grad, "the gradient of k", *k_same)),
-                        0 if q_weight is None else _vector(q_weight, "q_weight", dtype, width),
-                        0 if k_weight is None else _vector(k_weight, "k_weight", dtype, width),
-                        _vector(positions, "positions", torch.int64, tokens), plan.turns.data_ptr(), tokens, width, plan.part, plan.layout,
+                        0 if q_weight is None else _vector(q_weight, "q_weight", dtype, device, width),
+                        0 if k_weight is None else _vector(k_weight, "k_weight", dtype, device, width),
+                        _vector(positions, "positions", torch.int64, device, tokens), plan.turns.data_ptr(), tokens, width, plan.part, plan.layout,
                         1 if dtype is torch.bfloat16 else 0, transposed, plan.magnitude, eps, 0)
 
 
@@ -168,11 +181,12 @@ class KVCache:
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.pages, self.heads, self.page_tokens, self.bits = pages, heads, page_tokens, bits
         self.width = n * 2 if bits == 4 else n
+        self.device = k.get_device()
         self._fields = (k.data_ptr(), v.data_ptr(), 0 if k_scale is None else k_scale.data_ptr(), 0 if v_scale is None else v_scale.data_ptr(),
                         pages, heads, self.width, page_tokens, bits)
 
     @classmethod
-    def empty(cls, pages: int, heads: int, page_tokens: int, width: int, bits: int = 16, device: str = "cuda:0") -> "KVCache":
+    def empty(cls, pages: int, heads: int, page_tokens: int, width: int, bits: int = 16, device: str = "cuda") -> "KVCache":
         n, dtype = (width // 2, torch.uint8) if bits == 4 else (width, torch.uint8 if bits == 8 else torch.bfloat16)
         k = torch.empty((pages, heads, page_tokens, n), dtype=dtype, device=device)
         v = torch.empty((pages, heads, n, page_tokens), dtype=dtype, device=device)
@@ -180,12 +194,14 @@ class KVCache:
         return cls(k, v, *scales, bits=bits)
 
 
-def _batch(start, prefix, table) -> Tuple:
+def _batch(start, prefix, table, device: int) -> Tuple:
     sequences, stride = prefix.shape[0], table.stride()
-    if table.dim() != 2 or table.dtype is not torch.int32 or not table.is_cuda or stride[1] != 1 or table.shape[0] != sequences:
+    if table.dim() != 2 or table.dtype is not torch.int32 or stride[1] != 1 or table.shape[0] != sequences:
         raise ValueError("table must be a [sequences, columns] int32 device tensor with unit column stride")
+    if table.get_device() != device:
+        _elsewhere(table, "table", device)
     columns = table.shape[1]
-    return (_vector(start, "start", torch.int32, sequences + 1), _vector(prefix, "prefix", torch.int32, sequences), table.data_ptr(),
+    return (_vector(start, "start", torch.int32, device, sequences + 1), _vector(prefix, "prefix", torch.int32, device, sequences), table.data_ptr(),
             stride[0] if sequences > 1 else max(stride[0], columns), columns, sequences)
 
 
@@ -194,11 +210,12 @@ def append(cache: KVCache, k, v, start, prefix, table, values: bool = False, k_v
     token i lies in slot i % page_tokens of page table[b, i // page_tokens] (int32 device tensors).  values (8 or 4 bits): also returns
     what the cache holds of them, (k_values, v_values), in the given or in new bf16 tensors."""
     tokens = k.shape[0]
-    same = (torch.bfloat16, tokens, cache.heads, cache.width)
+    device = cache.device
+    same = (torch.bfloat16, device, tokens, cache.heads, cache.width)
     if values:
         k_values = _like(k) if k_values is None else k_values
         v_values = _like(v) if v_values is None else v_values
-    call = _APPEND.pack(*cache._fields, *_batch(start, prefix, table), *_rows(k, "k", *same), *_rows(v, "v", *same),
+    call = _APPEND.pack(*cache._fields, *_batch(start, prefix, table, device), *_rows(k, "k", *same), *_rows(v, "v", *same),
                         *(_ABSENT if k_values is None else _rows(k_values, "k_values", *same)),
                         *(_ABSENT if v_values is None else _rows(v_values, "v_values", *same)), tokens)
     _check(_run(binding.load().conqur_cache_append, k, call), "conqur_cache_append")
@@ -224,23 +241,26 @@ def tree_attention(q, cache: KVCache, start, prefix, table, mask=None, max_query
     holds; a closer bound shares the work out better).  scale: 1 / sqrt(width) unless given.  Returns out."""
     if q.dim() != 3:
         raise ValueError("q must be [tokens, heads, width]")
+    device = cache.device
+    if torch._C._cuda_getDevice() != device:       # (what is asked below is asked of the current device)
+        with torch.cuda.device(device):
+            return tree_attention(q, cache, start, prefix, table, mask, max_query, max_context, scale, out)
     tokens, heads, _ = q.shape
     width = cache.width
     if out is None:
         out = _like(q)
-    same = (torch.bfloat16, tokens, heads, width)
-    fields = (*cache._fields, *_batch(start, prefix, table), *_rows(q, "q", *same), *_rows(out, "out", *same),
-              0 if mask is None else _vector(mask, "mask", torch.int64, tokens), tokens,
+    same = (torch.bfloat16, device, tokens, heads, width)
+    fields = (*cache._fields, *_batch(start, prefix, table, device), *_rows(q, "q", *same), *_rows(out, "out", *same),
+              0 if mask is None else _vector(mask, "mask", torch.int64, device, tokens), tokens,
               table.shape[1] * cache.page_tokens if max_context is None else max_context)
     tail = (max_query, width ** -0.5 if scale is None else scale)
     lib = binding.load()
-    index = q.get_device()
-    at = index, torch._C._cuda_getCurrentRawStream(index)
+    at = device, torch._C._cuda_getCurrentRawStream(device)
     # (a graph keeps the room it was captured with: it takes its own, from its memory pool)
     capturing = torch._C._cuda_isCurrentStreamCapturing()
     rooms = _kept.rooms
     have = _NOTHING if capturing else rooms.get(at, _NOTHING)
-    status = _run(lib.conqur_tree_attention, q, _TREE.pack(*fields, *have[1:], *tail))
+    status = lib.conqur_tree_attention(_TREE.pack(*fields, *have[1:], *tail), at[1])
     if status == binding.EINVAL:       # perhaps for want of room alone: one that is large enough stays
         size = lib.conqur_tree_attention_workspace(_TREE.pack(*fields, 0, 0, *tail))
         if size > have[2]:
@@ -248,6 +268,6 @@ def tree_attention(q, cache: KVCache, start, prefix, table, mask=None, max_query
             have = (room, room.data_ptr(), size)
             if not capturing:
                 rooms[at] = have
-            status = _run(lib.conqur_tree_attention, q, _TREE.pack(*fields, *have[1:], *tail))
+            status = lib.conqur_tree_attention(_TREE.pack(*fields, *have[1:], *tail), at[1])
     _check(status, "conqur_tree_attention")
     return out

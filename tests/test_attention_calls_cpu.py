@@ -54,6 +54,7 @@ class Library:
 def library(monkeypatch):
     lib = Library()
     monkeypatch.setattr(binding, "load", lambda: lib)
+    monkeypatch.setattr(A, "_kept", A._Kept())
     monkeypatch.setattr(A, "_like", lambda x: None if x is None else Fake(*x.shape, dtype=x.dtype, index=x.index))
     for name, value in (("_cuda_getDevice", lambda: 0), ("_cuda_getCurrentRawStream", lambda i: 0x500 + i), ("_cuda_isCurrentStreamCapturing", lambda: False)):
         monkeypatch.setattr(torch._C, name, value, raising=False)
@@ -69,9 +70,9 @@ def batch_of(index=0):
 
 
 def test_where_the_workspace_is_in_a_call():
-    q = Fake(3, 4, 64)
-    fields = (*cache_of()._fields, *A._batch(*batch_of()), *A._rows(q, "q", torch.bfloat16, 3, 4, 64), *A._rows(q, "out", torch.bfloat16, 3, 4, 64))
-    assert struct.unpack_from("=QQ", A._TREE.pack(*fields, 0, 3, 100, 77, 99, 1, 1.0), WORKSPACE) == (77, 99)
+    codes = A._TREE.format.lstrip("=")
+    call = A._TREE.pack(*range(1, len(codes) + 1))
+    assert struct.unpack_from("=QQ", call, WORKSPACE) == (len(codes) - 3, len(codes) - 2)      # before max_query and scale
 
 
 def test_threads_do_not_share_a_workspace(library):
@@ -118,3 +119,103 @@ def test_streams_do_not_share_a_workspace(library, monkeypatch):
         monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i, s=stream: s)
         A.tree_attention(Fake(3, 4, 64), cache, *batch)
     assert len({at for _, _, at in library.calls}) == 2
+
+
+# ------------------------------------------------------------------------------------------------ devices
+
+def rotary_arguments(index=0):
+    return dict(q=Fake(3, 4, 64, index=index), positions=Fake(3, dtype=torch.int64, index=index), k=Fake(3, 2, 64, index=index))
+
+
+def norm_arguments(index=0):
+    return dict(rotary_arguments(index), q_weight=Fake(64, index=index), k_weight=Fake(64, index=index))
+
+
+def cache_arguments(index=0):
+    start, prefix, table = batch_of(index)
+    return dict(start=start, prefix=prefix, table=table)
+
+
+CALLS = {  # what is called, its tensors on a device, and whether it takes a plan or a cache
+    "rotary": (rotary_arguments, lambda a, at: A.rotary(a.pop("plan"), **a)),
+    "norm": (norm_arguments, lambda a, at: A.qk_norm_rotary(a.pop("plan"), **a)),
+    "gradient": (lambda i=0: dict(norm_arguments(i), q_grad=Fake(3, 4, 64, index=i), k_grad=Fake(3, 2, 64, index=i)),
+                 lambda a, at: A.qk_norm_rotary_backward(a.pop("plan"), **a)),
+    "append": (lambda i=0: dict(cache_arguments(i), k=Fake(3, 2, 64, index=i), v=Fake(3, 2, 64, index=i)), lambda a, at: A.append(cache_of(at), **a)),
+    "attention": (lambda i=0: dict(cache_arguments(i), q=Fake(3, 4, 64, index=i), mask=Fake(3, dtype=torch.int64, index=i), out=Fake(3, 4, 64, index=i)),
+                  lambda a, at: A.tree_attention(a.pop("q"), cache_of(at), **a)),
+}
+
+
+class Plan:
+    def __init__(self, index):
+        self.turns, self.part, self.layout, self.magnitude = Fake(32, dtype=torch.float64, index=index), 64, 0, 1.0
+
+
+@pytest.fixture
+def current(monkeypatch, library):
+    """The current device, which `torch.cuda.device` changes, its stream and whether that is being captured."""
+    at = [0]
+
+    class Device:
+        def __init__(self, index):
+            self.index = index
+
+        def __enter__(self):
+            self.before, at[0] = at[0], self.index
+
+        def __exit__(self, *_):
+            at[0] = self.before
+
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: at[0], raising=False)
+    return at
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_tensors_of_another_device_are_refused(library, current, name):
+    """The host's too: an address of another device's memory must not reach a kernel."""
+    make, call = CALLS[name]
+    takes_plan = name in ("rotary", "norm", "gradient")
+
+    def arguments(index):
+        return dict(make(index), plan=Plan(index)) if takes_plan else make(index)
+
+    for index in (0, 1):                   # all together on either: taken
+        call(arguments(index), index)
+    taken = len(library.calls)
+    assert taken >= 2
+    for other in (-1, 1):
+        for moved in arguments(0):
+            with pytest.raises(ValueError):
+                call(dict(arguments(0), **{moved: arguments(other)[moved]}), 0)
+        if not takes_plan:
+            with pytest.raises(ValueError):
+                call(arguments(0), 1)      # the cache
+    with pytest.raises(ValueError):
+        call(arguments(-1), 0)
+    assert len(library.calls) == taken
+
+
+def test_plans_and_caches_are_made_on_the_current_device(monkeypatch):
+    """A rank's own, not the first one's."""
+    made = []
+    monkeypatch.setattr(torch.Tensor, "to", lambda x, device: made.append(device) or x)
+    monkeypatch.setattr(torch, "empty", lambda *a, device=None, real=torch.empty, **more: made.append(device) or real(*a, **more))
+    monkeypatch.setattr(A.KVCache, "__init__", lambda self, *a, **more: None)
+    A.Rotary(64)
+    A.KVCache.empty(2, 1, 64, 128, 8)
+    assert [d for d in made if d is not None] == ["cuda"] * 5
+
+
+def test_capture_is_asked_of_the_cache_s_device(library, current, monkeypatch):
+    """While the other device's stream is captured, a workspace is kept; while its own is, none of those kept is handed over."""
+    for capturing, kept in ((0, True), (1, False)):
+        monkeypatch.setattr(torch._C, "_cuda_isCurrentStreamCapturing", lambda c=capturing: current[0] == c)
+        library.calls.clear()
+        held = []
+        for _ in range(2):
+            A.tree_attention(Fake(3, 4, 64, index=1), cache_of(1), *batch_of(1))
+            held.append(torch.empty(4096, dtype=torch.uint8))       # what a workspace given back would be
+        assert (len(A._kept.rooms) > 0) and ((library.calls[0][2] == library.calls[1][2]) or not kept)
+        assert any(at == room[1] for _, _, at in library.calls for room in A._kept.rooms.values()) == kept
