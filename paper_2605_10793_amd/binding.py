@@ -144,6 +144,7 @@ class Calibrator:
         self.d, self.heads, self.dh, self.dtype = d, heads, d // max(heads, 1), dtype
         if stream is None:
             stream = torch.cuda.current_stream(device).cuda_stream
+        self.device, self.stream = device, stream       # where every call of it works
         cfg = Config(d, heads, BF16 if dtype == "bf16" else F32, max_tokens, prox_lambda, polar_tol,
                      polar_max_iters, polar_precision, polar_verify, device, ctypes.c_void_p(stream))
         R0 = np.ascontiguousarray(R0, dtype=np.float32)

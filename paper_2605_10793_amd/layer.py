@@ -22,11 +22,13 @@ from . import attention, binding
 
 class AttentionLayer:
     """table: int32 [sequences, columns], the pages of `cache` that each sequence may use.  q_weight, k_weight: of the per-head norms.
-    calibrator: takes the outputs of the tokens that are committed, or None."""
+    calibrator: takes the outputs of the tokens that are committed, or None; it may have been made on any stream of the cache's device."""
 
     def __init__(self, plan: attention.Rotary, q_weight, k_weight, cache: attention.KVCache, table, eps: float = 1e-6,
                  calibrator: Optional[binding.Calibrator] = None):
         self.plan, self.q_weight, self.k_weight, self.cache, self.table, self.eps = plan, q_weight, k_weight, cache, table, eps
+        if calibrator is not None and calibrator.device != cache.device:
+            raise ValueError(f"the calibrator is on cuda:{calibrator.device}, the cache on cuda:{cache.device}")
         self.calibrator = calibrator
         self.prefix = torch.zeros(table.shape[0], dtype=torch.int32, device=table.device)      # committed tokens
         self._last = None
@@ -58,8 +60,20 @@ class AttentionLayer:
             out = out[rows]
             attention.append(self.cache, k_out[rows], v[rows], start, self.prefix, self.table)
         if self.calibrator is not None and out.shape[0]:
-            self.calibrator.step_batch_heads(out.flatten(1), 0, out.shape[1])
+            self._calibrate(out)
         self.prefix += start[1:] - start[:-1]
+
+    def _calibrate(self, out):
+        """The calibrator reads `out` on its own stream: not before it is written, and done before its memory may change."""
+        cal, x = self.calibrator, out.flatten(1)
+        if cal.stream == torch._C._cuda_getCurrentRawStream(cal.device):
+            cal.step_batch_heads(x, 0, out.shape[1])
+            return
+        here = torch.cuda.current_stream(out.device)
+        there = torch.cuda.ExternalStream(cal.stream, out.device) if cal.stream else torch.cuda.default_stream(out.device)
+        there.wait_stream(here)
+        cal.step_batch_heads(x, 0, out.shape[1])
+        here.wait_stream(there)
 
     def gradients(self, q_grad, k_grad):
         """From the gradients of the last step's normed and rotated queries and keys: those of its projections and of the two weights."""
