@@ -410,7 +410,8 @@ typedef struct {
 
 /* New tokens of several sequences, packed: sequence b's are [start[b], start[b + 1]) of the call's rows and become the tokens prefix[b],
  * prefix[b] + 1, ... of that sequence.  Entries are clamped to [0, tokens]; a negative count means none; tokens beyond the table's
- * row (table_columns * page_tokens) are dropped.                                                                        */
+ * row (table_columns * page_tokens) are dropped.  conqur_cache_append with more than 512 sequences: no start may lie below one before it
+ * (where one does, which tokens are written is unspecified).                                                            */
 typedef struct {
   const int32_t* start;      /* sequences + 1 */
   const int32_t* prefix;     /* sequences: tokens committed already, >= 0 */

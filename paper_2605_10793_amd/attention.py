@@ -207,7 +207,8 @@ def _batch(start, prefix, table, device: int) -> Tuple:
 
 def append(cache: KVCache, k, v, start, prefix, table, values: bool = False, k_values=None, v_values=None):
     """New keys and values (bf16) into the cache.  Sequence b's rows are [start[b], start[b + 1]) and become its tokens prefix[b] and on;
-    token i lies in slot i % page_tokens of page table[b, i // page_tokens] (int32 device tensors).  values (8 or 4 bits): also returns
+    token i lies in slot i % page_tokens of page table[b, i // page_tokens] (int32 device tensors).  A start below the one before it: no rows;
+    not with more than 512 sequences, whose starts must not fall.  values (8 or 4 bits): also returns
     what the cache holds of them, (k_values, v_values), in the given or in new bf16 tensors."""
     tokens = k.shape[0]
     device = cache.device
