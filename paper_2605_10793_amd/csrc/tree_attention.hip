@@ -774,7 +774,7 @@ Plan plan_of(const conqur_tree_call& c) {
   // enough to be cut (48 tokens of 8 sequences of 4096, 8 bits: 70 us for 77; 20 of 16 of 3000 to 6000, 4 bits, 80 rows a head: 87 for 96; one of 64 of
   // 501 to 8190, 4 bits: 87 for 92).  Few rows of bf16 values wait for memory, not for them (215 us either way).
   p.tail = p.wide || (c.cache.bits != 16 && blocks * sequences >= 8 * splits) ? 4 : 0;
-  p.splits = alone || sequences > kMaxScan || blocks * sequences >= 1ll << 31 ? 0 : (int)splits;
+  p.splits = alone || sequences > kMaxScan || (blocks + p.tail) * sequences + 2 * kMaxSplits >= 1ll << 31 ? 0 : (int)splits;      // (a run's end is counted too)
   return p;
 }
 
