@@ -33,6 +33,7 @@ struct AppendArgs {
   int64_t val_ts[2], val_hs[2];
   int64_t tokens;
   int wide[2], val_wide[2];       // rows start at multiples of 16 bytes
+  int first_block;                // number of the launch's first workgroup
 };
 
 __device__ __forceinline__ int clamp_to(int v, int64_t hi) { return v < 0 ? 0 : v > hi ? (int)hi : v; }
@@ -128,7 +129,7 @@ __global__ void __launch_bounds__(kThreads, 7) k_append(const AppendArgs a) {
   // Sequence b's blocks are those from start[b] / 64 + 2b on, to start[b + 1] / 64 + 2b + 1: enough for every count and place (n tokens touch at
   // most n / 64 + 2 blocks of slots).  Where starts rise a block is one sequence's or no one's; where one falls, whose sequence has no tokens,
   // blocks of those before and behind it may have one number, and a workgroup does them all.
-  const int id = blockIdx.x;        // below 2^26
+  const int id = a.first_block + (int)blockIdx.x;        // below 2^26
   const int head = blockIdx.y;
   const int sequences = (int)a.batch.sequences;
   auto bound = [&](int x) { return clamp_to(a.batch.start[x], a.tokens); };
@@ -298,12 +299,18 @@ bool is_wide(const conqur_heads& h) {
   return reinterpret_cast<uintptr_t>(h.data) % 16 == 0 && h.token_stride % 8 == 0 && h.head_stride % 8 == 0;
 }
 
+constexpr uint32_t kMostBlocks = 1u << 23;      // of a launch: a grid's threads are counted in 32 bits
+
 template <int BITS>
-void launch_width(const AppendArgs& a, dim3 grid, hipStream_t s) {
-  if (a.cache.width == 128)
-    k_append<BITS, 128><<<grid, kThreads, 0, s>>>(a);
-  else
-    k_append<BITS, 64><<<grid, kThreads, 0, s>>>(a);
+void launch_width(AppendArgs a, uint32_t blocks, hipStream_t s) {
+  for (uint32_t done = 0; done < blocks; done += kMostBlocks) {
+    const dim3 grid(blocks - done < kMostBlocks ? blocks - done : kMostBlocks, a.cache.heads);
+    a.first_block = (int)done;
+    if (a.cache.width == 128)
+      k_append<BITS, 128><<<grid, kThreads, 0, s>>>(a);
+    else
+      k_append<BITS, 64><<<grid, kThreads, 0, s>>>(a);
+  }
 }
 
 }  // namespace
@@ -354,13 +361,13 @@ extern "C" conqur_status conqur_cache_append(const conqur_append_call* c, void* 
     a.val_hs[i] = val[i]->head_stride;
     a.val_wide[i] = is_wide(*val[i]);
   }
-  const dim3 grid((uint32_t)(c->tokens / kBlock + 2 * (uint64_t)c->batch.sequences), c->cache.heads);
+  const uint32_t blocks = (uint32_t)(c->tokens / kBlock + 2 * (uint64_t)c->batch.sequences);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (c->cache.bits == 16)
-    launch_width<16>(a, grid, s);
+    launch_width<16>(a, blocks, s);
   else if (c->cache.bits == 8)
-    launch_width<8>(a, grid, s);
+    launch_width<8>(a, blocks, s);
   else
-    launch_width<4>(a, grid, s);
+    launch_width<4>(a, blocks, s);
   return hipGetLastError() == hipSuccess ? CONQUR_OK : CONQUR_EHIP;
 }

@@ -71,3 +71,23 @@ def test_rising_starts_with_empty_sequences(A, sequences):
         want = torch.full((sequences * columns * page, width), 7.0, dtype=torch.bfloat16, device="cuda:0")
         want[at] = y[:, 0]
         assert torch.equal(x, want)
+
+
+@pytest.mark.parametrize("tokens", [(1 << 29) + 5, (1 << 30) + 200, (1 << 31) - 1])
+def test_more_rows_than_a_grid_counts_threads(A, tokens):
+    """Rows far beyond what one launch's workgroups can be numbered by: the last of them are where they belong."""
+    import torch
+    width, page = 64, 64
+    cache = A.KVCache.empty(6, 1, page, width)
+    cache.k.fill_(7.0)
+    cache.v.fill_(7.0)
+    row = randn(3, 2, 1, width)
+    k, v = (row[i:i + 1].expand(tokens, 1, width) for i in range(2))         # one row for all tokens
+    A.append(cache, k, v, i32([0, 3, tokens - 70, tokens]), i32([0, 0, 20]), i32([[5, -1], [-1, -1], [1, 2]]))
+    want = torch.full((6 * page, width), 7.0, dtype=torch.bfloat16, device="cuda:0")
+    for first, last in ((5 * page, 5 * page + 3), (page + 20, page + 90)):
+        want[first:last] = row[0]
+    assert torch.equal(cache.k.view(-1, width), want)
+    for first, last in ((5 * page, 5 * page + 3), (page + 20, page + 90)):
+        want[first:last] = row[1]
+    assert torch.equal(cache.v.transpose(2, 3).reshape(-1, width), want)
