@@ -239,7 +239,9 @@ def tree_attention(q, cache: KVCache, start, prefix, table, mask=None, max_query
     """Attention of new tokens q (bf16 [tokens, heads, width]; packed as in `append`, which has put their keys and values into the cache) over
     the committed tokens and those new ones that mask (int64, bit j: new token j of the sequence) names; None: each sees itself and those
     before it.  max_query: most new tokens of a sequence (up to 64); max_context: most tokens, committed and new (default: what the table
-    holds; a closer bound shares the work out better).  scale: 1 / sqrt(width) unless given.  Returns out."""
+    holds; a closer bound shares the work out better).  scale: 1 / sqrt(width) unless given.  Returns out.  Rows beyond max_query of a sequence
+    and rows of no sequence have no result: they stay as they are in `out`; in a new tensor, rows beyond 64 of a sequence are zeros, and all of them
+    where there are more tokens than sequences of max_query hold."""
     if q.dim() != 3:
         raise ValueError("q must be [tokens, heads, width]")
     device = cache.device
@@ -250,6 +252,9 @@ def tree_attention(q, cache: KVCache, start, prefix, table, mask=None, max_query
     width = cache.width
     if out is None:
         out = _like(q)
+        # (a max_query below 64 is the caller's word, unless the tokens are too many for it)
+        if tokens > max_query and (max_query >= 64 or tokens > prefix.shape[0] * max_query):
+            out.zero_()
     same = (torch.bfloat16, device, tokens, heads, width)
     fields = (*cache._fields, *_batch(start, prefix, table, device), *_rows(q, "q", *same), *_rows(out, "out", *same),
               0 if mask is None else _vector(mask, "mask", torch.int64, device, tokens), tokens,

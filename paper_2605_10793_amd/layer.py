@@ -36,8 +36,11 @@ class AttentionLayer:
     def step(self, fused, start, depth=None, mask=None, max_query: int = 64, max_context: Optional[int] = None):
         """New tokens of every sequence, at most 64 each: fused [tokens, heads + 2 cache heads, width] holds their queries, keys and values,
         start (int32 [sequences + 1]) the first row of each sequence.  A tree of drafted tokens has its tokens' depths (int64) and masks
-        (attention.tree_attention); without them they are a chain.  Returns [tokens, heads, width].  Nothing is committed."""
+        (attention.tree_attention); without them they are a chain.  max_query: the most of a sequence, so that every token has a result.  Returns
+        [tokens, heads, width].  Nothing is committed."""
         tokens, kv = fused.shape[0], self.cache.heads
+        if tokens > self.table.shape[0] * max_query:
+            raise ValueError(f"{tokens} tokens are more than {max_query} for each of {self.table.shape[0]} sequences")
         heads = fused.shape[1] - 2 * kv
         q, k, v = fused[:, :heads], fused[:, heads:heads + kv], fused[:, heads + kv:]
         counts = (start[1:] - start[:-1]).long()

@@ -65,3 +65,10 @@ def test_a_calibrator_of_another_device_is_refused():
     other.device = 1
     with pytest.raises(ValueError):
         layer_of(other)
+
+
+@pytest.mark.parametrize("tokens,sequences,max_query", [(100, 1, 64), (129, 2, 64), (7, 2, 3)])
+def test_more_tokens_than_have_results_are_refused(tokens, sequences, max_query):
+    """Before any of them is in the cache."""
+    with pytest.raises(ValueError):
+        layer_of(sequences=sequences).step(torch.zeros(tokens, 8, 64), torch.zeros(sequences + 1, dtype=torch.int32), max_query=max_query)
