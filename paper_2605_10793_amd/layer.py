@@ -43,11 +43,10 @@ class AttentionLayer:
             raise ValueError(f"{tokens} tokens are more than {max_query} for each of {self.table.shape[0]} sequences")
         heads = fused.shape[1] - 2 * kv
         q, k, v = fused[:, :heads], fused[:, heads:heads + kv], fused[:, heads + kv:]
-        counts = (start[1:] - start[:-1]).long()
-        first = self.prefix.long()
-        if depth is None:                  # row number less the sequence's first
-            first, depth = first - start[:-1].long(), torch.arange(tokens, device=fused.device)
-        positions = torch.repeat_interleave(first, counts, output_size=tokens) + depth
+        rows = torch.arange(tokens, dtype=torch.int32, device=fused.device)
+        sequence = torch.searchsorted(start[1:], rows, right=True).clamp_(max=self.table.shape[0] - 1)      # (rows of no sequence: the last)
+        first = self.prefix if depth is not None else self.prefix - start[:-1]
+        positions = first[sequence] + (rows.long() if depth is None else depth)
         q_out, k_out = attention.qk_norm_rotary(self.plan, q, k, self.q_weight, self.k_weight, positions, eps=self.eps)
         attention.append(self.cache, k_out, v, start, self.prefix, self.table)
         out = attention.tree_attention(q_out, self.cache, start, self.prefix, self.table, mask=mask, max_query=max_query, max_context=max_context)
@@ -64,7 +63,8 @@ class AttentionLayer:
             attention.append(self.cache, k_out[rows], v[rows], start, self.prefix, self.table)
         if self.calibrator is not None and out.shape[0]:
             self._calibrate(out)
-        self.prefix += start[1:] - start[:-1]
+        start = start.clamp(0, out.shape[0])           # as the operators read it
+        self.prefix += (start[1:] - start[:-1]).clamp_(min=0)
 
     def _calibrate(self, out):
         """The calibrator reads `out` on its own stream: not before it is written, and done before its memory may change."""

@@ -72,3 +72,41 @@ def test_more_tokens_than_have_results_are_refused(tokens, sequences, max_query)
     """Before any of them is in the cache."""
     with pytest.raises(ValueError):
         layer_of(sequences=sequences).step(torch.zeros(tokens, 8, 64), torch.zeros(sequences + 1, dtype=torch.int32), max_query=max_query)
+
+
+@pytest.fixture
+def positions_of(monkeypatch):
+    """The positions that a step hands to the norms."""
+    from paper_2605_10793_amd import layer as module
+    seen = []
+    monkeypatch.setattr(module.attention, "qk_norm_rotary", lambda plan, q, k, qw, kw, positions, eps: seen.append(positions) or (q, k))
+    monkeypatch.setattr(module.attention, "append", lambda *a: None)
+    monkeypatch.setattr(module.attention, "tree_attention", lambda q, *a, **more: q)
+
+    def step(prefix, start, tokens, depth=None):
+        layer = layer_of(sequences=len(prefix))
+        layer.prefix = torch.tensor(prefix, dtype=torch.int32)
+        out = layer.step(torch.zeros(tokens, 8, 64), torch.tensor(start, dtype=torch.int32), depth)
+        assert out.shape == (tokens, 4, 64) and seen[-1].dtype == torch.int64 and seen[-1].shape == (tokens,)
+        layer.commit(torch.tensor(start, dtype=torch.int32))
+        return seen[-1].tolist(), layer.prefix.tolist()
+    return step
+
+
+def test_positions_of_a_chain_and_of_a_tree(positions_of):
+    assert positions_of([10, 20, 30, 40], [0, 0, 3, 3, 5], 5) == ([20, 21, 22, 40, 41], [10, 23, 30, 42])
+    assert positions_of([10, 20], [0, 3, 5], 5, torch.tensor([0, 1, 1, 0, 1])) == ([10, 11, 11, 20, 21], [13, 22])
+    assert positions_of([1 << 30, 5], [0, 0, 0], 0) == ([], [1 << 30, 5])
+
+
+def test_starts_that_do_not_fit_the_tokens(positions_of):
+    """Rows of no sequence, entries beyond the rows, negative counts: positions for the rows there are, and counts as the operators take them.
+    (What a count repeats must not be written past the rows that there are.)"""
+    got, prefix = positions_of([10, 20], [0, 2, 3], 6)
+    assert got[:3] == [10, 11, 20] and prefix == [12, 21]
+    got, prefix = positions_of([10, 20], [0, 2, 1000], 6)
+    assert got == [10, 11, 20, 21, 22, 23] and prefix == [12, 24]
+    got, prefix = positions_of([10, 20, 30], [0, 4, 2, 6], 6)
+    assert len(got) == 6 and prefix == [14, 20, 34]
+    got, prefix = positions_of([10, 20], [-5, -2, 6], 6)
+    assert prefix == [10, 26]
