@@ -20,6 +20,7 @@ import threading
 from typing import Optional, Tuple
 
 import torch
+from torch import _C, bfloat16, contiguous_format, empty_like, float32, int32, int64
 
 from . import binding
 
@@ -41,22 +42,22 @@ def _check(status: int, what: str) -> None:
 
 
 # A decode step makes three of these calls a layer, so what Python does around each counts as much as a small kernel: tensors are looked at with
-# as few attribute reads as the checks need, and the stream is asked for by device index (a pass of `rotary` 15.1 -> 10 us, of which the
-# launch is 3.7).
+# as few attribute reads as the checks need, torch's names are taken once, and the stream is asked for by device index (a pass of `rotary`
+# 15.1 -> 10 us, of which the launch is 3.7).
 
-def _rows(x, name: str, dtype, device: int, tokens: int, heads: int, width: int) -> Tuple[int, int, int, int]:
-    shape, stride = x.shape, x.stride()
-    if len(shape) != 3 or shape[0] != tokens or shape[1] != heads or shape[2] != width or stride[2] != 1 or x.dtype is not dtype:
-        raise ValueError(f"{name} must be a [{tokens}, {heads}, {width}] device tensor of {dtype} with unit stride along the width")
-    if x.get_device() != device or device < 0:
+def _rows(x, name: str, dtype, device: int, shape) -> Tuple[int, int, int, int]:
+    stride = x.stride()
+    if x.shape != shape or len(shape) != 3 or stride[2] != 1 or x.dtype is not dtype:
+        raise ValueError(f"{name} must be a {list(shape)} device tensor of {dtype} with unit stride along the width")
+    if x.get_device() != device:
         _elsewhere(x, name, device)
-    return x.data_ptr(), stride[0], stride[1], heads
+    return x.data_ptr(), stride[0], stride[1], shape[1]
 
 
 def _vector(x, name: str, dtype, device: int, n: int) -> int:
     if x.dtype is not dtype or x.shape != (n,) or not x.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} device tensor of {n} entries")
-    if x.get_device() != device or device < 0:
+    if x.get_device() != device:
         _elsewhere(x, name, device)
     return x.data_ptr()
 
@@ -66,17 +67,16 @@ def _elsewhere(x, name: str, device: int):
     raise ValueError(f"{name} lies on {x.device}, where a tensor on " + ("a GPU" if device < 0 else f"cuda:{device}") + " is needed")
 
 
-def _run(call, x, *args) -> int:
-    """A library call's status, on x's device and that device's current stream."""
-    index = x.get_device()
-    if index == torch._C._cuda_getDevice():
-        return call(*args, torch._C._cuda_getCurrentRawStream(index))
-    with torch.cuda.device(index):
-        return call(*args, torch._C._cuda_getCurrentRawStream(index))
+def _run(call, device: int, *args) -> int:
+    """A library call's status, on a device and its current stream."""
+    if device == _C._cuda_getDevice():
+        return call(*args, _C._cuda_getCurrentRawStream(device))
+    with torch.cuda.device(device):
+        return call(*args, _C._cuda_getCurrentRawStream(device))
 
 
 def _like(x):
-    return None if x is None else torch.empty_like(x, memory_format=torch.contiguous_format)
+    return None if x is None else empty_like(x, memory_format=contiguous_format)
 
 
 class Rotary:
@@ -98,25 +98,26 @@ class Rotary:
 
 def _rotary_call(plan, q, k, positions, q_out, k_out, q_grad=None, k_grad=None, q_weight=None, k_weight=None, transposed=0, eps=0.0) -> bytes:
     dtype = q.dtype
-    if dtype is not torch.bfloat16 and dtype is not torch.float32:
+    if dtype is not bfloat16 and dtype is not float32:
         raise ValueError("queries and keys must be bf16 or fp32")
-    if q.dim() != 3 or (k is not None and k.dim() != 3):
-        raise ValueError("queries and keys must be [tokens, heads, width]")
-    tokens, heads, width = q.shape
-    k_heads = 0 if k is None else k.shape[1]
+    shape, k_shape = q.shape, None if k is None else k.shape
+    if len(shape) != 3 or (k is not None and (len(k_shape) != 3 or k_shape[0] != shape[0] or k_shape[2] != shape[2])):
+        raise ValueError("queries and keys must be [tokens, heads, width], with as many tokens and as wide")
+    tokens, _, width = shape
     device = q.get_device()
+    if device < 0:
+        _elsewhere(q, "q", device)
     if plan.turns.get_device() != device:
         _elsewhere(plan.turns, "the plan", device)
-    same = (dtype, device, tokens, heads, width)
-    k_same = (dtype, device, tokens, k_heads, width)
+    same, k_same = (dtype, device, shape), (dtype, device, k_shape)
     return _ROTARY.pack(*_rows(q, "q", *same), *(_ABSENT if k is None else _rows(k, "k", *k_same)),
                         *_rows(q_out, "the result of q", *same), *(_ABSENT if k is None else _rows(k_out, "the result of k", *k_same)),
                         *(_ABSENT if q_grad is None else _rows(q_grad, "the gradient of q", *same)),
                         *(_ABSENT if k_grad is None else _rows(k_grad, "the gradient of k", *k_same)),
                         0 if q_weight is None else _vector(q_weight, "q_weight", dtype, device, width),
                         0 if k_weight is None else _vector(k_weight, "k_weight", dtype, device, width),
-                        _vector(positions, "positions", torch.int64, device, tokens), plan.turns.data_ptr(), tokens, width, plan.part, plan.layout,
-                        1 if dtype is torch.bfloat16 else 0, transposed, plan.magnitude, eps, 0)
+                        _vector(positions, "positions", int64, device, tokens), plan.turns.data_ptr(), tokens, width, plan.part, plan.layout,
+                        1 if dtype is bfloat16 else 0, transposed, plan.magnitude, eps, 0)
 
 
 def rotary(plan: Rotary, q, positions, k=None, out=None, k_out=None, transposed: bool = False):
@@ -127,7 +128,7 @@ def rotary(plan: Rotary, q, positions, k=None, out=None, k_out=None, transposed:
     if k_out is None and k is not None:
         k_out = _like(k)
     call = _rotary_call(plan, q, k, positions, out, k_out, transposed=1 if transposed else 0)
-    _check(_run(binding.load().conqur_rotary, q, call), "conqur_rotary")
+    _check(_run(binding.load().conqur_rotary, q.get_device(), call), "conqur_rotary")
     return out if k is None else (out, k_out)
 
 
@@ -138,7 +139,7 @@ def qk_norm_rotary(plan: Rotary, q, k, q_weight, k_weight, positions, eps: float
     if k_out is None:
         k_out = _like(k)
     call = _rotary_call(plan, q, k, positions, out, k_out, q_weight=q_weight, k_weight=k_weight, eps=eps)
-    _check(_run(binding.load().conqur_qk_norm_rotary, q, call), "conqur_qk_norm_rotary")
+    _check(_run(binding.load().conqur_qk_norm_rotary, q.get_device(), call), "conqur_qk_norm_rotary")
     return out, k_out
 
 
@@ -149,11 +150,11 @@ def qk_norm_rotary_backward(plan: Rotary, q, k, q_weight, k_weight, positions, q
     dq, dk = _like(q), _like(k)
     call = _rotary_call(plan, q, k, positions, dq, dk, q_grad, k_grad, q_weight, k_weight, eps=eps)
     width = q.shape[2]
-    dw = torch.empty((2, width), dtype=torch.float32, device=q.device)
+    dw = torch.empty((2, width), dtype=float32, device=q.device)
     size = lib.conqur_qk_norm_rotary_workspace(width)
     workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
     at = dw.data_ptr()
-    _check(_run(lib.conqur_qk_norm_rotary_backward, q, call, at, at + 4 * width, workspace.data_ptr(), size),
+    _check(_run(lib.conqur_qk_norm_rotary_backward, q.get_device(), call, at, at + 4 * width, workspace.data_ptr(), size),
            "conqur_qk_norm_rotary_backward")
     return dq, dk, dw[0], dw[1]
 
@@ -166,7 +167,7 @@ class KVCache:
     def __init__(self, k, v, k_scale=None, v_scale=None, bits: int = 16):
         if bits not in (16, 8, 4):
             raise ValueError("bits must be 16, 8 or 4")
-        dtype = torch.bfloat16 if bits == 16 else torch.uint8
+        dtype = bfloat16 if bits == 16 else torch.uint8
         if k.dim() != 4 or not k.is_cuda or k.dtype != dtype or not k.is_contiguous():
             raise ValueError(f"k must be a contiguous 4-D device tensor of {dtype}")
         pages, heads, page_tokens, n = k.shape
@@ -176,7 +177,7 @@ class KVCache:
             if bits == 16:
                 if s is not None:
                     raise ValueError("a bf16 cache has no scales")
-            elif s is None or s.dtype != torch.float32 or tuple(s.shape) != (pages, heads, page_tokens, 2) or s.device != k.device or not s.is_contiguous():
+            elif s is None or s.dtype != float32 or tuple(s.shape) != (pages, heads, page_tokens, 2) or s.device != k.device or not s.is_contiguous():
                 raise ValueError("codes need contiguous fp32 k_scale and v_scale [pages, heads, page_tokens, 2]")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.pages, self.heads, self.page_tokens, self.bits = pages, heads, page_tokens, bits
@@ -187,21 +188,21 @@ class KVCache:
 
     @classmethod
     def empty(cls, pages: int, heads: int, page_tokens: int, width: int, bits: int = 16, device: str = "cuda") -> "KVCache":
-        n, dtype = (width // 2, torch.uint8) if bits == 4 else (width, torch.uint8 if bits == 8 else torch.bfloat16)
+        n, dtype = (width // 2, torch.uint8) if bits == 4 else (width, torch.uint8 if bits == 8 else bfloat16)
         k = torch.empty((pages, heads, page_tokens, n), dtype=dtype, device=device)
         v = torch.empty((pages, heads, n, page_tokens), dtype=dtype, device=device)
-        scales = [None if bits == 16 else torch.empty((pages, heads, page_tokens, 2), dtype=torch.float32, device=device) for _ in range(2)]
+        scales = [None if bits == 16 else torch.empty((pages, heads, page_tokens, 2), dtype=float32, device=device) for _ in range(2)]
         return cls(k, v, *scales, bits=bits)
 
 
 def _batch(start, prefix, table, device: int) -> Tuple:
     sequences, stride = prefix.shape[0], table.stride()
-    if table.dim() != 2 or table.dtype is not torch.int32 or stride[1] != 1 or table.shape[0] != sequences:
+    if table.dim() != 2 or table.dtype is not int32 or stride[1] != 1 or table.shape[0] != sequences:
         raise ValueError("table must be a [sequences, columns] int32 device tensor with unit column stride")
     if table.get_device() != device:
         _elsewhere(table, "table", device)
     columns = table.shape[1]
-    return (_vector(start, "start", torch.int32, device, sequences + 1), _vector(prefix, "prefix", torch.int32, device, sequences), table.data_ptr(),
+    return (_vector(start, "start", int32, device, sequences + 1), _vector(prefix, "prefix", int32, device, sequences), table.data_ptr(),
             stride[0] if sequences > 1 else max(stride[0], columns), columns, sequences)
 
 
@@ -212,14 +213,14 @@ def append(cache: KVCache, k, v, start, prefix, table, values: bool = False, k_v
     what the cache holds of them, (k_values, v_values), in the given or in new bf16 tensors."""
     tokens = k.shape[0]
     device = cache.device
-    same = (torch.bfloat16, device, tokens, cache.heads, cache.width)
+    same = (bfloat16, device, (tokens, cache.heads, cache.width))
     if values:
         k_values = _like(k) if k_values is None else k_values
         v_values = _like(v) if v_values is None else v_values
     call = _APPEND.pack(*cache._fields, *_batch(start, prefix, table, device), *_rows(k, "k", *same), *_rows(v, "v", *same),
                         *(_ABSENT if k_values is None else _rows(k_values, "k_values", *same)),
                         *(_ABSENT if v_values is None else _rows(v_values, "v_values", *same)), tokens)
-    _check(_run(binding.load().conqur_cache_append, k, call), "conqur_cache_append")
+    _check(_run(binding.load().conqur_cache_append, device, call), "conqur_cache_append")
     return (k_values, v_values) if values else None
 
 
@@ -245,7 +246,7 @@ def tree_attention(q, cache: KVCache, start, prefix, table, mask=None, max_query
     if q.dim() != 3:
         raise ValueError("q must be [tokens, heads, width]")
     device = cache.device
-    if torch._C._cuda_getDevice() != device:       # (what is asked below is asked of the current device)
+    if _C._cuda_getDevice() != device:       # (what is asked below is asked of the current device)
         with torch.cuda.device(device):
             return tree_attention(q, cache, start, prefix, table, mask, max_query, max_context, scale, out)
     tokens, heads, _ = q.shape
@@ -255,15 +256,15 @@ def tree_attention(q, cache: KVCache, start, prefix, table, mask=None, max_query
         # (a max_query below 64 is the caller's word, unless the tokens are too many for it)
         if tokens > max_query and (max_query >= 64 or tokens > prefix.shape[0] * max_query):
             out.zero_()
-    same = (torch.bfloat16, device, tokens, heads, width)
+    same = (bfloat16, device, (tokens, heads, width))
     fields = (*cache._fields, *_batch(start, prefix, table, device), *_rows(q, "q", *same), *_rows(out, "out", *same),
-              0 if mask is None else _vector(mask, "mask", torch.int64, device, tokens), tokens,
+              0 if mask is None else _vector(mask, "mask", int64, device, tokens), tokens,
               table.shape[1] * cache.page_tokens if max_context is None else max_context)
     tail = (max_query, width ** -0.5 if scale is None else scale)
     lib = binding.load()
-    at = device, torch._C._cuda_getCurrentRawStream(device)
+    at = device, _C._cuda_getCurrentRawStream(device)
     # (a graph keeps the room it was captured with: it takes its own, from its memory pool)
-    capturing = torch._C._cuda_isCurrentStreamCapturing()
+    capturing = _C._cuda_isCurrentStreamCapturing()
     rooms = _kept.rooms
     have = _NOTHING if capturing else rooms.get(at, _NOTHING)
     status = lib.conqur_tree_attention(_TREE.pack(*fields, *have[1:], *tail), at[1])
