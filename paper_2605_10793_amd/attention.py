@@ -10,7 +10,8 @@ the stream (the current one of the tensors' device).  Nothing synchronises, noth
   tree_attention                      attention of new tokens (a tree of drafted ones, a chain, a single one) over the cache
 
 Rows are [tokens, heads, width] tensors of any token and head stride, e.g. slices of a fused projection's output.  All tensors of a call, its
-plan and its cache lie on one device.
+plan and its cache lie on one device.  Nothing here is recorded for autograd: tensors that require gradients are refused where gradients are
+enabled.
 """
 from __future__ import annotations
 
@@ -65,6 +66,11 @@ def _vector(x, name: str, dtype, device: int, n: int) -> int:
 def _elsewhere(x, name: str, device: int):
     """A kernel takes addresses as they are: what lies on the host or on another GPU must not get that far."""
     raise ValueError(f"{name} lies on {x.device}, where a tensor on " + ("a GPU" if device < 0 else f"cuda:{device}") + " is needed")
+
+
+def _no_gradient(what: str, instead: str) -> None:
+    """These calls are not part of autograd's graph: a result would end it without a word."""
+    raise ValueError(f"{what} records nothing for autograd: {instead}; call it under torch.no_grad() or on detached tensors")
 
 
 def _run(call, device: int, *args) -> int:
@@ -123,6 +129,8 @@ def _rotary_call(plan, q, k, positions, q_out, k_out, q_grad=None, k_grad=None, 
 def rotary(plan: Rotary, q, positions, k=None, out=None, k_out=None, transposed: bool = False):
     """Queries (and keys) rotated by their positions (int64, one per token), into new tensors unless `out` / `k_out` are given (they may
     be the inputs).  transposed: the transposed rotation, for gradients.  Returns the result of q, or of (q, k)."""
+    if (q.requires_grad or (k is not None and k.requires_grad)) and torch.is_grad_enabled():
+        _no_gradient("rotary", "transposed=True takes gradients back")
     if out is None:
         out = _like(q)
     if k_out is None and k is not None:
@@ -134,6 +142,8 @@ def rotary(plan: Rotary, q, positions, k=None, out=None, k_out=None, transposed:
 
 def qk_norm_rotary(plan: Rotary, q, k, q_weight, k_weight, positions, eps: float = 1e-6, out=None, k_out=None):
     """rotary(w x / sqrt(mean x^2 + eps)) of queries and keys, in one pass; returns (q, k)."""
+    if (q.requires_grad or k.requires_grad or q_weight.requires_grad or k_weight.requires_grad) and torch.is_grad_enabled():
+        _no_gradient("qk_norm_rotary", "qk_norm_rotary_backward gives its gradients")
     if out is None:
         out = _like(q)
     if k_out is None:
@@ -211,6 +221,8 @@ def append(cache: KVCache, k, v, start, prefix, table, values: bool = False, k_v
     token i lies in slot i % page_tokens of page table[b, i // page_tokens] (int32 device tensors).  A start below the one before it: no rows;
     not with more than 512 sequences, whose starts must not fall.  values (8 or 4 bits): also returns
     what the cache holds of them, (k_values, v_values), in the given or in new bf16 tensors."""
+    if (k.requires_grad or v.requires_grad) and torch.is_grad_enabled():
+        _no_gradient("append", "it has no gradient")
     tokens = k.shape[0]
     device = cache.device
     same = (bfloat16, device, (tokens, cache.heads, cache.width))
@@ -243,6 +255,8 @@ def tree_attention(q, cache: KVCache, start, prefix, table, mask=None, max_query
     holds; a closer bound shares the work out better).  scale: 1 / sqrt(width) unless given.  Returns out.  Rows beyond max_query of a sequence
     and rows of no sequence have no result: they stay as they are in `out`; in a new tensor, rows beyond 64 of a sequence are zeros, and all of them
     where there are more tokens than sequences of max_query hold."""
+    if q.requires_grad and torch.is_grad_enabled():
+        _no_gradient("tree_attention", "it has no gradient")
     if q.dim() != 3:
         raise ValueError("q must be [tokens, heads, width]")
     device = cache.device

@@ -219,3 +219,34 @@ def test_capture_is_asked_of_the_cache_s_device(library, current, monkeypatch):
             held.append(torch.empty(4096, dtype=torch.uint8))       # what a workspace given back would be
         assert (len(A._kept.rooms) > 0) and ((library.calls[0][2] == library.calls[1][2]) or not kept)
         assert any(at == room[1] for _, _, at in library.calls for room in A._kept.rooms.values()) == kept
+
+
+# ------------------------------------------------------------------------------------------------ gradients
+
+@pytest.mark.parametrize("name,of", [("rotary", "q"), ("rotary", "k"), ("norm", "q"), ("norm", "k"), ("norm", "q_weight"), ("norm", "k_weight"), ("append", "k"),
+                                     ("append", "v"), ("attention", "q")])
+def test_what_requires_gradients_is_refused(library, current, name, of):
+    """A result without one would end the graph silently.  Without gradients enabled there is nothing to lose."""
+    make, call = CALLS[name]
+
+    def arguments():
+        a = make(0)
+        a[of].requires_grad = True
+        return dict(a, plan=Plan(0)) if name in ("rotary", "norm") else a
+
+    with pytest.raises(ValueError, match="no_grad"):
+        call(arguments(), 0)
+    assert not library.calls
+    with torch.no_grad():
+        call(arguments(), 0)
+    assert library.calls
+
+
+def test_gradients_of_what_requires_them(library, current):
+    """The backward call itself takes any tensors."""
+    make, call = CALLS["gradient"]
+    a = make(0)
+    for x in a.values():
+        x.requires_grad = True
+    call(dict(a, plan=Plan(0)), 0)
+    assert library.calls
