@@ -444,7 +444,7 @@ typedef struct {
   const uint64_t* mask;      /* one per token: bit j is set if the token sees new token j of its sequence.  NULL: a chain, every token sees
                                 itself and those before it                                                                */
   uint64_t tokens;           /* rows of q, below 2^31; 0: nothing is done */
-  uint64_t max_context;      /* largest prefix + count of a sequence (at most table_columns * page_tokens is used); tokens of a
+  uint64_t max_context;      /* largest prefix + count of a sequence, below 2^31 (at most table_columns * page_tokens is used); tokens of a
                                 sequence beyond it are not seen                                                           */
   void* workspace;           /* 16-byte aligned, conqur_tree_attention_workspace bytes; its content does not matter.  Calls that overlap
                                 in time need one each                                                                     */

@@ -27,6 +27,8 @@ from . import binding
 
 SCALINGS = {"none": 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
 
+MOST_CONTEXT = (1 << 31) - 1       # tokens of a sequence that a call counts
+
 # The HOST structs of the header, field by field (conqur_heads: pointer, two strides, heads).
 _HEADS = "QqqQ"
 _ROTARY = struct.Struct("=" + 6 * _HEADS + "QQQQ" + "Q" + "IIIII" + "ff" + "I")
@@ -273,7 +275,7 @@ def tree_attention(q, cache: KVCache, start, prefix, table, mask=None, max_query
     same = (bfloat16, device, (tokens, heads, width))
     fields = (*cache._fields, *_batch(start, prefix, table, device), *_rows(q, "q", *same), *_rows(out, "out", *same),
               0 if mask is None else _vector(mask, "mask", int64, device, tokens), tokens,
-              table.shape[1] * cache.page_tokens if max_context is None else max_context)
+              min(table.shape[1] * cache.page_tokens, MOST_CONTEXT) if max_context is None else max_context)
     tail = (max_query, width ** -0.5 if scale is None else scale)
     lib = binding.load()
     at = device, _C._cuda_getCurrentRawStream(device)

@@ -250,3 +250,35 @@ def test_gradients_of_what_requires_them(library, current):
         x.requires_grad = True
     call(dict(a, plan=Plan(0)), 0)
     assert library.calls
+
+
+# ------------------------------------------------------------------------------------------------ contexts
+
+def test_a_table_wider_than_contexts_are_counted(library, current, monkeypatch):
+    """The default context is what the table holds, up to what a call takes."""
+    contexts = []
+    take = library.conqur_tree_attention
+    monkeypatch.setattr(library, "conqur_tree_attention", lambda call, stream: contexts.append(struct.unpack_from("=Q", call, WORKSPACE - 8)[0]) or take(call, stream),
+                        raising=False)
+    start, prefix, _ = batch_of()
+    for columns in (4, 1 << 26):
+        table = Fake(1, 1, dtype=torch.int32)
+        table.host = Wide(columns)
+        A.tree_attention(Fake(3, 4, 64), cache_of(), start, prefix, table)
+    assert set(contexts) == {4 * 32, (1 << 31) - 1}
+
+
+class Wide:
+    """A table's shape without its memory."""
+
+    def __init__(self, columns):
+        self.shape, self.dtype = (1, columns), torch.int32
+
+    def stride(self):
+        return self.shape[1], 1
+
+    def dim(self):
+        return 2
+
+    def data_ptr(self):
+        return 0x1000
