@@ -76,3 +76,33 @@ def test_tokens_of_one_value(A, bits, kind, group, count):
     want, terms = (x[:, 0].repeat_interleave(group, 0)[None].expand(count, -1, -1) for x in (value, terms[..., None]))
     # (a lane adds up to 64 terms in series, and half as many products' sums, each to 2^-24 of what it has: 2^-17 of the terms)
     assert to_bf16_of(got, want, 32 * terms) <= 1
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("kind", ["among", "above", "below"])
+@pytest.mark.parametrize("group,count", [(8, 1), (8, 3), (8, 8), (4, 40)])
+def test_errors_are_those_of_two_roundings(A, bits, kind, group, count):
+    """The squares of all errors together: the result's rounding, a unit^2 / 12 each, and the weights', up to 2^-14 / 12 of their squares, which the
+    sum that divides takes part in, so that they count by the distance of their values from the result.  A tenth more for some ten thousand draws."""
+    import torch
+    heads, width, prefix, scale = 8, 128, 640, 0.25
+    cache, table = filled_cache(A, [prefix + count], 64, heads, width, bits, 1)
+    k, v = randn(2, prefix + count, heads, width), rows_of(kind, 3, prefix + count, heads, width)
+    A.append(cache, k, v, i32([0, prefix + count]), i32([0]), i32(table))
+    square = limit = spread = 0.0
+    for seed in range(4):
+        q = randn(10 + seed, count, heads * group, width)
+        got = A.tree_attention(q, cache, i32([0, count]), i32([prefix]), i32(table), max_query=count, max_context=prefix + count, scale=scale)
+        keys, values = values_of(cache, "k", table[0], prefix + count)[0], values_of(cache, "v", table[0], prefix + count)[0]
+        for h in range(heads):
+            s = q[:, h * group:(h + 1) * group].double() @ keys[h].t().contiguous() * scale
+            hidden = torch.arange(prefix + count, device="cuda:0") > prefix + torch.arange(count, device="cuda:0")[:, None, None]
+            p = torch.softmax(s.masked_fill(hidden, -float("inf")), -1)
+            want = p @ values[h]
+            unit = torch.exp2(torch.floor(torch.log2(want.abs().clamp(min=1e-30))) - 7)
+            away = (p.square() @ values[h].square() - 2 * want * (p.square() @ values[h]) + want.square() * p.square().sum(-1, keepdim=True)).sum()
+            square += float((got[:, h * group:(h + 1) * group].double() - want).square().sum())
+            limit += float(unit.square().sum()) / 12 + float(away) * 2.0 ** -14 / 12
+            spread += float(p.square().sum(-1).mean()) / (4 * heads)
+    assert spread > 0.1            # few tokens count, or the weights' rounding would not
+    assert square <= 1.1 * limit, square / limit
