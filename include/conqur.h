@@ -391,8 +391,9 @@ conqur_status conqur_qk_norm_rotary_backward(const conqur_rotary_call* call, flo
  *            half) and j + width/2 (high half)
  * Values lie with the tokens side by side because attention contracts over tokens.  With codes, k_scale and v_scale hold two floats
  * { step, offset } for [pages][heads][page_tokens]: the value is step * code + offset.  One range per token and head, by the zero-point
- * quantiser of conqur_quant_error_zp over the head's entries (ratio 1): step = (hi - lo) / (2^bits - 1), code = clamp(rint(y / step) + zeta),
- * zeta = -rint(lo / step), offset = -step * zeta; a constant row has step 0, code 0 and offset lo.  All pools 16-byte aligned.
+ * quantiser's definition (conqur_quant_error_zp, ratio 1) over the head's entries: step = (hi - lo) / (2^bits - 1), code = clamp(rint(y / step) + zeta),
+ * zeta = -rint(lo / step), offset = -step * zeta; a constant row has step 0, code 0 and offset lo.  y / step is a division here, where the scores
+ * multiply by the rounded 1 / step: next to a tie the codes may differ, not the error.  All pools 16-byte aligned.
  * A sequence's token i lies in slot i % page_tokens of page table[i / page_tokens].  A table entry outside [0, pages) names no
  * page: tokens there are not written and not seen.
  */
@@ -431,8 +432,8 @@ typedef struct {
 
 /*
  * Put new keys and values into the cache, and optionally write out the values that it holds of them (what a quantisation-aware stream goes
- * on with, Sec. 3.4).  Tokens of no sequence leave their rows of k_values / v_values as they are.  A row with a NaN or an infinity gives
- * unspecified codes for that row.  Two sequences must not share a page that either appends to.
+ * on with, Sec. 3.4).  Tokens of no sequence leave their rows of k_values / v_values as they are.  A row with a NaN or an infinity, or
+ * whose hi - lo is beyond fp32, gets an unspecified pair and codes.  Two sequences must not share a page that either appends to.
  */
 conqur_status conqur_cache_append(const conqur_append_call* call, void* stream);
 

@@ -222,7 +222,8 @@ def append(cache: KVCache, k, v, start, prefix, table, values: bool = False, k_v
     """New keys and values (bf16) into the cache.  Sequence b's rows are [start[b], start[b + 1]) and become its tokens prefix[b] and on;
     token i lies in slot i % page_tokens of page table[b, i // page_tokens] (int32 device tensors).  A start below the one before it: no rows;
     not with more than 512 sequences, whose starts must not fall.  values (8 or 4 bits): also returns
-    what the cache holds of them, (k_values, v_values), in the given or in new bf16 tensors."""
+    what the cache holds of them, (k_values, v_values), in the given or in new bf16 tensors, where rows of
+    tokens without a place are not written."""
     if (k.requires_grad or v.requires_grad) and torch.is_grad_enabled():
         _no_gradient("append", "it has no gradient")
     tokens = k.shape[0]
