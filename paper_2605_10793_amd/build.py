@@ -21,7 +21,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-u
          "-Rpass-analysis=kernel-resource-usage"]
 
 
-MAX_SCRATCH = 64   # bytes per lane; every kernel has 0
+MAX_SCRATCH = 64   # bytes per lane; attention over 16-bit pages of less than 64 tokens, 128 wide, has 32, every other kernel 0
 
 
 def hipcc() -> str:

@@ -9,8 +9,9 @@
 // at a batch's ragged ends one by one.  W/16 lanes hold a row, both halves' entries of a code byte in the same lane, so that packing and
 // the row's extremes stay in registers.
 //
-// Measured: 8 prompts of 517 to 2048 tokens (8 heads of 128) into 16-bit pages 16.5 us (5.1 TB/s read and written); a token of each of 64 sequences into
-// 4 bits, values emitted, 10.9 us a call, of which the kernel is 6.0: a chain of four reads (bounds, page, row, ...), then single bytes.
+// Measured: 8 prompts of 517 to 2048 tokens (8 heads of 128) into 16-bit pages 17.7 to 18.9 us (4.4 to 4.7 TB/s read and written), into 4 or 8 bits with
+// the values emitted 26 and 26.5 (3.7 and 4.0 TB/s); a token of each of 64 sequences into 4 bits, values emitted, 10.9 us a call, of which the
+// kernel is 5.7: a chain of four reads (bounds, page, row, ...), then single bytes.
 #include "../../include/conqur.h"
 
 #include "kernels.h"

@@ -21,9 +21,9 @@
 //     launch, the workgroups, in a fixed order: no atomics, the same bits in every run.
 //
 // Measured, calls one behind the other: rotary of 4096 tokens of 32 + 8 heads of 128 in bf16 15.1 us (5.6 TB/s read and written), transposed of 1999
-// tokens of 32 + 32 heads of 80 in fp32 18 us (4.5 TB/s); norms and rotary of 8192 tokens of 32 + 8 heads of 128 in bf16 36 us (4.7 TB/s), their
-// gradients 59 us (4.3 TB/s; 49 and 4.6 in the two launches, and what lies between).  A token, or 64: 10 to 11 us a call, of which the kernel
-// is 3.6 and 4.3; the rest is the caller's.
+// tokens of 32 + 32 heads of 80 in fp32 16.2 us (5.1 TB/s); norms and rotary of 8192 tokens of 32 + 8 heads of 128 in bf16 36 us (4.7 TB/s), their
+// gradients 59 us (4.3 TB/s; 50 and 4.6 in the two launches, and what lies between), in fp32 72 and 107 us (4.7 TB/s).  A token, or 64: 10 to
+// 11 us a call, of which the kernel is 3.5 and 4.3; the rest is the caller's.
 #include "../../include/conqur.h"
 
 #include <math.h>

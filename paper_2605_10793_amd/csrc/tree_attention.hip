@@ -21,10 +21,10 @@
 //
 // The kernel below is for few rows, bound by HBM: each of a workgroup's four wavefronts takes 64 keys at a time by itself, from memory straight into
 // operands, and has the next 64 under way; their results meet in LDS at the end.  Measured, 32 query and 8 cache heads of 128: a
-// token of 64 sequences of 501 to 8190 tokens, 16 bits, 204 to 210 us (5.4 to 5.6 TB/s); in 8 bits 122 us (5.0 TB/s), in 4 bits 87 us (3.7 TB/s, as
-// much work as in 16 bits for a third of the bytes); 5 tokens of 2 sequences of 131000 tokens, 4 bits, 20 rows a cache head, 89 us (3.3
+// token of 64 sequences of 501 to 8190 tokens, 16 bits, 204 to 210 us (5.4 to 5.6 TB/s); in 8 bits 121 us (5.0 TB/s), in 4 bits 86 us (3.7 TB/s, as
+// much work as in 16 bits for a third of the bytes); 5 tokens of 2 sequences of 131000 tokens, 4 bits, 20 rows a cache head, 88 us (3.3
 // TB/s): there the conversions, exponentials and the two products of a wavefront, two wavefronts a SIMD, are what takes the time.  One token of one
-// sequence of 777 tokens 13.8 us, two launches of a chain of dependent reads.
+// sequence of 777 tokens 13.9 us, two launches of a chain of dependent reads.
 #include "tree_attention.h"
 
 using namespace conqur;
@@ -771,7 +771,8 @@ Plan plan_of(const conqur_tree_call& c) {
   const int64_t workgroups = sequences * groups;
   const bool alone = blocks <= kWaves || (blocks <= 32 && workgroups >= kSlots) || (blocks <= 128 && workgroups >= 4 * kSlots);
   // The new tokens, with their masks, take a workgroup as long as some four blocks of committed ones, so they count for as many, where a run is long
-  // enough to be cut (48 tokens of 8 sequences of 4096, 8 bits: 70 us for 77; 20 of 16 of 3000 to 6000, 4 bits, 80 rows a head: 87 for 96; one of 64 of
+  // enough to be cut (48 tokens of 8 sequences of 4096, 8 bits: 70 us for 77; 20 of 16 of 3000 to 6000, 4 bits, 80 rows a head: 87 for 96, both before the
+  // sums took rounded weights, which made it 92; one of 64 of
   // 501 to 8190, 4 bits: 87 for 92).  Few rows of bf16 values wait for memory, not for them (215 us either way).
   p.tail = p.wide || (c.cache.bits != 16 && blocks * sequences >= 8 * splits) ? 4 : 0;
   p.splits = alone || sequences > kMaxScan || (blocks + p.tail) * sequences + 2 * kMaxSplits >= 1ll << 31 ? 0 : (int)splits;      // (a run's end is counted too)
