@@ -465,6 +465,51 @@ typedef struct {
 uint64_t conqur_tree_attention_workspace(const conqur_tree_call* call);
 conqur_status conqur_tree_attention(const conqur_tree_call* call, void* stream);
 
+/*
+ * Attention of packed sequences over themselves: rows [start[b], start[b + 1]) of q, k and v are sequence b's tokens 0, 1, ...  Row i of a
+ * sequence of n tokens sees its keys j with max(0, first, i - window + 1) <= j < min(n, last), with the score
+ *   s_ij = c tanh(scale q_i k_j / c) - slope |i - j|   (cap c = 0: scale q_i k_j - slope |i - j|)
+ * and gets out_i = sum_j p_ij v_j, p_ij = e^(s_ij - lse_i), lse_i = log sum_j e^(s_ij) over the keys it sees; a row that sees nothing, or whose every
+ * score is -inf, gets zeros (lse -inf).  What a row does not see has no influence on it, whatever it holds.  Scores, maxima, sums and results in
+ * 32 bits; the weights are rounded to bf16 as factors of the second product, and summed so.
+ */
+typedef struct {
+  conqur_heads q, k, v;      /* bf16, [tokens][heads][width]; k and v of as many heads, q of a multiple of that, at most 64 times it: query head j
+                                reads head j / (q.heads / k.heads)                                                         */
+  conqur_heads out;          /* conqur_attention: the result, may be q.  Backward: what conqur_attention gave               */
+  conqur_heads out_grad;     /* backward only: the gradient of the result                                                   */
+  conqur_heads q_grad, k_grad, v_grad;  /* backward only: gradients; none may overlap an input or another                   */
+  float* lse;                /* [tokens][q.heads]: written by conqur_attention (NULL: not wanted), read by its backward      */
+  const int32_t* start;      /* sequences + 1; entries are clamped to [0, tokens].  They must not fall (where one does, which rows are written is
+                                unspecified)                                                                                */
+  const int32_t* first;      /* one per token, in tokens of its sequence: the first key that it sees; NULL: 0               */
+  const int32_t* last;       /* ... the last key that it sees, plus 1 (clamped to the sequence's tokens); NULL: itself       */
+  const float* slopes;       /* one per query head; NULL: none                                                              */
+  uint64_t tokens;           /* tokens * (q.heads / k.heads) below 2^31 - 256; 0: nothing is done                            */
+  uint32_t sequences;        /* 1 to 65535                                                                                  */
+  uint32_t width;            /* 32, 64, 80, 96 or 128                                                                       */
+  uint32_t window;           /* tokens that a token sees at most, itself the last; 0: no such limit                          */
+  float cap;                 /* >= 0, finite; 0: none                                                                       */
+  float scale;               /* finite                                                                                      */
+  uint32_t zero_rest;        /* 1: rows of no sequence get zeros (lse -inf); 0: they stay as they are                        */
+  void* workspace;           /* 16-byte aligned; its content does not matter.  Calls that overlap in time need one each      */
+  uint64_t workspace_bytes;
+} conqur_attention_call;
+
+/* Bytes of workspace: none for rows that start at multiples of 16 bytes (and lie less than 16 MiB apart); others are laid out there first. */
+uint64_t conqur_attention_workspace(const conqur_attention_call* call);
+conqur_status conqur_attention(const conqur_attention_call* call, void* stream);
+
+/*
+ * Its gradients, for the gradient g of the result: with D_i = sum g_i out_i, ds_ij = p_ij (g_i v_j - D_i), du_ij = ds_ij (1 - tanh^2 of that score),
+ *   q_grad_i = scale sum_j du_ij k_j,  k_grad_j = scale sum_i du_ij q_i,  v_grad_j = sum_i p_ij g_i,
+ * the latter two over all query heads of the key head, each sum in 32 bits and in an order that depends on the call's sizes and starts alone; p and du are
+ * rounded to bf16 as factors.  A row that sees nothing has no part in any, whatever its gradient holds; keys that no row sees get zeros.  A gradient that is
+ * not finite reaches nothing that its row does not see; what it sees may become NaN throughout.
+ */
+uint64_t conqur_attention_backward_workspace(const conqur_attention_call* call);
+conqur_status conqur_attention_backward(const conqur_attention_call* call, void* stream);
+
 /* Device times (ms) of the most recent call of each kind, measured with HIP events on the
  * context's stream.  level 0: off.  level 1: one event pair around each whole call (what a
  * caller's pipeline sees: the call's kernels run back to back).  level 2: additionally one

@@ -8,6 +8,7 @@ the stream (the current one of the tensors' device).  Nothing synchronises, noth
   qk_norm_rotary, .._backward         per-head norms and positions in one pass, and that pass's gradients
   KVCache, append                     a paged cache of keys and values in bf16 or in 8- or 4-bit zero-point codes
   tree_attention                      attention of new tokens (a tree of drafted ones, a chain, a single one) over the cache
+  attention, attention_backward       attention of packed sequences over themselves, and its gradients
 
 Rows are [tokens, heads, width] tensors of any token and head stride, e.g. slices of a fused projection's output.  All tensors of a call, its
 plan and its cache lie on one device.  Nothing here is recorded for autograd: tensors that require gradients are refused where gradients are
@@ -35,6 +36,7 @@ _ROTARY = struct.Struct("=" + 6 * _HEADS + "QQQQ" + "Q" + "IIIII" + "ff" + "I")
 _CACHE_BATCH = "QQQQQIIII" + "QQQqII"
 _APPEND = struct.Struct("=" + _CACHE_BATCH + 4 * _HEADS + "Q")
 _TREE = struct.Struct("=" + _CACHE_BATCH + 2 * _HEADS + "QQQQQ" + "If")
+_ATTENTION = struct.Struct("=" + 8 * _HEADS + "QQQQQ" + "Q" + "III" + "ff" + "I" + "QQ")
 _ABSENT = (0, 0, 0, 0)
 _NOTHING = (None, 0, 0)
 
@@ -295,3 +297,76 @@ def tree_attention(q, cache: KVCache, start, prefix, table, mask=None, max_query
             status = lib.conqur_tree_attention(_TREE.pack(*fields, *have[1:], *tail), at[1])
     _check(status, "conqur_tree_attention")
     return out
+
+
+def _attention_call(q, k, v, out, start, first, last, window: int, cap: float, slopes, scale: Optional[float], lse: int, zero_rest: bool, gradients=None) -> Tuple:
+    """The call's fields but for its workspace, and its device."""
+    shape, k_shape = q.shape, k.shape
+    if len(shape) != 3 or len(k_shape) != 3 or k_shape[0] != shape[0] or k_shape[2] != shape[2]:
+        raise ValueError("queries, keys and values must be [tokens, heads, width], with as many tokens and as wide")
+    tokens, heads, width = shape
+    device = q.get_device()
+    if device < 0:
+        _elsewhere(q, "q", device)
+    if start.dim() != 1 or start.shape[0] < 2:
+        raise ValueError("start must hold the sequences' first rows and the last one's end")
+    same, k_same = (bfloat16, device, shape), (bfloat16, device, k_shape)
+    rows = (*_rows(q, "q", *same), *_rows(k, "k", *k_same), *_rows(v, "v", *k_same), *_rows(out, "out", *same))
+    if gradients is None:
+        rows += 4 * _ABSENT
+    else:
+        grad, dq, dk, dv = gradients
+        rows += (*_rows(grad, "grad", *same), *_rows(dq, "the gradient of q", *same), *_rows(dk, "the gradient of k", *k_same),
+                 *_rows(dv, "the gradient of v", *k_same))
+    if not 0 <= window < 1 << 31:
+        raise ValueError("window must be 0 (none) or a number of tokens")
+    sequences = start.shape[0] - 1
+    return (*rows, lse, _vector(start, "start", int32, device, sequences + 1), 0 if first is None else _vector(first, "first", int32, device, tokens),
+            0 if last is None else _vector(last, "last", int32, device, tokens), 0 if slopes is None else _vector(slopes, "slopes", float32, device, heads),
+            tokens, sequences, width, window, cap, width ** -0.5 if scale is None else scale, 1 if zero_rest else 0), device
+
+
+def _with_room(call, size_of, fields, x, device: int) -> int:
+    """A call's status, with the workspace that it asks for, if any."""
+    size = size_of(_ATTENTION.pack(*fields, 0, 0))
+    if not size:
+        return _run(call, device, _ATTENTION.pack(*fields, 0, 0))
+    room = torch.empty(size, dtype=torch.uint8, device=x.device)
+    return _run(call, device, _ATTENTION.pack(*fields, room.data_ptr(), size))
+
+
+def attention(q, k, v, start, first=None, last=None, window: int = 0, cap: float = 0.0, slopes=None, scale: Optional[float] = None, lse: bool = False,
+              out=None):
+    """Attention of packed sequences over themselves: q [tokens, heads, width], k and v [tokens, key heads, width], bf16, heads a multiple of the key
+    heads (up to 64 times); start (int32 [sequences + 1], not falling): sequence b's tokens are the rows [start[b], start[b + 1]).  width: 32, 64, 80, 96
+    or 128.  A token sees itself and those before it, or, of its sequence's tokens, those from first on up to, not including, last (int32, one per
+    row of q): documents in a sequence, prefixes seen from both sides, padding that sees nothing (first >= last: zeros); window: and at most that many, itself the
+    last.  cap: scores become cap tanh(score / cap); slopes (fp32 [heads]): less slope times the distance.  scale: 1 / sqrt(width) unless given.
+    Returns out, or (out, lse): fp32 [tokens, heads], the logarithms of the rows' sums.  Rows of no sequence are zeros in a new tensor (lse -inf)
+    and stay as they are in a given `out` (their lse is then not written)."""
+    if (q.requires_grad or k.requires_grad or v.requires_grad) and torch.is_grad_enabled():
+        _no_gradient("attention", "attention_backward gives its gradients")
+    new = out is None
+    if new:
+        out = _like(q)
+    sums = torch.empty((q.shape[0], q.shape[1]), dtype=float32, device=q.device) if lse else None
+    fields, device = _attention_call(q, k, v, out, start, first, last, window, cap, slopes, scale, 0 if sums is None else sums.data_ptr(), new)
+    lib = binding.load()
+    _check(_with_room(lib.conqur_attention, lib.conqur_attention_workspace, fields, q, device), "conqur_attention")
+    return (out, sums) if lse else out
+
+
+def attention_backward(q, k, v, out, lse, grad, start, first=None, last=None, window: int = 0, cap: float = 0.0, slopes=None,
+                       scale: Optional[float] = None):
+    """Gradients of attention (of q, of k, of v) for the gradient `grad` of its result `out` (bf16), with the lse that it gave and the other arguments as
+    it took them.  Rows of no sequence get zeros."""
+    tokens, heads = q.shape[0], q.shape[1]
+    if lse.dtype is not float32 or lse.shape != (tokens, heads) or not lse.is_contiguous():
+        raise ValueError(f"lse must be a contiguous fp32 device tensor [{tokens}, {heads}]")
+    if lse.get_device() != q.get_device():
+        _elsewhere(lse, "lse", q.get_device())
+    gradients = grad, _like(q), _like(k), _like(v)
+    fields, device = _attention_call(q, k, v, out, start, first, last, window, cap, slopes, scale, lse.data_ptr(), True, gradients)
+    lib = binding.load()
+    _check(_with_room(lib.conqur_attention_backward, lib.conqur_attention_backward_workspace, fields, q, device), "conqur_attention_backward")
+    return gradients[1:]

@@ -1,0 +1,315 @@
+// What the kernels of attention over packed sequences share: arguments, how the work is cut, which keys a row sees, tiles of rows in LDS.
+#pragma once
+#include <limits.h>
+#include <math.h>
+
+#include <type_traits>
+#include <utility>
+
+#include "../../include/conqur.h"
+#include "kernels.h"
+
+namespace conqur {
+namespace packed {
+
+constexpr int kWaves = 4;
+constexpr int kTile = 64;                         // keys, or rows, that lie in LDS at a time
+constexpr int kRows = 32 * kWaves;                // rows of a workgroup: query heads of a key head, token by token
+constexpr float kRise = 16.0f;                    // by how much (log2) scores may exceed the maximum they are taken against, before it and all results are raised
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct Rows {
+  bf16_bits* data;
+  int64_t ts, hs;            // elements
+};
+
+struct PackedArgs {
+  Rows q, k, v, out;
+  Rows q_grad, k_grad, v_grad, out_grad;
+  float* lse;                // [token][query head], natural logarithms; may be null
+  const int32_t* start;
+  const int32_t* first;      // of each token; may be null
+  const int32_t* last;
+  const float* slopes;       // of each query head; may be null
+  int64_t tokens;
+  int sequences, heads, group, width, window;      // heads: of keys; window 0: none
+  int rest;                  // rows of no sequence are written, too: zeros
+  float scale, scale_log2, cap_log2, cap_in;       // cap_log2 = cap log2 e (0: none), cap_in = 2 log2 e scale / cap
+  // Of the backward pass.  Rows are numbered token * group + query head of the key head.
+  float2* stat;              // [key head][row] logarithm (base 2) of the row's sum (+inf: there is none), sum over its gradient times its result
+  int2* seen;                // [row] first key and last + 1
+  int4* span;                // [32 rows of an item] lowest first, highest last, highest first, lowest last (a row that sees nothing: highest first is INT_MAX)
+};
+
+// The arguments as a kernel reads them, where they lie: what a part of a kernel needs of them is read there and not kept in registers.
+typedef const __attribute__((address_space(4))) PackedArgs* Args;
+__device__ __forceinline__ Args kernel_args() {
+  Args p = (Args)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return p;
+}
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+// Sequences are numbered from 1 on; 0 is the rows before the first and `sequences` + 1 those behind the last.
+__device__ __forceinline__ int edge_of(Args a, int i) {
+  if (i <= 0) return 0;
+  const int64_t tokens = a->tokens;
+  if (i > a->sequences + 1) return (int)tokens;
+  const int v = a->start[i - 1];
+  return v < 0 ? 0 : v > tokens ? (int)tokens : v;
+}
+
+// A piece of a sequence: its parts are numbered from edge * of / per + (number of the sequence) on, of = 1 (tokens) or group (rows), which leaves room
+// for ceil(count * of / per) of each, so that a part's sequence is found by halving and no table is made.
+struct Item {
+  int first, count;      // rows of the call that are the sequence's tokens
+  int part, parts;
+  int number;            // of the sequence
+  int base;              // number of its first part
+  bool rest;             // of no sequence
+  __device__ __forceinline__ bool find(Args a, int id, int shift, int of) {
+    const int lane = (int)threadIdx.x & 63;
+    int lo = 0, hi = a->sequences + 2;
+    while (hi - lo > 1) {
+      const int step = (hi - lo + 63) >> 6, i = lo + lane * step;
+      const bool at_most = i < hi && (int)(((int64_t)edge_of(a, i) * of) >> shift) + i <= id;
+      const int c = __popcll(__ballot(at_most));
+      lo += (c > 0 ? c - 1 : 0) * step;
+      hi = hi - lo < step ? hi : lo + step;
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    first = __builtin_amdgcn_readfirstlane(edge_of(a, lo));
+    count = __builtin_amdgcn_readfirstlane(edge_of(a, lo + 1)) - first;
+    if (count < 0) count = 0;
+    number = lo;
+    rest = lo == 0 || lo == a->sequences + 1;
+    base = (int)(((int64_t)first * of) >> shift) + lo;
+    parts = (int)(((int64_t)count * of + (1 << shift) - 1) >> shift);
+    part = id - base;
+    return part >= 0 && part < parts && !(rest && !a->rest);
+  }
+};
+
+// Keys [lo, hi) that token p of a sequence sees.
+__device__ __forceinline__ int2 keys_of(Args a, const Item& s, int p) {
+  int lo = 0, hi = p + 1;
+  if (a->first) lo = a->first[s.first + p];
+  if (a->last) hi = a->last[s.first + p];
+  if (lo < 0) lo = 0;
+  if (a->window && p - a->window + 1 > lo) lo = p - a->window + 1;
+  if (hi > s.count) hi = s.count;
+  if (s.rest) hi = 0;
+  return hi > lo ? make_int2(lo, hi) : make_int2(0, 0);
+}
+
+template <typename Op>
+__device__ __forceinline__ int wave_reduce_int(int v, Op op) {
+  const auto a = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
+  const int w = op((int)a[0], (int)a[1]);
+  const auto b = __builtin_amdgcn_permlane16_swap((uint32_t)w, (uint32_t)w, false, false);
+  const uint32_t x = row16_reduce((uint32_t)op((int)b[0], (int)b[1]), [&](uint32_t x, uint32_t y) { return (uint32_t)op((int)x, (int)y); });
+  return __builtin_amdgcn_readfirstlane((int)x);
+}
+__device__ __forceinline__ int wave_min(int v) { return wave_reduce_int(v, [](int a, int b) { return a < b ? a : b; }); }
+__device__ __forceinline__ int wave_max_int(int v) { return wave_reduce_int(v, [](int a, int b) { return a > b ? a : b; }); }
+
+// Over the two lanes that share a column of a 32x32 product.
+template <typename Op>
+__device__ __forceinline__ float halves(float v, Op op) {
+  const uint32_t u = __float_as_uint(v);
+  const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return op(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+
+__device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ bf16x8 frag_of(uint32_t a, uint32_t b, uint32_t c, uint32_t d) { return __builtin_bit_cast(bf16x8, u32x4{a, b, c, d}); }
+// Row (of a product's result) that register r of a lane in half h holds.
+__device__ __forceinline__ constexpr int row_of(int r, int h) { return 8 * (r / 4) + 4 * h + r % 4; }
+
+template <typename F, int... I>
+__device__ __forceinline__ void each_of(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void each(F&& f) {
+  each_of(f, std::make_integer_sequence<int, N>{});
+}
+
+// The lane, counted anew: what is made of it is made where it is used, not kept in registers from one use, far off, to the next.
+__device__ __forceinline__ int lane_anew() {
+  int none = 0;
+  asm volatile("" : "+s"(none));
+  return (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, (uint32_t)none));
+}
+
+// A value that the compiler takes for a new one: constants on top of it become an instruction's offset.
+__device__ __forceinline__ uint32_t anew(uint32_t v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
+// 64 rows of KS * 16 entries in LDS, rows of kPitch bytes.  Chunk c (16 bytes) of a row lies at c ^ f(row): f takes 16 neighbouring rows (8 of pairs of rows
+// of 128 bytes) to different places, for operands whose lanes read a chunk of a row each, and four neighbouring rows to different quarters, for those
+// that are turned round on the way (ds_read_b64_tr_b16: 16 lanes read 4 rows of 16 entries and receive 4 rows' values of one entry each).
+template <int KS>
+struct Tile {
+  static constexpr int kPitch = KS <= 4 ? 128 : 256;
+  static constexpr int kChunks = kPitch / 16;
+  static constexpr int kRowsAt = 64 / kChunks;             // rows that a wavefront fetches with one load
+  static constexpr int kLoads = kTile / kRowsAt / kWaves;
+  static constexpr int kBytes = kTile * kPitch;
+  static constexpr int kTiles = (KS + 1) / 2;              // 32 entries each
+  static __device__ __forceinline__ int f(int row) {
+    return kChunks == 16 ? ((row & 3) << 2 | ((row >> 2) & 3)) : (((row >> 1) & 1) << 2 | ((row >> 2) & 3));
+  }
+  // Operand s of 32 rows from LDS: lane's row `row`, entries 16 s + 8 h to 16 s + 8 h + 7.  row_at: for s = 0.
+  static __device__ __forceinline__ uint32_t row_at(int lane) { return (lane & 31) * kPitch + ((((lane >> 5) ^ f(lane & 31))) << 4); }
+  static __device__ __forceinline__ uint32_t rows_from(uint32_t lds, uint32_t at, int s) { return anew(lds + (at ^ (uint32_t)(s << 5))); }
+  static __device__ __forceinline__ bf16x8 rows(uint32_t from, int u) {
+    return *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)(from + u * 32 * kPitch);
+  }
+  // Turned round: lane's entry 32 t + (lane & 31), rows 16 k + {4 h .. 4 h + 3, 8 + 4 h .. 8 + 4 h + 3}.
+  static __device__ __forceinline__ uint32_t turned_at(int lane) {
+    const int l = lane & 15, half = lane >> 5, part = (lane >> 4) & 1, row = 4 * half + (l >> 2);
+    return row * kPitch + (((2 * part + ((l & 3) >> 1)) ^ f(row)) << 4) + (l & 1) * 8;
+  }
+  struct Turned {
+    uint32_t a, b;
+  };
+  static __device__ __forceinline__ Turned turned_from(uint32_t lds, uint32_t at, int t) {
+    return Turned{anew(lds + (at ^ (uint32_t)(t << 6))), anew(lds + (at ^ (uint32_t)(t << 6) ^ 32u))};
+  }
+  static __device__ __forceinline__ bf16x8 turned(Turned from, int k) {
+    typedef __attribute__((address_space(3))) s16x4* P;
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(from.a + k * 16 * kPitch));
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(from.b + (k * 16 + 8) * kPitch));
+    const u32x2 p = __builtin_bit_cast(u32x2, a), q = __builtin_bit_cast(u32x2, b);
+    return frag_of(p[0], p[1], q[0], q[1]);
+  }
+};
+
+__device__ __forceinline__ uint32_t lds_of(const void* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) unsigned char*)p; }
+
+// 16 bytes a lane from memory to LDS, 64 lanes side by side: what lies `lane_offset` (each lane's) and `offset` behind `from`.  In assembly, because the
+// compiler lets reads that turn rows round wait for all that is on its way to LDS, wherever it goes; wait_loads() and a barrier say when it is there.
+__device__ __forceinline__ void send16(u32x4 from, uint32_t lds, int lane_offset, int offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+               :
+               : "s"(lds), "v"(lane_offset), "s"(from), "s"(offset)
+               : "memory", "m0");
+}
+__device__ __forceinline__ u32x4 memory_at(const void* p) {
+  const uint64_t x = (uint64_t)(uintptr_t)p;
+  return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)x), (uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32) & 0xffff), 0x7fffffffu, 0x00020000u};
+}
+
+// Sends for rows [at, at + 64) of one head to a tile; rows behind `count` are the last one again, as are chunks behind the width.
+template <int KS>
+__device__ __forceinline__ void send_tile(const bf16_bits* rows, int stride, int count, uint32_t lds, int wave) {
+  using T = Tile<KS>;
+  const u32x4 from = memory_at(rows);
+  const int lane = lane_anew();
+  const int in = lane / T::kChunks, c0 = (lane % T::kChunks) ^ (T::kChunks == 16 ? in << 2 : ((in >> 1) & 1) << 2 | in >> 2);
+  auto chunk = [&](int i) {
+    int c = c0 ^ (T::kChunks == 16 ? i & 3 : (i & 1) << 1);
+    if (KS * 2 < T::kChunks) c = c < KS * 2 ? c : KS * 2 - 1;
+    return c * 16;
+  };
+  if (count >= kTile) {
+    const int at = in * stride;
+#pragma unroll
+    for (int i = 0; i < T::kLoads; ++i) {
+      const int r0 = (wave * T::kLoads + i) * T::kRowsAt;
+      send16(from, lds + r0 * T::kPitch, at + chunk(i), r0 * stride);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < T::kLoads; ++i) {
+      const int r0 = (wave * T::kLoads + i) * T::kRowsAt, r = r0 + in < count ? r0 + in : count - 1;
+      send16(from, lds + r0 * T::kPitch, r * stride + chunk(i), 0);
+    }
+  }
+}
+
+template <int N>
+__device__ __forceinline__ void wait_loads() {          // until no more than the N last loads of the wavefront are under way
+  static_assert(N < 16, "");
+  __builtin_amdgcn_s_waitcnt(0x0F70 | N);
+  asm volatile("" ::: "memory");
+}
+// A barrier that leaves loads under way; LDS accesses before it are done.
+__device__ __forceinline__ void pipeline_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Operands of 32 rows, straight from memory: lane's row, entries 16 s + 8 h on.
+template <int KS>
+__device__ __forceinline__ void load_rows(bf16x8 (&f)[KS], const bf16_bits* row, int h) {
+#pragma unroll
+  for (int s = 0; s < KS; ++s) f[s] = *reinterpret_cast<const bf16x8*>(row + 16 * s + 8 * h);
+}
+
+// Entries 0, 1 or 2 of what a word holds that is neither finite nor ...: words with those halves that are infinities or NaNs taken out.
+__device__ __forceinline__ uint32_t finite_only(uint32_t x) {
+  if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
+  if ((x & 0x7f800000u) == 0x7f800000u) x &= 0x0000ffffu;
+  return x;
+}
+__device__ __forceinline__ bf16x8 finite_only(bf16x8 f) {
+  u32x4 x = __builtin_bit_cast(u32x4, f);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] = finite_only(x[j]);
+  return __builtin_bit_cast(bf16x8, x);
+}
+// Ones where a value is `sign`'s infinity or NaN.
+__device__ __forceinline__ bf16x8 infinite(bf16x8 f, uint32_t sign) {
+  u32x4 x = __builtin_bit_cast(u32x4, f);
+  u32x4 y;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t lo = x[j] & 0xffffu, hi = x[j] >> 16;
+    const bool is_lo = (lo & 0x7fffu) > 0x7f80u || lo == (0x7f80u | sign), is_hi = (hi & 0x7fffu) > 0x7f80u || hi == (0x7f80u | sign);
+    y[j] = (is_lo ? 0x3f80u : 0u) | (is_hi ? 0x3f800000u : 0u);
+  }
+  return __builtin_bit_cast(bf16x8, y);
+}
+// Whether a product of operands with zeros left anything but zeros.
+__device__ __forceinline__ bool any_left(const f32x16& z) {
+  float s = 0.0f;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) s += z[r];
+  return __any(!(s == 0.0f));
+}
+
+// A score in base 2 from a product q k, less the bias; `r` receives 1 / (1 + e^(2 u / cap)), from which 1 - tanh^2 = 4 r (1 - r) follows.
+__device__ __forceinline__ float capped(float dot, float cap_log2, float cap_in, float* r) {
+  *r = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(dot * cap_in));
+  return fmaf(-2.0f * cap_log2, *r, cap_log2);
+}
+
+// Four neighbouring entries of a row's result.
+__device__ __forceinline__ void store4(bf16_bits* to, f32x4 x, bool wide) {
+  const uint32_t a = f32x2_to_bf16x2(x[0], x[1]), b = f32x2_to_bf16x2(x[2], x[3]);
+  if (wide) {
+    *reinterpret_cast<u32x2*>(to) = u32x2{a, b};
+  } else {
+    to[0] = (bf16_bits)a;
+    to[1] = (bf16_bits)(a >> 16);
+    to[2] = (bf16_bits)b;
+    to[3] = (bf16_bits)(b >> 16);
+  }
+}
+__device__ __forceinline__ bool wide8(const bf16_bits* p, int64_t ts, int64_t hs) {
+  return ((uintptr_t)p & 7) == 0 && (ts & 3) == 0 && (hs & 3) == 0;
+}
+
+// Items of the rows, and of the keys, of a call.
+static inline int64_t row_items(const PackedArgs& a) { return a.tokens * a.group / kRows + a.sequences + 2; }
+static inline int64_t key_items(const PackedArgs& a) { return a.tokens / kTile + a.sequences + 2; }
+
+hipError_t launch_forward(const PackedArgs& a, hipStream_t s);
+hipError_t launch_backward(const PackedArgs& a, hipStream_t s);
+
+}  // namespace packed
+}  // namespace conqur

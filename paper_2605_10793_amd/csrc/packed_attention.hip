@@ -1,0 +1,403 @@
+// Attention of packed sequences over themselves.
+//
+//   u_ij = scale q_i k_j, s_ij = cap tanh(u_ij / cap) (cap 0: u_ij) - slope |i - j|, seen are max(0, first_i, i - window + 1) <= j < min(count, last_i)
+//   o_i = sum_j e^(s_ij - m_i) v_j / sum_j e^(s_ij - m_i),  m_i = max_j s_ij,  lse_i = m_i + log sum_j e^(s_ij - m_i)
+//
+// in one pass over the keys, with running maxima and sums (in base 2).  The rows of a key head are its query heads times the tokens, token by token, so
+// that a workgroup's 128 rows are few tokens whose keys nearly coincide.  Both products run transposed, S^T = K Q^T and O^T = V^T P^T (32x32x16 bf16 MFMA): a
+// column is a row of the call, so that a lane holds scores of one row, the maximum needs one exchange, factors on O^T are the lane's own, and S^T leaves the
+// first product as P^T has to enter the second: weights stay in registers.  64 keys and values at a time come to LDS without passing registers, one block
+// ahead of the products; V is turned round as it is read from there.
+#include "packed_attention.h"
+
+namespace conqur {
+namespace packed {
+
+namespace {
+
+template <int KS, bool OPTIONS>
+__global__ void __launch_bounds__(64 * kWaves, 2) k_packed(const PackedArgs) {
+  using T = Tile<KS>;
+  Args a = kernel_args();
+  extern __shared__ __attribute__((aligned(1024))) unsigned char shared[];
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
+  const int head = blockIdx.x % a->heads;
+  Item item;
+  if (!item.find(a, blockIdx.x / a->heads, 7, a->group)) return;
+  static_assert(kRows == 128, "");
+  // The last rows, which see the most in a causal call, first.
+  const int part = item.parts - 1 - item.part, group = a->group;
+  const int rows = item.count * group;
+  auto token_of = [&](int row) { return (int)((uint32_t)(row < rows ? row : rows - 1) / (uint32_t)group); };
+  const int row = part * kRows + wave * 32 + (lane & 31), token = token_of(row);
+  const int2 mine = keys_of(a, item, token);
+
+  // Keys that any row of the workgroup sees, any of the wavefront, all of the wavefront.
+  int begin, end, low, high, low_all, high_all;
+  {
+    auto none = [](int2 x) { return x.x >= x.y; };
+    const bool empty = none(mine);
+    low = wave_min(empty ? INT_MAX : mine.x);
+    high = wave_max_int(mine.y);
+    low_all = wave_max_int(empty ? INT_MAX : mine.x);
+    high_all = wave_min(mine.y);
+    const int2 x = keys_of(a, item, token_of(part * kRows + lane)), y = keys_of(a, item, token_of(part * kRows + 64 + lane));
+    begin = wave_min(min(none(x) ? INT_MAX : x.x, none(y) ? INT_MAX : y.x));
+    end = wave_max_int(max(x.y, y.y));
+    if (part * kRows + wave * 32 >= rows) high = 0;
+  }
+  begin = begin / kTile * kTile;
+
+  const int64_t row_token = item.first + token;
+  const int q_head = head * group + (row < rows ? row : rows - 1) - token * group;
+  bf16x8 qf[KS];
+  load_rows<KS>(qf, a->q.data + row_token * a->q.ts + q_head * a->q.hs, h);
+
+  const int k_stride = (int)(a->k.ts * 2), v_stride = (int)(a->v.ts * 2);
+  const bf16_bits* const k0 = a->k.data + (int64_t)item.first * a->k.ts + head * a->k.hs;
+  const bf16_bits* const v0 = a->v.data + (int64_t)item.first * a->v.ts + head * a->v.hs;
+  const uint32_t lds = lds_of(shared);
+  auto send = [&](int kb, int which) {
+    send_tile<KS>(k0 + (int64_t)kb * a->k.ts, k_stride, item.count - kb, lds + which * 2 * T::kBytes, wave);
+    send_tile<KS>(v0 + (int64_t)kb * a->v.ts, v_stride, item.count - kb, lds + which * 2 * T::kBytes + T::kBytes, wave);
+  };
+
+  f32x16 o[T::kTiles];
+#pragma unroll
+  for (int t = 0; t < T::kTiles; ++t) o[t] = f32x16{};
+  float m = -INFINITY, l = 0.0f;
+  const float scale = a->scale_log2, cap = a->cap_log2, cap_in = a->cap_in, slope = OPTIONS && a->slopes ? a->slopes[q_head] * kLog2e : 0.0f;
+  const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+
+  if (begin < end) send(begin, 0);
+  int which = 0;
+  for (int kb = begin; kb < end; kb += kTile, which ^= 1) {
+    wait_loads<0>();
+    pipeline_barrier();
+    if (kb + kTile < end) send(kb + kTile, which ^ 1);
+    if (kb >= high || kb + kTile <= low) continue;
+    const uint32_t sk = lds + which * 2 * T::kBytes, sv = sk + T::kBytes;
+    const bool all = kb >= low_all && kb + kTile <= high_all;
+
+    const int here = lane_anew();
+    const uint32_t row_at = T::row_at(here), turned_at = T::turned_at(here);
+    f32x16 s[2] = {f32x16{}, f32x16{}};
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      const uint32_t from = T::rows_from(sk, row_at, i);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) s[u] = mfma32(T::rows(from, u), qf[i], s[u]);
+    }
+
+    const float base = m == -INFINITY ? 0.0f : m;
+    if (!OPTIONS && all) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[u][r] = fmaf(s[u][r], scale, -base);
+    } else {
+      if (OPTIONS && cap != 0.0f) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            float x;
+            s[u][r] = capped(s[u][r], cap, cap_in, &x) - base;
+          }
+      } else {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[u][r] = fmaf(s[u][r], scale, -base);
+      }
+      if (OPTIONS && slope != 0.0f) {
+        const float at = (float)(token - kb - 4 * h);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[u][r] = fmaf(-slope, fabsf(at - (float)(32 * u + row_of(r, 0))), s[u][r]);
+      }
+      if (!all) {
+        const int lo = mine.x - kb - 4 * h, hi = mine.y - kb - 4 * h;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[u][r] = 32 * u + row_of(r, 0) >= lo && 32 * u + row_of(r, 0) < hi ? s[u][r] : -INFINITY;
+      }
+    }
+
+    float top = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+    for (int r = 1; r < 16; ++r) top = fmaxf(top, fmaxf(s[0][r], s[1][r]));
+    if (__any(top > (m == -INFINITY ? -INFINITY : kRise))) {
+      top = halves(top, [](float x, float y) { return fmaxf(x, y); });
+      const bool unset = m == -INFINITY;
+      const float by = unset ? (top == -INFINITY ? 0.0f : top) : fmaxf(top, 0.0f);
+      m = unset ? top : m + by;
+      const float f = __builtin_amdgcn_exp2f(-fmaxf(by, 0.0f));          // (before the first score the sums are 0)
+      l *= f;
+#pragma unroll
+      for (int t = 0; t < T::kTiles; ++t) o[t] *= f;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) s[u] -= by;
+    }
+
+    // Weights rounded to bf16, as the second product takes them; the sum that divides takes them so, too.
+    uint32_t p[2][8];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        p[u][r] = f32x2_to_bf16x2(__builtin_amdgcn_exp2f(s[u][2 * r]), __builtin_amdgcn_exp2f(s[u][2 * r + 1]));
+        l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, p[u][r]), ones, l, false);
+      }
+    bool odd = false;
+    if (!all) {          // infinities and NaNs must not reach rows that do not see them: 0 * NaN is NaN
+      f32x16 z = f32x16{};
+#pragma unroll
+      for (int t = 0; t < T::kTiles; ++t) {
+        const auto from = T::turned_from(sv, turned_at, t);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) z = mfma32(T::turned(from, k), frag_of(0, 0, 0, 0), z);
+      }
+      odd = any_left(z);
+    }
+    if (!odd) {
+      typename T::Turned from[T::kTiles];
+#pragma unroll
+      for (int t = 0; t < T::kTiles; ++t) from[t] = T::turned_from(sv, turned_at, t);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t* w = &p[k / 2][k % 2 * 4];
+        const bf16x8 pf = frag_of(w[0], w[1], w[2], w[3]);
+#pragma unroll
+        for (int t = 0; t < T::kTiles; ++t) o[t] = mfma32(T::turned(from[t], k), pf, o[t]);
+      }
+    } else {             // finite values as always; the others are counted over the rows that see them
+      const int lo = mine.x - kb - 4 * h, hi = mine.y - kb - 4 * h;
+#pragma unroll
+      for (int t = 0; t < T::kTiles; ++t) {
+        const auto from = T::turned_from(sv, turned_at, t);
+        f32x16 above = f32x16{}, below = f32x16{};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const bf16x8 v = T::turned(from, k);
+          uint32_t see[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int x = 16 * k + row_of(2 * j, 0);
+            see[j] = (x >= lo && x < hi ? 0x3f80u : 0u) | (x + 1 >= lo && x + 1 < hi ? 0x3f800000u : 0u);
+          }
+          const bf16x8 seen = frag_of(see[0], see[1], see[2], see[3]);
+          const uint32_t* w = &p[k / 2][k % 2 * 4];
+          o[t] = mfma32(finite_only(v), frag_of(w[0], w[1], w[2], w[3]), o[t]);
+          above = mfma32(infinite(v, 0), seen, above);
+          below = mfma32(infinite(v, 0x8000u), seen, below);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          if (above[r] > 0.0f) o[t][r] += INFINITY;
+          if (below[r] > 0.0f) o[t][r] -= INFINITY;
+        }
+      }
+    }
+  }
+
+  a = kernel_args();
+  if (row >= rows) return;
+  l = halves(l, [](float x, float y) { return x + y; });
+  // Nothing seen, or every score -inf: zeros.
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  bf16_bits* const to = a->out.data + row_token * a->out.ts + q_head * a->out.hs + 4 * h;
+  const bool wide = wide8(a->out.data, a->out.ts, a->out.hs);
+#pragma unroll
+  for (int t = 0; t < T::kTiles; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (32 * t + 8 * r < KS * 16) store4(to + 32 * t + 8 * r, f32x4{o[t][4 * r], o[t][4 * r + 1], o[t][4 * r + 2], o[t][4 * r + 3]} * inv, wide);
+  if (a->lse && h == 0) a->lse[row_token * (a->heads * group) + q_head] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * (1.0f / kLog2e);
+}
+
+template <int KS, bool OPTIONS>
+hipError_t launch(const PackedArgs& a, hipStream_t s) {
+  constexpr int kShared = 4 * Tile<KS>::kBytes;
+  static PerDeviceOnce once;
+  const hipError_t e = once.run([] { return hipFuncSetAttribute(reinterpret_cast<const void*>(k_packed<KS, OPTIONS>), hipFuncAttributeMaxDynamicSharedMemorySize, kShared); });
+  if (e != hipSuccess) return e;
+  k_packed<KS, OPTIONS><<<dim3((uint32_t)(row_items(a) * a.heads)), 64 * kWaves, kShared, s>>>(a);
+  return hipGetLastError();
+}
+
+template <int KS>
+hipError_t launch(const PackedArgs& a, hipStream_t s) { return a.cap_log2 != 0.0f || a.slopes ? launch<KS, true>(a, s) : launch<KS, false>(a, s); }
+
+}  // namespace
+
+hipError_t launch_forward(const PackedArgs& a, hipStream_t s) {
+  switch (a.width) {
+    case 32: return launch<2>(a, s);
+    case 64: return launch<4>(a, s);
+    case 80: return launch<5>(a, s);
+    case 96: return launch<6>(a, s);
+    default: return launch<8>(a, s);
+  }
+}
+
+namespace {
+
+// Rows that the kernels cannot read as they lie, laid out side by side.
+__global__ void __launch_bounds__(256) k_lay(Rows from, bf16_bits* to, int64_t tokens, int heads, int width) {
+  const int64_t n = tokens * heads * width;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int e = (int)(i % width);
+    const int64_t row = i / width;
+    to[i] = from.data[row / heads * from.ts + row % heads * from.hs + e];
+  }
+}
+
+constexpr int64_t kMaxStride = 1ll << 40, kNear = 1ll << 23;      // elements; 64 rows kNear apart are addressed in 31 bits
+
+bool heads_fine(const conqur_heads& h, uint64_t heads, uint32_t width, uint64_t tokens, bool output) {
+  if (h.heads != heads || !h.data || reinterpret_cast<uintptr_t>(h.data) % 2) return false;
+  if (h.token_stride < 0 || h.token_stride >= kMaxStride || h.head_stride < 0 || h.head_stride >= kMaxStride) return false;
+  if (!output) return true;
+  const __int128 w = width, ts = h.token_stride, hs = h.head_stride, heads_ = h.heads, n = tokens;
+  if ((heads > 1 && hs < w) || (n > 1 && ts < w)) return false;
+  return !(heads > 1 && n > 1 && ts < (heads_ - 1) * hs + w && hs < (n - 1) * ts + w);
+}
+
+// As the kernels read them: from multiples of 16 bytes, and (64 tokens' rows of a key head) within 31 bits.
+bool plain(const conqur_heads& h) {
+  return reinterpret_cast<uintptr_t>(h.data) % 16 == 0 && h.token_stride % 8 == 0 && h.head_stride % 8 == 0 && h.token_stride < kNear && h.head_stride < kNear;
+}
+
+bool call_fine(const conqur_attention_call* c) {
+  if (!c || c->sequences < 1 || c->sequences > 65535 || !isfinite(c->scale) || !isfinite(c->cap) || c->cap < 0.0f || c->window >= 1u << 31) return false;
+  if (c->width != 32 && c->width != 64 && c->width != 80 && c->width != 96 && c->width != 128) return false;
+  if (c->k.heads < 1 || c->k.heads > 65535 || c->q.heads < 1 || c->q.heads % c->k.heads || c->q.heads / c->k.heads > 64) return false;
+  if (c->tokens >= 1ull << 31 || c->tokens * (c->q.heads / c->k.heads) >= (1ull << 31) - 256) return false;
+  return ((c->tokens * (c->q.heads / c->k.heads)) / kRows + c->tokens / kTile + c->sequences + 2) * c->k.heads < 1ull << 31;
+}
+
+uint64_t lay_bytes(const conqur_attention_call& c, const conqur_heads& h) { return plain(h) ? 0 : (c.tokens * h.heads * c.width * 2 + 255) / 256 * 256; }
+struct BackwardSizes {
+  uint64_t stat, seen, span;
+};
+BackwardSizes backward_sizes(const conqur_attention_call& c) {
+  auto up = [](uint64_t n) { return (n + 255) / 256 * 256; };
+  const uint64_t rows = c.tokens * (c.q.heads / c.k.heads);      // (loads of 64 rows' may reach 128 rows behind the last)
+  return {up((rows * c.k.heads + 128) * sizeof(float2)), up((rows + 128) * sizeof(int2)), up((rows / kRows + c.sequences + 2) * kWaves * sizeof(int4))};
+}
+
+PackedArgs args_of(const conqur_attention_call& c) {
+  PackedArgs a = {};
+  auto rows = [](const conqur_heads& h) { return Rows{static_cast<bf16_bits*>(h.data), h.token_stride, h.head_stride}; };
+  a.q = rows(c.q);
+  a.k = rows(c.k);
+  a.v = rows(c.v);
+  a.out = rows(c.out);
+  a.lse = c.lse;
+  a.start = c.start;
+  a.first = c.first;
+  a.last = c.last;
+  a.slopes = c.slopes;
+  a.tokens = (int64_t)c.tokens;
+  a.sequences = (int)c.sequences;
+  a.heads = (int)c.k.heads;
+  a.group = (int)(c.q.heads / c.k.heads);
+  a.width = (int)c.width;
+  a.window = (int)c.window;
+  a.rest = c.zero_rest != 0;
+  a.scale = c.scale;
+  a.scale_log2 = c.scale * kLog2e;
+  a.cap_log2 = c.cap * kLog2e;
+  a.cap_in = c.cap == 0.0f ? 0.0f : 2.0f * kLog2e * c.scale / c.cap;
+  return a;
+}
+
+// Takes rows that are not plain to `at`, which moves on.
+hipError_t lay(const conqur_attention_call& c, const conqur_heads& h, Rows* r, unsigned char** at, hipStream_t s) {
+  const uint64_t bytes = lay_bytes(c, h);
+  if (!bytes) return hipSuccess;
+  bf16_bits* const to = reinterpret_cast<bf16_bits*>(*at);
+  const uint64_t blocks = (c.tokens * h.heads * c.width + 255) / 256;
+  k_lay<<<dim3((uint32_t)(blocks < 65536 ? blocks : 65536)), 256, 0, s>>>(*r, to, (int64_t)c.tokens, (int)h.heads, (int)c.width);
+  *r = Rows{to, (int64_t)h.heads * c.width, (int64_t)c.width};
+  *at += bytes;
+  return hipGetLastError();
+}
+
+bool room_fine(const conqur_attention_call& c, uint64_t need) {
+  return need == 0 || (c.workspace && reinterpret_cast<uintptr_t>(c.workspace) % 16 == 0 && c.workspace_bytes >= need);
+}
+bool aligned4(const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
+bool arrays_fine(const conqur_attention_call& c) {
+  return c.start && aligned4(c.start) && aligned4(c.first) && aligned4(c.last) && aligned4(c.slopes) && aligned4(c.lse);
+}
+
+}  // namespace
+
+}  // namespace packed
+}  // namespace conqur
+
+using namespace conqur;
+using namespace conqur::packed;
+
+extern "C" uint64_t conqur_attention_workspace(const conqur_attention_call* c) {
+  if (!call_fine(c)) return 0;
+  return lay_bytes(*c, c->q) + lay_bytes(*c, c->k) + lay_bytes(*c, c->v);
+}
+
+extern "C" conqur_status conqur_attention(const conqur_attention_call* c, void* stream) {
+  if (!call_fine(c)) return CONQUR_EINVAL;
+  if (c->tokens == 0) return CONQUR_OK;
+  if (!heads_fine(c->q, c->q.heads, c->width, c->tokens, false) || !heads_fine(c->k, c->k.heads, c->width, c->tokens, false) ||
+      !heads_fine(c->v, c->k.heads, c->width, c->tokens, false) || !heads_fine(c->out, c->q.heads, c->width, c->tokens, true) || !arrays_fine(*c) ||
+      !room_fine(*c, conqur_attention_workspace(c)))
+    return CONQUR_EINVAL;
+  PackedArgs a = args_of(*c);
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  unsigned char* at = static_cast<unsigned char*>(c->workspace);
+  hipError_t e = lay(*c, c->q, &a.q, &at, s);
+  if (e == hipSuccess) e = lay(*c, c->k, &a.k, &at, s);
+  if (e == hipSuccess) e = lay(*c, c->v, &a.v, &at, s);
+  if (e == hipSuccess) e = launch_forward(a, s);
+  return e == hipSuccess ? CONQUR_OK : CONQUR_EHIP;
+}
+
+extern "C" uint64_t conqur_attention_backward_workspace(const conqur_attention_call* c) {
+  if (!call_fine(c)) return 0;
+  const BackwardSizes z = backward_sizes(*c);
+  return z.stat + z.seen + z.span + lay_bytes(*c, c->q) + lay_bytes(*c, c->k) + lay_bytes(*c, c->v) + lay_bytes(*c, c->out) + lay_bytes(*c, c->out_grad);
+}
+
+extern "C" conqur_status conqur_attention_backward(const conqur_attention_call* c, void* stream) {
+  if (!call_fine(c)) return CONQUR_EINVAL;
+  if (c->tokens == 0) return CONQUR_OK;
+  const uint64_t q = c->q.heads, k = c->k.heads;
+  if (!heads_fine(c->q, q, c->width, c->tokens, false) || !heads_fine(c->k, k, c->width, c->tokens, false) ||
+      !heads_fine(c->v, k, c->width, c->tokens, false) || !heads_fine(c->out, q, c->width, c->tokens, false) ||
+      !heads_fine(c->out_grad, q, c->width, c->tokens, false) || !heads_fine(c->q_grad, q, c->width, c->tokens, true) ||
+      !heads_fine(c->k_grad, k, c->width, c->tokens, true) || !heads_fine(c->v_grad, k, c->width, c->tokens, true) || !c->lse || !arrays_fine(*c) ||
+      !room_fine(*c, conqur_attention_backward_workspace(c)))
+    return CONQUR_EINVAL;
+  PackedArgs a = args_of(*c);
+  a.out_grad = Rows{static_cast<bf16_bits*>(c->out_grad.data), c->out_grad.token_stride, c->out_grad.head_stride};
+  a.q_grad = Rows{static_cast<bf16_bits*>(c->q_grad.data), c->q_grad.token_stride, c->q_grad.head_stride};
+  a.k_grad = Rows{static_cast<bf16_bits*>(c->k_grad.data), c->k_grad.token_stride, c->k_grad.head_stride};
+  a.v_grad = Rows{static_cast<bf16_bits*>(c->v_grad.data), c->v_grad.token_stride, c->v_grad.head_stride};
+  const BackwardSizes z = backward_sizes(*c);
+  unsigned char* at = static_cast<unsigned char*>(c->workspace);
+  a.stat = reinterpret_cast<float2*>(at);
+  a.seen = reinterpret_cast<int2*>(at + z.stat);
+  a.span = reinterpret_cast<int4*>(at + z.stat + z.seen);
+  at += z.stat + z.seen + z.span;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  hipError_t e = lay(*c, c->q, &a.q, &at, s);
+  if (e == hipSuccess) e = lay(*c, c->k, &a.k, &at, s);
+  if (e == hipSuccess) e = lay(*c, c->v, &a.v, &at, s);
+  if (e == hipSuccess) e = lay(*c, c->out, &a.out, &at, s);
+  if (e == hipSuccess) e = lay(*c, c->out_grad, &a.out_grad, &at, s);
+  if (e == hipSuccess) e = launch_backward(a, s);
+  return e == hipSuccess ? CONQUR_OK : CONQUR_EHIP;
+}

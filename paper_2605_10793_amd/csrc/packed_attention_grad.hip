@@ -1,0 +1,427 @@
+// Gradients of attention of packed sequences (packed_attention.hip has the formulas of the forward pass).
+//
+//   p_ij = e^(s_ij - lse_i), D_i = sum_d g_id o_id, ds_ij = p_ij (g_i v_j - D_i), du_ij = ds_ij (1 - tanh(u_ij / cap)^2)
+//   dq_i = scale sum_j du_ij k_j,  dk_j = scale sum_i du_ij q_i,  dv_j = sum_i p_ij g_i      (g: the result's gradient)
+//
+// Two kernels, so that no sum's order depends on which workgroup comes first: one walks through the keys for some rows and leaves dq, the other walks through
+// the rows for some keys, all query heads of the key head among them, and leaves dk and dv.  Scores are computed in both (7 products of the 5 that one pass
+// would take).  The first also writes what the second needs of each row: lse, D, the keys it sees, and for 32 rows which keys any and all of them see.
+#include "packed_attention.h"
+
+namespace conqur {
+namespace packed {
+
+namespace {
+
+template <int KS, bool OPTIONS>
+__global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dq(const PackedArgs) {
+  using T = Tile<KS>;
+  Args a = kernel_args();
+  extern __shared__ __attribute__((aligned(1024))) unsigned char shared[];
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
+  const int head = blockIdx.x % a->heads;
+  Item item;
+  if (!item.find(a, blockIdx.x / a->heads, 7, a->group)) return;
+  const int part = item.parts - 1 - item.part, group = a->group;
+  const int rows = item.count * group;
+  auto token_of = [&](int row) { return (int)((uint32_t)(row < rows ? row : rows - 1) / (uint32_t)group); };
+  const int row = part * kRows + wave * 32 + (lane & 31), token = token_of(row);
+  const int2 mine = keys_of(a, item, token);
+  const bool empty = mine.x >= mine.y;
+
+  int begin, end, low, high, low_all, high_all;
+  {
+    auto none = [](int2 x) { return x.x >= x.y; };
+    low = wave_min(empty ? INT_MAX : mine.x);
+    high = wave_max_int(mine.y);
+    low_all = wave_max_int(empty || row >= rows ? INT_MAX : mine.x);
+    high_all = wave_min(mine.y);
+    const int2 x = keys_of(a, item, token_of(part * kRows + lane)), y = keys_of(a, item, token_of(part * kRows + 64 + lane));
+    begin = wave_min(min(none(x) ? INT_MAX : x.x, none(y) ? INT_MAX : y.x));
+    end = wave_max_int(max(x.y, y.y));
+    if (part * kRows + wave * 32 >= rows) high = 0;
+  }
+  begin = begin / kTile * kTile;
+
+  const int64_t row_token = item.first + token;
+  const int q_head = head * group + (row < rows ? row : rows - 1) - token * group;
+  bf16x8 qf[KS], gf[KS];
+  load_rows<KS>(qf, a->q.data + row_token * a->q.ts + q_head * a->q.hs, h);
+  load_rows<KS>(gf, a->out_grad.data + row_token * a->out_grad.ts + q_head * a->out_grad.hs, h);
+  float dot = 0.0f, lse = INFINITY;
+  if (!empty) {
+    bf16x8 of[KS];
+    load_rows<KS>(of, a->out.data + row_token * a->out.ts + q_head * a->out.hs, h);
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) dot = fmaf((float)gf[s][j], (float)of[s][j], dot);
+    lse = a->lse[row_token * (a->heads * group) + q_head] * kLog2e;
+    if (lse == -INFINITY) lse = INFINITY;          // every score is -inf: no weights
+  }
+  dot = halves(dot, [](float x, float y) { return x + y; });
+  {
+    const int64_t at = (int64_t)item.first * group + row;
+    if (row < rows && h == 0) {
+      a->stat[(int64_t)head * a->tokens * group + at] = make_float2(lse, dot);
+      if (head == 0) a->seen[at] = mine;
+    }
+    if (head == 0 && lane == 0) a->span[(int64_t)(item.base + part) * kWaves + wave] = make_int4(low, high, low_all, high_all);
+  }
+
+  const int k_stride = (int)(a->k.ts * 2), v_stride = (int)(a->v.ts * 2);
+  const bf16_bits* const k0 = a->k.data + (int64_t)item.first * a->k.ts + head * a->k.hs;
+  const bf16_bits* const v0 = a->v.data + (int64_t)item.first * a->v.ts + head * a->v.hs;
+  const uint32_t lds = lds_of(shared);
+  auto send = [&](int kb, int which) {
+    send_tile<KS>(k0 + (int64_t)kb * a->k.ts, k_stride, item.count - kb, lds + which * 2 * T::kBytes, wave);
+    send_tile<KS>(v0 + (int64_t)kb * a->v.ts, v_stride, item.count - kb, lds + which * 2 * T::kBytes + T::kBytes, wave);
+  };
+
+  f32x16 dq[T::kTiles];
+#pragma unroll
+  for (int t = 0; t < T::kTiles; ++t) dq[t] = f32x16{};
+  const float scale = a->scale_log2, cap = a->cap_log2, cap_in = a->cap_in, slope = OPTIONS && a->slopes ? a->slopes[q_head] * kLog2e : 0.0f;
+
+  if (begin < end) send(begin, 0);
+  int which = 0;
+  for (int kb = begin; kb < end; kb += kTile, which ^= 1) {
+    wait_loads<0>();
+    pipeline_barrier();
+    if (kb + kTile < end) send(kb + kTile, which ^ 1);
+    if (kb >= high || kb + kTile <= low) continue;
+    const uint32_t sk = lds + which * 2 * T::kBytes, sv = sk + T::kBytes;
+    const bool all = kb >= low_all && kb + kTile <= high_all;
+    const int here = lane_anew();
+    const uint32_t row_at = T::row_at(here), turned_at = T::turned_at(here);
+    bool odd = false;
+    if (!all) {
+      f32x16 z = f32x16{};
+#pragma unroll
+      for (int t = 0; t < T::kTiles; ++t) {
+        const auto from = T::turned_from(sk, turned_at, t);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) z = mfma32(T::turned(from, k), frag_of(0, 0, 0, 0), z);
+      }
+      odd = any_left(z);
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      f32x16 s = f32x16{}, d = f32x16{};
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        s = mfma32(T::rows(T::rows_from(sk, row_at, i), u), qf[i], s);
+        d = mfma32(T::rows(T::rows_from(sv, row_at, i), u), gf[i], d);
+      }
+      if (OPTIONS && cap != 0.0f) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          float x;
+          s[r] = capped(s[r], cap, cap_in, &x) - lse;
+          d[r] = (d[r] - dot) * (4.0f * (x - x * x));
+        }
+      } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[r] = fmaf(s[r], scale, -lse);
+          d[r] -= dot;
+        }
+      }
+      if (OPTIONS && slope != 0.0f) {
+        const float at = (float)(token - kb - 4 * h - 32 * u);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = fmaf(-slope, fabsf(at - (float)row_of(r, 0)), s[r]);
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) d[r] *= __builtin_amdgcn_exp2f(s[r]);
+      if (!all) {
+        const int lo = mine.x - kb - 4 * h - 32 * u, hi = mine.y - kb - 4 * h - 32 * u;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) d[r] = row_of(r, 0) >= lo && row_of(r, 0) < hi ? d[r] : 0.0f;
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const bf16x8 df = frag_of(f32x2_to_bf16x2(d[8 * k], d[8 * k + 1]), f32x2_to_bf16x2(d[8 * k + 2], d[8 * k + 3]),
+                                  f32x2_to_bf16x2(d[8 * k + 4], d[8 * k + 5]), f32x2_to_bf16x2(d[8 * k + 6], d[8 * k + 7]));
+#pragma unroll
+        for (int t = 0; t < T::kTiles; ++t) {
+          bf16x8 f = T::turned(T::turned_from(sk, turned_at, t), 2 * u + k);
+          // A key that is not finite makes the factor of every row that sees it NaN; the others must not meet it.
+          if (odd) f = finite_only(f);
+          dq[t] = mfma32(f, df, dq[t]);
+        }
+      }
+    }
+  }
+
+  a = kernel_args();
+  if (row >= rows) return;
+  bf16_bits* const to = a->q_grad.data + row_token * a->q_grad.ts + q_head * a->q_grad.hs + 4 * h;
+  const bool wide = wide8(a->q_grad.data, a->q_grad.ts, a->q_grad.hs);
+  const float by = a->scale;
+#pragma unroll
+  for (int t = 0; t < T::kTiles; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (32 * t + 8 * r < KS * 16) store4(to + 32 * t + 8 * r, f32x4{dq[t][4 * r], dq[t][4 * r + 1], dq[t][4 * r + 2], dq[t][4 * r + 3]} * by, wide);
+}
+
+constexpr int kStatAt = 0, kSeenAt = 1024, kRowBytes = 2048;      // of 64 rows (and the 64 behind them, which the same loads bring)
+
+// Two wavefronts take 32 of the workgroup's 64 keys each, for the first 32 of 64 rows at a time, two for the others; their sums meet in LDS at the end.
+template <int KS, bool OPTIONS>
+__global__ void __launch_bounds__(64 * kWaves, KS > 6 ? 1 : 2) k_packed_dkv(const PackedArgs) {
+  using T = Tile<KS>;
+  constexpr int kBuffer = 2 * T::kBytes + kRowBytes;
+  Args a = kernel_args();
+  extern __shared__ __attribute__((aligned(1024))) unsigned char shared[];
+  float* const s_slope = reinterpret_cast<float*>(shared + 2 * kBuffer);
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
+  const int head = blockIdx.x % a->heads;
+  Item item;
+  if (!item.find(a, blockIdx.x / a->heads, 6, 1)) return;
+  static_assert(kTile == 64, "");
+  const int group = a->group, rows = item.count * group;
+  const int k0 = item.part * kTile, key0 = k0 + 32 * (wave & 1), at_rows = wave >> 1;      // keys of the workgroup, of the wavefront; which 32 rows
+  const int key = key0 + (lane & 31);
+  const int64_t key_token = item.first + (key < item.count ? key : item.count - 1);
+  if (OPTIONS) {
+    if (a->slopes && (int)threadIdx.x < group) s_slope[threadIdx.x] = a->slopes[head * group + threadIdx.x] * kLog2e;
+    __syncthreads();
+  }
+
+  bf16x8 kf[KS], vf[KS];
+  load_rows<KS>(kf, a->k.data + key_token * a->k.ts + head * a->k.hs, h);
+  load_rows<KS>(vf, a->v.data + key_token * a->v.ts + head * a->v.hs, h);
+
+  // Rows in thirty-twos, 64 of which (`chunk`) a wavefront looks at together; of those any of whose rows sees a key, two by two.
+  const int4* const span = a->span + ((((int64_t)item.first * group) >> 7) + item.number) * kWaves;
+  const int subs = item.rest ? 0 : (rows + 31) / 32;
+  int next_chunk = a->last ? 0 : (int)((int64_t)k0 * group / 64) * 2, chunk = 0;
+  uint64_t active = 0, some = 0, whole = 0;
+  struct Rows64 {
+    int sub;
+    bool some, all;
+  };
+  auto next = [&](Rows64* x) {
+    while (!active) {
+      if (next_chunk >= subs) return false;
+      chunk = next_chunk;
+      next_chunk += 64;
+      const int sub = chunk + lane;
+      int4 s = make_int4(INT_MAX, 0, INT_MAX, 0);
+      if (sub < subs) s = span[sub];
+      const uint64_t near = __ballot(s.x < k0 + kTile && s.y > k0);
+      some = __ballot(s.x < key0 + 32 && s.y > key0);
+      whole = __ballot(s.z <= key0 && s.w >= key0 + 32);
+      active = (near | near >> 1) & 0x5555555555555555ull;
+    }
+    const int bit = __builtin_ctzll(active);
+    active &= active - 1;
+    x->sub = chunk + bit;
+    x->some = (some >> (bit + at_rows)) & 1;
+    x->all = (whole >> (bit + at_rows)) & 1;
+    return true;
+  };
+
+  const bf16_bits* const q0 = a->q.data + (int64_t)item.first * a->q.ts + (int64_t)head * group * a->q.hs;
+  const bf16_bits* const g0 = a->out_grad.data + (int64_t)item.first * a->out_grad.ts + (int64_t)head * group * a->out_grad.hs;
+  const float2* const stat0 = a->stat + ((int64_t)head * a->tokens + item.first) * group;
+  const int2* const seen0 = a->seen + (int64_t)item.first * group;
+  const int q_ts = (int)(a->q.ts * 2), q_hs = (int)(a->q.hs * 2), g_ts = (int)(a->out_grad.ts * 2), g_hs = (int)(a->out_grad.hs * 2);
+  const uint32_t over = (65536 + group - 1) / group;      // n * over >> 16 is n / group for n up to 128, group up to 64
+  const uint32_t lds = lds_of(shared);
+  auto send = [&](int sub, int which) {
+    const int row0 = sub * 32, token0 = (int)((uint32_t)row0 / (uint32_t)group), lead = row0 - token0 * group;
+    const u32x4 from_q = memory_at(q0 + token0 * a->q.ts), from_g = memory_at(g0 + token0 * a->out_grad.ts);
+    const uint32_t to = lds + which * kBuffer;
+    const int me = lane_anew();
+    const int in = me / T::kChunks, c0 = (me % T::kChunks) ^ (T::kChunks == 16 ? in << 2 : ((in >> 1) & 1) << 2 | in >> 2);
+    const int last = rows - 1 - row0;
+#pragma unroll
+    for (int i = 0; i < T::kLoads; ++i) {
+      const int r0 = (wave * T::kLoads + i) * T::kRowsAt, n = lead + (r0 + in < last ? r0 + in : last);
+      const int token = (int)(((uint32_t)n * over) >> 16), member = n - token * group;
+      int c = c0 ^ (T::kChunks == 16 ? i & 3 : (i & 1) << 1);
+      if (KS * 2 < T::kChunks) c = c < KS * 2 ? c : KS * 2 - 1;
+      send16(from_q, to + r0 * T::kPitch, token * q_ts + member * q_hs + c * 16, 0);
+      send16(from_g, to + T::kBytes + r0 * T::kPitch, token * g_ts + member * g_hs + c * 16, 0);
+    }
+    if (wave == 0) send16(memory_at(stat0 + row0), to + 2 * T::kBytes + kStatAt, me * 16, 0);
+    if (wave == 1) send16(memory_at(seen0 + row0), to + 2 * T::kBytes + kSeenAt, me * 16, 0);
+  };
+
+  f32x16 dk[T::kTiles], dv[T::kTiles];
+#pragma unroll
+  for (int t = 0; t < T::kTiles; ++t) dk[t] = dv[t] = f32x16{};
+  const float scale = a->scale_log2, cap = a->cap_log2, cap_in = a->cap_in;
+  const bool biased = OPTIONS && a->slopes;
+
+  Rows64 now, then;
+  bool more = next(&now);
+  if (more) send(now.sub, 0);
+  for (int which = 0; more; which ^= 1, now = then) {
+    wait_loads<0>();
+    pipeline_barrier();
+    more = next(&then);
+    if (more) send(then.sub, which ^ 1);
+    if (!now.some) continue;
+    const uint32_t sq = lds + which * kBuffer, sg = sq + T::kBytes;
+    const unsigned char* const s_rows = shared + which * kBuffer + 2 * T::kBytes + at_rows * 32 * 8;
+    const int here = lane_anew();
+    const uint32_t row_at = T::row_at(here), turned_at = T::turned_at(here);
+    const int half = here >> 5;
+
+    f32x16 s = f32x16{}, d = f32x16{};
+#pragma unroll
+    for (int i = 0; i < KS; ++i) s = mfma32(T::rows(T::rows_from(sq, row_at, i), at_rows), kf[i], s);
+#pragma unroll
+    for (int i = 0; i < KS; ++i) d = mfma32(T::rows(T::rows_from(sg, row_at, i), at_rows), vf[i], d);
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      const f32x4* const at = reinterpret_cast<const f32x4*>(s_rows + kStatAt + (8 * r4 + 4 * half) * 8);
+      const f32x4 x = at[0], y = at[1];
+      const float lse[4] = {x[0], x[2], y[0], y[2]}, dot[4] = {x[1], x[3], y[1], y[3]};
+      if (OPTIONS && cap != 0.0f) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float z;
+          s[4 * r4 + j] = capped(s[4 * r4 + j], cap, cap_in, &z) - lse[j];
+          d[4 * r4 + j] = (d[4 * r4 + j] - dot[j]) * (4.0f * (z - z * z));
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          s[4 * r4 + j] = fmaf(s[4 * r4 + j], scale, -lse[j]);
+          d[4 * r4 + j] -= dot[j];
+        }
+      }
+    }
+    if (biased) {
+      const int row0 = (now.sub + at_rows) * 32, token0 = (int)((uint32_t)row0 / (uint32_t)group), lead = row0 - token0 * group + 4 * half;
+      const float away = (float)(token0 - key);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int n = lead + row_of(r, 0), token = (int)(((uint32_t)n * over) >> 16);
+        s[r] = fmaf(-s_slope[n - token * group], fabsf(away + (float)token), s[r]);
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[r] = __builtin_amdgcn_exp2f(s[r]);
+      d[r] *= s[r];
+    }
+    bool odd = false;
+    if (!now.all) {
+      const int left = rows - (now.sub + at_rows) * 32 - 4 * half;
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        typedef int i32x4 __attribute__((ext_vector_type(4)));
+        const i32x4* const at = reinterpret_cast<const i32x4*>(s_rows + kSeenAt + (8 * r4 + 4 * half) * 8);
+        const i32x4 x = at[0], y = at[1];
+        const int lo[4] = {x[0], x[2], y[0], y[2]}, hi[4] = {x[1], x[3], y[1], y[3]};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const bool see = key >= lo[j] && key < hi[j] && row_of(4 * r4 + j, 0) < left;
+          // A gradient that is not finite makes D so, and must not reach keys that its row does not see: they meet zeros below, the others NaN.
+          const float dot = *reinterpret_cast<const float*>(s_rows + kStatAt + (8 * r4 + 4 * half + j) * 8 + 4);
+          s[4 * r4 + j] = see ? s[4 * r4 + j] + (dot - dot) : 0.0f;
+          d[4 * r4 + j] = see ? d[4 * r4 + j] : 0.0f;
+        }
+      }
+      f32x16 z = f32x16{};
+#pragma unroll
+      for (int t = 0; t < T::kTiles; ++t) {
+        const auto from = T::turned_from(sq, turned_at, t), from_g = T::turned_from(sg, turned_at, t);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          z = mfma32(T::turned(from, 2 * at_rows + k), frag_of(0, 0, 0, 0), z);
+          z = mfma32(T::turned(from_g, 2 * at_rows + k), frag_of(0, 0, 0, 0), z);
+        }
+      }
+      odd = any_left(z);
+    }
+    auto pack = [](const f32x16& x, int k) {
+      return frag_of(f32x2_to_bf16x2(x[8 * k], x[8 * k + 1]), f32x2_to_bf16x2(x[8 * k + 2], x[8 * k + 3]), f32x2_to_bf16x2(x[8 * k + 4], x[8 * k + 5]),
+                     f32x2_to_bf16x2(x[8 * k + 6], x[8 * k + 7]));
+    };
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const bf16x8 pf = pack(s, k), df = pack(d, k);
+#pragma unroll
+      for (int t = 0; t < T::kTiles; ++t) {
+        bf16x8 f = T::turned(T::turned_from(sg, turned_at, t), 2 * at_rows + k);
+        if (odd) f = finite_only(f);
+        dv[t] = mfma32(f, pf, dv[t]);
+      }
+#pragma unroll
+      for (int t = 0; t < T::kTiles; ++t) {
+        bf16x8 f = T::turned(T::turned_from(sq, turned_at, t), 2 * at_rows + k);
+        if (odd) f = finite_only(f);
+        dk[t] = mfma32(f, df, dk[t]);
+      }
+    }
+  }
+
+  __syncthreads();
+  f32x4* const s_sum = reinterpret_cast<f32x4*>(shared) + (wave & 1) * 64 * 8 * T::kTiles + lane;
+  if (wave >= 2) {
+#pragma unroll
+    for (int t = 0; t < T::kTiles; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        s_sum[(t * 4 + r) * 64] = f32x4{dk[t][4 * r], dk[t][4 * r + 1], dk[t][4 * r + 2], dk[t][4 * r + 3]};
+        s_sum[((T::kTiles + t) * 4 + r) * 64] = f32x4{dv[t][4 * r], dv[t][4 * r + 1], dv[t][4 * r + 2], dv[t][4 * r + 3]};
+      }
+  }
+  __syncthreads();
+  a = kernel_args();
+  if (wave >= 2 || key >= item.count) return;
+  const bool k_wide = wide8(a->k_grad.data, a->k_grad.ts, a->k_grad.hs), v_wide = wide8(a->v_grad.data, a->v_grad.ts, a->v_grad.hs);
+  bf16_bits* const to_k = a->k_grad.data + key_token * a->k_grad.ts + head * a->k_grad.hs + 4 * h;
+  bf16_bits* const to_v = a->v_grad.data + key_token * a->v_grad.ts + head * a->v_grad.hs + 4 * h;
+  const float by = a->scale;
+#pragma unroll
+  for (int t = 0; t < T::kTiles; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      if (32 * t + 8 * r >= KS * 16) continue;
+      store4(to_k + 32 * t + 8 * r, (f32x4{dk[t][4 * r], dk[t][4 * r + 1], dk[t][4 * r + 2], dk[t][4 * r + 3]} + s_sum[(t * 4 + r) * 64]) * by, k_wide);
+      store4(to_v + 32 * t + 8 * r, f32x4{dv[t][4 * r], dv[t][4 * r + 1], dv[t][4 * r + 2], dv[t][4 * r + 3]} + s_sum[((T::kTiles + t) * 4 + r) * 64], v_wide);
+    }
+}
+
+template <int KS, bool OPTIONS>
+hipError_t launch(const PackedArgs& a, hipStream_t s) {
+  constexpr int kDq = 4 * Tile<KS>::kBytes, kDkv = 2 * (2 * Tile<KS>::kBytes + kRowBytes) + 256;
+  static_assert(2 * 64 * 8 * Tile<KS>::kTiles * 16 <= kDkv, "sums meet where the tiles were");
+  static PerDeviceOnce once;
+  hipError_t e = once.run([] {
+    const hipError_t x = hipFuncSetAttribute(reinterpret_cast<const void*>(k_packed_dq<KS, OPTIONS>), hipFuncAttributeMaxDynamicSharedMemorySize, kDq);
+    return x != hipSuccess ? x : hipFuncSetAttribute(reinterpret_cast<const void*>(k_packed_dkv<KS, OPTIONS>), hipFuncAttributeMaxDynamicSharedMemorySize, kDkv);
+  });
+  if (e != hipSuccess) return e;
+  k_packed_dq<KS, OPTIONS><<<dim3((uint32_t)(row_items(a) * a.heads)), 64 * kWaves, kDq, s>>>(a);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  k_packed_dkv<KS, OPTIONS><<<dim3((uint32_t)(key_items(a) * a.heads)), 64 * kWaves, kDkv, s>>>(a);
+  return hipGetLastError();
+}
+
+template <int KS>
+hipError_t launch(const PackedArgs& a, hipStream_t s) { return a.cap_log2 != 0.0f || a.slopes ? launch<KS, true>(a, s) : launch<KS, false>(a, s); }
+
+}  // namespace
+
+hipError_t launch_backward(const PackedArgs& a, hipStream_t s) {
+  switch (a.width) {
+    case 32: return launch<2>(a, s);
+    case 64: return launch<4>(a, s);
+    case 80: return launch<5>(a, s);
+    case 96: return launch<6>(a, s);
+    default: return launch<8>(a, s);
+  }
+}
+
+}  // namespace packed
+}  // namespace conqur
