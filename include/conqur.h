@@ -439,6 +439,29 @@ conqur_status conqur_cache_append(const conqur_append_call* call, void* stream);
 
 typedef struct {
   conqur_cache cache;
+  const int32_t* tokens;     /* count: tokens of the sequences that are moved, those of sequence b at [start[b], start[b + 1]) */
+  const int32_t* start;      /* sequences + 1, clamped to [0, count]; they must not fall (where one does, what is moved is unspecified) */
+  const int32_t* table;      /* [sequences][table_stride]: the pages that they lie in */
+  const int32_t* to_table;   /* [sequences][to_stride]: the pages that they go to */
+  int64_t table_stride;
+  int64_t to_stride;
+  uint64_t count;            /* below 2^31; 0: nothing is done */
+  uint32_t table_columns;
+  uint32_t to_columns;
+  uint32_t sequences;        /* 1 to 65535 */
+  uint32_t reserved;
+} conqur_gather_call;
+
+/*
+ * Move tokens of a cache, all heads, as they are held: the i-th of sequence b's goes to slot i % page_tokens of page to_table[b][i / page_tokens], and stays
+ * where it was.  A sequence is forked by copying the page that is not full, compacted by naming the tokens that it keeps; several sequences of the call may read
+ * one page.  A slot that is written must not be one that the call reads, nor be written twice.  Tokens that a table's row does not reach, or whose
+ * page (from or to) is none, are not moved.
+ */
+conqur_status conqur_cache_gather(const conqur_gather_call* call, void* stream);
+
+typedef struct {
+  conqur_cache cache;
   conqur_batch batch;
   conqur_heads q, out;       /* bf16, [tokens][heads][width]; heads a multiple of cache.heads, at most 64 times it: query head j reads
                                 head j / (heads / cache.heads) of the cache.  out may be q                                */
@@ -464,6 +487,33 @@ typedef struct {
  */
 uint64_t conqur_tree_attention_workspace(const conqur_tree_call* call);
 conqur_status conqur_tree_attention(const conqur_tree_call* call, void* stream);
+
+typedef struct {
+  conqur_cache cache;
+  conqur_batch batch;
+  conqur_heads q, out;       /* as in conqur_tree_call */
+  const int32_t* first;      /* one per token, in tokens of its sequence: the first key that it sees; NULL: 0 */
+  const int32_t* last;       /* ... the last key that it sees, plus 1 (clamped to the sequence's tokens in sight); NULL: itself */
+  const float* slopes;       /* one per query head; NULL: none */
+  uint64_t tokens;           /* rows of q, below 2^31; 0: nothing is done */
+  uint64_t max_context;      /* as in conqur_tree_call */
+  void* workspace;           /* 16-byte aligned, conqur_chunk_attention_workspace bytes; as in conqur_tree_call */
+  uint64_t workspace_bytes;
+  uint32_t max_query;        /* largest count of new tokens of a sequence, times the query heads of a cache head below 2^24; tokens beyond it get no result */
+  uint32_t window;           /* tokens that a token sees at most, itself the last; 0: no such limit */
+  float cap;                 /* >= 0, finite; 0: none */
+  float scale;               /* finite */
+  uint32_t zero_rest;        /* 1: rows that get no result (of no sequence, beyond max_query) get zeros; 0: they stay as they are */
+  uint32_t reserved;
+} conqur_chunk_call;
+
+/*
+ * Attention of a chunk of new tokens of each sequence, one or thousands, over a cache that holds them already: the token in place i of its
+ * sequence sees keys max(0, first, i - window + 1) <= j < min(length, last) with the score cap tanh(scale q_i k_j / cap) (cap 0: scale q_i k_j) -
+ * slope |i - j|.  Arithmetic, rounding, missing pages and rows that see nothing as in conqur_tree_attention.
+ */
+uint64_t conqur_chunk_attention_workspace(const conqur_chunk_call* call);
+conqur_status conqur_chunk_attention(const conqur_chunk_call* call, void* stream);
 
 /*
  * Attention of packed sequences over themselves: rows [start[b], start[b + 1]) of q, k and v are sequence b's tokens 0, 1, ...  Row i of a

@@ -7,7 +7,9 @@ the stream (the current one of the tensors' device).  Nothing synchronises, noth
   rotary                              positions into queries and keys, or back out of their gradients
   qk_norm_rotary, .._backward         per-head norms and positions in one pass, and that pass's gradients
   KVCache, append                     a paged cache of keys and values in bf16 or in 8- or 4-bit zero-point codes
+  gather                              tokens of a cache into other pages: forks, tokens that are kept, beams
   tree_attention                      attention of new tokens (a tree of drafted ones, a chain, a single one) over the cache
+  chunk_attention                     attention of any number of new tokens over the cache, with windows, bounds, capped scores, a bias by distance
   attention, attention_backward       attention of packed sequences over themselves, and its gradients
 
 Rows are [tokens, heads, width] tensors of any token and head stride, e.g. slices of a fused projection's output.  All tensors of a call, its
@@ -36,6 +38,8 @@ _ROTARY = struct.Struct("=" + 6 * _HEADS + "QQQQ" + "Q" + "IIIII" + "ff" + "I")
 _CACHE_BATCH = "QQQQQIIII" + "QQQqII"
 _APPEND = struct.Struct("=" + _CACHE_BATCH + 4 * _HEADS + "Q")
 _TREE = struct.Struct("=" + _CACHE_BATCH + 2 * _HEADS + "QQQQQ" + "If")
+_GATHER = struct.Struct("=QQQQQIIII" + "QQQQ" + "qq" + "Q" + "IIII")
+_CHUNK = struct.Struct("=" + _CACHE_BATCH + 2 * _HEADS + "QQQQQQQ" + "II" + "ff" + "II")
 _ATTENTION = struct.Struct("=" + 8 * _HEADS + "QQQQQ" + "Q" + "III" + "ff" + "I" + "QQ")
 _ABSENT = (0, 0, 0, 0)
 _NOTHING = (None, 0, 0)
@@ -241,6 +245,28 @@ def append(cache: KVCache, k, v, start, prefix, table, values: bool = False, k_v
     return (k_values, v_values) if values else None
 
 
+def gather(cache: KVCache, tokens, start, table, to_table) -> None:
+    """Tokens of a cache into other pages, all heads, as they are held: tokens (int32) of sequence b, [start[b], start[b + 1]) of them (int32
+    [sequences + 1], not falling), counted in its pages table[b], become tokens 0, 1, ... of the pages to_table[b] (both int32 [sequences, columns]).  A fork copies
+    the page that is not full; a sequence that drops tokens names those that it keeps.  A slot that is written must not be one that the call reads, nor be
+    written twice; tokens without a place in either table are not moved."""
+    device = cache.device
+    count, sequences = tokens.shape[0], start.shape[0] - 1
+    if sequences < 1:
+        raise ValueError("start must hold the sequences' first tokens and the last one's end")
+    strides = []
+    for x, name in ((table, "table"), (to_table, "to_table")):
+        stride = x.stride()
+        if x.dim() != 2 or x.dtype is not int32 or stride[1] != 1 or x.shape[0] != sequences:
+            raise ValueError(f"{name} must be a [sequences, columns] int32 device tensor with unit column stride")
+        if x.get_device() != device:
+            _elsewhere(x, name, device)
+        strides.append(stride[0] if sequences > 1 else max(stride[0], x.shape[1]))
+    call = _GATHER.pack(*cache._fields, _vector(tokens, "tokens", int32, device, count), _vector(start, "start", int32, device, sequences + 1),
+                        table.data_ptr(), to_table.data_ptr(), *strides, count, table.shape[1], to_table.shape[1], sequences, 0)
+    _check(_run(binding.load().conqur_cache_gather, device, call), "conqur_cache_gather")
+
+
 class _Kept(threading.local):
     """The workspaces of tree_attention, each thread its own, by device and stream.  A call's launches meet in it: the calls of one thread on one
     stream come one behind the other, whatever their caches, those of two threads may be enqueued between each other's launches."""
@@ -281,21 +307,62 @@ def tree_attention(q, cache: KVCache, start, prefix, table, mask=None, max_query
               min(table.shape[1] * cache.page_tokens, MOST_CONTEXT) if max_context is None else max_context)
     tail = (max_query, width ** -0.5 if scale is None else scale)
     lib = binding.load()
+    _in_room(lib.conqur_tree_attention, lib.conqur_tree_attention_workspace, _TREE, fields, tail, q, "conqur_tree_attention")
+    return out
+
+
+def _in_room(call, size_of, form, fields, tail, x, what: str) -> None:
+    """A call in the thread's workspace for the stream of x's device, which is the current one; its address and size stand between `fields` and `tail`."""
+    device = x.get_device()
     at = device, _C._cuda_getCurrentRawStream(device)
     # (a graph keeps the room it was captured with: it takes its own, from its memory pool)
     capturing = _C._cuda_isCurrentStreamCapturing()
     rooms = _kept.rooms
     have = _NOTHING if capturing else rooms.get(at, _NOTHING)
-    status = lib.conqur_tree_attention(_TREE.pack(*fields, *have[1:], *tail), at[1])
+    status = call(form.pack(*fields, *have[1:], *tail), at[1])
     if status == binding.EINVAL:       # perhaps for want of room alone: one that is large enough stays
-        size = lib.conqur_tree_attention_workspace(_TREE.pack(*fields, 0, 0, *tail))
+        size = size_of(form.pack(*fields, 0, 0, *tail))
         if size > have[2]:
-            room = torch.empty(size, dtype=torch.uint8, device=q.device)
+            room = torch.empty(size, dtype=torch.uint8, device=x.device)
             have = (room, room.data_ptr(), size)
             if not capturing:
                 rooms[at] = have
-            status = lib.conqur_tree_attention(_TREE.pack(*fields, *have[1:], *tail), at[1])
-    _check(status, "conqur_tree_attention")
+            status = call(form.pack(*fields, *have[1:], *tail), at[1])
+    _check(status, what)
+
+
+def chunk_attention(q, cache: KVCache, start, prefix, table, first=None, last=None, window: int = 0, cap: float = 0.0, slopes=None,
+                    max_query: Optional[int] = None, max_context: Optional[int] = None, scale: Optional[float] = None, out=None):
+    """Attention of any number of new tokens q (bf16 [tokens, heads, width]; packed as in `append`, which has put their keys and values into the
+    cache) over their sequences' tokens, committed and new.  A token sees itself and those before it, or those from first on up to, not including, last
+    (int32, one per row of q, counted in tokens of the sequence; first >= last: nothing, zeros); window: and at most that many, itself the last.
+    cap: scores become cap tanh(score / cap); slopes (fp32 [heads]): less slope times the distance.  max_query: most new tokens of a
+    sequence, max_context: most tokens, committed and new (default: what q and the table hold; closer bounds choose the quicker kernel and share the work
+    out better).  scale: 1 / sqrt(width) unless given.  Returns out.  Rows beyond max_query of a sequence and rows of no sequence are zeros in a new tensor and stay as
+    they are in a given `out`."""
+    if q.requires_grad and torch.is_grad_enabled():
+        _no_gradient("chunk_attention", "it has no gradient")
+    if q.dim() != 3:
+        raise ValueError("q must be [tokens, heads, width]")
+    device = cache.device
+    if _C._cuda_getDevice() != device:
+        with torch.cuda.device(device):
+            return chunk_attention(q, cache, start, prefix, table, first, last, window, cap, slopes, max_query, max_context, scale, out)
+    tokens, heads, _ = q.shape
+    width = cache.width
+    new = out is None
+    if new:
+        out = _like(q)
+    if not 0 <= window < 1 << 31:
+        raise ValueError("window must be 0 (none) or a number of tokens")
+    same = (bfloat16, device, (tokens, heads, width))
+    fields = (*cache._fields, *_batch(start, prefix, table, device), *_rows(q, "q", *same), *_rows(out, "out", *same),
+              0 if first is None else _vector(first, "first", int32, device, tokens), 0 if last is None else _vector(last, "last", int32, device, tokens),
+              0 if slopes is None else _vector(slopes, "slopes", float32, device, heads), tokens,
+              min(table.shape[1] * cache.page_tokens, MOST_CONTEXT) if max_context is None else max_context)
+    tail = (max(tokens, 1) if max_query is None else max_query, window, cap, width ** -0.5 if scale is None else scale, 1 if new else 0, 0)
+    lib = binding.load()
+    _in_room(lib.conqur_chunk_attention, lib.conqur_chunk_attention_workspace, _CHUNK, fields, tail, q, "conqur_chunk_attention")
     return out
 
 

@@ -25,8 +25,8 @@ EXPORTS = [
     "conqur_init", "conqur_step_batch", "conqur_step_batch_heads", "conqur_step_batch_quant", "conqur_get_batch_stats", "conqur_update_rotation",
     "conqur_quant_error", "conqur_quant_error_zp", "conqur_rotate", "conqur_rotate_quant", "conqur_row_diagnostics", "conqur_get_state", "conqur_set_state", "conqur_get_last_corners",
     "conqur_score_rows_static", "conqur_rotary_frequencies", "conqur_rotary", "conqur_qk_norm_rotary", "conqur_qk_norm_rotary_workspace", "conqur_qk_norm_rotary_backward",
-    "conqur_cache_append", "conqur_tree_attention_workspace", "conqur_tree_attention",
-    "conqur_attention_workspace", "conqur_attention", "conqur_attention_backward_workspace", "conqur_attention_backward",
+    "conqur_cache_append", "conqur_cache_gather", "conqur_tree_attention_workspace", "conqur_tree_attention",
+    "conqur_chunk_attention_workspace", "conqur_chunk_attention", "conqur_attention_workspace", "conqur_attention", "conqur_attention_backward_workspace", "conqur_attention_backward",
     "conqur_set_taps", "conqur_set_timing", "conqur_get_timing", "conqur_get_clock_probe", "conqur_last_error", "conqur_destroy", "conqur_version",
 ]
 
@@ -105,7 +105,7 @@ def load() -> ctypes.CDLL:
         f64 = ctypes.c_double
         L.conqur_rotary_frequencies.restype = i32
         L.conqur_rotary_frequencies.argtypes = [u32, u32, f64, f64, f64, f64, f64, vp, vp]
-        for name in ("conqur_rotary", "conqur_qk_norm_rotary", "conqur_cache_append", "conqur_tree_attention"):
+        for name in ("conqur_rotary", "conqur_qk_norm_rotary", "conqur_cache_append", "conqur_cache_gather", "conqur_cache_gather", "conqur_tree_attention"):
             getattr(L, name).restype = i32
             getattr(L, name).argtypes = [vp, vp]
         L.conqur_qk_norm_rotary_workspace.restype = u64
@@ -114,7 +114,7 @@ def load() -> ctypes.CDLL:
         L.conqur_qk_norm_rotary_backward.argtypes = [vp, vp, vp, vp, u64, vp]
         L.conqur_tree_attention_workspace.restype = u64
         L.conqur_tree_attention_workspace.argtypes = [vp]
-        for name in ("conqur_attention", "conqur_attention_backward"):
+        for name in ("conqur_chunk_attention", "conqur_attention", "conqur_attention_backward"):
             getattr(L, name).restype = i32
             getattr(L, name).argtypes = [vp, vp]
             getattr(L, name + "_workspace").restype = u64

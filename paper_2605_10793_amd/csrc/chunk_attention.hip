@@ -1,0 +1,158 @@
+// Attention of a chunk of new tokens of each sequence, any number of them, over a paged cache that holds them already.
+//
+//   u_ij = scale q_i k_j, s_ij = cap tanh(u_ij / cap) (cap 0: u_ij) - slope |i - j|, seen are max(0, first_i, i - window + 1) <= j < min(length, last_i)
+//   o_i = sum_j e^(s_ij - m_i) v_j / sum_j e^(s_ij - m_i)
+//
+// i, j: places in the sequence.  Few rows of a cache head (its query heads times the new tokens) are bound by HBM and take the kernel of
+// tree_attention_few.h, many the one of tree_attention_wide.h, with bounds in the place of masks: blocks of 64 keys that all rows see take the way of committed
+// tokens there, the others the way with every case.
+#include "tree_attention_few.h"
+
+using namespace conqur;
+using namespace conqur::tree;
+
+namespace {
+
+// Sixteens of rows that a wavefront takes straight from memory (more would not fit its registers).
+constexpr int few_tiles(int bits, int width, int kind) { return bits == 16 || (bits == 8 && width == 128 && kind == kOptions) ? 1 : 2; }
+
+template <int BITS, int W, int KIND>
+hipError_t launch(const TreeArgs& a, int qt, dim3 grid, hipStream_t s) {
+  constexpr int kMostTiles = few_tiles(BITS, W, KIND);
+  const bool one_page = a.cache.page_tokens >= (uint32_t)kBlock;
+  if (qt == 1 && one_page)
+    k_tree<BITS, W, 1, true, KIND><<<grid, 64 * kWaves, 0, s>>>(a);
+  else if (qt == 1)
+    k_tree<BITS, W, 1, false, KIND><<<grid, 64 * kWaves, 0, s>>>(a);
+  else if (one_page)
+    k_tree<BITS, W, kMostTiles, true, KIND><<<grid, 64 * kWaves, 0, s>>>(a);
+  else
+    k_tree<BITS, W, kMostTiles, false, KIND><<<grid, 64 * kWaves, 0, s>>>(a);
+  return hipGetLastError();
+}
+template <int BITS, int W>
+hipError_t launch(const TreeArgs& a, int qt, dim3 grid, hipStream_t s) {
+  return a.cap_log2 != 0.0f || a.slopes ? launch<BITS, W, kOptions>(a, qt, grid, s) : launch<BITS, W, kChunk>(a, qt, grid, s);
+}
+
+constexpr int64_t kMaxStride = 1ll << 40;
+
+struct Plan {
+  bool wide;
+  int qt, tile_rows, row_tiles, splits, min_blocks, tail;
+  int64_t context;
+};
+
+Plan plan_of(const conqur_chunk_call& c) {
+  Plan p;
+  const int64_t room = (int64_t)c.batch.table_columns * c.cache.page_tokens;
+  p.context = (int64_t)(c.max_context < (uint64_t)room ? c.max_context : (uint64_t)room);
+  const int64_t rows = (int64_t)c.max_query * (c.q.heads / c.cache.heads);
+  p.wide = rows > 16 * few_tiles((int)c.cache.bits, (int)c.cache.width, c.cap != 0.0f || c.slopes ? kOptions : kChunk);
+  p.qt = rows <= 16 ? 1 : 2;
+  if (p.wide) {
+    const int most = c.cache.bits == 16 && c.cache.width == 128 ? 2 : 3;
+    int64_t least = 1ll << 62;
+    for (int qt = 1; qt <= most; ++qt) {
+      const int64_t padded = (rows + 64 * qt - 1) / (64 * qt) * qt;
+      if (padded <= least) {
+        least = padded;
+        p.qt = qt;
+      }
+    }
+  }
+  p.tile_rows = 16 * p.qt * (p.wide ? kWaves : 1);
+  p.row_tiles = (int)((rows + p.tile_rows - 1) / p.tile_rows);
+  const int64_t groups = (int64_t)c.cache.heads * p.row_tiles, sequences = c.batch.sequences;
+  const int64_t blocks = p.context > kBlock ? (p.context + kBlock - 1) / kBlock : 1;
+  p.min_blocks = kWaves;
+  int64_t splits = kSlots / groups;
+  const int64_t most = (blocks * sequences + p.min_blocks - 1) / p.min_blocks;
+  if (splits > most) splits = most;
+  if (splits > kMaxSplits) splits = kMaxSplits;
+  if (splits < 1) splits = 1;
+  const int64_t workgroups = sequences * groups;
+  const bool alone = blocks <= kWaves || (blocks <= 32 && workgroups >= kSlots) || (blocks <= 128 && workgroups >= 4 * kSlots);
+  p.tail = p.wide || (c.cache.bits != 16 && blocks * sequences >= 8 * splits) ? 4 : 0;
+  p.splits = alone || sequences > kMaxScan || (blocks + p.tail) * sequences + 2 * kMaxSplits >= 1ll << 31 ? 0 : (int)splits;
+  return p;
+}
+
+uint64_t workspace_of(const conqur_chunk_call& c, const Plan& p) {
+  return (uint64_t)c.cache.heads * p.row_tiles * 2 * p.splits * p.tile_rows * (c.cache.width + 2) * sizeof(float);
+}
+
+bool call_fine(const conqur_chunk_call* c) {
+  if (!c || !cache_fine(c->cache) || !batch_fine(c->batch) || c->tokens >= 1ull << 31 || c->max_context >= 1ull << 31) return false;
+  if (!isfinite(c->scale) || !isfinite(c->cap) || c->cap < 0.0f || c->window >= 1u << 31 || c->max_query < 1) return false;
+  if (c->q.heads < 1 || c->q.heads % c->cache.heads || c->q.heads / c->cache.heads > 64 || c->out.heads != c->q.heads) return false;
+  return c->max_query * (c->q.heads / c->cache.heads) < 1ull << 24;
+}
+
+bool rows_fine(const conqur_heads& h, uint32_t width, uint64_t tokens, bool output) {
+  if (!h.data || reinterpret_cast<uintptr_t>(h.data) % 2) return false;
+  if (h.token_stride < 0 || h.token_stride >= kMaxStride || h.head_stride < 0 || h.head_stride >= kMaxStride) return false;
+  if (!output) return true;
+  const __int128 w = width, ts = h.token_stride, hs = h.head_stride, heads = h.heads, n = tokens;
+  if ((heads > 1 && hs < w) || (n > 1 && ts < w)) return false;
+  return !(heads > 1 && n > 1 && ts < (heads - 1) * hs + w && hs < (n - 1) * ts + w);
+}
+
+}  // namespace
+
+hipError_t conqur::tree::launch_chunk_few(const TreeArgs& a, int qt, dim3 grid, hipStream_t s) {
+  if (a.cache.width == 128)
+    return a.cache.bits == 16 ? launch<16, 128>(a, qt, grid, s) : a.cache.bits == 8 ? launch<8, 128>(a, qt, grid, s) : launch<4, 128>(a, qt, grid, s);
+  return a.cache.bits == 16 ? launch<16, 64>(a, qt, grid, s) : a.cache.bits == 8 ? launch<8, 64>(a, qt, grid, s) : launch<4, 64>(a, qt, grid, s);
+}
+
+extern "C" uint64_t conqur_chunk_attention_workspace(const conqur_chunk_call* call) {
+  if (!call_fine(call)) return 0;
+  return workspace_of(*call, plan_of(*call));
+}
+
+extern "C" conqur_status conqur_chunk_attention(const conqur_chunk_call* c, void* stream) {
+  if (!call_fine(c)) return CONQUR_EINVAL;
+  if (c->tokens == 0) return CONQUR_OK;
+  if (!rows_fine(c->q, c->cache.width, c->tokens, false) || !rows_fine(c->out, c->cache.width, c->tokens, true)) return CONQUR_EINVAL;
+  if (reinterpret_cast<uintptr_t>(c->first) % 4 || reinterpret_cast<uintptr_t>(c->last) % 4 || reinterpret_cast<uintptr_t>(c->slopes) % 4) return CONQUR_EINVAL;
+  const Plan p = plan_of(*c);
+  const uint64_t need = workspace_of(*c, p);
+  if (need && (!c->workspace || reinterpret_cast<uintptr_t>(c->workspace) % 16 || c->workspace_bytes < need)) return CONQUR_EINVAL;
+  TreeArgs a = {};
+  a.cache = c->cache;
+  a.batch = c->batch;
+  a.q = static_cast<const bf16_bits*>(c->q.data);
+  a.out = static_cast<bf16_bits*>(c->out.data);
+  a.q_ts = c->q.token_stride;
+  a.q_hs = c->q.head_stride;
+  a.out_ts = c->out.token_stride;
+  a.out_hs = c->out.head_stride;
+  a.q_wide = reinterpret_cast<uintptr_t>(c->q.data) % 16 == 0 && a.q_ts % 8 == 0 && a.q_hs % 8 == 0;
+  a.out_wide = reinterpret_cast<uintptr_t>(c->out.data) % 8 == 0 && a.out_ts % 4 == 0 && a.out_hs % 4 == 0;
+  a.tokens = (int64_t)c->tokens;
+  a.context = p.context;
+  a.splits = p.splits;
+  a.min_blocks = p.min_blocks;
+  a.tail = p.splits ? p.tail : 0;
+  a.max_query = (int)c->max_query;
+  a.group = (int)(c->q.heads / c->cache.heads);
+  a.tile_rows = p.tile_rows;
+  a.row_tiles = p.row_tiles;
+  a.part = static_cast<float*>(c->workspace);
+  a.part_ml = reinterpret_cast<float2*>(a.part + (uint64_t)c->cache.heads * p.row_tiles * 2 * p.splits * p.tile_rows * c->cache.width);
+  a.scale_log2 = c->scale * 1.4426950408889634f;
+  a.chunk = 1;
+  a.window = (int)c->window;
+  a.zero_rest = c->zero_rest != 0;
+  a.first = c->first;
+  a.last = c->last;
+  a.slopes = c->slopes;
+  a.cap_log2 = c->cap * 1.4426950408889634f;
+  a.cap_in = c->cap == 0.0f ? 0.0f : 2.0f / c->cap;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  const dim3 grid((uint32_t)(a.cache.heads * p.row_tiles), p.splits ? p.splits : a.batch.sequences);
+  hipError_t e = p.wide ? launch_chunk_wide(a, p.qt, grid, s) : launch_chunk_few(a, p.qt, grid, s);
+  if (e == hipSuccess && p.splits > 1) e = launch_join(a, p.wide, s);
+  return e == hipSuccess ? CONQUR_OK : CONQUR_EHIP;
+}

@@ -62,8 +62,22 @@ __device__ __forceinline__ int edge_of(Args a, int i) {
   return v < 0 ? 0 : v > tokens ? (int)tokens : v;
 }
 
-// A piece of a sequence: its parts are numbered from edge * of / per + (number of the sequence) on, of = 1 (tokens) or group (rows), which leaves room
-// for ceil(count * of / per) of each, so that a part's sequence is found by halving and no table is made.
+// Pieces of sequences.  A sequence's parts are numbered from edge * of / per + (number of the sequence) on, per = 2^shift, of = 1 (tokens) or more (rows of a
+// token), which leaves room for ceil(count * of / per) of each: a part's sequence is found by halving (here into 64), and no table is made.
+// edge(i): first row of sequence i, up to `edges`, not falling.  By a whole wavefront; the same for all lanes.
+template <typename Edge>
+__device__ __forceinline__ int sequence_of_part(int id, int edges, int shift, int of, Edge edge) {
+  const int lane = (int)threadIdx.x & 63;
+  int lo = 0, hi = edges;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 63) >> 6, i = lo + lane * step;
+    const bool at_most = i < hi && (int)(((int64_t)edge(i) * of) >> shift) + i <= id;
+    const int c = __popcll(__ballot(at_most));
+    lo += (c > 0 ? c - 1 : 0) * step;
+    hi = hi - lo < step ? hi : lo + step;
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
 struct Item {
   int first, count;      // rows of the call that are the sequence's tokens
   int part, parts;
@@ -71,22 +85,12 @@ struct Item {
   int base;              // number of its first part
   bool rest;             // of no sequence
   __device__ __forceinline__ bool find(Args a, int id, int shift, int of) {
-    const int lane = (int)threadIdx.x & 63;
-    int lo = 0, hi = a->sequences + 2;
-    while (hi - lo > 1) {
-      const int step = (hi - lo + 63) >> 6, i = lo + lane * step;
-      const bool at_most = i < hi && (int)(((int64_t)edge_of(a, i) * of) >> shift) + i <= id;
-      const int c = __popcll(__ballot(at_most));
-      lo += (c > 0 ? c - 1 : 0) * step;
-      hi = hi - lo < step ? hi : lo + step;
-    }
-    lo = __builtin_amdgcn_readfirstlane(lo);
-    first = __builtin_amdgcn_readfirstlane(edge_of(a, lo));
-    count = __builtin_amdgcn_readfirstlane(edge_of(a, lo + 1)) - first;
+    number = sequence_of_part(id, a->sequences + 2, shift, of, [&](int i) { return edge_of(a, i); });
+    first = __builtin_amdgcn_readfirstlane(edge_of(a, number));
+    count = __builtin_amdgcn_readfirstlane(edge_of(a, number + 1)) - first;
     if (count < 0) count = 0;
-    number = lo;
-    rest = lo == 0 || lo == a->sequences + 1;
-    base = (int)(((int64_t)first * of) >> shift) + lo;
+    rest = number == 0 || number == a->sequences + 1;
+    base = (int)(((int64_t)first * of) >> shift) + number;
     parts = (int)(((int64_t)count * of + (1 << shift) - 1) >> shift);
     part = id - base;
     return part >= 0 && part < parts && !(rest && !a->rest);

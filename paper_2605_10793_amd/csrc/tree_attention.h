@@ -43,7 +43,16 @@ struct TreeArgs {
   int max_query, group, tile_rows, row_tiles;
   int q_wide, out_wide;
   float scale_log2;
+  // Of a chunk of new tokens (kinds kChunk and kOptions): keys by bounds, a window, a cap in base 2 and 2 / cap in base 2, a bias by distance.
+  int chunk, window, zero_rest;
+  const int32_t* first;
+  const int32_t* last;
+  const float* slopes;
+  float cap_log2, cap_in;
 };
+
+// What a row sees and how: a tree's masks; bounds and windows; those with capped scores or a bias by distance.
+enum { kMasks = 0, kChunk = 1, kOptions = 2 };
 
 // The arguments as a kernel reads them, where they lie: each call gives an address that the compiler takes for a new one, so that what a part of a
 // kernel needs of them is read there and not kept in (some hundred) registers from the kernel's beginning.
@@ -92,10 +101,57 @@ __device__ __forceinline__ int lane_anew() {
   return (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, (uint32_t)none));
 }
 
+// Keys that a row tile which begins at row0 (below the sequence's rows) may see: from 64 times the first block on, up to the end.  In a chunk whose tokens see
+// no later ones, the tile's last token bounds it; its first one's window leaves blocks out.
+__device__ __forceinline__ int64_t tile_end(Args a, const Sequence& s, int row0) {
+  if (!a->chunk || a->last) return s.length;
+  const int rows = s.count * a->group, row = row0 + a->tile_rows < rows ? row0 + a->tile_rows - 1 : rows - 1;
+  const int64_t end = s.prefix + (uint32_t)row / (uint32_t)a->group + 1;
+  return end < s.length ? end : s.length;
+}
+__device__ __forceinline__ int first_block(Args a, const Sequence& s, int row0) {
+  if (!a->chunk || a->window == 0) return 0;
+  const int64_t from = s.prefix + (uint32_t)row0 / (uint32_t)a->group + 1 - a->window;
+  return from > 0 ? (int)((from < s.length ? from : s.length) / kBlock) : 0;
+}
 // Blocks of a sequence for a row tile that begins at row0: none if it has no such rows, otherwise one at least (which writes zeros if nothing is seen).
 __device__ __forceinline__ int blocks_in(Args a, const Sequence& s, int row0) {
   if (row0 >= s.count * a->group) return 0;
-  return (s.length > kBlock ? (int)((s.length + kBlock - 1) / kBlock) : 1) + a->tail;
+  const int64_t end = tile_end(a, s, row0);
+  const int n = (end > kBlock ? (int)((end + kBlock - 1) / kBlock) : 1) - first_block(a, s, row0);
+  return (n > 1 ? n : 1) + a->tail;
+}
+
+// Keys [x, y) that new token `node` of a chunk sees; (0, 0): none.
+__device__ __forceinline__ int2 chunk_keys(Args a, const Sequence& s, int node) {
+  const int64_t place = s.prefix + node;
+  int64_t lo = 0, hi = place + 1;
+  if (a->first) lo = a->first[s.first + node];
+  if (a->last) hi = a->last[s.first + node];
+  if (lo < 0) lo = 0;
+  if (a->window && place - a->window + 1 > lo) lo = place - a->window + 1;
+  if (hi > s.length) hi = s.length;
+  return lo < hi ? make_int2((int)lo, (int)hi) : make_int2(0, 0);
+}
+// Bits j of 16: whether lo <= pos + j < hi.
+__device__ __forceinline__ uint32_t between(int64_t pos, int2 keys) {
+  const int64_t lo = keys.x - pos, hi = keys.y - pos;
+  const int from = lo < 0 ? 0 : lo > 16 ? 16 : (int)lo, to = hi < 0 ? 0 : hi > 16 ? 16 : (int)hi;
+  return to > from ? ((1u << to) - 1) & ~((1u << from) - 1) : 0;
+}
+template <typename Op>
+__device__ __forceinline__ int wave_reduce_int(int v, Op op) {
+  const auto a = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
+  const int w = op((int)a[0], (int)a[1]);
+  const auto b = __builtin_amdgcn_permlane16_swap((uint32_t)w, (uint32_t)w, false, false);
+  const uint32_t x = row16_reduce((uint32_t)op((int)b[0], (int)b[1]), [&](uint32_t x, uint32_t y) { return (uint32_t)op((int)x, (int)y); });
+  return __builtin_amdgcn_readfirstlane((int)x);
+}
+__device__ __forceinline__ int wave_min(int v) { return wave_reduce_int(v, [](int a, int b) { return a < b ? a : b; }); }
+__device__ __forceinline__ int wave_max_int(int v) { return wave_reduce_int(v, [](int a, int b) { return a > b ? a : b; }); }
+// A score in base 2, capped.
+__device__ __forceinline__ float capped(float y, float cap_log2, float cap_in) {
+  return fmaf(-2.0f * cap_log2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(y * cap_in)), cap_log2);
 }
 
 // Sum over the lanes up to a lane.
@@ -314,8 +370,38 @@ __device__ __forceinline__ void store_row4(Args a, const Sequence& sq, int head,
   }
 }
 
+// Zeros to a key head's rows of out that get no result: of no sequence, or beyond max_query of one.  By a whole workgroup.
+__device__ __forceinline__ void zero_rows(Args a, int head) {
+  const int width = (int)a->cache.width, per = a->group * width;
+  auto zeros = [&](int64_t from, int64_t to) {
+    for (int64_t i = from * per + threadIdx.x; i < to * per; i += blockDim.x) {
+      const int in = (int)(i % per);
+      a->out[i / per * a->out_ts + (int64_t)(head * a->group + in / width) * a->out_hs + in % width] = 0;
+    }
+  };
+  auto edge = [&](int i) {
+    const int v = a->batch.start[i];
+    return v < 0 ? (int64_t)0 : (int64_t)v > a->tokens ? a->tokens : (int64_t)v;
+  };
+  const int sequences = (int)a->batch.sequences;
+  zeros(0, edge(0));
+  zeros(edge(sequences), a->tokens);
+  for (int b0 = 0; b0 < sequences; b0 += 64) {
+    const int b = b0 + ((int)threadIdx.x & 63);
+    const bool more = b < sequences && edge(b + 1) - edge(b) > a->max_query;
+    for (uint64_t which = __ballot(more); which; which &= which - 1) {
+      const int at = b0 + __builtin_ctzll(which);
+      zeros(edge(at) + a->max_query, edge(at + 1));
+    }
+  }
+}
+
 // Rows of more than some tens (tree_attention_wide.hip): 64 qt rows a workgroup.
 hipError_t launch_wide(const TreeArgs& a, int qt, dim3 grid, hipStream_t s);
+// A chunk's (chunk_attention.hip, chunk_attention_wide.hip).
+hipError_t launch_join(const TreeArgs& a, bool wide, hipStream_t s);
+hipError_t launch_chunk_few(const TreeArgs& a, int qt, dim3 grid, hipStream_t s);
+hipError_t launch_chunk_wide(const TreeArgs& a, int qt, dim3 grid, hipStream_t s);
 
 }  // namespace tree
 }  // namespace conqur

@@ -6,9 +6,10 @@ import torch
 HALF = 2.0 ** -8          # a rounding to bf16, relative
 
 
-def attend(q, k, v, seen, place, scale, cap=0.0, slopes=None, grad=None):
+def attend(q, k, v, seen, place, scale, cap=0.0, slopes=None, grad=None, sizes=None):
     """One sequence: q [rows, heads, width] at `place` [rows], k, v [keys, key heads, width], seen [rows, keys].  Returns a dict of values and their
-    tolerances: out, lse, and with `grad` dq, dk, dv."""
+    tolerances: out, lse, and with `grad` dq, dk, dv.  sizes: for keys and values held as codes, what their entries are summed from at most, [keys, key heads]
+    each (an offset, and a step times up to 128 + 255): 32-bit sums are off by parts of that, not of the values that are left."""
     q, k, v = q.double(), k.double(), v.double()
     heads, kv, width = q.shape[1], k.shape[1], q.shape[2]
     group = heads // kv
@@ -32,11 +33,15 @@ def attend(q, k, v, seen, place, scale, cap=0.0, slopes=None, grad=None):
         # by that over ln 2, the weight by that again; the weight and the sum each by a few more units.
         visible = torch.where(seen, torch.ones_like(s), torch.zeros_like(s))
         size = (abs(scale) * qh.abs() @ kh.abs().T + (cap if cap else 0.0) + (slopes[h].double() * distance if slopes is not None else 0.0)) * visible
+        if sizes is not None:
+            size = torch.maximum(size, abs(scale) * qh.abs().sum(-1, keepdim=True) * sizes[0][:, h // group].double()[None] * visible)
         eps = (width + 16) * 2.0 ** -24 * size.amax(-1, keepdim=True) + 2.0 ** -20 if s.shape[1] else torch.zeros_like(top)
         o, a = p @ vh, p @ vh.abs()
         res["out"][:, h] = o
         # weights rounded, and divided by their sum as rounded; then the result
         res["out_tol"][:, h] = 1.02 * (HALF * (a + o.abs()) + HALF * o.abs() + 2 * eps * a) + 1e-30
+        if sizes is not None:      # a chain of sums over blocks of 64 keys, 32 of them in one product
+            res["out_tol"][:, h] += (s.shape[1] / 64 + 64) * 2.0 ** -24 * (sizes[1][:, h // group].double() * visible).amax(-1, keepdim=True)
         res["lse"][:, h] = (top + torch.log(total))[:, 0]
         res["lse_tol"][:, h] = (1.02 * HALF + 2 * eps[:, 0] + 2.0 ** -22 * torch.where(top == -math.inf, torch.zeros_like(top), top).abs()[:, 0])
         if grad is None:
