@@ -427,9 +427,8 @@ def attention_backward(q, k, v, out, lse, grad, start, first=None, last=None, wi
                        scale: Optional[float] = None):
     """Gradients of attention (of q, of k, of v) for the gradient `grad` of its result `out` (bf16), with the lse that it gave and the other arguments as
     it took them.  Rows of no sequence get zeros."""
-    tokens, heads = q.shape[0], q.shape[1]
-    if lse.dtype is not float32 or lse.shape != (tokens, heads) or not lse.is_contiguous():
-        raise ValueError(f"lse must be a contiguous fp32 device tensor [{tokens}, {heads}]")
+    if lse.dtype is not float32 or q.dim() != 3 or lse.shape != (q.shape[0], q.shape[1]) or not lse.is_contiguous():
+        raise ValueError("lse must be a contiguous fp32 device tensor [tokens, heads]")
     if lse.get_device() != q.get_device():
         _elsewhere(lse, "lse", q.get_device())
     gradients = grad, _like(q), _like(k), _like(v)

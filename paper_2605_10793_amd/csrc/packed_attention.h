@@ -169,31 +169,42 @@ struct Tile {
   static __device__ __forceinline__ int f(int row) {
     return kChunks == 16 ? ((row & 3) << 2 | ((row >> 2) & 3)) : (((row >> 1) & 1) << 2 | ((row >> 2) & 3));
   }
-  // Operand s of 32 rows from LDS: lane's row `row`, entries 16 s + 8 h to 16 s + 8 h + 7.  row_at: for s = 0.
+  // Operands from LDS.  `at`: a tile's place (a multiple of 256 bytes, more rows or tiles behind it as a constant) plus what the lane adds, row_at() or turned_at().
+  // Lane's row (lane & 31), entries 16 s + 8 h to 16 s + 8 h + 7.
   static __device__ __forceinline__ uint32_t row_at(int lane) { return (lane & 31) * kPitch + ((((lane >> 5) ^ f(lane & 31))) << 4); }
-  static __device__ __forceinline__ uint32_t rows_from(uint32_t lds, uint32_t at, int s) { return anew(lds + (at ^ (uint32_t)(s << 5))); }
-  static __device__ __forceinline__ bf16x8 rows(uint32_t from, int u) {
-    return *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)(from + u * 32 * kPitch);
+  template <int BEHIND>
+  static __device__ __forceinline__ bf16x8 rows(uint32_t at, int s) {
+    return *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)(anew(at ^ (uint32_t)(s << 5)) + BEHIND);
   }
-  // Turned round: lane's entry 32 t + (lane & 31), rows 16 k + {4 h .. 4 h + 3, 8 + 4 h .. 8 + 4 h + 3}.
+  // Turned round: lane's entry 32 t + (lane & 31), rows {4 h .. 4 h + 3, 8 + 4 h .. 8 + 4 h + 3}.
   static __device__ __forceinline__ uint32_t turned_at(int lane) {
     const int l = lane & 15, half = lane >> 5, part = (lane >> 4) & 1, row = 4 * half + (l >> 2);
     return row * kPitch + (((2 * part + ((l & 3) >> 1)) ^ f(row)) << 4) + (l & 1) * 8;
   }
-  struct Turned {
-    uint32_t a, b;
-  };
-  static __device__ __forceinline__ Turned turned_from(uint32_t lds, uint32_t at, int t) {
-    return Turned{anew(lds + (at ^ (uint32_t)(t << 6))), anew(lds + (at ^ (uint32_t)(t << 6) ^ 32u))};
-  }
-  static __device__ __forceinline__ bf16x8 turned(Turned from, int k) {
+  template <int BEHIND>
+  static __device__ __forceinline__ bf16x8 turned(uint32_t at, int t) {
     typedef __attribute__((address_space(3))) s16x4* P;
-    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(from.a + k * 16 * kPitch));
-    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(from.b + (k * 16 + 8) * kPitch));
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(anew(at ^ (uint32_t)(t << 6)) + BEHIND));
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(anew(at ^ (uint32_t)(t << 6) ^ 32u) + BEHIND + 8 * kPitch));
     const u32x2 p = __builtin_bit_cast(u32x2, a), q = __builtin_bit_cast(u32x2, b);
     return frag_of(p[0], p[1], q[0], q[1]);
   }
 };
+
+// N products whose operands come from LDS: RING of them are on their way ahead of the products that take them, and nothing but arithmetic passes from one to
+// the next (the compiler would hold more of them than there are registers).  load(i), use(i, operand): i as a constant.
+constexpr int kArithmetic = 0x6;
+template <int N, int RING = 4, typename Load, typename Use>
+__device__ __forceinline__ void in_turn(Load load, Use use) {
+  decltype(load(std::integral_constant<int, 0>{})) ring[RING];
+  each<(N < RING ? N : RING)>([&](auto i) { ring[decltype(i)::value] = load(i); });
+  each<N>([&](auto i) {
+    constexpr int I = decltype(i)::value;
+    use(i, ring[I % RING]);
+    if constexpr (I + RING < N) ring[I % RING] = load(std::integral_constant<int, I + RING>{});
+    __builtin_amdgcn_sched_barrier(kArithmetic);
+  });
+}
 
 __device__ __forceinline__ uint32_t lds_of(const void* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) unsigned char*)p; }
 
@@ -210,29 +221,32 @@ __device__ __forceinline__ u32x4 memory_at(const void* p) {
   return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)x), (uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32) & 0xffff), 0x7fffffffu, 0x00020000u};
 }
 
-// Sends for rows [at, at + 64) of one head to a tile; rows behind `count` are the last one again, as are chunks behind the width.
-template <int KS>
+// Sends for ROWS rows of one head to a tile, from `rows` on; rows behind `count` are the last one again, as are chunks behind the width.
+template <int KS, int ROWS = kTile>
 __device__ __forceinline__ void send_tile(const bf16_bits* rows, int stride, int count, uint32_t lds, int wave) {
   using T = Tile<KS>;
+  constexpr int kLoads = ROWS / T::kRowsAt / kWaves;
+  static_assert(kLoads > 0, "");
   const u32x4 from = memory_at(rows);
   const int lane = lane_anew();
-  const int in = lane / T::kChunks, c0 = (lane % T::kChunks) ^ (T::kChunks == 16 ? in << 2 : ((in >> 1) & 1) << 2 | in >> 2);
+  const int in = lane / T::kChunks, c0 = (lane % T::kChunks) ^ T::f(wave * kLoads * T::kRowsAt + in);
   auto chunk = [&](int i) {
-    int c = c0 ^ (T::kChunks == 16 ? i & 3 : (i & 1) << 1);
+    int c = c0 ^ T::f(i * T::kRowsAt);
     if (KS * 2 < T::kChunks) c = c < KS * 2 ? c : KS * 2 - 1;
     return c * 16;
   };
-  if (count >= kTile) {
+  static_assert(kLoads * T::kRowsAt <= 16, "f of a sum is the exclusive or of its parts'");
+  if (count >= ROWS) {
     const int at = in * stride;
 #pragma unroll
-    for (int i = 0; i < T::kLoads; ++i) {
-      const int r0 = (wave * T::kLoads + i) * T::kRowsAt;
+    for (int i = 0; i < kLoads; ++i) {
+      const int r0 = (wave * kLoads + i) * T::kRowsAt;
       send16(from, lds + r0 * T::kPitch, at + chunk(i), r0 * stride);
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < T::kLoads; ++i) {
-      const int r0 = (wave * T::kLoads + i) * T::kRowsAt, r = r0 + in < count ? r0 + in : count - 1;
+    for (int i = 0; i < kLoads; ++i) {
+      const int r0 = (wave * kLoads + i) * T::kRowsAt, r = r0 + in < count ? r0 + in : count - 1;
       send16(from, lds + r0 * T::kPitch, r * stride + chunk(i), 0);
     }
   }
@@ -266,6 +280,34 @@ __device__ __forceinline__ bf16x8 finite_only(bf16x8 f) {
   for (int j = 0; j < 4; ++j) x[j] = finite_only(x[j]);
   return __builtin_bit_cast(bf16x8, x);
 }
+// A wavefront's quarter of a tile's ROWS rows: infinities and NaNs become zeros.  256 / ROWS neighbouring lanes share a row; they receive whether it had any.
+template <int KS, int ROWS>
+__device__ __forceinline__ bool clear_nonfinite(uint32_t tile, int wave, int lane) {
+  using T = Tile<KS>;
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  typedef __attribute__((address_space(3))) u32x4* P;
+  constexpr int kLanes = 256 / ROWS, kEach = T::kPitch / kLanes / 16;
+  const uint32_t at = tile + (wave * (ROWS / 4) + lane / kLanes) * T::kPitch + lane % kLanes * (T::kPitch / kLanes);
+  u16x2 most = {0, 0};
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const u32x4 x = *(P)(uintptr_t)(at + 16 * i);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, x[j] & 0x7fff7fffu));
+  }
+  const uint64_t found = __ballot(most[0] >= 0x7f80 || most[1] >= 0x7f80);
+  if (found) {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      u32x4 x = *(P)(uintptr_t)(at + 16 * i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = finite_only(x[j]);
+      *(P)(uintptr_t)(at + 16 * i) = x;
+    }
+  }
+  return (found >> (lane / kLanes * kLanes)) & ((1 << kLanes) - 1);
+}
+
 // Ones where a value is `sign`'s infinity or NaN.
 __device__ __forceinline__ bf16x8 infinite(bf16x8 f, uint32_t sign) {
   u32x4 x = __builtin_bit_cast(u32x4, f);

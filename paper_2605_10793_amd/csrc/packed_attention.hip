@@ -80,14 +80,10 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed(const PackedArgs) {
     const bool all = kb >= low_all && kb + kTile <= high_all;
 
     const int here = lane_anew();
-    const uint32_t row_at = T::row_at(here), turned_at = T::turned_at(here);
+    const uint32_t row_at = sk + T::row_at(here), turned_at = sv + T::turned_at(here);
     f32x16 s[2] = {f32x16{}, f32x16{}};
-#pragma unroll
-    for (int i = 0; i < KS; ++i) {
-      const uint32_t from = T::rows_from(sk, row_at, i);
-#pragma unroll
-      for (int u = 0; u < 2; ++u) s[u] = mfma32(T::rows(from, u), qf[i], s[u]);
-    }
+    in_turn<2 * KS>([&](auto i) { return T::template rows<decltype(i)::value % 2 * 32 * T::kPitch>(row_at, decltype(i)::value / 2); },
+                    [&](auto i, bf16x8 f) { s[decltype(i)::value % 2] = mfma32(f, qf[decltype(i)::value / 2], s[decltype(i)::value % 2]); });
 
     const float base = m == -INFINITY ? 0.0f : m;
     if (!OPTIONS && all) {
@@ -151,55 +147,49 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed(const PackedArgs) {
         p[u][r] = f32x2_to_bf16x2(__builtin_amdgcn_exp2f(s[u][2 * r]), __builtin_amdgcn_exp2f(s[u][2 * r + 1]));
         l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, p[u][r]), ones, l, false);
       }
+    // Operand i of V: 16 keys, 32 entries.
+    auto value = [&](auto i) {
+      constexpr int I = decltype(i)::value, K = I / T::kTiles;
+      return T::template turned<K * 16 * T::kPitch>(turned_at, I % T::kTiles);
+    };
     bool odd = false;
     if (!all) {          // infinities and NaNs must not reach rows that do not see them: 0 * NaN is NaN
       f32x16 z = f32x16{};
-#pragma unroll
-      for (int t = 0; t < T::kTiles; ++t) {
-        const auto from = T::turned_from(sv, turned_at, t);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) z = mfma32(T::turned(from, k), frag_of(0, 0, 0, 0), z);
-      }
+      in_turn<4 * T::kTiles>(value, [&](auto, bf16x8 f) { z = mfma32(f, frag_of(0, 0, 0, 0), z); });
       odd = any_left(z);
     }
     if (!odd) {
-      typename T::Turned from[T::kTiles];
-#pragma unroll
-      for (int t = 0; t < T::kTiles; ++t) from[t] = T::turned_from(sv, turned_at, t);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const uint32_t* w = &p[k / 2][k % 2 * 4];
-        const bf16x8 pf = frag_of(w[0], w[1], w[2], w[3]);
-#pragma unroll
-        for (int t = 0; t < T::kTiles; ++t) o[t] = mfma32(T::turned(from[t], k), pf, o[t]);
-      }
+      in_turn<4 * T::kTiles>(value, [&](auto i, bf16x8 f) {
+        constexpr int I = decltype(i)::value, K = I / T::kTiles;
+        const uint32_t* w = &p[K / 2][K % 2 * 4];
+        o[I % T::kTiles] = mfma32(f, frag_of(w[0], w[1], w[2], w[3]), o[I % T::kTiles]);
+      });
     } else {             // finite values as always; the others are counted over the rows that see them
       const int lo = mine.x - kb - 4 * h, hi = mine.y - kb - 4 * h;
-#pragma unroll
-      for (int t = 0; t < T::kTiles; ++t) {
-        const auto from = T::turned_from(sv, turned_at, t);
+      each<T::kTiles>([&](auto t) {
+        constexpr int D = decltype(t)::value;
         f32x16 above = f32x16{}, below = f32x16{};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const bf16x8 v = T::turned(from, k);
+        each<4>([&](auto k) {
+          constexpr int K = decltype(k)::value;
+          const bf16x8 v = value(std::integral_constant<int, K * T::kTiles + D>{});
           uint32_t see[4];
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const int x = 16 * k + row_of(2 * j, 0);
+            const int x = 16 * K + row_of(2 * j, 0);
             see[j] = (x >= lo && x < hi ? 0x3f80u : 0u) | (x + 1 >= lo && x + 1 < hi ? 0x3f800000u : 0u);
           }
           const bf16x8 seen = frag_of(see[0], see[1], see[2], see[3]);
-          const uint32_t* w = &p[k / 2][k % 2 * 4];
-          o[t] = mfma32(finite_only(v), frag_of(w[0], w[1], w[2], w[3]), o[t]);
+          const uint32_t* w = &p[K / 2][K % 2 * 4];
+          o[D] = mfma32(finite_only(v), frag_of(w[0], w[1], w[2], w[3]), o[D]);
           above = mfma32(infinite(v, 0), seen, above);
           below = mfma32(infinite(v, 0x8000u), seen, below);
-        }
+        });
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          if (above[r] > 0.0f) o[t][r] += INFINITY;
-          if (below[r] > 0.0f) o[t][r] -= INFINITY;
+          if (above[r] > 0.0f) o[D][r] += INFINITY;
+          if (below[r] > 0.0f) o[D][r] -= INFINITY;
         }
-      }
+      });
     }
   }
 
@@ -211,10 +201,12 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed(const PackedArgs) {
   bf16_bits* const to = a->out.data + row_token * a->out.ts + q_head * a->out.hs + 4 * h;
   const bool wide = wide8(a->out.data, a->out.ts, a->out.hs);
 #pragma unroll
-  for (int t = 0; t < T::kTiles; ++t)
+  for (int t = 0; t < T::kTiles; ++t) {
+    o[t] *= inv;
 #pragma unroll
     for (int r = 0; r < 4; ++r)
-      if (32 * t + 8 * r < KS * 16) store4(to + 32 * t + 8 * r, f32x4{o[t][4 * r], o[t][4 * r + 1], o[t][4 * r + 2], o[t][4 * r + 3]} * inv, wide);
+      if (32 * t + 8 * r < KS * 16) store4(to + 32 * t + 8 * r, f32x4{o[t][4 * r], o[t][4 * r + 1], o[t][4 * r + 2], o[t][4 * r + 3]}, wide);
+  }
   if (a->lse && h == 0) a->lse[row_token * (a->heads * group) + q_head] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * (1.0f / kLog2e);
 }
 

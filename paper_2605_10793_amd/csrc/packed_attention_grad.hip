@@ -13,11 +13,23 @@ namespace packed {
 
 namespace {
 
+// Registers 8 k to 8 k + 7 as an operand.
+__device__ __forceinline__ bf16x8 pack8(const f32x16& x, int k) {
+  return frag_of(f32x2_to_bf16x2(x[8 * k], x[8 * k + 1]), f32x2_to_bf16x2(x[8 * k + 2], x[8 * k + 3]), f32x2_to_bf16x2(x[8 * k + 4], x[8 * k + 5]),
+                 f32x2_to_bf16x2(x[8 * k + 6], x[8 * k + 7]));
+}
+
+constexpr int kKeys = 32;          // keys that lie in LDS at a time for k_packed_dq
+
 template <int KS, bool OPTIONS>
 __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dq(const PackedArgs) {
   using T = Tile<KS>;
+  constexpr int kBytes = kKeys * T::kPitch, kBuffer = 2 * kBytes;
   Args a = kernel_args();
   extern __shared__ __attribute__((aligned(1024))) unsigned char shared[];
+  unsigned char* const s_grad = shared + 2 * kBuffer;                                             // the wavefronts' operands of the gradient, each lane's own
+  float* const s_bad = reinterpret_cast<float*>(s_grad + kWaves * KS * 1024);                     // of each buffer's keys: NaN for those that were not finite, 0
+  int* const s_odd = reinterpret_cast<int*>(s_bad + 2 * kKeys);                                   // whether any was
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
   const int head = blockIdx.x % a->heads;
   Item item;
@@ -29,7 +41,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dq(const PackedArgs) 
   const int2 mine = keys_of(a, item, token);
   const bool empty = mine.x >= mine.y;
 
-  int begin, end, low, high, low_all, high_all;
+  int begin, end, low, high, low_all, high_all, low_both, high_both;      // (both: all rows of the workgroup)
   {
     auto none = [](int2 x) { return x.x >= x.y; };
     low = wave_min(empty ? INT_MAX : mine.x);
@@ -39,143 +51,191 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dq(const PackedArgs) 
     const int2 x = keys_of(a, item, token_of(part * kRows + lane)), y = keys_of(a, item, token_of(part * kRows + 64 + lane));
     begin = wave_min(min(none(x) ? INT_MAX : x.x, none(y) ? INT_MAX : y.x));
     end = wave_max_int(max(x.y, y.y));
+    low_both = wave_max_int(max(none(x) ? INT_MAX : x.x, none(y) ? INT_MAX : y.x));
+    high_both = wave_min(min(x.y, y.y));
     if (part * kRows + wave * 32 >= rows) high = 0;
   }
-  begin = begin / kTile * kTile;
+  begin = begin / kKeys * kKeys;
+  if (head == 0 && lane == 0) a->span[(int64_t)(item.base + part) * kWaves + wave] = make_int4(low, high, low_all, high_all);
 
   const int64_t row_token = item.first + token;
   const int q_head = head * group + (row < rows ? row : rows - 1) - token * group;
-  bf16x8 qf[KS], gf[KS];
-  load_rows<KS>(qf, a->q.data + row_token * a->q.ts + q_head * a->q.hs, h);
-  load_rows<KS>(gf, a->out_grad.data + row_token * a->out_grad.ts + q_head * a->out_grad.hs, h);
   float dot = 0.0f, lse = INFINITY;
-  if (!empty) {
-    bf16x8 of[KS];
-    load_rows<KS>(of, a->out.data + row_token * a->out.ts + q_head * a->out.hs, h);
+  u32x4* const own_grad = reinterpret_cast<u32x4*>(s_grad + wave * KS * 1024) + lane;
+  {
+    bf16x8 gf[KS];
+    load_rows<KS>(gf, a->out_grad.data + row_token * a->out_grad.ts + q_head * a->out_grad.hs, h);
 #pragma unroll
-    for (int s = 0; s < KS; ++s)
+    for (int s = 0; s < KS; ++s) own_grad[s * 64] = __builtin_bit_cast(u32x4, gf[s]);
+    if (!empty) {
+      bf16x8 of[KS];
+      load_rows<KS>(of, a->out.data + row_token * a->out.ts + q_head * a->out.hs, h);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) dot = fmaf((float)gf[s][j], (float)of[s][j], dot);
-    lse = a->lse[row_token * (a->heads * group) + q_head] * kLog2e;
-    if (lse == -INFINITY) lse = INFINITY;          // every score is -inf: no weights
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dot = fmaf((float)gf[s][j], (float)of[s][j], dot);
+      lse = a->lse[row_token * (a->heads * group) + q_head] * kLog2e;
+      if (lse == -INFINITY) lse = INFINITY;          // every score is -inf: no weights
+    }
   }
   dot = halves(dot, [](float x, float y) { return x + y; });
-  {
-    const int64_t at = (int64_t)item.first * group + row;
-    if (row < rows && h == 0) {
-      a->stat[(int64_t)head * a->tokens * group + at] = make_float2(lse, dot);
-      if (head == 0) a->seen[at] = mine;
-    }
-    if (head == 0 && lane == 0) a->span[(int64_t)(item.base + part) * kWaves + wave] = make_int4(low, high, low_all, high_all);
-  }
+  bf16x8 qf[KS];
+  load_rows<KS>(qf, a->q.data + row_token * a->q.ts + q_head * a->q.hs, h);
 
   const int k_stride = (int)(a->k.ts * 2), v_stride = (int)(a->v.ts * 2);
   const bf16_bits* const k0 = a->k.data + (int64_t)item.first * a->k.ts + head * a->k.hs;
   const bf16_bits* const v0 = a->v.data + (int64_t)item.first * a->v.ts + head * a->v.hs;
-  const uint32_t lds = lds_of(shared);
+  const uint32_t lds = lds_of(shared), own_lds = lds_of(own_grad);
   auto send = [&](int kb, int which) {
-    send_tile<KS>(k0 + (int64_t)kb * a->k.ts, k_stride, item.count - kb, lds + which * 2 * T::kBytes, wave);
-    send_tile<KS>(v0 + (int64_t)kb * a->v.ts, v_stride, item.count - kb, lds + which * 2 * T::kBytes + T::kBytes, wave);
+    send_tile<KS, kKeys>(k0 + (int64_t)kb * a->k.ts, k_stride, item.count - kb, lds + which * kBuffer, wave);
+    send_tile<KS, kKeys>(v0 + (int64_t)kb * a->v.ts, v_stride, item.count - kb, lds + which * kBuffer + kBytes, wave);
   };
 
-  f32x16 dq[T::kTiles];
+  // The result, and the sum in lse, are of rounded weights: with D' and p' from them, l = sum p' and e = sum p' (g v - D') say by how much both are off: p = p' / l,
+  // D = D' + e / l, and
+  //   dq = scale / l (sum p' (g v - D') (..) k - e / l sum p' (..) k)
+  // The factors of the first sum, which largely cancel, enter its product in two bf16 parts.  (Of dq's size, two sequences of 2048 tokens: 0.0036 off without
+  // either, 0.0027 without the parts, 0.0023 with both, where the rounding of the result alone makes 0.0017.)
+  f32x16 dq[T::kTiles], pk[T::kTiles];
 #pragma unroll
-  for (int t = 0; t < T::kTiles; ++t) dq[t] = f32x16{};
+  for (int t = 0; t < T::kTiles; ++t) dq[t] = pk[t] = f32x16{};
+  float sum = 0.0f, off = 0.0f;
   const float scale = a->scale_log2, cap = a->cap_log2, cap_in = a->cap_in, slope = OPTIONS && a->slopes ? a->slopes[q_head] * kLog2e : 0.0f;
 
+  if (threadIdx.x == 0) *s_odd = 0;
   if (begin < end) send(begin, 0);
   int which = 0;
-  for (int kb = begin; kb < end; kb += kTile, which ^= 1) {
+  for (int kb = begin; kb < end; kb += kKeys, which ^= 1) {
     wait_loads<0>();
     pipeline_barrier();
-    if (kb + kTile < end) send(kb + kTile, which ^ 1);
-    if (kb >= high || kb + kTile <= low) continue;
-    const uint32_t sk = lds + which * 2 * T::kBytes, sv = sk + T::kBytes;
-    const bool all = kb >= low_all && kb + kTile <= high_all;
-    const int here = lane_anew();
-    const uint32_t row_at = T::row_at(here), turned_at = T::turned_at(here);
+    if (kb + kKeys < end) send(kb + kKeys, which ^ 1);
+    const uint32_t sk = lds + which * kBuffer;           // the values lie behind the keys
+    // Keys that are not finite must not meet rows that do not see them, for 0 * NaN is NaN: where some rows of the workgroup do not see all of the block they
+    // become zeros, and what sees them NaN by itself.
     bool odd = false;
+    if (kb < low_both || kb + kKeys > high_both) {
+      const int me = lane_anew();
+      const bool bad = clear_nonfinite<KS, kKeys>(sk, wave, me);
+      if (bad) *s_odd = 1;
+      if ((me & 7) == 0) s_bad[which * kKeys + wave * 8 + (me >> 3)] = bad ? NAN : 0.0f;
+      pipeline_barrier();
+      odd = *(volatile int*)s_odd;
+    }
+    if (kb >= high || kb + kKeys <= low) continue;
+    const bool all = kb >= low_all && kb + kKeys <= high_all;
+    const int here = lane_anew();
+    const uint32_t row_at = sk + T::row_at(here), turned_at = sk + T::turned_at(here);
+    struct Operands {
+      bf16x8 k, v, g;
+    };
+    f32x16 s = f32x16{}, d = f32x16{};
+    in_turn<KS, 2>(
+        [&](auto i) {
+          constexpr int I = decltype(i)::value;
+          return Operands{T::template rows<0>(row_at, I), T::template rows<kBytes>(row_at, I),
+                          *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)(own_lds + I * 1024)};
+        },
+        [&](auto i, const Operands& f) {
+          s = mfma32(f.k, qf[decltype(i)::value], s);
+          d = mfma32(f.v, f.g, d);
+        });
+    float near[OPTIONS ? 16 : 1];
+    if (OPTIONS && cap != 0.0f) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        float x;
+        s[r] = capped(s[r], cap, cap_in, &x) - lse;
+        near[r] = 4.0f * (x - x * x);
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], scale, -lse);
+    }
+    if (OPTIONS && slope != 0.0f) {
+      const float at = (float)(token - kb - 4 * h);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = fmaf(-slope, fabsf(at - (float)row_of(r, 0)), s[r]);
+    }
+    if (odd) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] += s_bad[which * kKeys + row_of(r, h)];
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[r] = __builtin_amdgcn_exp2f(s[r]);
+      d[r] = (d[r] - dot) * s[r];
+    }
     if (!all) {
-      f32x16 z = f32x16{};
+      const int lo = mine.x - kb - 4 * h, hi = mine.y - kb - 4 * h;
 #pragma unroll
-      for (int t = 0; t < T::kTiles; ++t) {
-        const auto from = T::turned_from(sk, turned_at, t);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) z = mfma32(T::turned(from, k), frag_of(0, 0, 0, 0), z);
-      }
-      odd = any_left(z);
-    }
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      f32x16 s = f32x16{}, d = f32x16{};
-#pragma unroll
-      for (int i = 0; i < KS; ++i) {
-        s = mfma32(T::rows(T::rows_from(sk, row_at, i), u), qf[i], s);
-        d = mfma32(T::rows(T::rows_from(sv, row_at, i), u), gf[i], d);
-      }
-      if (OPTIONS && cap != 0.0f) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          float x;
-          s[r] = capped(s[r], cap, cap_in, &x) - lse;
-          d[r] = (d[r] - dot) * (4.0f * (x - x * x));
-        }
-      } else {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          s[r] = fmaf(s[r], scale, -lse);
-          d[r] -= dot;
-        }
-      }
-      if (OPTIONS && slope != 0.0f) {
-        const float at = (float)(token - kb - 4 * h - 32 * u);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = fmaf(-slope, fabsf(at - (float)row_of(r, 0)), s[r]);
-      }
-#pragma unroll
-      for (int r = 0; r < 16; ++r) d[r] *= __builtin_amdgcn_exp2f(s[r]);
-      if (!all) {
-        const int lo = mine.x - kb - 4 * h - 32 * u, hi = mine.y - kb - 4 * h - 32 * u;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) d[r] = row_of(r, 0) >= lo && row_of(r, 0) < hi ? d[r] : 0.0f;
-      }
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const bf16x8 df = frag_of(f32x2_to_bf16x2(d[8 * k], d[8 * k + 1]), f32x2_to_bf16x2(d[8 * k + 2], d[8 * k + 3]),
-                                  f32x2_to_bf16x2(d[8 * k + 4], d[8 * k + 5]), f32x2_to_bf16x2(d[8 * k + 6], d[8 * k + 7]));
-#pragma unroll
-        for (int t = 0; t < T::kTiles; ++t) {
-          bf16x8 f = T::turned(T::turned_from(sk, turned_at, t), 2 * u + k);
-          // A key that is not finite makes the factor of every row that sees it NaN; the others must not meet it.
-          if (odd) f = finite_only(f);
-          dq[t] = mfma32(f, df, dq[t]);
-        }
+      for (int r = 0; r < 16; ++r) {
+        const bool see = row_of(r, 0) >= lo && row_of(r, 0) < hi;
+        s[r] = see ? s[r] : 0.0f;
+        d[r] = see ? d[r] : 0.0f;
+        if constexpr (OPTIONS) near[r] = see ? near[r] : 0.0f;
       }
     }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      sum += s[r];
+      off += d[r];
+    }
+    if (OPTIONS && cap != 0.0f) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[r] *= near[r];
+        d[r] *= near[r];
+      }
+    }
+    const bf16x8 pf[2] = {pack8(s, 0), pack8(s, 1)}, df[2] = {pack8(d, 0), pack8(d, 1)};
+#pragma unroll
+    for (int r = 0; r < 16; ++r) d[r] -= (float)df[r / 8][r % 8];
+    const bf16x8 rest[2] = {pack8(d, 0), pack8(d, 1)};
+    __builtin_amdgcn_sched_barrier(0);
+    in_turn<2 * T::kTiles>([&](auto i) { return T::template turned<decltype(i)::value / T::kTiles * 16 * T::kPitch>(turned_at, decltype(i)::value % T::kTiles); },
+                           [&](auto i, bf16x8 f) {
+                             constexpr int I = decltype(i)::value, t = I % T::kTiles;
+                             dq[t] = mfma32(f, df[I / T::kTiles], dq[t]);
+                             pk[t] = mfma32(f, pf[I / T::kTiles], pk[t]);
+                             dq[t] = mfma32(f, rest[I / T::kTiles], dq[t]);
+                           });
   }
 
+  sum = halves(sum, [](float x, float y) { return x + y; });
+  off = halves(off, [](float x, float y) { return x + y; });
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  off *= inv;
   a = kernel_args();
   if (row >= rows) return;
+  if (h == 0) {
+    const int64_t at = (int64_t)item.first * group + row;
+    a->stat[(int64_t)head * a->tokens * group + at] = make_float2(sum == 0.0f ? INFINITY : lse + __builtin_amdgcn_logf(sum), dot + off);
+    if (head == 0) a->seen[at] = mine;
+  }
   bf16_bits* const to = a->q_grad.data + row_token * a->q_grad.ts + q_head * a->q_grad.hs + 4 * h;
   const bool wide = wide8(a->q_grad.data, a->q_grad.ts, a->q_grad.hs);
-  const float by = a->scale;
+  const float by = a->scale * inv;
 #pragma unroll
-  for (int t = 0; t < T::kTiles; ++t)
+  for (int t = 0; t < T::kTiles; ++t) {
+    dq[t] -= off * pk[t];
 #pragma unroll
     for (int r = 0; r < 4; ++r)
       if (32 * t + 8 * r < KS * 16) store4(to + 32 * t + 8 * r, f32x4{dq[t][4 * r], dq[t][4 * r + 1], dq[t][4 * r + 2], dq[t][4 * r + 3]} * by, wide);
+  }
 }
 
 constexpr int kStatAt = 0, kSeenAt = 1024, kRowBytes = 2048;      // of 64 rows (and the 64 behind them, which the same loads bring)
 
 // Two wavefronts take 32 of the workgroup's 64 keys each, for the first 32 of 64 rows at a time, two for the others; their sums meet in LDS at the end.
 template <int KS, bool OPTIONS>
-__global__ void __launch_bounds__(64 * kWaves, KS > 6 ? 1 : 2) k_packed_dkv(const PackedArgs) {
+__global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dkv(const PackedArgs) {
   using T = Tile<KS>;
   constexpr int kBuffer = 2 * T::kBytes + kRowBytes;
   Args a = kernel_args();
   extern __shared__ __attribute__((aligned(1024))) unsigned char shared[];
   float* const s_slope = reinterpret_cast<float*>(shared + 2 * kBuffer);
+  float* const s_bad = s_slope + 64;                                              // of each buffer's rows: NaN for those that were not finite, 0
+  int* const s_odd = reinterpret_cast<int*>(s_bad + 2 * kTile);                   // whether any was
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
   const int head = blockIdx.x % a->heads;
   Item item;
@@ -190,6 +250,7 @@ __global__ void __launch_bounds__(64 * kWaves, KS > 6 ? 1 : 2) k_packed_dkv(cons
     __syncthreads();
   }
 
+  if (threadIdx.x == 0) *s_odd = 0;
   bf16x8 kf[KS], vf[KS];
   load_rows<KS>(kf, a->k.data + key_token * a->k.ts + head * a->k.hs, h);
   load_rows<KS>(vf, a->v.data + key_token * a->v.ts + head * a->v.hs, h);
@@ -198,10 +259,10 @@ __global__ void __launch_bounds__(64 * kWaves, KS > 6 ? 1 : 2) k_packed_dkv(cons
   const int4* const span = a->span + ((((int64_t)item.first * group) >> 7) + item.number) * kWaves;
   const int subs = item.rest ? 0 : (rows + 31) / 32;
   int next_chunk = a->last ? 0 : (int)((int64_t)k0 * group / 64) * 2, chunk = 0;
-  uint64_t active = 0, some = 0, whole = 0;
+  uint64_t active = 0, some = 0, whole = 0, every = 0;
   struct Rows64 {
     int sub;
-    bool some, all;
+    bool some, all, every;      // of the wavefront's keys and rows: any are seen, all are; all of the workgroup's
   };
   auto next = [&](Rows64* x) {
     while (!active) {
@@ -214,6 +275,7 @@ __global__ void __launch_bounds__(64 * kWaves, KS > 6 ? 1 : 2) k_packed_dkv(cons
       const uint64_t near = __ballot(s.x < k0 + kTile && s.y > k0);
       some = __ballot(s.x < key0 + 32 && s.y > key0);
       whole = __ballot(s.z <= key0 && s.w >= key0 + 32);
+      every = __ballot(s.z <= k0 && s.w >= k0 + kTile);
       active = (near | near >> 1) & 0x5555555555555555ull;
     }
     const int bit = __builtin_ctzll(active);
@@ -221,6 +283,7 @@ __global__ void __launch_bounds__(64 * kWaves, KS > 6 ? 1 : 2) k_packed_dkv(cons
     x->sub = chunk + bit;
     x->some = (some >> (bit + at_rows)) & 1;
     x->all = (whole >> (bit + at_rows)) & 1;
+    x->every = ((every >> bit) & 3) == 3;
     return true;
   };
 
@@ -265,18 +328,36 @@ __global__ void __launch_bounds__(64 * kWaves, KS > 6 ? 1 : 2) k_packed_dkv(cons
     pipeline_barrier();
     more = next(&then);
     if (more) send(then.sub, which ^ 1);
+    bool odd = false;          // (as in k_packed_dq: queries and gradients that are not finite)
+    if (!now.every) {
+      const int me = lane_anew();
+      const bool bad_q = clear_nonfinite<KS, kTile>(lds + which * kBuffer, wave, me), bad_g = clear_nonfinite<KS, kTile>(lds + which * kBuffer + T::kBytes, wave, me);
+      if (bad_q || bad_g) *s_odd = 1;
+      if ((me & 3) == 0) s_bad[which * kTile + wave * 16 + (me >> 2)] = bad_q || bad_g ? NAN : 0.0f;
+      pipeline_barrier();
+      odd = *(volatile int*)s_odd;
+    }
     if (!now.some) continue;
-    const uint32_t sq = lds + which * kBuffer, sg = sq + T::kBytes;
+    const uint32_t sq = lds + which * kBuffer + at_rows * 32 * T::kPitch;           // the gradients lie behind the queries
     const unsigned char* const s_rows = shared + which * kBuffer + 2 * T::kBytes + at_rows * 32 * 8;
     const int here = lane_anew();
-    const uint32_t row_at = T::row_at(here), turned_at = T::turned_at(here);
+    const uint32_t row_at = sq + T::row_at(here), turned_at = sq + T::turned_at(here);
     const int half = here >> 5;
 
+    // Operands of the queries and, odd ones, of the gradients: 16 rows, 32 entries.
+    auto turned = [&](auto i) {
+      constexpr int I = decltype(i)::value;
+      return T::template turned<I % 2 * T::kBytes + I / 2 / T::kTiles * 16 * T::kPitch>(turned_at, I / 2 % T::kTiles);
+    };
     f32x16 s = f32x16{}, d = f32x16{};
-#pragma unroll
-    for (int i = 0; i < KS; ++i) s = mfma32(T::rows(T::rows_from(sq, row_at, i), at_rows), kf[i], s);
-#pragma unroll
-    for (int i = 0; i < KS; ++i) d = mfma32(T::rows(T::rows_from(sg, row_at, i), at_rows), vf[i], d);
+    in_turn<2 * KS>([&](auto i) { return T::template rows<decltype(i)::value % 2 * T::kBytes>(row_at, decltype(i)::value / 2); },
+                    [&](auto i, bf16x8 f) {
+                      constexpr int I = decltype(i)::value;
+                      if constexpr (I % 2)
+                        d = mfma32(f, vf[I / 2], d);
+                      else
+                        s = mfma32(f, kf[I / 2], s);
+                    });
 #pragma unroll
     for (int r4 = 0; r4 < 4; ++r4) {
       const f32x4* const at = reinterpret_cast<const f32x4*>(s_rows + kStatAt + (8 * r4 + 4 * half) * 8);
@@ -306,12 +387,15 @@ __global__ void __launch_bounds__(64 * kWaves, KS > 6 ? 1 : 2) k_packed_dkv(cons
         s[r] = fmaf(-s_slope[n - token * group], fabsf(away + (float)token), s[r]);
       }
     }
+    if (odd) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] += s_bad[which * kTile + at_rows * 32 + row_of(r, half)];
+    }
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       s[r] = __builtin_amdgcn_exp2f(s[r]);
       d[r] *= s[r];
     }
-    bool odd = false;
     if (!now.all) {
       const int left = rows - (now.sub + at_rows) * 32 - 4 * half;
 #pragma unroll
@@ -322,45 +406,21 @@ __global__ void __launch_bounds__(64 * kWaves, KS > 6 ? 1 : 2) k_packed_dkv(cons
         const int lo[4] = {x[0], x[2], y[0], y[2]}, hi[4] = {x[1], x[3], y[1], y[3]};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const bool see = key >= lo[j] && key < hi[j] && row_of(4 * r4 + j, 0) < left;
-          // A gradient that is not finite makes D so, and must not reach keys that its row does not see: they meet zeros below, the others NaN.
-          const float dot = *reinterpret_cast<const float*>(s_rows + kStatAt + (8 * r4 + 4 * half + j) * 8 + 4);
-          s[4 * r4 + j] = see ? s[4 * r4 + j] + (dot - dot) : 0.0f;
-          d[4 * r4 + j] = see ? d[4 * r4 + j] : 0.0f;
+          const uint32_t see = -(uint32_t)((key >= lo[j]) & (key < hi[j]) & (row_of(4 * r4 + j, 0) < left));
+          s[4 * r4 + j] = __uint_as_float(__float_as_uint(s[4 * r4 + j]) & see);
+          d[4 * r4 + j] = __uint_as_float(__float_as_uint(d[4 * r4 + j]) & see);
         }
       }
-      f32x16 z = f32x16{};
-#pragma unroll
-      for (int t = 0; t < T::kTiles; ++t) {
-        const auto from = T::turned_from(sq, turned_at, t), from_g = T::turned_from(sg, turned_at, t);
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          z = mfma32(T::turned(from, 2 * at_rows + k), frag_of(0, 0, 0, 0), z);
-          z = mfma32(T::turned(from_g, 2 * at_rows + k), frag_of(0, 0, 0, 0), z);
-        }
-      }
-      odd = any_left(z);
     }
-    auto pack = [](const f32x16& x, int k) {
-      return frag_of(f32x2_to_bf16x2(x[8 * k], x[8 * k + 1]), f32x2_to_bf16x2(x[8 * k + 2], x[8 * k + 3]), f32x2_to_bf16x2(x[8 * k + 4], x[8 * k + 5]),
-                     f32x2_to_bf16x2(x[8 * k + 6], x[8 * k + 7]));
-    };
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const bf16x8 pf = pack(s, k), df = pack(d, k);
-#pragma unroll
-      for (int t = 0; t < T::kTiles; ++t) {
-        bf16x8 f = T::turned(T::turned_from(sg, turned_at, t), 2 * at_rows + k);
-        if (odd) f = finite_only(f);
-        dv[t] = mfma32(f, pf, dv[t]);
-      }
-#pragma unroll
-      for (int t = 0; t < T::kTiles; ++t) {
-        bf16x8 f = T::turned(T::turned_from(sq, turned_at, t), 2 * at_rows + k);
-        if (odd) f = finite_only(f);
-        dk[t] = mfma32(f, df, dk[t]);
-      }
-    }
+    const bf16x8 pf[2] = {pack8(s, 0), pack8(s, 1)}, df[2] = {pack8(d, 0), pack8(d, 1)};
+    __builtin_amdgcn_sched_barrier(0);
+    in_turn<4 * T::kTiles>(turned, [&](auto i, bf16x8 f) {
+      constexpr int I = decltype(i)::value, t = I / 2 % T::kTiles, k = I / 2 / T::kTiles;
+      if constexpr (I % 2)
+        dv[t] = mfma32(f, pf[k], dv[t]);
+      else
+        dk[t] = mfma32(f, df[k], dk[t]);
+    });
   }
 
   __syncthreads();
@@ -393,7 +453,7 @@ __global__ void __launch_bounds__(64 * kWaves, KS > 6 ? 1 : 2) k_packed_dkv(cons
 
 template <int KS, bool OPTIONS>
 hipError_t launch(const PackedArgs& a, hipStream_t s) {
-  constexpr int kDq = 4 * Tile<KS>::kBytes, kDkv = 2 * (2 * Tile<KS>::kBytes + kRowBytes) + 256;
+  constexpr int kDq = 4 * kKeys * Tile<KS>::kPitch + kWaves * KS * 1024 + 2 * kKeys * 4 + 16, kDkv = 2 * (2 * Tile<KS>::kBytes + kRowBytes) + 256 + 2 * kTile * 4 + 16;
   static_assert(2 * 64 * 8 * Tile<KS>::kTiles * 16 <= kDkv, "sums meet where the tiles were");
   static PerDeviceOnce once;
   hipError_t e = once.run([] {

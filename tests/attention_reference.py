@@ -50,7 +50,7 @@ def attend(q, k, v, seen, place, scale, cap=0.0, slopes=None, grad=None, sizes=N
         dp = g @ vh.T
         d = (g * o).sum(-1, keepdim=True)
         ds = p * (dp - d) * near
-        # D takes the rounded result; weights come from an lse whose sum was of rounded weights, and are rounded as factors
+        # D takes the result; weights come from an lse whose sum was of rounded weights, and are rounded as factors
         d_tol = (g.abs() * res["out_tol"][:, h]).sum(-1, keepdim=True) + (width + 16) * 2.0 ** -24 * (g.abs() * o.abs()).sum(-1, keepdim=True)
         p_tol = p * (2 * HALF + 2 * eps) * 1.02
         ds_tol = 1.02 * (p * near * (d_tol + (width + 16) * 2.0 ** -24 * (g.abs() @ vh.abs().T)) + ds.abs() * (2 * HALF + 2 * eps) + p * (dp - d).abs() * 2.0 ** -20)
