@@ -194,7 +194,7 @@ struct Tile {
 // N products whose operands come from LDS: RING of them are on their way ahead of the products that take them, and nothing but arithmetic passes from one to
 // the next (the compiler would hold more of them than there are registers).  load(i), use(i, operand): i as a constant.
 constexpr int kArithmetic = 0x6;
-template <int N, int RING = 4, typename Load, typename Use>
+template <int N, int RING = 4, int FENCE = kArithmetic, typename Load, typename Use>
 __device__ __forceinline__ void in_turn(Load load, Use use) {
   decltype(load(std::integral_constant<int, 0>{})) ring[RING];
   each<(N < RING ? N : RING)>([&](auto i) { ring[decltype(i)::value] = load(i); });
@@ -202,7 +202,7 @@ __device__ __forceinline__ void in_turn(Load load, Use use) {
     constexpr int I = decltype(i)::value;
     use(i, ring[I % RING]);
     if constexpr (I + RING < N) ring[I % RING] = load(std::integral_constant<int, I + RING>{});
-    __builtin_amdgcn_sched_barrier(kArithmetic);
+    if constexpr (FENCE >= 0) __builtin_amdgcn_sched_barrier(FENCE);
   });
 }
 
@@ -308,24 +308,11 @@ __device__ __forceinline__ bool clear_nonfinite(uint32_t tile, int wave, int lan
   return (found >> (lane / kLanes * kLanes)) & ((1 << kLanes) - 1);
 }
 
-// Ones where a value is `sign`'s infinity or NaN.
-__device__ __forceinline__ bf16x8 infinite(bf16x8 f, uint32_t sign) {
-  u32x4 x = __builtin_bit_cast(u32x4, f);
-  u32x4 y;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const uint32_t lo = x[j] & 0xffffu, hi = x[j] >> 16;
-    const bool is_lo = (lo & 0x7fffu) > 0x7f80u || lo == (0x7f80u | sign), is_hi = (hi & 0x7fffu) > 0x7f80u || hi == (0x7f80u | sign);
-    y[j] = (is_lo ? 0x3f80u : 0u) | (is_hi ? 0x3f800000u : 0u);
-  }
-  return __builtin_bit_cast(bf16x8, y);
-}
-// Whether a product of operands with zeros left anything but zeros.
-__device__ __forceinline__ bool any_left(const f32x16& z) {
-  float s = 0.0f;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) s += z[r];
-  return __any(!(s == 0.0f));
+// The largest of three, whatever their sign; a NaN loses.  (For fmaxf of fmaxf the compiler first makes each argument canonical, an instruction more for each.)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float x;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(x) : "v"(a), "v"(b), "v"(c));
+  return x;
 }
 
 // A score in base 2 from a product q k, less the bias; `r` receives 1 / (1 + e^(2 u / cap)), from which 1 - tanh^2 = 4 r (1 - r) follows.
@@ -348,6 +335,22 @@ __device__ __forceinline__ void store4(bf16_bits* to, f32x4 x, bool wide) {
 }
 __device__ __forceinline__ bool wide8(const bf16_bits* p, int64_t ts, int64_t hs) {
   return ((uintptr_t)p & 7) == 0 && (ts & 3) == 0 && (hs & 3) == 0;
+}
+
+// A row's entries as a lane holds them, times `by`; `to`: the lane's first.
+template <int KS>
+__device__ __forceinline__ void store_row(bf16_bits* to, const f32x16 (&x)[(KS + 1) / 2], float by, bool wide) {
+  auto all = [&](bool w) {
+#pragma unroll
+    for (int t = 0; t < (KS + 1) / 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (32 * t + 8 * r < KS * 16) store4(to + 32 * t + 8 * r, f32x4{x[t][4 * r], x[t][4 * r + 1], x[t][4 * r + 2], x[t][4 * r + 3]} * by, w);
+  };
+  if (wide)
+    all(true);
+  else
+    all(false);
 }
 
 // Items of the rows, and of the keys, of a call.

@@ -20,6 +20,8 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed(const PackedArgs) {
   using T = Tile<KS>;
   Args a = kernel_args();
   extern __shared__ __attribute__((aligned(1024))) unsigned char shared[];
+  int* const s_bad = reinterpret_cast<int*>(shared + 4 * T::kBytes);          // of each buffer's values: whether they were not finite
+  int* const s_odd = s_bad + 2 * kTile;                                       // whether any was
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
   const int head = blockIdx.x % a->heads;
   Item item;
@@ -32,8 +34,8 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed(const PackedArgs) {
   const int row = part * kRows + wave * 32 + (lane & 31), token = token_of(row);
   const int2 mine = keys_of(a, item, token);
 
-  // Keys that any row of the workgroup sees, any of the wavefront, all of the wavefront.
-  int begin, end, low, high, low_all, high_all;
+  // Keys that any row of the workgroup sees, any of the wavefront, all of the wavefront, all of the workgroup.
+  int begin, end, low, high, low_all, high_all, low_both, high_both;
   {
     auto none = [](int2 x) { return x.x >= x.y; };
     const bool empty = none(mine);
@@ -44,6 +46,8 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed(const PackedArgs) {
     const int2 x = keys_of(a, item, token_of(part * kRows + lane)), y = keys_of(a, item, token_of(part * kRows + 64 + lane));
     begin = wave_min(min(none(x) ? INT_MAX : x.x, none(y) ? INT_MAX : y.x));
     end = wave_max_int(max(x.y, y.y));
+    low_both = wave_max_int(max(none(x) ? INT_MAX : x.x, none(y) ? INT_MAX : y.x));
+    high_both = wave_min(min(x.y, y.y));
     if (part * kRows + wave * 32 >= rows) high = 0;
   }
   begin = begin / kTile * kTile;
@@ -69,14 +73,26 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed(const PackedArgs) {
   const float scale = a->scale_log2, cap = a->cap_log2, cap_in = a->cap_in, slope = OPTIONS && a->slopes ? a->slopes[q_head] * kLog2e : 0.0f;
   const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
 
+  if (threadIdx.x == 0) *s_odd = 0;
   if (begin < end) send(begin, 0);
   int which = 0;
   for (int kb = begin; kb < end; kb += kTile, which ^= 1) {
     wait_loads<0>();
     pipeline_barrier();
     if (kb + kTile < end) send(kb + kTile, which ^ 1);
-    if (kb >= high || kb + kTile <= low) continue;
     const uint32_t sk = lds + which * 2 * T::kBytes, sv = sk + T::kBytes;
+    // Values that are not finite must not meet rows that do not see them, for 0 * NaN is NaN: where some rows of the workgroup do not see all of the block they
+    // become zeros, and are added by themselves to the rows that do.
+    bool odd = false;
+    if (kb < low_both || kb + kTile > high_both) {
+      const int me = lane_anew();
+      const bool bad = clear_nonfinite<KS, kTile>(sv, wave, me);
+      if (bad) *s_odd = 1;
+      if ((me & 3) == 0) s_bad[which * kTile + wave * 16 + (me >> 2)] = bad;
+      pipeline_barrier();
+      odd = *(volatile int*)s_odd;
+    }
+    if (kb >= high || kb + kTile <= low) continue;
     const bool all = kb >= low_all && kb + kTile <= high_all;
 
     const int here = lane_anew();
@@ -122,9 +138,10 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed(const PackedArgs) {
       }
     }
 
-    float top = fmaxf(s[0][0], s[1][0]);
+    float top = max3(s[0][0], s[1][0], s[0][1]);
 #pragma unroll
-    for (int r = 1; r < 16; ++r) top = fmaxf(top, fmaxf(s[0][r], s[1][r]));
+    for (int r = 1; r < 15; ++r) top = max3(top, s[1][r], s[0][r + 1]);
+    top = fmaxf(top, s[1][15]);
     if (__any(top > (m == -INFINITY ? -INFINITY : kRise))) {
       top = halves(top, [](float x, float y) { return fmaxf(x, y); });
       const bool unset = m == -INFINITY;
@@ -152,44 +169,26 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed(const PackedArgs) {
       constexpr int I = decltype(i)::value, K = I / T::kTiles;
       return T::template turned<K * 16 * T::kPitch>(turned_at, I % T::kTiles);
     };
-    bool odd = false;
-    if (!all) {          // infinities and NaNs must not reach rows that do not see them: 0 * NaN is NaN
-      f32x16 z = f32x16{};
-      in_turn<4 * T::kTiles>(value, [&](auto, bf16x8 f) { z = mfma32(f, frag_of(0, 0, 0, 0), z); });
-      odd = any_left(z);
-    }
-    if (!odd) {
-      in_turn<4 * T::kTiles>(value, [&](auto i, bf16x8 f) {
-        constexpr int I = decltype(i)::value, K = I / T::kTiles;
-        const uint32_t* w = &p[K / 2][K % 2 * 4];
-        o[I % T::kTiles] = mfma32(f, frag_of(w[0], w[1], w[2], w[3]), o[I % T::kTiles]);
-      });
-    } else {             // finite values as always; the others are counted over the rows that see them
-      const int lo = mine.x - kb - 4 * h, hi = mine.y - kb - 4 * h;
-      each<T::kTiles>([&](auto t) {
-        constexpr int D = decltype(t)::value;
-        f32x16 above = f32x16{}, below = f32x16{};
-        each<4>([&](auto k) {
-          constexpr int K = decltype(k)::value;
-          const bf16x8 v = value(std::integral_constant<int, K * T::kTiles + D>{});
-          uint32_t see[4];
+    in_turn<4 * T::kTiles>(value, [&](auto i, bf16x8 f) {
+      constexpr int I = decltype(i)::value, K = I / T::kTiles;
+      const uint32_t* w = &p[K / 2][K % 2 * 4];
+      o[I % T::kTiles] = mfma32(f, frag_of(w[0], w[1], w[2], w[3]), o[I % T::kTiles]);
+    });
+    if (odd) {
+      for (int j = 0; j < kTile; ++j) {
+        const int key = kb + j;
+        if (!s_bad[which * kTile + j] || key >= item.count) continue;
+        const bool see = key >= mine.x && key < mine.y;
+        const bf16_bits* const from = v0 + (int64_t)key * a->v.ts + 4 * h;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int x = 16 * K + row_of(2 * j, 0);
-            see[j] = (x >= lo && x < hi ? 0x3f80u : 0u) | (x + 1 >= lo && x + 1 < hi ? 0x3f800000u : 0u);
+        for (int t = 0; t < T::kTiles; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int entry = 32 * t + row_of(r, 0);
+            const uint32_t x = entry < KS * 16 ? from[entry] : 0;
+            o[t][r] += see && (x & 0x7f80u) == 0x7f80u ? __uint_as_float(x << 16) : 0.0f;
           }
-          const bf16x8 seen = frag_of(see[0], see[1], see[2], see[3]);
-          const uint32_t* w = &p[K / 2][K % 2 * 4];
-          o[D] = mfma32(finite_only(v), frag_of(w[0], w[1], w[2], w[3]), o[D]);
-          above = mfma32(infinite(v, 0), seen, above);
-          below = mfma32(infinite(v, 0x8000u), seen, below);
-        });
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          if (above[r] > 0.0f) o[D][r] += INFINITY;
-          if (below[r] > 0.0f) o[D][r] -= INFINITY;
-        }
-      });
+      }
     }
   }
 
@@ -199,20 +198,13 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed(const PackedArgs) {
   // Nothing seen, or every score -inf: zeros.
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   bf16_bits* const to = a->out.data + row_token * a->out.ts + q_head * a->out.hs + 4 * h;
-  const bool wide = wide8(a->out.data, a->out.ts, a->out.hs);
-#pragma unroll
-  for (int t = 0; t < T::kTiles; ++t) {
-    o[t] *= inv;
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if (32 * t + 8 * r < KS * 16) store4(to + 32 * t + 8 * r, f32x4{o[t][4 * r], o[t][4 * r + 1], o[t][4 * r + 2], o[t][4 * r + 3]}, wide);
-  }
+  store_row<KS>(to, o, inv, wide8(a->out.data, a->out.ts, a->out.hs));
   if (a->lse && h == 0) a->lse[row_token * (a->heads * group) + q_head] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * (1.0f / kLog2e);
 }
 
 template <int KS, bool OPTIONS>
 hipError_t launch(const PackedArgs& a, hipStream_t s) {
-  constexpr int kShared = 4 * Tile<KS>::kBytes;
+  constexpr int kShared = 4 * Tile<KS>::kBytes + 2 * kTile * 4 + 16;
   static PerDeviceOnce once;
   const hipError_t e = once.run([] { return hipFuncSetAttribute(reinterpret_cast<const void*>(k_packed<KS, OPTIONS>), hipFuncAttributeMaxDynamicSharedMemorySize, kShared); });
   if (e != hipSuccess) return e;

@@ -213,15 +213,9 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dq(const PackedArgs) 
     if (head == 0) a->seen[at] = mine;
   }
   bf16_bits* const to = a->q_grad.data + row_token * a->q_grad.ts + q_head * a->q_grad.hs + 4 * h;
-  const bool wide = wide8(a->q_grad.data, a->q_grad.ts, a->q_grad.hs);
-  const float by = a->scale * inv;
 #pragma unroll
-  for (int t = 0; t < T::kTiles; ++t) {
-    dq[t] -= off * pk[t];
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if (32 * t + 8 * r < KS * 16) store4(to + 32 * t + 8 * r, f32x4{dq[t][4 * r], dq[t][4 * r + 1], dq[t][4 * r + 2], dq[t][4 * r + 3]} * by, wide);
-  }
+  for (int t = 0; t < T::kTiles; ++t) dq[t] -= off * pk[t];
+  store_row<KS>(to, dq, a->scale * inv, wide8(a->q_grad.data, a->q_grad.ts, a->q_grad.hs));
 }
 
 constexpr int kStatAt = 0, kSeenAt = 1024, kRowBytes = 2048;      // of 64 rows (and the 64 behind them, which the same loads bring)
@@ -440,15 +434,19 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dkv(const PackedArgs)
   const bool k_wide = wide8(a->k_grad.data, a->k_grad.ts, a->k_grad.hs), v_wide = wide8(a->v_grad.data, a->v_grad.ts, a->v_grad.hs);
   bf16_bits* const to_k = a->k_grad.data + key_token * a->k_grad.ts + head * a->k_grad.hs + 4 * h;
   bf16_bits* const to_v = a->v_grad.data + key_token * a->v_grad.ts + head * a->v_grad.hs + 4 * h;
-  const float by = a->scale;
 #pragma unroll
   for (int t = 0; t < T::kTiles; ++t)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      if (32 * t + 8 * r >= KS * 16) continue;
-      store4(to_k + 32 * t + 8 * r, (f32x4{dk[t][4 * r], dk[t][4 * r + 1], dk[t][4 * r + 2], dk[t][4 * r + 3]} + s_sum[(t * 4 + r) * 64]) * by, k_wide);
-      store4(to_v + 32 * t + 8 * r, f32x4{dv[t][4 * r], dv[t][4 * r + 1], dv[t][4 * r + 2], dv[t][4 * r + 3]} + s_sum[((T::kTiles + t) * 4 + r) * 64], v_wide);
+      const f32x4 x = s_sum[(t * 4 + r) * 64], y = s_sum[((T::kTiles + t) * 4 + r) * 64];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        dk[t][4 * r + j] += x[j];
+        dv[t][4 * r + j] += y[j];
+      }
     }
+  store_row<KS>(to_k, dk, a->scale, k_wide);
+  store_row<KS>(to_v, dv, 1.0f, v_wide);
 }
 
 template <int KS, bool OPTIONS>
