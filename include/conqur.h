@@ -546,7 +546,7 @@ typedef struct {
   uint64_t workspace_bytes;
 } conqur_attention_call;
 
-/* Bytes of workspace: none for rows that start at multiples of 16 bytes (and lie less than 16 MiB apart); others are laid out there first. */
+/* Bytes of workspace: none for rows that start at multiples of 16 bytes (and lie less than 8 MiB apart); others are laid out there first. */
 uint64_t conqur_attention_workspace(const conqur_attention_call* call);
 conqur_status conqur_attention(const conqur_attention_call* call, void* stream);
 

@@ -280,14 +280,14 @@ __device__ __forceinline__ bf16x8 finite_only(bf16x8 f) {
   for (int j = 0; j < 4; ++j) x[j] = finite_only(x[j]);
   return __builtin_bit_cast(bf16x8, x);
 }
-// A wavefront's quarter of a tile's ROWS rows: infinities and NaNs become zeros.  256 / ROWS neighbouring lanes share a row; they receive whether it had any.
-template <int KS, int ROWS>
+// A wavefront's EACH rows of a tile: infinities and NaNs become zeros.  64 / EACH neighbouring lanes share a row; they receive whether it had any.
+template <int KS, int EACH>
 __device__ __forceinline__ bool clear_nonfinite(uint32_t tile, int wave, int lane) {
   using T = Tile<KS>;
   typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
   typedef __attribute__((address_space(3))) u32x4* P;
-  constexpr int kLanes = 256 / ROWS, kEach = T::kPitch / kLanes / 16;
-  const uint32_t at = tile + (wave * (ROWS / 4) + lane / kLanes) * T::kPitch + lane % kLanes * (T::kPitch / kLanes);
+  constexpr int kLanes = 64 / EACH, kEach = T::kPitch / kLanes / 16;
+  const uint32_t at = tile + (wave * EACH + lane / kLanes) * T::kPitch + lane % kLanes * (T::kPitch / kLanes);
   u16x2 most = {0, 0};
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {

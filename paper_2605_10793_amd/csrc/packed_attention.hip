@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed(const PackedArgs) {
     bool odd = false;
     if (kb < low_both || kb + kTile > high_both) {
       const int me = lane_anew();
-      const bool bad = clear_nonfinite<KS, kTile>(sv, wave, me);
+      const bool bad = clear_nonfinite<KS, kTile / kWaves>(sv, wave, me);
       if (bad) *s_odd = 1;
       if ((me & 3) == 0) s_bad[which * kTile + wave * 16 + (me >> 2)] = bad;
       pipeline_barrier();
@@ -239,7 +239,7 @@ __global__ void __launch_bounds__(256) k_lay(Rows from, bf16_bits* to, int64_t t
   }
 }
 
-constexpr int64_t kMaxStride = 1ll << 40, kNear = 1ll << 23;      // elements; 64 rows kNear apart are addressed in 31 bits
+constexpr int64_t kMaxStride = 1ll << 40, kNear = 1ll << 22;      // elements; 128 rows kNear apart are addressed in 31 bits
 
 bool heads_fine(const conqur_heads& h, uint64_t heads, uint32_t width, uint64_t tokens, bool output) {
   if (h.heads != heads || !h.data || reinterpret_cast<uintptr_t>(h.data) % 2) return false;

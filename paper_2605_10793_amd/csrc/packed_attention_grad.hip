@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dq(const PackedArgs) 
     bool odd = false;
     if (kb < low_both || kb + kKeys > high_both) {
       const int me = lane_anew();
-      const bool bad = clear_nonfinite<KS, kKeys>(sk, wave, me);
+      const bool bad = clear_nonfinite<KS, kKeys / kWaves>(sk, wave, me);
       if (bad) *s_odd = 1;
       if ((me & 7) == 0) s_bad[which * kKeys + wave * 8 + (me >> 3)] = bad ? NAN : 0.0f;
       pipeline_barrier();
@@ -218,18 +218,19 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dq(const PackedArgs) 
   store_row<KS>(to, dq, a->scale * inv, wide8(a->q_grad.data, a->q_grad.ts, a->q_grad.hs));
 }
 
-constexpr int kStatAt = 0, kSeenAt = 1024, kRowBytes = 2048;      // of 64 rows (and the 64 behind them, which the same loads bring)
+constexpr int kKeyWaves = 8, kStep = 128;                         // wavefronts of k_packed_dkv, rows that lie in LDS at a time
+constexpr int kStatAt = 0, kSeenAt = 8 * kStep, kRowBytes = 16 * kStep;
 
-// Two wavefronts take 32 of the workgroup's 64 keys each, for the first 32 of 64 rows at a time, two for the others; their sums meet in LDS at the end.
+// Wavefronts take 32 of the workgroup's 64 keys and 32 of 128 rows at a time each; their sums meet in LDS at the end.
 template <int KS, bool OPTIONS>
-__global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dkv(const PackedArgs) {
+__global__ void __launch_bounds__(64 * kKeyWaves, 2) k_packed_dkv(const PackedArgs) {
   using T = Tile<KS>;
-  constexpr int kBuffer = 2 * T::kBytes + kRowBytes;
+  constexpr int kBytes = kStep * T::kPitch, kBuffer = 2 * kBytes + kRowBytes;
   Args a = kernel_args();
   extern __shared__ __attribute__((aligned(1024))) unsigned char shared[];
   float* const s_slope = reinterpret_cast<float*>(shared + 2 * kBuffer);
   float* const s_bad = s_slope + 64;                                              // of each buffer's rows: NaN for those that were not finite, 0
-  int* const s_odd = reinterpret_cast<int*>(s_bad + 2 * kTile);                   // whether any was
+  int* const s_odd = reinterpret_cast<int*>(s_bad + 2 * kStep);                   // whether any was
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
   const int head = blockIdx.x % a->heads;
   Item item;
@@ -249,16 +250,16 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dkv(const PackedArgs)
   load_rows<KS>(kf, a->k.data + key_token * a->k.ts + head * a->k.hs, h);
   load_rows<KS>(vf, a->v.data + key_token * a->v.ts + head * a->v.hs, h);
 
-  // Rows in thirty-twos, 64 of which (`chunk`) a wavefront looks at together; of those any of whose rows sees a key, two by two.
+  // Rows in thirty-twos, 64 of which (`chunk`) a wavefront looks at together; of those any of whose rows sees a key, four by four.
   const int4* const span = a->span + ((((int64_t)item.first * group) >> 7) + item.number) * kWaves;
   const int subs = item.rest ? 0 : (rows + 31) / 32;
-  int next_chunk = a->last ? 0 : (int)((int64_t)k0 * group / 64) * 2, chunk = 0;
+  int next_chunk = a->last ? 0 : (int)((int64_t)k0 * group / kStep) * (kStep / 32), chunk = 0;
   uint64_t active = 0, some = 0, whole = 0, every = 0;
-  struct Rows64 {
+  struct Step {
     int sub;
     bool some, all, every;      // of the wavefront's keys and rows: any are seen, all are; all of the workgroup's
   };
-  auto next = [&](Rows64* x) {
+  auto next = [&](Step* x) {
     while (!active) {
       if (next_chunk >= subs) return false;
       chunk = next_chunk;
@@ -270,14 +271,14 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dkv(const PackedArgs)
       some = __ballot(s.x < key0 + 32 && s.y > key0);
       whole = __ballot(s.z <= key0 && s.w >= key0 + 32);
       every = __ballot(s.z <= k0 && s.w >= k0 + kTile);
-      active = (near | near >> 1) & 0x5555555555555555ull;
+      active = (near | near >> 1 | near >> 2 | near >> 3) & 0x1111111111111111ull;
     }
     const int bit = __builtin_ctzll(active);
     active &= active - 1;
     x->sub = chunk + bit;
     x->some = (some >> (bit + at_rows)) & 1;
     x->all = (whole >> (bit + at_rows)) & 1;
-    x->every = ((every >> bit) & 3) == 3;
+    x->every = ((every >> bit) & 15) == 15;
     return true;
   };
 
@@ -286,7 +287,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dkv(const PackedArgs)
   const float2* const stat0 = a->stat + ((int64_t)head * a->tokens + item.first) * group;
   const int2* const seen0 = a->seen + (int64_t)item.first * group;
   const int q_ts = (int)(a->q.ts * 2), q_hs = (int)(a->q.hs * 2), g_ts = (int)(a->out_grad.ts * 2), g_hs = (int)(a->out_grad.hs * 2);
-  const uint32_t over = (65536 + group - 1) / group;      // n * over >> 16 is n / group for n up to 128, group up to 64
+  const uint32_t over = (65536 + group - 1) / group;      // n * over >> 16 is n / group for n up to 192, group up to 64
   const uint32_t lds = lds_of(shared);
   auto send = [&](int sub, int which) {
     const int row0 = sub * 32, token0 = (int)((uint32_t)row0 / (uint32_t)group), lead = row0 - token0 * group;
@@ -302,10 +303,10 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dkv(const PackedArgs)
       int c = c0 ^ (T::kChunks == 16 ? i & 3 : (i & 1) << 1);
       if (KS * 2 < T::kChunks) c = c < KS * 2 ? c : KS * 2 - 1;
       send16(from_q, to + r0 * T::kPitch, token * q_ts + member * q_hs + c * 16, 0);
-      send16(from_g, to + T::kBytes + r0 * T::kPitch, token * g_ts + member * g_hs + c * 16, 0);
+      send16(from_g, to + kBytes + r0 * T::kPitch, token * g_ts + member * g_hs + c * 16, 0);
     }
-    if (wave == 0) send16(memory_at(stat0 + row0), to + 2 * T::kBytes + kStatAt, me * 16, 0);
-    if (wave == 1) send16(memory_at(seen0 + row0), to + 2 * T::kBytes + kSeenAt, me * 16, 0);
+    if (wave == 0) send16(memory_at(stat0 + row0), to + 2 * kBytes + kStatAt, me * 16, 0);
+    if (wave == 1) send16(memory_at(seen0 + row0), to + 2 * kBytes + kSeenAt, me * 16, 0);
   };
 
   f32x16 dk[T::kTiles], dv[T::kTiles];
@@ -314,7 +315,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dkv(const PackedArgs)
   const float scale = a->scale_log2, cap = a->cap_log2, cap_in = a->cap_in;
   const bool biased = OPTIONS && a->slopes;
 
-  Rows64 now, then;
+  Step now, then;
   bool more = next(&now);
   if (more) send(now.sub, 0);
   for (int which = 0; more; which ^= 1, now = then) {
@@ -325,15 +326,15 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dkv(const PackedArgs)
     bool odd = false;          // (as in k_packed_dq: queries and gradients that are not finite)
     if (!now.every) {
       const int me = lane_anew();
-      const bool bad_q = clear_nonfinite<KS, kTile>(lds + which * kBuffer, wave, me), bad_g = clear_nonfinite<KS, kTile>(lds + which * kBuffer + T::kBytes, wave, me);
+      const bool bad_q = clear_nonfinite<KS, kStep / kKeyWaves>(lds + which * kBuffer, wave, me), bad_g = clear_nonfinite<KS, kStep / kKeyWaves>(lds + which * kBuffer + kBytes, wave, me);
       if (bad_q || bad_g) *s_odd = 1;
-      if ((me & 3) == 0) s_bad[which * kTile + wave * 16 + (me >> 2)] = bad_q || bad_g ? NAN : 0.0f;
+      if ((me & 3) == 0) s_bad[which * kStep + wave * 16 + (me >> 2)] = bad_q || bad_g ? NAN : 0.0f;
       pipeline_barrier();
       odd = *(volatile int*)s_odd;
     }
     if (!now.some) continue;
     const uint32_t sq = lds + which * kBuffer + at_rows * 32 * T::kPitch;           // the gradients lie behind the queries
-    const unsigned char* const s_rows = shared + which * kBuffer + 2 * T::kBytes + at_rows * 32 * 8;
+    const unsigned char* const s_rows = shared + which * kBuffer + 2 * kBytes + at_rows * 32 * 8;
     const int here = lane_anew();
     const uint32_t row_at = sq + T::row_at(here), turned_at = sq + T::turned_at(here);
     const int half = here >> 5;
@@ -341,10 +342,10 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dkv(const PackedArgs)
     // Operands of the queries and, odd ones, of the gradients: 16 rows, 32 entries.
     auto turned = [&](auto i) {
       constexpr int I = decltype(i)::value;
-      return T::template turned<I % 2 * T::kBytes + I / 2 / T::kTiles * 16 * T::kPitch>(turned_at, I / 2 % T::kTiles);
+      return T::template turned<I % 2 * kBytes + I / 2 / T::kTiles * 16 * T::kPitch>(turned_at, I / 2 % T::kTiles);
     };
     f32x16 s = f32x16{}, d = f32x16{};
-    in_turn<2 * KS>([&](auto i) { return T::template rows<decltype(i)::value % 2 * T::kBytes>(row_at, decltype(i)::value / 2); },
+    in_turn<2 * KS>([&](auto i) { return T::template rows<decltype(i)::value % 2 * kBytes>(row_at, decltype(i)::value / 2); },
                     [&](auto i, bf16x8 f) {
                       constexpr int I = decltype(i)::value;
                       if constexpr (I % 2)
@@ -383,7 +384,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dkv(const PackedArgs)
     }
     if (odd) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] += s_bad[which * kTile + at_rows * 32 + row_of(r, half)];
+      for (int r = 0; r < 16; ++r) s[r] += s_bad[which * kStep + at_rows * 32 + row_of(r, half)];
     }
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
@@ -418,41 +419,48 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dkv(const PackedArgs)
   }
 
   __syncthreads();
-  f32x4* const s_sum = reinterpret_cast<f32x4*>(shared) + (wave & 1) * 64 * 8 * T::kTiles + lane;
-  if (wave >= 2) {
+  // The sums of the rows' last two quarters to the first two, then the second's to the first.
 #pragma unroll
-    for (int t = 0; t < T::kTiles; ++t)
+  for (int half = 2; half > 0; half /= 2) {
+    f32x4* const s_sum = reinterpret_cast<f32x4*>(shared) + (wave & (2 * half - 1)) * 64 * 8 * T::kTiles + lane;
+    if (at_rows >= half && at_rows < 2 * half) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        s_sum[(t * 4 + r) * 64] = f32x4{dk[t][4 * r], dk[t][4 * r + 1], dk[t][4 * r + 2], dk[t][4 * r + 3]};
-        s_sum[((T::kTiles + t) * 4 + r) * 64] = f32x4{dv[t][4 * r], dv[t][4 * r + 1], dv[t][4 * r + 2], dv[t][4 * r + 3]};
-      }
+      for (int t = 0; t < T::kTiles; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          s_sum[(t * 4 + r) * 64] = f32x4{dk[t][4 * r], dk[t][4 * r + 1], dk[t][4 * r + 2], dk[t][4 * r + 3]};
+          s_sum[((T::kTiles + t) * 4 + r) * 64] = f32x4{dv[t][4 * r], dv[t][4 * r + 1], dv[t][4 * r + 2], dv[t][4 * r + 3]};
+        }
+    }
+    __syncthreads();
+    if (at_rows < half) {
+#pragma unroll
+      for (int t = 0; t < T::kTiles; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const f32x4 x = s_sum[(t * 4 + r) * 64], y = s_sum[((T::kTiles + t) * 4 + r) * 64];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            dk[t][4 * r + j] += x[j];
+            dv[t][4 * r + j] += y[j];
+          }
+        }
+    }
+    __syncthreads();
   }
-  __syncthreads();
   a = kernel_args();
   if (wave >= 2 || key >= item.count) return;
   const bool k_wide = wide8(a->k_grad.data, a->k_grad.ts, a->k_grad.hs), v_wide = wide8(a->v_grad.data, a->v_grad.ts, a->v_grad.hs);
   bf16_bits* const to_k = a->k_grad.data + key_token * a->k_grad.ts + head * a->k_grad.hs + 4 * h;
   bf16_bits* const to_v = a->v_grad.data + key_token * a->v_grad.ts + head * a->v_grad.hs + 4 * h;
-#pragma unroll
-  for (int t = 0; t < T::kTiles; ++t)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const f32x4 x = s_sum[(t * 4 + r) * 64], y = s_sum[((T::kTiles + t) * 4 + r) * 64];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        dk[t][4 * r + j] += x[j];
-        dv[t][4 * r + j] += y[j];
-      }
-    }
   store_row<KS>(to_k, dk, a->scale, k_wide);
   store_row<KS>(to_v, dv, 1.0f, v_wide);
 }
 
 template <int KS, bool OPTIONS>
 hipError_t launch(const PackedArgs& a, hipStream_t s) {
-  constexpr int kDq = 4 * kKeys * Tile<KS>::kPitch + kWaves * KS * 1024 + 2 * kKeys * 4 + 16, kDkv = 2 * (2 * Tile<KS>::kBytes + kRowBytes) + 256 + 2 * kTile * 4 + 16;
-  static_assert(2 * 64 * 8 * Tile<KS>::kTiles * 16 <= kDkv, "sums meet where the tiles were");
+  constexpr int kDq = 4 * kKeys * Tile<KS>::kPitch + kWaves * KS * 1024 + 2 * kKeys * 4 + 16, kDkv = 2 * (2 * kStep * Tile<KS>::kPitch + kRowBytes) + 256 + 2 * kStep * 4 + 16;
+  static_assert(4 * 64 * 8 * Tile<KS>::kTiles * 16 <= kDkv, "sums meet where the tiles were");
   static PerDeviceOnce once;
   hipError_t e = once.run([] {
     const hipError_t x = hipFuncSetAttribute(reinterpret_cast<const void*>(k_packed_dq<KS, OPTIONS>), hipFuncAttributeMaxDynamicSharedMemorySize, kDq);
@@ -462,7 +470,7 @@ hipError_t launch(const PackedArgs& a, hipStream_t s) {
   k_packed_dq<KS, OPTIONS><<<dim3((uint32_t)(row_items(a) * a.heads)), 64 * kWaves, kDq, s>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  k_packed_dkv<KS, OPTIONS><<<dim3((uint32_t)(key_items(a) * a.heads)), 64 * kWaves, kDkv, s>>>(a);
+  k_packed_dkv<KS, OPTIONS><<<dim3((uint32_t)(key_items(a) * a.heads)), 64 * kKeyWaves, kDkv, s>>>(a);
   return hipGetLastError();
 }
 
