@@ -36,7 +36,8 @@ struct PackedArgs {
   int rest;                  // rows of no sequence are written, too: zeros
   float scale, scale_log2, cap_log2, cap_in;       // cap_log2 = cap log2 e (0: none), cap_in = 2 log2 e scale / cap
   // Of the backward pass.  Rows are numbered token * group + query head of the key head.
-  float2* stat;              // [key head][row] logarithm (base 2) of the row's sum (+inf: there is none), sum over its gradient times its result
+  float2* stat;              // [key head][row] logarithm (base 2) of the row's sum (+inf: there is none), sum over its gradient times its result; with a cap or
+                             // slopes four floats: the row's slope (base 2) and token behind them
   int2* seen;                // [row] first key and last + 1
   int4* span;                // [32 rows of an item] lowest first, highest last, highest first, lowest last (a row that sees nothing: highest first is INT_MAX)
 };

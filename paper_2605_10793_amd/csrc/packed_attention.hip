@@ -270,7 +270,8 @@ struct BackwardSizes {
 BackwardSizes backward_sizes(const conqur_attention_call& c) {
   auto up = [](uint64_t n) { return (n + 255) / 256 * 256; };
   const uint64_t rows = c.tokens * (c.q.heads / c.k.heads);      // (loads of 64 rows' may reach 128 rows behind the last)
-  return {up((rows * c.k.heads + 128) * sizeof(float2)), up((rows + 128) * sizeof(int2)), up((rows / kRows + c.sequences + 2) * kWaves * sizeof(int4))};
+  const uint64_t stat = c.cap != 0.0f || c.slopes ? sizeof(float4) : sizeof(float2);
+  return {up((rows * c.k.heads + 128) * stat), up((rows + 128) * sizeof(int2)), up((rows / kRows + c.sequences + 2) * kWaves * sizeof(int4))};
 }
 
 PackedArgs args_of(const conqur_attention_call& c) {

@@ -21,14 +21,18 @@ __device__ __forceinline__ bf16x8 pack8(const f32x16& x, int k) {
 
 constexpr int kKeys = 32;          // keys that lie in LDS at a time for k_packed_dq
 
+// Operands that each lane keeps in LDS because its registers are full: what goes to scratch memory instead comes back behind all that is on its way to LDS.
+constexpr int queries_in_lds(int steps) { return steps == 8 ? 3 : 0; }
+constexpr int keys_in_lds(int steps) { return steps == 8 ? 4 : 0; }
+
 template <int KS, bool OPTIONS>
 __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dq(const PackedArgs) {
   using T = Tile<KS>;
-  constexpr int kBytes = kKeys * T::kPitch, kBuffer = 2 * kBytes;
+  constexpr int kBytes = kKeys * T::kPitch, kBuffer = 2 * kBytes, kQueriesInLds = queries_in_lds(KS), kOwn = (KS + kQueriesInLds) * 1024;
   Args a = kernel_args();
   extern __shared__ __attribute__((aligned(1024))) unsigned char shared[];
-  unsigned char* const s_grad = shared + 2 * kBuffer;                                             // the wavefronts' operands of the gradient, each lane's own
-  float* const s_bad = reinterpret_cast<float*>(s_grad + kWaves * KS * 1024);                     // of each buffer's keys: NaN for those that were not finite, 0
+  unsigned char* const s_grad = shared + 2 * kBuffer;                                             // the wavefronts' operands of the gradient, and some of the queries
+  float* const s_bad = reinterpret_cast<float*>(s_grad + kWaves * kOwn);                          // of each buffer's keys: NaN for those that were not finite, 0
   int* const s_odd = reinterpret_cast<int*>(s_bad + 2 * kKeys);                                   // whether any was
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
   const int head = blockIdx.x % a->heads;
@@ -61,7 +65,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dq(const PackedArgs) 
   const int64_t row_token = item.first + token;
   const int q_head = head * group + (row < rows ? row : rows - 1) - token * group;
   float dot = 0.0f, lse = INFINITY;
-  u32x4* const own_grad = reinterpret_cast<u32x4*>(s_grad + wave * KS * 1024) + lane;
+  u32x4* const own_grad = reinterpret_cast<u32x4*>(s_grad + wave * kOwn) + lane;
   {
     bf16x8 gf[KS];
     load_rows<KS>(gf, a->out_grad.data + row_token * a->out_grad.ts + q_head * a->out_grad.hs, h);
@@ -79,13 +83,21 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dq(const PackedArgs) 
     }
   }
   dot = halves(dot, [](float x, float y) { return x + y; });
-  bf16x8 qf[KS];
-  load_rows<KS>(qf, a->q.data + row_token * a->q.ts + q_head * a->q.hs, h);
+  bf16x8 qf[KS - kQueriesInLds];
+#pragma unroll
+  for (int i = 0; i < KS; ++i) {
+    const bf16x8 x = *reinterpret_cast<const bf16x8*>(a->q.data + row_token * a->q.ts + q_head * a->q.hs + 16 * i + 8 * h);
+    if (i < kQueriesInLds)
+      own_grad[(KS + i) * 64] = __builtin_bit_cast(u32x4, x);
+    else
+      qf[i - kQueriesInLds] = x;
+  }
 
   const int k_stride = (int)(a->k.ts * 2), v_stride = (int)(a->v.ts * 2);
   const bf16_bits* const k0 = a->k.data + (int64_t)item.first * a->k.ts + head * a->k.hs;
   const bf16_bits* const v0 = a->v.data + (int64_t)item.first * a->v.ts + head * a->v.hs;
   const uint32_t lds = lds_of(shared), own_lds = lds_of(own_grad);
+  auto own = [&](auto i) { return *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)(own_lds + decltype(i)::value * 1024); };
   auto send = [&](int kb, int which) {
     send_tile<KS, kKeys>(k0 + (int64_t)kb * a->k.ts, k_stride, item.count - kb, lds + which * kBuffer, wave);
     send_tile<KS, kKeys>(v0 + (int64_t)kb * a->v.ts, v_stride, item.count - kb, lds + which * kBuffer + kBytes, wave);
@@ -126,67 +138,65 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dq(const PackedArgs) 
     const int here = lane_anew();
     const uint32_t row_at = sk + T::row_at(here), turned_at = sk + T::turned_at(here);
     struct Operands {
-      bf16x8 k, v, g;
+      bf16x8 rows, mine;
     };
     f32x16 s = f32x16{}, d = f32x16{};
-    in_turn<KS, 2>(
+    in_turn<2 * KS, 3>(
         [&](auto i) {
-          constexpr int I = decltype(i)::value;
-          return Operands{T::template rows<0>(row_at, I), T::template rows<kBytes>(row_at, I),
-                          *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)(own_lds + I * 1024)};
+          constexpr int I = decltype(i)::value / 2;
+          if constexpr (decltype(i)::value % 2)
+            return Operands{T::template rows<kBytes>(row_at, I), own(std::integral_constant<int, I>{})};
+          else if constexpr (I < kQueriesInLds)
+            return Operands{T::template rows<0>(row_at, I), own(std::integral_constant<int, KS + I>{})};
+          else
+            return Operands{T::template rows<0>(row_at, I), qf[I - kQueriesInLds]};
         },
         [&](auto i, const Operands& f) {
-          s = mfma32(f.k, qf[decltype(i)::value], s);
-          d = mfma32(f.v, f.g, d);
+          if constexpr (decltype(i)::value % 2)
+            d = mfma32(f.rows, f.mine, d);
+          else
+            s = mfma32(f.rows, f.mine, s);
         });
-    float near[OPTIONS ? 16 : 1];
-    if (OPTIONS && cap != 0.0f) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        float x;
-        s[r] = capped(s[r], cap, cap_in, &x) - lse;
-        near[r] = 4.0f * (x - x * x);
-      }
-    } else {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], scale, -lse);
-    }
-    if (OPTIONS && slope != 0.0f) {
-      const float at = (float)(token - kb - 4 * h);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = fmaf(-slope, fabsf(at - (float)row_of(r, 0)), s[r]);
-    }
     if (odd) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] += s_bad[which * kKeys + row_of(r, h)];
     }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      s[r] = __builtin_amdgcn_exp2f(s[r]);
-      d[r] = (d[r] - dot) * s[r];
-    }
-    if (!all) {
-      const int lo = mine.x - kb - 4 * h, hi = mine.y - kb - 4 * h;
+    const int lo = mine.x - kb - 4 * h, hi = mine.y - kb - 4 * h;
+    const float at = (float)(token - kb - 4 * h);
+    // The factors of an entry at a time, so that nothing but they stays in registers.
+    auto factors = [&](auto all_seen, auto caps) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const bool see = row_of(r, 0) >= lo && row_of(r, 0) < hi;
-        s[r] = see ? s[r] : 0.0f;
-        d[r] = see ? d[r] : 0.0f;
-        if constexpr (OPTIONS) near[r] = see ? near[r] : 0.0f;
+        float x = 0.0f, y;
+        if constexpr (decltype(caps)::value)
+          y = capped(s[r], cap, cap_in, &x) - lse;
+        else
+          y = fmaf(s[r], scale, -lse);
+        if constexpr (OPTIONS) y = fmaf(-slope, fabsf(at - (float)row_of(r, 0)), y);
+        float p = __builtin_amdgcn_exp2f(y), e = (d[r] - dot) * p;
+        if constexpr (!decltype(all_seen)::value) {
+          const uint32_t see = -(uint32_t)((row_of(r, 0) >= lo) & (row_of(r, 0) < hi));
+          p = __uint_as_float(__float_as_uint(p) & see);
+          e = __uint_as_float(__float_as_uint(e) & see);
+          if constexpr (decltype(caps)::value) x = __uint_as_float(__float_as_uint(x) & see);
+        }
+        sum += p;
+        off += e;
+        if constexpr (decltype(caps)::value) {
+          x = 4.0f * (x - x * x);
+          p *= x;
+          e *= x;
+        }
+        s[r] = p;
+        d[r] = e;
       }
-    }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      sum += s[r];
-      off += d[r];
-    }
-    if (OPTIONS && cap != 0.0f) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        s[r] *= near[r];
-        d[r] *= near[r];
-      }
-    }
+    };
+    if (OPTIONS && cap != 0.0f)
+      factors(std::false_type{}, std::true_type{});
+    else if (all)
+      factors(std::true_type{}, std::false_type{});
+    else
+      factors(std::false_type{}, std::false_type{});
     const bf16x8 pf[2] = {pack8(s, 0), pack8(s, 1)}, df[2] = {pack8(d, 0), pack8(d, 1)};
 #pragma unroll
     for (int r = 0; r < 16; ++r) d[r] -= (float)df[r / 8][r % 8];
@@ -209,7 +219,12 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dq(const PackedArgs) 
   if (row >= rows) return;
   if (h == 0) {
     const int64_t at = (int64_t)item.first * group + row;
-    a->stat[(int64_t)head * a->tokens * group + at] = make_float2(sum == 0.0f ? INFINITY : lse + __builtin_amdgcn_logf(sum), dot + off);
+    const float2 stat = make_float2(sum == 0.0f ? INFINITY : lse + __builtin_amdgcn_logf(sum), dot + off);
+    const int64_t to = (int64_t)head * a->tokens * group + at;
+    if constexpr (OPTIONS)
+      reinterpret_cast<float4*>(a->stat)[to] = make_float4(stat.x, stat.y, slope, (float)token);
+    else
+      a->stat[to] = stat;
     if (head == 0) a->seen[at] = mine;
   }
   bf16_bits* const to = a->q_grad.data + row_token * a->q_grad.ts + q_head * a->q_grad.hs + 4 * h;
@@ -218,18 +233,30 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dq(const PackedArgs) 
   store_row<KS>(to, dq, a->scale * inv, wide8(a->q_grad.data, a->q_grad.ts, a->q_grad.hs));
 }
 
-constexpr int kKeyWaves = 8, kStep = 128;                         // wavefronts of k_packed_dkv, rows that lie in LDS at a time
-constexpr int kStatAt = 0, kSeenAt = 8 * kStep, kRowBytes = 16 * kStep;
+// Eight wavefronts, which take 32 of the workgroup's 64 keys and 32 of 128 rows at a time each; their sums meet in LDS at the end.  (Four, two workgroups to a
+// compute unit: 274 us for 193, two sequences of 2048 tokens.  A workgroup's time is what the rows of its keys take one after the other, and the first keys' rows
+// are all there are.)
+constexpr int kKeyWaves = 8, kStep = 16 * kKeyWaves;                  // kStep: rows that lie in LDS at a time
+template <int KS, bool OPTIONS>
+struct KeySide {
+  static constexpr int kBytes = kStep * Tile<KS>::kPitch;             // of their queries, and of their gradients
+  static constexpr int kStat = OPTIONS ? 16 : 8;                      // of a row: lse, D; slope, token
+  static constexpr int kSeenAt = kStep * kStat;
+  static constexpr int kBuffer = 2 * kBytes + kSeenAt + kStep * 8;
+  static constexpr int kKeysAt = 2 * kBuffer;                         // operands of the keys
+  static constexpr int kBadAt = kKeysAt + 2 * keys_in_lds(KS) * 1024;
+  static constexpr int kShared = kBadAt + 2 * kStep * 4 + 16;
+  static_assert(kKeyWaves / 2 * 64 * 8 * Tile<KS>::kTiles * 16 <= kShared, "sums meet where the tiles were");
+};
 
-// Wavefronts take 32 of the workgroup's 64 keys and 32 of 128 rows at a time each; their sums meet in LDS at the end.
 template <int KS, bool OPTIONS>
 __global__ void __launch_bounds__(64 * kKeyWaves, 2) k_packed_dkv(const PackedArgs) {
   using T = Tile<KS>;
-  constexpr int kBytes = kStep * T::kPitch, kBuffer = 2 * kBytes + kRowBytes;
+  using D = KeySide<KS, OPTIONS>;
+  constexpr int kBytes = D::kBytes, kBuffer = D::kBuffer, kStat = D::kStat, kSeenAt = D::kSeenAt;
   Args a = kernel_args();
   extern __shared__ __attribute__((aligned(1024))) unsigned char shared[];
-  float* const s_slope = reinterpret_cast<float*>(shared + 2 * kBuffer);
-  float* const s_bad = s_slope + 64;                                              // of each buffer's rows: NaN for those that were not finite, 0
+  float* const s_bad = reinterpret_cast<float*>(shared + D::kBadAt);              // of each buffer's rows: NaN for those that were not finite, 0
   int* const s_odd = reinterpret_cast<int*>(s_bad + 2 * kStep);                   // whether any was
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
   const int head = blockIdx.x % a->heads;
@@ -240,15 +267,20 @@ __global__ void __launch_bounds__(64 * kKeyWaves, 2) k_packed_dkv(const PackedAr
   const int k0 = item.part * kTile, key0 = k0 + 32 * (wave & 1), at_rows = wave >> 1;      // keys of the workgroup, of the wavefront; which 32 rows
   const int key = key0 + (lane & 31);
   const int64_t key_token = item.first + (key < item.count ? key : item.count - 1);
-  if (OPTIONS) {
-    if (a->slopes && (int)threadIdx.x < group) s_slope[threadIdx.x] = a->slopes[head * group + threadIdx.x] * kLog2e;
-    __syncthreads();
-  }
-
   if (threadIdx.x == 0) *s_odd = 0;
-  bf16x8 kf[KS], vf[KS];
-  load_rows<KS>(kf, a->k.data + key_token * a->k.ts + head * a->k.hs, h);
+  constexpr int kKeysInLds = keys_in_lds(KS);
+  bf16x8 kf[KS - kKeysInLds], vf[KS];
+  u32x4* const own_keys = reinterpret_cast<u32x4*>(shared + D::kKeysAt + (wave & 1) * kKeysInLds * 1024) + lane;      // (all wavefronts of 32 keys write the same)
+#pragma unroll
+  for (int i = 0; i < KS; ++i) {
+    const bf16x8 x = *reinterpret_cast<const bf16x8*>(a->k.data + key_token * a->k.ts + head * a->k.hs + 16 * i + 8 * h);
+    if (i < kKeysInLds)
+      own_keys[i * 64] = __builtin_bit_cast(u32x4, x);
+    else
+      kf[i - kKeysInLds] = x;
+  }
   load_rows<KS>(vf, a->v.data + key_token * a->v.ts + head * a->v.hs, h);
+  const uint32_t keys_lds = lds_of(own_keys);
 
   // Rows in thirty-twos, 64 of which (`chunk`) a wavefront looks at together; of those any of whose rows sees a key, four by four.
   const int4* const span = a->span + ((((int64_t)item.first * group) >> 7) + item.number) * kWaves;
@@ -278,13 +310,13 @@ __global__ void __launch_bounds__(64 * kKeyWaves, 2) k_packed_dkv(const PackedAr
     x->sub = chunk + bit;
     x->some = (some >> (bit + at_rows)) & 1;
     x->all = (whole >> (bit + at_rows)) & 1;
-    x->every = ((every >> bit) & 15) == 15;
+    x->every = ((every >> bit) & ((1 << kStep / 32) - 1)) == (1 << kStep / 32) - 1;
     return true;
   };
 
   const bf16_bits* const q0 = a->q.data + (int64_t)item.first * a->q.ts + (int64_t)head * group * a->q.hs;
   const bf16_bits* const g0 = a->out_grad.data + (int64_t)item.first * a->out_grad.ts + (int64_t)head * group * a->out_grad.hs;
-  const float2* const stat0 = a->stat + ((int64_t)head * a->tokens + item.first) * group;
+  const unsigned char* const stat0 = reinterpret_cast<const unsigned char*>(a->stat) + ((int64_t)head * a->tokens + item.first) * group * kStat;
   const int2* const seen0 = a->seen + (int64_t)item.first * group;
   const int q_ts = (int)(a->q.ts * 2), q_hs = (int)(a->q.hs * 2), g_ts = (int)(a->out_grad.ts * 2), g_hs = (int)(a->out_grad.hs * 2);
   const uint32_t over = (65536 + group - 1) / group;      // n * over >> 16 is n / group for n up to 192, group up to 64
@@ -305,28 +337,28 @@ __global__ void __launch_bounds__(64 * kKeyWaves, 2) k_packed_dkv(const PackedAr
       send16(from_q, to + r0 * T::kPitch, token * q_ts + member * q_hs + c * 16, 0);
       send16(from_g, to + kBytes + r0 * T::kPitch, token * g_ts + member * g_hs + c * 16, 0);
     }
-    if (wave == 0) send16(memory_at(stat0 + row0), to + 2 * kBytes + kStatAt, me * 16, 0);
-    if (wave == 1) send16(memory_at(seen0 + row0), to + 2 * kBytes + kSeenAt, me * 16, 0);
+    if (wave < kStat / 8) send16(memory_at(stat0 + (int64_t)row0 * kStat), to + 2 * kBytes + wave * 1024, wave * 1024 + me * 16, 0);
+    if (wave == 2) send16(memory_at(seen0 + row0), to + 2 * kBytes + kSeenAt, me * 16, 0);
   };
 
   f32x16 dk[T::kTiles], dv[T::kTiles];
 #pragma unroll
   for (int t = 0; t < T::kTiles; ++t) dk[t] = dv[t] = f32x16{};
   const float scale = a->scale_log2, cap = a->cap_log2, cap_in = a->cap_in;
-  const bool biased = OPTIONS && a->slopes;
+  const float place = (float)key;
 
   Step now, then;
   bool more = next(&now);
   if (more) send(now.sub, 0);
   for (int which = 0; more; which ^= 1, now = then) {
+    more = next(&then);
     wait_loads<0>();
     pipeline_barrier();
-    more = next(&then);
     if (more) send(then.sub, which ^ 1);
     bool odd = false;          // (as in k_packed_dq: queries and gradients that are not finite)
     if (!now.every) {
       const int me = lane_anew();
-      const bool bad_q = clear_nonfinite<KS, kStep / kKeyWaves>(lds + which * kBuffer, wave, me), bad_g = clear_nonfinite<KS, kStep / kKeyWaves>(lds + which * kBuffer + kBytes, wave, me);
+      const bool bad_q = clear_nonfinite<KS, 16>(lds + which * kBuffer, wave, me), bad_g = clear_nonfinite<KS, 16>(lds + which * kBuffer + kBytes, wave, me);
       if (bad_q || bad_g) *s_odd = 1;
       if ((me & 3) == 0) s_bad[which * kStep + wave * 16 + (me >> 2)] = bad_q || bad_g ? NAN : 0.0f;
       pipeline_barrier();
@@ -334,7 +366,7 @@ __global__ void __launch_bounds__(64 * kKeyWaves, 2) k_packed_dkv(const PackedAr
     }
     if (!now.some) continue;
     const uint32_t sq = lds + which * kBuffer + at_rows * 32 * T::kPitch;           // the gradients lie behind the queries
-    const unsigned char* const s_rows = shared + which * kBuffer + 2 * kBytes + at_rows * 32 * 8;
+    const unsigned char* const s_rows = shared + which * kBuffer + 2 * kBytes;
     const int here = lane_anew();
     const uint32_t row_at = sq + T::row_at(here), turned_at = sq + T::turned_at(here);
     const int half = here >> 5;
@@ -345,58 +377,63 @@ __global__ void __launch_bounds__(64 * kKeyWaves, 2) k_packed_dkv(const PackedAr
       return T::template turned<I % 2 * kBytes + I / 2 / T::kTiles * 16 * T::kPitch>(turned_at, I / 2 % T::kTiles);
     };
     f32x16 s = f32x16{}, d = f32x16{};
-    in_turn<2 * KS>([&](auto i) { return T::template rows<decltype(i)::value % 2 * kBytes>(row_at, decltype(i)::value / 2); },
-                    [&](auto i, bf16x8 f) {
-                      constexpr int I = decltype(i)::value;
-                      if constexpr (I % 2)
-                        d = mfma32(f, vf[I / 2], d);
-                      else
-                        s = mfma32(f, kf[I / 2], s);
-                    });
-#pragma unroll
-    for (int r4 = 0; r4 < 4; ++r4) {
-      const f32x4* const at = reinterpret_cast<const f32x4*>(s_rows + kStatAt + (8 * r4 + 4 * half) * 8);
-      const f32x4 x = at[0], y = at[1];
-      const float lse[4] = {x[0], x[2], y[0], y[2]}, dot[4] = {x[1], x[3], y[1], y[3]};
-      if (OPTIONS && cap != 0.0f) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float z;
-          s[4 * r4 + j] = capped(s[4 * r4 + j], cap, cap_in, &z) - lse[j];
-          d[4 * r4 + j] = (d[4 * r4 + j] - dot[j]) * (4.0f * (z - z * z));
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          s[4 * r4 + j] = fmaf(s[4 * r4 + j], scale, -lse[j]);
-          d[4 * r4 + j] -= dot[j];
-        }
-      }
-    }
-    if (biased) {
-      const int row0 = (now.sub + at_rows) * 32, token0 = (int)((uint32_t)row0 / (uint32_t)group), lead = row0 - token0 * group + 4 * half;
-      const float away = (float)(token0 - key);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int n = lead + row_of(r, 0), token = (int)(((uint32_t)n * over) >> 16);
-        s[r] = fmaf(-s_slope[n - token * group], fabsf(away + (float)token), s[r]);
-      }
-    }
+    struct Operands {
+      bf16x8 rows, keys;
+    };
+    in_turn<2 * KS>(
+        [&](auto i) {
+          constexpr int I = decltype(i)::value / 2;
+          if constexpr (decltype(i)::value % 2)
+            return Operands{T::template rows<kBytes>(row_at, I), vf[I]};
+          else if constexpr (I < kKeysInLds)
+            return Operands{T::template rows<0>(row_at, I), *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)(keys_lds + I * 1024)};
+          else
+            return Operands{T::template rows<0>(row_at, I), kf[I - kKeysInLds]};
+        },
+        [&](auto i, const Operands& f) {
+          if constexpr (decltype(i)::value % 2)
+            d = mfma32(f.rows, f.keys, d);
+          else
+            s = mfma32(f.rows, f.keys, s);
+        });
     if (odd) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] += s_bad[which * kStep + at_rows * 32 + row_of(r, half)];
     }
+    auto factors = [&](auto caps) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      s[r] = __builtin_amdgcn_exp2f(s[r]);
-      d[r] *= s[r];
-    }
+      for (int r = 0; r < 16; ++r) {
+        float lse, dot, slope = 0.0f, token = 0.0f;
+        if constexpr (OPTIONS) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(s_rows + (at_rows * 32 + row_of(r, half)) * kStat);
+          lse = x[0], dot = x[1], slope = x[2], token = x[3];
+        } else {
+          const f32x2 x = *reinterpret_cast<const f32x2*>(s_rows + (at_rows * 32 + row_of(r, half)) * kStat);
+          lse = x[0], dot = x[1];
+        }
+        float x = 0.0f, y;
+        if constexpr (decltype(caps)::value)
+          y = capped(s[r], cap, cap_in, &x) - lse;
+        else
+          y = fmaf(s[r], scale, -lse);
+        if constexpr (OPTIONS) y = fmaf(-slope, fabsf(token - place), y);
+        const float p = __builtin_amdgcn_exp2f(y);
+        float e = (d[r] - dot) * p;
+        if constexpr (decltype(caps)::value) e *= 4.0f * (x - x * x);
+        s[r] = p;
+        d[r] = e;
+      }
+    };
+    if (OPTIONS && cap != 0.0f)
+      factors(std::true_type{});
+    else
+      factors(std::false_type{});
     if (!now.all) {
       const int left = rows - (now.sub + at_rows) * 32 - 4 * half;
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
         typedef int i32x4 __attribute__((ext_vector_type(4)));
-        const i32x4* const at = reinterpret_cast<const i32x4*>(s_rows + kSeenAt + (8 * r4 + 4 * half) * 8);
+        const i32x4* const at = reinterpret_cast<const i32x4*>(s_rows + kSeenAt + (at_rows * 32 + 8 * r4 + 4 * half) * 8);
         const i32x4 x = at[0], y = at[1];
         const int lo[4] = {x[0], x[2], y[0], y[2]}, hi[4] = {x[1], x[3], y[1], y[3]};
 #pragma unroll
@@ -419,9 +456,9 @@ __global__ void __launch_bounds__(64 * kKeyWaves, 2) k_packed_dkv(const PackedAr
   }
 
   __syncthreads();
-  // The sums of the rows' last two quarters to the first two, then the second's to the first.
+  // The sums of the last rows' wavefronts to the first ones'.
 #pragma unroll
-  for (int half = 2; half > 0; half /= 2) {
+  for (int half = kKeyWaves / 4; half > 0; half /= 2) {
     f32x4* const s_sum = reinterpret_cast<f32x4*>(shared) + (wave & (2 * half - 1)) * 64 * 8 * T::kTiles + lane;
     if (at_rows >= half && at_rows < 2 * half) {
 #pragma unroll
@@ -459,8 +496,7 @@ __global__ void __launch_bounds__(64 * kKeyWaves, 2) k_packed_dkv(const PackedAr
 
 template <int KS, bool OPTIONS>
 hipError_t launch(const PackedArgs& a, hipStream_t s) {
-  constexpr int kDq = 4 * kKeys * Tile<KS>::kPitch + kWaves * KS * 1024 + 2 * kKeys * 4 + 16, kDkv = 2 * (2 * kStep * Tile<KS>::kPitch + kRowBytes) + 256 + 2 * kStep * 4 + 16;
-  static_assert(4 * 64 * 8 * Tile<KS>::kTiles * 16 <= kDkv, "sums meet where the tiles were");
+  constexpr int kDq = 4 * kKeys * Tile<KS>::kPitch + kWaves * (KS + queries_in_lds(KS)) * 1024 + 2 * kKeys * 4 + 16, kDkv = KeySide<KS, OPTIONS>::kShared;
   static PerDeviceOnce once;
   hipError_t e = once.run([] {
     const hipError_t x = hipFuncSetAttribute(reinterpret_cast<const void*>(k_packed_dq<KS, OPTIONS>), hipFuncAttributeMaxDynamicSharedMemorySize, kDq);
