@@ -14,11 +14,11 @@ using namespace conqur::tree;
 namespace {
 
 // Sixteens of rows that a wavefront takes straight from memory (more would not fit its registers).
-constexpr int few_tiles(int bits, int width, int kind) { return bits == 16 || (bits == 8 && width == 128 && kind == kOptions) ? 1 : 2; }
+constexpr int few_tiles(int bits, int width, bool options) { return bits == 16 || (bits == 8 && width == 128 && options) ? 1 : 2; }
 
 template <int BITS, int W, int KIND>
 hipError_t launch(const TreeArgs& a, int qt, dim3 grid, hipStream_t s) {
-  constexpr int kMostTiles = few_tiles(BITS, W, KIND);
+  constexpr int kMostTiles = few_tiles(BITS, W, KIND == kOptions);
   const bool one_page = a.cache.page_tokens >= (uint32_t)kBlock;
   if (qt == 1 && one_page)
     k_tree<BITS, W, 1, true, KIND><<<grid, 64 * kWaves, 0, s>>>(a);
@@ -48,12 +48,15 @@ Plan plan_of(const conqur_chunk_call& c) {
   const int64_t room = (int64_t)c.batch.table_columns * c.cache.page_tokens;
   p.context = (int64_t)(c.max_context < (uint64_t)room ? c.max_context : (uint64_t)room);
   const int64_t rows = (int64_t)c.max_query * (c.q.heads / c.cache.heads);
-  p.wide = rows > 16 * few_tiles((int)c.cache.bits, (int)c.cache.width, c.cap != 0.0f || c.slopes ? kOptions : kChunk);
-  p.qt = rows <= 16 ? 1 : 2;
+  // (17 to 32 rows of codes take two tiles of 16 where one of 32 does not fit: 28 rows of 8 bits with a bias 104 us, in the kernel of many rows 317.)
+  p.wide = rows > (c.cache.bits == 16 ? 16 : 32);
+  p.qt = rows <= 16 ? 1 : few_tiles((int)c.cache.bits, (int)c.cache.width, c.cap != 0.0f || c.slopes);
   if (p.wide) {
+    // Rows of a wavefront in sixteens: as few as pad the rows least, but for more than three full wavefronts' all that its registers hold (3108 rows of 8 bits: 16 a
+    // wavefront 1433 us, 32 990, 48 870).
     const int most = c.cache.bits == 16 && c.cache.width == 128 ? 2 : 3;
     int64_t least = 1ll << 62;
-    for (int qt = 1; qt <= most; ++qt) {
+    for (int qt = rows > 192 ? most : 1; qt <= most; ++qt) {
       const int64_t padded = (rows + 64 * qt - 1) / (64 * qt) * qt;
       if (padded <= least) {
         least = padded;
@@ -66,8 +69,18 @@ Plan plan_of(const conqur_chunk_call& c) {
   const int64_t groups = (int64_t)c.cache.heads * p.row_tiles, sequences = c.batch.sequences;
   const int64_t blocks = p.context > kBlock ? (p.context + kBlock - 1) / kBlock : 1;
   p.min_blocks = kWaves;
-  int64_t splits = kSlots / groups;
+  // As many runs as fill the device, or a few times that: the smallest number whose last turn leaves less than a tenth of it idle (17 tiles of 8 heads, 30011
+  // tokens in 8 bits: 3 runs 870 us with 408 workgroups, 7 runs 650).
   const int64_t most = (blocks * sequences + p.min_blocks - 1) / p.min_blocks;
+  int64_t splits = kSlots / groups < 1 ? 1 : kSlots / groups;
+  for (int64_t s = splits, least = 0; s <= 16; ++s) {
+    const int64_t share = 1000 * groups * s / ((groups * s + kSlots - 1) / kSlots * kSlots);
+    if (share > least) {
+      least = share;
+      splits = s;
+    }
+    if (share >= 900) break;
+  }
   if (splits > most) splits = most;
   if (splits > kMaxSplits) splits = kMaxSplits;
   if (splits < 1) splits = 1;

@@ -19,13 +19,14 @@ __device__ __forceinline__ bf16x8 pack8(const f32x16& x, int k) {
                  f32x2_to_bf16x2(x[8 * k + 6], x[8 * k + 7]));
 }
 
+enum { kBiased = 1, kCapped = 2 };      // OPTIONS: a bias by distance; capped scores, with or without it
 constexpr int kKeys = 32;          // keys that lie in LDS at a time for k_packed_dq
 
 // Operands that each lane keeps in LDS because its registers are full: what goes to scratch memory instead comes back behind all that is on its way to LDS.
 constexpr int queries_in_lds(int steps) { return steps == 8 ? 3 : 0; }
 constexpr int keys_in_lds(int steps) { return steps == 8 ? 4 : 0; }
 
-template <int KS, bool OPTIONS>
+template <int KS, int OPTIONS>
 __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dq(const PackedArgs) {
   using T = Tile<KS>;
   constexpr int kBytes = kKeys * T::kPitch, kBuffer = 2 * kBytes, kQueriesInLds = queries_in_lds(KS), kOwn = (KS + kQueriesInLds) * 1024;
@@ -191,7 +192,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dq(const PackedArgs) 
         d[r] = e;
       }
     };
-    if (OPTIONS && cap != 0.0f)
+    if constexpr (OPTIONS == kCapped)
       factors(std::false_type{}, std::true_type{});
     else if (all)
       factors(std::true_type{}, std::false_type{});
@@ -237,7 +238,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dq(const PackedArgs) 
 // compute unit: 274 us for 193, two sequences of 2048 tokens.  A workgroup's time is what the rows of its keys take one after the other, and the first keys' rows
 // are all there are.)
 constexpr int kKeyWaves = 8, kStep = 16 * kKeyWaves;                  // kStep: rows that lie in LDS at a time
-template <int KS, bool OPTIONS>
+template <int KS, int OPTIONS>
 struct KeySide {
   static constexpr int kBytes = kStep * Tile<KS>::kPitch;             // of their queries, and of their gradients
   static constexpr int kStat = OPTIONS ? 16 : 8;                      // of a row: lse, D; slope, token
@@ -249,7 +250,7 @@ struct KeySide {
   static_assert(kKeyWaves / 2 * 64 * 8 * Tile<KS>::kTiles * 16 <= kShared, "sums meet where the tiles were");
 };
 
-template <int KS, bool OPTIONS>
+template <int KS, int OPTIONS>
 __global__ void __launch_bounds__(64 * kKeyWaves, 2) k_packed_dkv(const PackedArgs) {
   using T = Tile<KS>;
   using D = KeySide<KS, OPTIONS>;
@@ -400,7 +401,7 @@ __global__ void __launch_bounds__(64 * kKeyWaves, 2) k_packed_dkv(const PackedAr
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] += s_bad[which * kStep + at_rows * 32 + row_of(r, half)];
     }
-    auto factors = [&](auto caps) {
+    {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         float lse, dot, slope = 0.0f, token = 0.0f;
@@ -412,22 +413,18 @@ __global__ void __launch_bounds__(64 * kKeyWaves, 2) k_packed_dkv(const PackedAr
           lse = x[0], dot = x[1];
         }
         float x = 0.0f, y;
-        if constexpr (decltype(caps)::value)
+        if constexpr (OPTIONS == kCapped)
           y = capped(s[r], cap, cap_in, &x) - lse;
         else
           y = fmaf(s[r], scale, -lse);
         if constexpr (OPTIONS) y = fmaf(-slope, fabsf(token - place), y);
         const float p = __builtin_amdgcn_exp2f(y);
         float e = (d[r] - dot) * p;
-        if constexpr (decltype(caps)::value) e *= 4.0f * (x - x * x);
+        if constexpr (OPTIONS == kCapped) e *= 4.0f * (x - x * x);
         s[r] = p;
         d[r] = e;
       }
-    };
-    if (OPTIONS && cap != 0.0f)
-      factors(std::true_type{});
-    else
-      factors(std::false_type{});
+    }
     if (!now.all) {
       const int left = rows - (now.sub + at_rows) * 32 - 4 * half;
 #pragma unroll
@@ -494,7 +491,7 @@ __global__ void __launch_bounds__(64 * kKeyWaves, 2) k_packed_dkv(const PackedAr
   store_row<KS>(to_v, dv, 1.0f, v_wide);
 }
 
-template <int KS, bool OPTIONS>
+template <int KS, int OPTIONS>
 hipError_t launch(const PackedArgs& a, hipStream_t s) {
   constexpr int kDq = 4 * kKeys * Tile<KS>::kPitch + kWaves * (KS + queries_in_lds(KS)) * 1024 + 2 * kKeys * 4 + 16, kDkv = KeySide<KS, OPTIONS>::kShared;
   static PerDeviceOnce once;
@@ -511,7 +508,9 @@ hipError_t launch(const PackedArgs& a, hipStream_t s) {
 }
 
 template <int KS>
-hipError_t launch(const PackedArgs& a, hipStream_t s) { return a.cap_log2 != 0.0f || a.slopes ? launch<KS, true>(a, s) : launch<KS, false>(a, s); }
+hipError_t launch(const PackedArgs& a, hipStream_t s) {
+  return a.cap_log2 != 0.0f ? launch<KS, kCapped>(a, s) : a.slopes ? launch<KS, kBiased>(a, s) : launch<KS, 0>(a, s);
+}
 
 }  // namespace
 

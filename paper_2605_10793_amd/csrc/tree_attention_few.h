@@ -128,12 +128,13 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree(const TreeArgs) {
     const Sequence sq = sequence_of(a, b);
     const int rows = sq.count * a->group;
     const int64_t base_key = KIND == kMasks ? 0 : (int64_t)first_block(a, sq, row0) * kBlock, limit = KIND == kMasks ? sq.length : tile_end(a, sq, row0);
-    const int64_t begin = base_key + (int64_t)piece.first * kBlock, piece_end = base_key + (int64_t)piece.last * kBlock, end = piece_end < limit ? piece_end : limit;
+    const int64_t piece_end = base_key + (int64_t)piece.last * kBlock;
+    int64_t begin = base_key + (int64_t)piece.first * kBlock, end = piece_end < limit ? piece_end : limit;
     // A chunk: the keys of each row, and those that all rows see.  A row that sees nothing is taken to see all, and gets zeros at the end.
-    int low_all = 0, high_all = 0;
+    int low_all = 0, high_all = 0, low_any = 0, high_any = 0;
     float slope[QT], place[QT];
     if constexpr (KIND != kMasks) {
-      high_all = INT_MAX;
+      high_all = low_any = INT_MAX;
 #pragma unroll
       for (int x = 0; x < QT; ++x) {
         const int row = row0 + x * 16 + col, node = (uint32_t)(row < rows ? row : 0) / (uint32_t)a->group;
@@ -141,11 +142,18 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree(const TreeArgs) {
         const bool any = row < rows && k.x < k.y;
         low_all = max(low_all, wave_max_int(any ? k.x : 0));
         high_all = min(high_all, wave_min(any ? k.y : INT_MAX));
+        low_any = min(low_any, wave_min(any ? k.x : INT_MAX));
+        high_any = max(high_any, wave_max_int(any ? k.y : 0));
         if constexpr (KIND == kOptions) {
           slope[x] = a->slopes ? a->slopes[head * a->group + (row < rows ? row : 0) - node * a->group] * 1.4426950408889634f : 0.0f;
           place[x] = (float)node - 16.0f * g;      // less the block's first key and the committed tokens' number
         }
       }
+    }
+
+    if constexpr (KIND != kMasks) {          // what no row sees is left out
+      if (high_any < end) end = high_any;
+      if (low_any / kBlock * kBlock > begin) begin = low_any / kBlock * kBlock;
     }
 
     // Queries: operand i of column `col`, in the order in which the keys' operands have the entries.

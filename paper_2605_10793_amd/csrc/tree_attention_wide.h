@@ -116,12 +116,13 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs) {
   const bool idle = row0 >= rows;        // still loads and meets the barriers
   const int tile_row0 = row_tile * 64 * QT;
   const int64_t base_key = KIND == kMasks ? 0 : (int64_t)first_block(a, sq, tile_row0) * kBlock, limit = KIND == kMasks ? sq.length : tile_end(a, sq, tile_row0);
-  const int64_t piece_to = base_key + (int64_t)piece.last * kBlock, piece_end = piece_to < limit ? piece_to : limit;
+  const int64_t piece_to = base_key + (int64_t)piece.last * kBlock;
+  int64_t piece_from = base_key + (int64_t)piece.first * kBlock, piece_end = piece_to < limit ? piece_to : limit;
   // A chunk: the keys of each row, and those that all rows of the workgroup see.  A row that sees nothing is taken to see all, and gets zeros at the end.
-  int low_all = 0, high_all = 0;
+  int low_all = 0, high_all = 0, low_any = 0, high_any = 0;
   float slope[QT], place[QT];
   if constexpr (KIND != kMasks) {
-    high_all = INT_MAX;
+    high_all = low_any = INT_MAX;
 #pragma unroll
     for (int x = 0; x < QT; ++x) {
       const int other = tile_row0 + x * 64 + lane;
@@ -129,12 +130,19 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs) {
       const bool any = other < rows && k.x < k.y;
       low_all = max(low_all, wave_max_int(any ? k.x : 0));
       high_all = min(high_all, wave_min(any ? k.y : INT_MAX));
+      low_any = min(low_any, wave_min(any ? k.x : INT_MAX));
+      high_any = max(high_any, wave_max_int(any ? k.y : 0));
       if constexpr (KIND == kOptions) {
         const int row = row0 + x * 16 + col, node = (uint32_t)(row < rows ? row : 0) / (uint32_t)a->group;
         slope[x] = a->slopes ? a->slopes[head * a->group + (row < rows ? row : 0) - node * a->group] * 1.4426950408889634f : 0.0f;
         place[x] = (float)node - 16.0f * g;      // less the block's first key and the committed tokens' number
       }
     }
+  }
+
+  if constexpr (KIND != kMasks) {          // what no row of the workgroup sees is left out
+    if (high_any < piece_end) piece_end = high_any;
+    if (low_any / kBlock * kBlock > piece_from) piece_from = low_any / kBlock * kBlock;
   }
 
   bf16x8 qf[QT][kOps];
@@ -354,7 +362,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs) {
     }
   };
 
-  for (int64_t begin = base_key + (int64_t)piece.first * kBlock; begin < piece_end; begin += kRun) {
+  for (int64_t begin = piece_from; begin < piece_end; begin += kRun) {
   end = begin + kRun < piece_end ? begin + kRun : piece_end;
   __syncthreads();
   // First the blocks of committed tokens, nearly all.  Codes: when turn n begins, block n's and n + 1's are on their way to LDS; the turn turns the
