@@ -65,19 +65,24 @@ __device__ __forceinline__ int edge_of(Args a, int i) {
 
 // Pieces of sequences.  A sequence's parts are numbered from edge * of / per + (number of the sequence) on, per = 2^shift, of = 1 (tokens) or more (rows of a
 // token), which leaves room for ceil(count * of / per) of each: a part's sequence is found by halving (here into 64), and no table is made.
-// edge(i): first row of sequence i, up to `edges`, not falling.  By a whole wavefront; the same for all lanes.
+// edge(i): first row of sequence i, up to `edges`, not falling.  By a whole wavefront; the same for all lanes.  first, next: the sequence's edges.
 template <typename Edge>
-__device__ __forceinline__ int sequence_of_part(int id, int edges, int shift, int of, Edge edge) {
+__device__ __forceinline__ int sequence_of_part(int id, int edges, int shift, int of, Edge edge, int* first, int* next) {
   const int lane = (int)threadIdx.x & 63;
   int lo = 0, hi = edges;
-  while (hi - lo > 1) {
-    const int step = (hi - lo + 63) >> 6, i = lo + lane * step;
-    const bool at_most = i < hi && (int)(((int64_t)edge(i) * of) >> shift) + i <= id;
-    const int c = __popcll(__ballot(at_most));
-    lo += (c > 0 ? c - 1 : 0) * step;
+  for (;;) {
+    const int step = hi - lo > 63 ? (hi - lo + 63) >> 6 : 1, i = lo + lane * step;          // (with a step of 1, one lane at least for the end)
+    const int e = i <= edges ? edge(i) : 0;
+    const bool at_most = i < hi && (int)(((int64_t)e * of) >> shift) + i <= id;
+    const int c = __popcll(__ballot(at_most)), at = c > 0 ? c - 1 : 0;
+    if (step == 1) {
+      *first = __builtin_amdgcn_readlane(e, at);
+      *next = __builtin_amdgcn_readlane(e, at + 1);
+      return __builtin_amdgcn_readfirstlane(lo + at);
+    }
+    lo += at * step;
     hi = hi - lo < step ? hi : lo + step;
   }
-  return __builtin_amdgcn_readfirstlane(lo);
 }
 struct Item {
   int first, count;      // rows of the call that are the sequence's tokens
@@ -86,9 +91,9 @@ struct Item {
   int base;              // number of its first part
   bool rest;             // of no sequence
   __device__ __forceinline__ bool find(Args a, int id, int shift, int of) {
-    number = sequence_of_part(id, a->sequences + 2, shift, of, [&](int i) { return edge_of(a, i); });
-    first = __builtin_amdgcn_readfirstlane(edge_of(a, number));
-    count = __builtin_amdgcn_readfirstlane(edge_of(a, number + 1)) - first;
+    int next;
+    number = sequence_of_part(id, a->sequences + 2, shift, of, [&](int i) { return edge_of(a, i); }, &first, &next);
+    count = next - first;
     if (count < 0) count = 0;
     rest = number == 0 || number == a->sequences + 1;
     base = (int)(((int64_t)first * of) >> shift) + number;
