@@ -7,6 +7,7 @@ the stream (the current one of the tensors' device).  Nothing synchronises, noth
   rotary                              positions into queries and keys, or back out of their gradients
   qk_norm_rotary, .._backward         per-head norms and positions in one pass, and that pass's gradients
   KVCache, append                     a paged cache of keys and values in bf16 or in 8- or 4-bit zero-point codes
+  Pages                               which of its pages are taken, and by how many sequences (on the host)
   gather                              tokens of a cache into other pages: forks, tokens that are kept, beams
   tree_attention                      attention of new tokens (a tree of drafted ones, a chain, a single one) over the cache
   chunk_attention                     attention of any number of new tokens over the cache, with windows, bounds, capped scores, a bias by distance
@@ -243,6 +244,63 @@ def append(cache: KVCache, k, v, start, prefix, table, values: bool = False, k_v
                         *(_ABSENT if v_values is None else _rows(v_values, "v_values", *same)), tokens)
     _check(_run(binding.load().conqur_cache_append, device, call), "conqur_cache_append")
     return (k_values, v_values) if values else None
+
+
+class Pages:
+    """Which pages of a cache are taken, and how often, on the host: a program takes pages for new tokens, shares those that a fork has in common with
+    its parent, and gives back what a sequence no longer needs.  A page is free again when every holder has given it back; the cache is not touched, and
+    work that is under way on the device may still read a page that was given back: what is taken next is written behind it on the same stream."""
+
+    def __init__(self, pages: int):
+        self._free = list(range(pages - 1, -1, -1))
+        self._held = [0] * pages
+
+    @property
+    def left(self) -> int:
+        return len(self._free)
+
+    def held(self, page: int) -> int:
+        """By how many sequences a page is held."""
+        return self._held[self._known(page)]
+
+    def _known(self, page: int) -> int:
+        if not 0 <= page < len(self._held):
+            raise ValueError(f"page {page} is none of {len(self._held)}")
+        return page
+
+    def take(self, n: int) -> list:
+        """n free pages, the lowest first among those never given back; none are taken if there are not enough."""
+        if n < 0 or n > len(self._free):
+            raise ValueError(f"{n} pages asked for, {len(self._free)} are free")
+        taken = [self._free.pop() for _ in range(n)]
+        for page in taken:
+            self._held[page] = 1
+        return taken
+
+    def share(self, pages) -> None:
+        """One more holder for each of the pages (a page named twice: two more)."""
+        pages = list(pages)
+        for page in pages:
+            if not self._held[self._known(page)]:
+                raise ValueError(f"page {page} is free")
+        for page in pages:
+            self._held[page] += 1
+
+    def release(self, pages) -> list:
+        """One holder fewer for each; returns the pages that are free now.  All or, with an error, none are given back."""
+        pages = list(pages)
+        less = {}
+        for page in pages:
+            less[page] = less.get(page, 0) + 1
+            if less[page] > self._held[self._known(page)]:
+                raise ValueError(f"page {page} is not held that often")
+        freed = []
+        for page in pages:
+            self._held[page] -= 1
+            if not self._held[page]:
+                freed.append(page)
+        self._free += reversed(freed)
+        return freed
 
 
 def gather(cache: KVCache, tokens, start, table, to_table) -> None:
