@@ -64,14 +64,14 @@ __device__ __forceinline__ int edge_of(Args a, int i) {
 }
 
 // Pieces of sequences.  A sequence's parts are numbered from edge * of / per + (number of the sequence) on, per = 2^shift, of = 1 (tokens) or more (rows of a
-// token), which leaves room for ceil(count * of / per) of each: a part's sequence is found by halving (here into 64), and no table is made.
+// token), which leaves room for ceil(count * of / per) of each: a part's sequence is found by halving (here into 63), and no table is made.
 // edge(i): first row of sequence i, up to `edges`, not falling.  By a whole wavefront; the same for all lanes.  first, next: the sequence's edges.
 template <typename Edge>
 __device__ __forceinline__ int sequence_of_part(int id, int edges, int shift, int of, Edge edge, int* first, int* next) {
   const int lane = (int)threadIdx.x & 63;
   int lo = 0, hi = edges;
   for (;;) {
-    const int step = hi - lo > 63 ? (hi - lo + 63) >> 6 : 1, i = lo + lane * step;          // (with a step of 1, one lane at least for the end)
+    const int step = (hi - lo + 62) / 63, i = lo + lane * step;      // (63 and not 64: with a step of 1, a lane is left for the edge behind the last)
     const int e = i <= edges ? edge(i) : 0;
     const bool at_most = i < hi && (int)(((int64_t)e * of) >> shift) + i <= id;
     const int c = __popcll(__ballot(at_most)), at = c > 0 ? c - 1 : 0;
@@ -200,7 +200,7 @@ struct Tile {
 // N products whose operands come from LDS: RING of them are on their way ahead of the products that take them, and nothing but arithmetic passes from one to
 // the next (the compiler would hold more of them than there are registers).  load(i), use(i, operand): i as a constant.
 constexpr int kArithmetic = 0x6;
-template <int N, int RING = 4, int FENCE = kArithmetic, typename Load, typename Use>
+template <int N, int RING = 4, typename Load, typename Use>
 __device__ __forceinline__ void in_turn(Load load, Use use) {
   decltype(load(std::integral_constant<int, 0>{})) ring[RING];
   each<(N < RING ? N : RING)>([&](auto i) { ring[decltype(i)::value] = load(i); });
@@ -208,7 +208,7 @@ __device__ __forceinline__ void in_turn(Load load, Use use) {
     constexpr int I = decltype(i)::value;
     use(i, ring[I % RING]);
     if constexpr (I + RING < N) ring[I % RING] = load(std::integral_constant<int, I + RING>{});
-    if constexpr (FENCE >= 0) __builtin_amdgcn_sched_barrier(FENCE);
+    __builtin_amdgcn_sched_barrier(kArithmetic);
   });
 }
 

@@ -190,6 +190,29 @@ def test_gather(bits, page, width, what):
         assert torch.equal(want.view(torch.uint8), y.cpu().view(torch.uint8))
 
 
+@pytest.mark.parametrize("n", [1, 63, 64, 65, 4032, 4096])
+def test_gather_counts_of_sequences(n):
+    """Around those where a part's sequence is found in one read more: every sequence is moved, the last one too."""
+    from paper_2605_10793_amd import attention as A
+    lengths = [1 + i % 3 for i in range(n - 1)] + [70]
+    cache = A.KVCache.empty(2 * (n + 1), 1, 64, 64, 16, DEV)
+    cache.k.copy_(torch.arange(cache.k.numel(), dtype=torch.int32, device=DEV).view(torch.int16)[:cache.k.numel()].view(cache.k.shape).view(torch.bfloat16))
+    cache.v.zero_()
+    table = torch.full((n, 2), -1, dtype=torch.int32)
+    table[:, 0] = torch.arange(n, dtype=torch.int32)
+    table[n - 1, 1] = n
+    to_table = torch.where(table < 0, table, table + n + 1)
+    tokens = torch.cat([torch.arange(m, dtype=torch.int32).flip(0) for m in lengths])
+    start = torch.tensor([0] + lengths).cumsum(0).to(torch.int32)
+    want = cache.k.cpu().view(torch.int16).clone()
+    for b, m in enumerate(lengths):
+        for i in range(m):
+            t = m - 1 - i
+            want[to_table[b, i // 64], 0, i % 64] = want[table[b, t // 64], 0, t % 64]
+    A.gather(cache, tokens.to(DEV), start.to(DEV), table.to(DEV), to_table.to(DEV))
+    assert torch.equal(want, cache.k.cpu().view(torch.int16))
+
+
 def test_gather_without_places():
     """Tokens out of a table's reach, and pages that are none, are not moved."""
     from paper_2605_10793_amd import attention as A

@@ -125,5 +125,11 @@ def test_many_sequences():
     check([1] * 5000, 1, 1, 32, seed=23)
 
 
+@pytest.mark.parametrize("n", [61, 62, 63, 64, 4030, 4094])
+def test_counts_of_sequences(n):
+    """Around those where a part's sequence is found in one read more: every sequence, the last one too, and the rows behind it."""
+    check([1 + (i * 5) % 3 for i in range(n - 1)] + [70], 1, 1, 32, seed=n, lead=2, behind=70)
+
+
 def test_contiguous_rows():
     check([100, 30], 4, 4, 128, seed=24, strided=False)
