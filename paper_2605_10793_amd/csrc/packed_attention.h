@@ -40,6 +40,8 @@ struct PackedArgs {
                              // slopes four floats: the row's slope (base 2) and token behind them
   int2* seen;                // [row] first key and last + 1
   int4* span;                // [32 rows of an item] lowest first, highest last, highest first, lowest last (a row that sees nothing: highest first is INT_MAX)
+  float* part;               // [part of the rows][64 keys][key head][32 of them][dk, dv]: sums over the part, as registers hold them
+  int parts;                 // in which the rows that see 64 keys are taken
 };
 
 // The arguments as a kernel reads them, where they lie: what a part of a kernel needs of them is read there and not kept in registers.

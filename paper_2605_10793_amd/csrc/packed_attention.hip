@@ -265,13 +265,28 @@ bool call_fine(const conqur_attention_call* c) {
 
 uint64_t lay_bytes(const conqur_attention_call& c, const conqur_heads& h) { return plain(h) ? 0 : (c.tokens * h.heads * c.width * 2 + 255) / 256 * 256; }
 struct BackwardSizes {
-  uint64_t stat, seen, span;
+  uint64_t stat, seen, span, part;
+  int parts;
 };
+// In how many parts the rows of 64 keys are taken, by as many workgroups, whose sums a kernel of its own adds up.  A workgroup takes what sees its keys one step
+// of 128 rows after the other; with fewer workgroups than the device takes at a time (one to a compute unit), the first keys' rows are what the others wait for.
+// As many parts as make 512 workgroups (half the rows see a key, on average), of four steps or more: gradients of 2000 tokens, 8 heads, 1 key head, width 128:
+// 344 us in one part, 200 in 15; 1000 tokens, 32 heads, 8 key heads: 125 and 115; 2 of 1500 tokens, 40 heads, 8 key heads (384 workgroups): 280, and 314 in two.
+int key_parts(const conqur_attention_call& c, uint64_t workgroups) {
+  if (!c.sequences) return 1;
+  uint64_t seeing = c.tokens / c.sequences;
+  if (c.window && c.window < seeing) seeing = c.window;
+  const uint64_t steps = seeing * (c.q.heads / c.k.heads) / 128, fill = 512 / workgroups, most = fill < 16 ? fill : 16;
+  return steps / 4 < 2 || most < 2 ? 1 : (int)(steps / 4 < most ? steps / 4 : most);
+}
 BackwardSizes backward_sizes(const conqur_attention_call& c) {
   auto up = [](uint64_t n) { return (n + 255) / 256 * 256; };
   const uint64_t rows = c.tokens * (c.q.heads / c.k.heads);      // (loads of 64 rows' may reach 128 rows behind the last)
   const uint64_t stat = c.cap != 0.0f || c.slopes ? sizeof(float4) : sizeof(float2);
-  return {up((rows * c.k.heads + 128) * stat), up((rows + 128) * sizeof(int2)), up((rows / kRows + c.sequences + 2) * kWaves * sizeof(int4))};
+  const uint64_t items = (c.tokens / kTile + c.sequences + 2) * c.k.heads, width = (c.width + 31) / 32 * 32;
+  const int parts = key_parts(c, items);
+  return {up((rows * c.k.heads + 128) * stat), up((rows + 128) * sizeof(int2)), up((rows / kRows + c.sequences + 2) * kWaves * sizeof(int4)),
+          parts > 1 ? parts * items * kTile * width * 2 * sizeof(float) : 0, parts};
 }
 
 PackedArgs args_of(const conqur_attention_call& c) {
@@ -353,7 +368,7 @@ extern "C" conqur_status conqur_attention(const conqur_attention_call* c, void* 
 extern "C" uint64_t conqur_attention_backward_workspace(const conqur_attention_call* c) {
   if (!call_fine(c)) return 0;
   const BackwardSizes z = backward_sizes(*c);
-  return z.stat + z.seen + z.span + lay_bytes(*c, c->q) + lay_bytes(*c, c->k) + lay_bytes(*c, c->v) + lay_bytes(*c, c->out) + lay_bytes(*c, c->out_grad);
+  return z.stat + z.seen + z.span + z.part + lay_bytes(*c, c->q) + lay_bytes(*c, c->k) + lay_bytes(*c, c->v) + lay_bytes(*c, c->out) + lay_bytes(*c, c->out_grad);
 }
 
 extern "C" conqur_status conqur_attention_backward(const conqur_attention_call* c, void* stream) {
@@ -376,7 +391,9 @@ extern "C" conqur_status conqur_attention_backward(const conqur_attention_call* 
   a.stat = reinterpret_cast<float2*>(at);
   a.seen = reinterpret_cast<int2*>(at + z.stat);
   a.span = reinterpret_cast<int4*>(at + z.stat + z.seen);
-  at += z.stat + z.seen + z.span;
+  a.part = reinterpret_cast<float*>(at + z.stat + z.seen + z.span);
+  a.parts = z.parts;
+  at += z.stat + z.seen + z.span + z.part;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   hipError_t e = lay(*c, c->q, &a.q, &at, s);
   if (e == hipSuccess) e = lay(*c, c->k, &a.k, &at, s);

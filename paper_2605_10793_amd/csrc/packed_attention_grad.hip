@@ -142,6 +142,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dq(const PackedArgs) 
       bf16x8 rows, mine;
     };
     f32x16 s = f32x16{}, d = f32x16{};
+    __builtin_amdgcn_s_setprio(1);           // before the other wavefront's arithmetic: 200 -> 190 us, two sequences of 2048 tokens
     in_turn<2 * KS, 3>(
         [&](auto i) {
           constexpr int I = decltype(i)::value / 2;
@@ -158,6 +159,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dq(const PackedArgs) 
           else
             s = mfma32(f.rows, f.mine, s);
         });
+    __builtin_amdgcn_s_setprio(0);
     if (odd) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] += s_bad[which * kKeys + row_of(r, h)];
@@ -203,6 +205,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dq(const PackedArgs) 
     for (int r = 0; r < 16; ++r) d[r] -= (float)df[r / 8][r % 8];
     const bf16x8 rest[2] = {pack8(d, 0), pack8(d, 1)};
     __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(1);
     in_turn<2 * T::kTiles>([&](auto i) { return T::template turned<decltype(i)::value / T::kTiles * 16 * T::kPitch>(turned_at, decltype(i)::value % T::kTiles); },
                            [&](auto i, bf16x8 f) {
                              constexpr int I = decltype(i)::value, t = I % T::kTiles;
@@ -210,6 +213,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dq(const PackedArgs) 
                              pk[t] = mfma32(f, pf[I / T::kTiles], pk[t]);
                              dq[t] = mfma32(f, rest[I / T::kTiles], dq[t]);
                            });
+    __builtin_amdgcn_s_setprio(0);
   }
 
   sum = halves(sum, [](float x, float y) { return x + y; });
@@ -234,9 +238,15 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dq(const PackedArgs) 
   store_row<KS>(to, dq, a->scale * inv, wide8(a->q_grad.data, a->q_grad.ts, a->q_grad.hs));
 }
 
+// Where the sums over part `p` of the rows are, of 32 keys of a workgroup.
+template <int KS>
+__device__ __forceinline__ f32x4* part_of(Args a, int p, int workgroup, int half) {
+  return reinterpret_cast<f32x4*>(a->part) + (((int64_t)p * gridDim.x + workgroup) * 2 + half) * (2 * Tile<KS>::kTiles * 4 * 64);
+}
+
 // Eight wavefronts, which take 32 of the workgroup's 64 keys and 32 of 128 rows at a time each; their sums meet in LDS at the end.  (Four, two workgroups to a
 // compute unit: 274 us for 193, two sequences of 2048 tokens.  A workgroup's time is what the rows of its keys take one after the other, and the first keys' rows
-// are all there are.)
+// are all there are.)  If there are few workgroups, several share the rows of 64 keys, step by step in turn.
 constexpr int kKeyWaves = 8, kStep = 16 * kKeyWaves;                  // kStep: rows that lie in LDS at a time
 template <int KS, int OPTIONS>
 struct KeySide {
@@ -292,27 +302,32 @@ __global__ void __launch_bounds__(64 * kKeyWaves, 2) k_packed_dkv(const PackedAr
     int sub;
     bool some, all, every;      // of the wavefront's keys and rows: any are seen, all are; all of the workgroup's
   };
+  int turn = blockIdx.y;        // steps until the next that is this workgroup's
   auto next = [&](Step* x) {
-    while (!active) {
-      if (next_chunk >= subs) return false;
-      chunk = next_chunk;
-      next_chunk += 64;
-      const int sub = chunk + lane;
-      int4 s = make_int4(INT_MAX, 0, INT_MAX, 0);
-      if (sub < subs) s = span[sub];
-      const uint64_t near = __ballot(s.x < k0 + kTile && s.y > k0);
-      some = __ballot(s.x < key0 + 32 && s.y > key0);
-      whole = __ballot(s.z <= key0 && s.w >= key0 + 32);
-      every = __ballot(s.z <= k0 && s.w >= k0 + kTile);
-      active = (near | near >> 1 | near >> 2 | near >> 3) & 0x1111111111111111ull;
+    for (;;) {
+      while (!active) {
+        if (next_chunk >= subs) return false;
+        chunk = next_chunk;
+        next_chunk += 64;
+        const int sub = chunk + lane;
+        int4 s = make_int4(INT_MAX, 0, INT_MAX, 0);
+        if (sub < subs) s = span[sub];
+        const uint64_t near = __ballot(s.x < k0 + kTile && s.y > k0);
+        some = __ballot(s.x < key0 + 32 && s.y > key0);
+        whole = __ballot(s.z <= key0 && s.w >= key0 + 32);
+        every = __ballot(s.z <= k0 && s.w >= k0 + kTile);
+        active = (near | near >> 1 | near >> 2 | near >> 3) & 0x1111111111111111ull;
+      }
+      const int bit = __builtin_ctzll(active);
+      active &= active - 1;
+      if (turn-- > 0) continue;
+      turn = (int)gridDim.y - 1;
+      x->sub = chunk + bit;
+      x->some = (some >> (bit + at_rows)) & 1;
+      x->all = (whole >> (bit + at_rows)) & 1;
+      x->every = ((every >> bit) & ((1 << kStep / 32) - 1)) == (1 << kStep / 32) - 1;
+      return true;
     }
-    const int bit = __builtin_ctzll(active);
-    active &= active - 1;
-    x->sub = chunk + bit;
-    x->some = (some >> (bit + at_rows)) & 1;
-    x->all = (whole >> (bit + at_rows)) & 1;
-    x->every = ((every >> bit) & ((1 << kStep / 32) - 1)) == (1 << kStep / 32) - 1;
-    return true;
   };
 
   const bf16_bits* const q0 = a->q.data + (int64_t)item.first * a->q.ts + (int64_t)head * group * a->q.hs;
@@ -483,12 +498,57 @@ __global__ void __launch_bounds__(64 * kKeyWaves, 2) k_packed_dkv(const PackedAr
     __syncthreads();
   }
   a = kernel_args();
-  if (wave >= 2 || key >= item.count) return;
+  if (wave >= 2) return;
+  if (gridDim.y > 1) {
+    f32x4* const to = part_of<KS>(a, (int)blockIdx.y, (int)blockIdx.x, wave) + lane;
+#pragma unroll
+    for (int t = 0; t < T::kTiles; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        to[(t * 4 + r) * 64] = f32x4{dk[t][4 * r], dk[t][4 * r + 1], dk[t][4 * r + 2], dk[t][4 * r + 3]};
+        to[((T::kTiles + t) * 4 + r) * 64] = f32x4{dv[t][4 * r], dv[t][4 * r + 1], dv[t][4 * r + 2], dv[t][4 * r + 3]};
+      }
+    return;
+  }
+  if (key >= item.count) return;
   const bool k_wide = wide8(a->k_grad.data, a->k_grad.ts, a->k_grad.hs), v_wide = wide8(a->v_grad.data, a->v_grad.ts, a->v_grad.hs);
   bf16_bits* const to_k = a->k_grad.data + key_token * a->k_grad.ts + head * a->k_grad.hs + 4 * h;
   bf16_bits* const to_v = a->v_grad.data + key_token * a->v_grad.ts + head * a->v_grad.hs + 4 * h;
   store_row<KS>(to_k, dk, a->scale, k_wide);
   store_row<KS>(to_v, dv, 1.0f, v_wide);
+}
+
+// The sums of the rows' parts, in their order.
+template <int KS>
+__global__ void __launch_bounds__(128) k_packed_sum(const PackedArgs) {
+  using T = Tile<KS>;
+  const Args a = kernel_args();
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
+  const int head = blockIdx.x % a->heads;
+  Item item;
+  if (!item.find(a, blockIdx.x / a->heads, 6, 1)) return;
+  const int key = item.part * kTile + 32 * wave + (lane & 31);
+  f32x16 dk[T::kTiles], dv[T::kTiles];
+#pragma unroll
+  for (int t = 0; t < T::kTiles; ++t) dk[t] = dv[t] = f32x16{};
+  for (int p = 0; p < a->parts; ++p) {
+    const f32x4* const from = part_of<KS>(a, p, (int)blockIdx.x, wave) + lane;
+#pragma unroll
+    for (int t = 0; t < T::kTiles; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const f32x4 x = from[(t * 4 + r) * 64], y = from[((T::kTiles + t) * 4 + r) * 64];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          dk[t][4 * r + j] += x[j];
+          dv[t][4 * r + j] += y[j];
+        }
+      }
+  }
+  if (key >= item.count) return;
+  const int64_t token = item.first + key;
+  store_row<KS>(a->k_grad.data + token * a->k_grad.ts + head * a->k_grad.hs + 4 * h, dk, a->scale, wide8(a->k_grad.data, a->k_grad.ts, a->k_grad.hs));
+  store_row<KS>(a->v_grad.data + token * a->v_grad.ts + head * a->v_grad.hs + 4 * h, dv, 1.0f, wide8(a->v_grad.data, a->v_grad.ts, a->v_grad.hs));
 }
 
 template <int KS, int OPTIONS>
@@ -503,7 +563,11 @@ hipError_t launch(const PackedArgs& a, hipStream_t s) {
   k_packed_dq<KS, OPTIONS><<<dim3((uint32_t)(row_items(a) * a.heads)), 64 * kWaves, kDq, s>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  k_packed_dkv<KS, OPTIONS><<<dim3((uint32_t)(key_items(a) * a.heads)), 64 * kKeyWaves, kDkv, s>>>(a);
+  const uint32_t workgroups = (uint32_t)(key_items(a) * a.heads);
+  k_packed_dkv<KS, OPTIONS><<<dim3(workgroups, (uint32_t)a.parts), 64 * kKeyWaves, kDkv, s>>>(a);
+  e = hipGetLastError();
+  if (e != hipSuccess || a.parts == 1) return e;
+  k_packed_sum<KS><<<dim3(workgroups), 128, 0, s>>>(a);
   return hipGetLastError();
 }
 

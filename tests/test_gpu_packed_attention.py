@@ -131,5 +131,13 @@ def test_counts_of_sequences(n):
     check([1 + (i * 5) % 3 for i in range(n - 1)] + [70], 1, 1, 32, seed=n, lead=2, behind=70)
 
 
+@pytest.mark.parametrize("counts, heads, kv, width, options", [
+    ([1300, 0, 1100], 8, 1, 64, dict(kind="documents")), ([1200], 4, 2, 128, dict(kind="prefix", cap=20.0, lead=3, behind=200)),
+    ([900, 5, 1500], 6, 1, 96, dict(kind="holes", biased=True)), ([1900], 3, 1, 32, dict(window=700)), ([2050], 2, 2, 80, dict(kind="far"))])
+def test_rows_in_parts(counts, heads, kv, width, options):
+    """Few keys and many rows: several workgroups share the rows of 64 keys."""
+    check(counts, heads, kv, width, seed=sum(counts), **options)
+
+
 def test_contiguous_rows():
     check([100, 30], 4, 4, 128, seed=24, strided=False)
