@@ -323,10 +323,10 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return x;
 }
 
-// A score in base 2 from a product q k, less the bias; `r` receives 1 / (1 + e^(2 u / cap)), from which 1 - tanh^2 = 4 r (1 - r) follows.
-__device__ __forceinline__ float capped(float dot, float cap_log2, float cap_in, float* r) {
+// A score in base 2 from a product q k, less the bias and `base`; `r` receives 1 / (1 + e^(2 u / cap)), from which 1 - tanh^2 = 4 r (1 - r) follows.
+__device__ __forceinline__ float capped(float dot, float cap_log2, float cap_in, float base, float* r) {
   *r = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(dot * cap_in));
-  return fmaf(-2.0f * cap_log2, *r, cap_log2);
+  return fmaf(-2.0f * cap_log2, *r, cap_log2 - base);
 }
 
 // Four neighbouring entries of a row's result.

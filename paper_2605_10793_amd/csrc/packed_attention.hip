@@ -114,7 +114,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed(const PackedArgs) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             float x;
-            s[u][r] = capped(s[u][r], cap, cap_in, &x) - base;
+            s[u][r] = capped(s[u][r], cap, cap_in, base, &x);
           }
       } else {
 #pragma unroll

@@ -172,7 +172,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dq(const PackedArgs) 
       for (int r = 0; r < 16; ++r) {
         float x = 0.0f, y;
         if constexpr (decltype(caps)::value)
-          y = capped(s[r], cap, cap_in, &x) - lse;
+          y = capped(s[r], cap, cap_in, lse, &x);
         else
           y = fmaf(s[r], scale, -lse);
         if constexpr (OPTIONS) y = fmaf(-slope, fabsf(at - (float)row_of(r, 0)), y);
@@ -429,7 +429,7 @@ __global__ void __launch_bounds__(64 * kKeyWaves, 2) k_packed_dkv(const PackedAr
         }
         float x = 0.0f, y;
         if constexpr (OPTIONS == kCapped)
-          y = capped(s[r], cap, cap_in, &x) - lse;
+          y = capped(s[r], cap, cap_in, lse, &x);
         else
           y = fmaf(s[r], scale, -lse);
         if constexpr (OPTIONS) y = fmaf(-slope, fabsf(token - place), y);
