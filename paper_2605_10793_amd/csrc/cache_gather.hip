@@ -5,7 +5,8 @@
 // them under way before it stores any (one after the other, keys, pairs, values: 83 us for 77, 32 sequences that keep three quarters of 501 to 8000 tokens in 4 bits; several heads to a workgroup cost more than finding the tokens
 // anew for each).  Keys go in 16 bytes a lane; values lie with the tokens of a page side by side, so a lane takes four
 // neighbouring target tokens of a V row: four reads of one entry each, one where the four lie side by side in the source too, and one store.
-#include "packed_attention.h"
+#include "../../include/conqur.h"
+#include "common.h"
 
 namespace conqur {
 
@@ -42,7 +43,7 @@ __global__ void __launch_bounds__(256) k_gather(const GatherArgs a) {
   const int id = blockIdx.x / heads;
   // (rows before the first sequence have no parts: its parts are numbered from its own edge on)
   int first, next;
-  const int b = packed::sequence_of_part(id, a.sequences, kShift, 1, edge, &first, &next);
+  const int b = sequence_of_part(id, a.sequences, kShift, 1, edge, &first, &next);
   const int count = next - first, part = id - ((first >> kShift) + b);
   if (part < 0 || part * kSlots >= count) return;
   const int page_tokens = (int)a.cache.page_tokens, shift = 31 - __builtin_clz(page_tokens);

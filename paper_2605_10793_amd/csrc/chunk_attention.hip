@@ -39,7 +39,8 @@ constexpr int64_t kMaxStride = 1ll << 40;
 
 struct Plan {
   bool wide;
-  int qt, tile_rows, row_tiles, splits, min_blocks, tail;
+  int qt, tile_rows, row_tiles, row_shift, splits, min_blocks, tail;
+  uint64_t tiles;            // row tiles of all sequences at most
   int64_t context;
 };
 
@@ -66,6 +67,8 @@ Plan plan_of(const conqur_chunk_call& c) {
   }
   p.tile_rows = 16 * p.qt * (p.wide ? kWaves : 1);
   p.row_tiles = (int)((rows + p.tile_rows - 1) / p.tile_rows);
+  p.row_shift = 31 - __builtin_clz(p.tile_rows);
+  p.tiles = p.row_tiles == 1 ? c.batch.sequences : ((c.tokens * (c.q.heads / c.cache.heads)) >> p.row_shift) + c.batch.sequences;
   const int64_t groups = (int64_t)c.cache.heads * p.row_tiles, sequences = c.batch.sequences;
   const int64_t blocks = p.context > kBlock ? (p.context + kBlock - 1) / kBlock : 1;
   p.min_blocks = kWaves;
@@ -83,9 +86,8 @@ Plan plan_of(const conqur_chunk_call& c) {
   }
   if (splits > most) splits = most;
   if (splits > kMaxSplits) splits = kMaxSplits;
-  if (splits < 1) splits = 1;
-  const int64_t workgroups = sequences * groups;
-  const bool alone = blocks <= kWaves || (blocks <= 32 && workgroups >= kSlots) || (blocks <= 128 && workgroups >= 4 * kSlots);
+  const int64_t workgroups = (int64_t)c.cache.heads * (sequences * p.row_tiles < (int64_t)p.tiles ? sequences * p.row_tiles : (int64_t)p.tiles);
+  const bool alone = splits < 2 || blocks <= kWaves || (blocks <= 32 && workgroups >= kSlots) || (blocks <= 128 && workgroups >= 4 * kSlots);
   p.tail = p.wide || (c.cache.bits != 16 && blocks * sequences >= 8 * splits) ? 4 : 0;
   p.splits = alone || sequences > kMaxScan || (blocks + p.tail) * sequences + 2 * kMaxSplits >= 1ll << 31 ? 0 : (int)splits;
   return p;
@@ -132,6 +134,8 @@ extern "C" conqur_status conqur_chunk_attention(const conqur_chunk_call* c, void
   const Plan p = plan_of(*c);
   const uint64_t need = workspace_of(*c, p);
   if (need && (!c->workspace || reinterpret_cast<uintptr_t>(c->workspace) % 16 || c->workspace_bytes < need)) return CONQUR_EINVAL;
+  const uint64_t workgroups = c->cache.heads * (p.splits ? (uint64_t)p.row_tiles : p.tiles);
+  if (workgroups >= 1u << 24) return CONQUR_EINVAL;          // (of 256 threads, which 32 bits count)
   TreeArgs a = {};
   a.cache = c->cache;
   a.batch = c->batch;
@@ -152,6 +156,7 @@ extern "C" conqur_status conqur_chunk_attention(const conqur_chunk_call* c, void
   a.group = (int)(c->q.heads / c->cache.heads);
   a.tile_rows = p.tile_rows;
   a.row_tiles = p.row_tiles;
+  a.row_shift = p.row_shift;
   a.part = static_cast<float*>(c->workspace);
   a.part_ml = reinterpret_cast<float2*>(a.part + (uint64_t)c->cache.heads * p.row_tiles * 2 * p.splits * p.tile_rows * c->cache.width);
   a.scale_log2 = c->scale * 1.4426950408889634f;
@@ -164,7 +169,7 @@ extern "C" conqur_status conqur_chunk_attention(const conqur_chunk_call* c, void
   a.cap_log2 = c->cap * 1.4426950408889634f;
   a.cap_in = c->cap == 0.0f ? 0.0f : 2.0f / c->cap;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  const dim3 grid((uint32_t)(a.cache.heads * p.row_tiles), p.splits ? p.splits : a.batch.sequences);
+  const dim3 grid((uint32_t)workgroups, p.splits ? p.splits : 1);
   hipError_t e = p.wide ? launch_chunk_wide(a, p.qt, grid, s) : launch_chunk_few(a, p.qt, grid, s);
   if (e == hipSuccess && p.splits > 1) e = launch_join(a, p.wide, s);
   return e == hipSuccess ? CONQUR_OK : CONQUR_EHIP;

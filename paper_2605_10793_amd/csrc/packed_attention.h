@@ -65,27 +65,6 @@ __device__ __forceinline__ int edge_of(Args a, int i) {
   return v < 0 ? 0 : v > tokens ? (int)tokens : v;
 }
 
-// Pieces of sequences.  A sequence's parts are numbered from edge * of / per + (number of the sequence) on, per = 2^shift, of = 1 (tokens) or more (rows of a
-// token), which leaves room for ceil(count * of / per) of each: a part's sequence is found by halving (here into 63), and no table is made.
-// edge(i): first row of sequence i, up to `edges`, not falling.  By a whole wavefront; the same for all lanes.  first, next: the sequence's edges.
-template <typename Edge>
-__device__ __forceinline__ int sequence_of_part(int id, int edges, int shift, int of, Edge edge, int* first, int* next) {
-  const int lane = (int)threadIdx.x & 63;
-  int lo = 0, hi = edges;
-  for (;;) {
-    const int step = (hi - lo + 62) / 63, i = lo + lane * step;      // (63 and not 64: with a step of 1, a lane is left for the edge behind the last)
-    const int e = i <= edges ? edge(i) : 0;
-    const bool at_most = i < hi && (int)(((int64_t)e * of) >> shift) + i <= id;
-    const int c = __popcll(__ballot(at_most)), at = c > 0 ? c - 1 : 0;
-    if (step == 1) {
-      *first = __builtin_amdgcn_readlane(e, at);
-      *next = __builtin_amdgcn_readlane(e, at + 1);
-      return __builtin_amdgcn_readfirstlane(lo + at);
-    }
-    lo += at * step;
-    hi = hi - lo < step ? hi : lo + step;
-  }
-}
 struct Item {
   int first, count;      // rows of the call that are the sequence's tokens
   int part, parts;

@@ -107,14 +107,16 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree(const TreeArgs) {
   __shared__ __attribute__((aligned(16))) float s_o[2][QT * kTiles][64][4];
   __shared__ float s_ml[2][QT][2][64];
 
-  const int head = blockIdx.x / a->row_tiles, row_tile = blockIdx.x % a->row_tiles;
+  int head, row_tile, own;
+  place_of<KIND>(a, &head, &row_tile, &own);
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int row0 = row_tile * 16 * QT;
   if constexpr (KIND != kMasks) {
-    if (a->zero_rest && row_tile == 0 && blockIdx.y == 0) zero_rows(a, head);
+    if (a->zero_rest && blockIdx.x < a->cache.heads && blockIdx.y == 0) zero_rows(a, head);
   }
   const bf16x8 ones = as_frag(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);      // a row of the sums of the weights as they are rounded
   Pieces piece;
+  piece.b = own;
   for (bool first = true; piece.next(a, row0, first); first = false) {
     int lane, col, g;
     auto number = [&] {

@@ -150,6 +150,15 @@ def test_scales():
     check(4, 64, 64, [100], [70], 2, 1, seed=13, scale=-0.3, cap=10.0)
 
 
+@pytest.mark.parametrize("bits, page, width", [(16, 64, 128), (8, 32, 128), (4, 16, 64)])
+@pytest.mark.parametrize("counts, heads", [([1] * 40 + [230] + [1] * 30 + [65, 0, 3], 8), ([1, 2, 0, 1] * 16, 4), ([66] * 63, 4), ([130] * 5, 4), ([17] * 65, 2)])
+def test_prompts_among_tokens(bits, page, width, counts, heads):
+    """Sequences of a call that bring very different numbers of tokens, over little that is committed and with limits that the table and q give."""
+    committed = [(i * 53) % 130 for i in range(len(counts))]
+    check(bits, page, width, committed, counts, heads, 2, seed=len(counts) + bits, closer=heads == 4)
+    check(bits, page, width, committed, counts, heads, 2, seed=len(counts) + bits, max_query=40)
+
+
 @pytest.mark.parametrize("bits, page, width", FORMATS)
 @pytest.mark.parametrize("what", ["fork", "keep", "all", "shift"])
 def test_gather(bits, page, width, what):
