@@ -105,7 +105,7 @@ def load() -> ctypes.CDLL:
         f64 = ctypes.c_double
         L.conqur_rotary_frequencies.restype = i32
         L.conqur_rotary_frequencies.argtypes = [u32, u32, f64, f64, f64, f64, f64, vp, vp]
-        for name in ("conqur_rotary", "conqur_qk_norm_rotary", "conqur_cache_append", "conqur_cache_gather", "conqur_cache_gather", "conqur_tree_attention"):
+        for name in ("conqur_rotary", "conqur_qk_norm_rotary", "conqur_cache_append", "conqur_cache_gather", "conqur_tree_attention"):
             getattr(L, name).restype = i32
             getattr(L, name).argtypes = [vp, vp]
         L.conqur_qk_norm_rotary_workspace.restype = u64

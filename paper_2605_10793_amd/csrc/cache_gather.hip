@@ -23,6 +23,7 @@ struct GatherArgs {
   int64_t table_stride, to_stride;
   int64_t count;
   int columns, to_columns, sequences;
+  int from;                  // number of the launch's first part
 };
 
 constexpr int kSlots = 64, kShift = 6, kFours = kSlots / 4;      // targets of a workgroup
@@ -40,7 +41,7 @@ __global__ void __launch_bounds__(256) k_gather(const GatherArgs a) {
     const int v = a.start[i];
     return v < 0 ? 0 : v > a.count ? (int)a.count : v;
   };
-  const int id = blockIdx.x / heads;
+  const int id = a.from + (int)(blockIdx.x / heads);
   // (rows before the first sequence have no parts: its parts are numbered from its own edge on)
   int first, next;
   const int b = sequence_of_part(id, a.sequences, kShift, 1, edge, &first, &next);
@@ -147,16 +148,21 @@ extern "C" conqur_status conqur_cache_gather(const conqur_gather_call* c, void* 
   if (!fine(c->tokens) || !fine(c->start) || !fine(c->table) || !fine(c->to_table)) return CONQUR_EINVAL;
   if (c->table_stride < (int64_t)(c->sequences > 1 ? c->table_columns : 0) || c->to_stride < (int64_t)(c->sequences > 1 ? c->to_columns : 0)) return CONQUR_EINVAL;
   if (c->table_stride >= 1ll << 40 || c->to_stride >= 1ll << 40) return CONQUR_EINVAL;
-  const uint64_t blocks = (c->count / kSlots + c->sequences + 1) * c->cache.heads;
-  if (blocks >= 1ull << 31) return CONQUR_EINVAL;
-  const GatherArgs a = {c->cache, c->tokens, c->start, c->table, c->to_table, c->table_stride, c->to_stride, (int64_t)c->count, (int)c->table_columns,
-                        (int)c->to_columns, (int)c->sequences};
+  const uint64_t parts = c->count / kSlots + c->sequences + 1;
+  GatherArgs a = {c->cache, c->tokens, c->start, c->table, c->to_table, c->table_stride, c->to_stride, (int64_t)c->count, (int)c->table_columns,
+                        (int)c->to_columns, (int)c->sequences, 0};
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  if (c->cache.bits == 16)
-    launch<16>(a, (uint32_t)blocks, s);
-  else if (c->cache.bits == 8)
-    launch<8>(a, (uint32_t)blocks, s);
-  else
-    launch<4>(a, (uint32_t)blocks, s);
-  return hipGetLastError() == hipSuccess ? CONQUR_OK : CONQUR_EHIP;
+  const uint64_t most = ((1ull << 24) - 1) / c->cache.heads;          // parts of a launch, whose threads 32 bits count
+  for (uint64_t from = 0; from < parts; from += most) {
+    const uint32_t blocks = (uint32_t)((parts - from < most ? parts - from : most) * c->cache.heads);
+    a.from = (int)from;
+    if (c->cache.bits == 16)
+      launch<16>(a, blocks, s);
+    else if (c->cache.bits == 8)
+      launch<8>(a, blocks, s);
+    else
+      launch<4>(a, blocks, s);
+    if (hipGetLastError() != hipSuccess) return CONQUR_EHIP;
+  }
+  return CONQUR_OK;
 }

@@ -244,3 +244,24 @@ def test_gather_without_places():
             if 0 <= f < cache.pages and 0 <= to < cache.pages:
                 want[to, :, i % 16] = k[f, :, t % 16]
     assert torch.equal(want.view(torch.int16), cache.k.cpu().view(torch.int16))
+
+
+def test_gather_of_many_sequences_and_heads():
+    """More workgroups than a launch holds: the first sequences' tokens, some between and the last one's."""
+    from paper_2605_10793_amd import attention as A
+    heads, n = 512, 65535
+    cache = A.KVCache.empty(8, heads, 16, 64, 16, DEV)
+    cache.k.copy_(torch.arange(cache.k.numel(), dtype=torch.int32, device=DEV).view(torch.int16)[:cache.k.numel()].view(cache.k.shape).view(torch.bfloat16))
+    cache.v.copy_(cache.k.flip(0).reshape(cache.v.shape))
+    counts = torch.zeros(n, dtype=torch.int32)
+    table, to_table = torch.full((n, 1), -1, dtype=torch.int32), torch.full((n, 1), -1, dtype=torch.int32)
+    for b, to in ((0, 1), (32764, 2), (32768, 3), (n - 1, 4)):
+        counts[b], table[b], to_table[b] = 3, 0, to
+    tokens = torch.tensor([9, 2, 11] * 4, dtype=torch.int32)
+    start = torch.cat([torch.zeros(1, dtype=torch.int32), counts.cumsum(0).to(torch.int32)])
+    k, v = (x.view(torch.int16).clone() for x in (cache.k, cache.v))
+    A.gather(cache, tokens.to(DEV), start.to(DEV), table.to(DEV), to_table.to(DEV))
+    for to in (1, 2, 3, 4):
+        k[to, :, :3] = k[0][:, [9, 2, 11]]
+        v[to, :, :, :3] = v[0][:, :, [9, 2, 11]]
+    assert torch.equal(k, cache.k.view(torch.int16)) and torch.equal(v, cache.v.view(torch.int16))
