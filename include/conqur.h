@@ -501,8 +501,8 @@ typedef struct {
   uint64_t workspace_bytes;
   uint32_t max_query;        /* largest count of new tokens of a sequence, times the query heads of a cache head below 2^24; tokens beyond it get no result */
   uint32_t window;           /* tokens that a token sees at most, itself the last; 0: no such limit */
-  float cap;                 /* >= 0, finite; 0: none */
-  float scale;               /* finite */
+  float cap;                 /* 0: none; up to 4096 (of larger caps 32 bits leave less of a score than weights in bf16 hold); 1 / cap and scale / cap finite */
+  float scale;               /* finite, as is 3 scale */
   uint32_t zero_rest;        /* 1: rows that get no result (of no sequence, beyond max_query) get zeros; 0: they stay as they are */
   uint32_t reserved;
 } conqur_chunk_call;
@@ -535,12 +535,14 @@ typedef struct {
   const int32_t* first;      /* one per token, in tokens of its sequence: the first key that it sees; NULL: 0               */
   const int32_t* last;       /* ... the last key that it sees, plus 1 (clamped to the sequence's tokens); NULL: itself       */
   const float* slopes;       /* one per query head; NULL: none                                                              */
-  uint64_t tokens;           /* tokens * (q.heads / k.heads) below 2^31 - 256; 0: nothing is done                            */
+  uint64_t tokens;           /* tokens * (q.heads / k.heads) below 2^31 - 256; 0: nothing is done.  (That product / 128 + sequences + 2) * k.heads
+                                below 2^24; backward: (tokens / 64 + sequences + 2) * k.heads below 2^23                    */
   uint32_t sequences;        /* 1 to 65535                                                                                  */
   uint32_t width;            /* 32, 64, 80, 96 or 128                                                                       */
   uint32_t window;           /* tokens that a token sees at most, itself the last; 0: no such limit                          */
-  float cap;                 /* >= 0, finite; 0: none                                                                       */
-  float scale;               /* finite                                                                                      */
+  float cap;                 /* 0: none; up to 4096 (of larger caps 32 bits leave less of a score than weights in bf16 hold);
+                                1 / cap and scale / cap finite                                                              */
+  float scale;               /* finite, as is 3 scale                                                                       */
   uint32_t zero_rest;        /* 1: rows of no sequence get zeros (lse -inf); 0: they stay as they are                        */
   void* workspace;           /* 16-byte aligned; its content does not matter.  Calls that overlap in time need one each      */
   uint64_t workspace_bytes;

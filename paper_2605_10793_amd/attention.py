@@ -394,7 +394,7 @@ def chunk_attention(q, cache: KVCache, start, prefix, table, first=None, last=No
     """Attention of any number of new tokens q (bf16 [tokens, heads, width]; packed as in `append`, which has put their keys and values into the
     cache) over their sequences' tokens, committed and new.  A token sees itself and those before it, or those from first on up to, not including, last
     (int32, one per row of q, counted in tokens of the sequence; first >= last: nothing, zeros); window: and at most that many, itself the last.
-    cap: scores become cap tanh(score / cap); slopes (fp32 [heads]): less slope times the distance.  max_query: most new tokens of a
+    cap (up to 4096): scores become cap tanh(score / cap); slopes (fp32 [heads]): less slope times the distance.  max_query: most new tokens of a
     sequence, max_context: most tokens, committed and new (default: what q and the table hold; closer bounds choose the quicker kernel and share the work
     out better).  scale: 1 / sqrt(width) unless given.  Returns out.  Rows beyond max_query of a sequence and rows of no sequence are zeros in a new tensor and stay as
     they are in a given `out`."""
@@ -466,7 +466,7 @@ def attention(q, k, v, start, first=None, last=None, window: int = 0, cap: float
     heads (up to 64 times); start (int32 [sequences + 1], not falling): sequence b's tokens are the rows [start[b], start[b + 1]).  width: 32, 64, 80, 96
     or 128.  A token sees itself and those before it, or, of its sequence's tokens, those from first on up to, not including, last (int32, one per
     row of q): documents in a sequence, prefixes seen from both sides, padding that sees nothing (first >= last: zeros); window: and at most that many, itself the
-    last.  cap: scores become cap tanh(score / cap); slopes (fp32 [heads]): less slope times the distance.  scale: 1 / sqrt(width) unless given.
+    last.  cap (up to 4096): scores become cap tanh(score / cap); slopes (fp32 [heads]): less slope times the distance.  scale: 1 / sqrt(width) unless given.
     Returns out, or (out, lse): fp32 [tokens, heads], the logarithms of the rows' sums.  Rows of no sequence are zeros in a new tensor (lse -inf)
     and stay as they are in a given `out` (their lse is then not written)."""
     if (q.requires_grad or k.requires_grad or v.requires_grad) and torch.is_grad_enabled():

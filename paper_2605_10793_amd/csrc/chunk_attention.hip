@@ -99,7 +99,7 @@ uint64_t workspace_of(const conqur_chunk_call& c, const Plan& p) {
 
 bool call_fine(const conqur_chunk_call* c) {
   if (!c || !cache_fine(c->cache) || !batch_fine(c->batch) || c->tokens >= 1ull << 31 || c->max_context >= 1ull << 31) return false;
-  if (!isfinite(c->scale) || !isfinite(c->cap) || c->cap < 0.0f || c->window >= 1u << 31 || c->max_query < 1) return false;
+  if (!scores_fine(c->scale, c->cap) || c->window >= 1u << 31 || c->max_query < 1) return false;
   if (c->q.heads < 1 || c->q.heads % c->cache.heads || c->q.heads / c->cache.heads > 64 || c->out.heads != c->q.heads) return false;
   return c->max_query * (c->q.heads / c->cache.heads) < 1ull << 24;
 }

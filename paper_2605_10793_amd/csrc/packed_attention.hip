@@ -256,11 +256,14 @@ bool plain(const conqur_heads& h) {
 }
 
 bool call_fine(const conqur_attention_call* c) {
-  if (!c || c->sequences < 1 || c->sequences > 65535 || !isfinite(c->scale) || !isfinite(c->cap) || c->cap < 0.0f || c->window >= 1u << 31) return false;
+  if (!c || c->sequences < 1 || c->sequences > 65535 || !scores_fine(c->scale, c->cap) || c->window >= 1u << 31) return false;
   if (c->width != 32 && c->width != 64 && c->width != 80 && c->width != 96 && c->width != 128) return false;
   if (c->k.heads < 1 || c->k.heads > 65535 || c->q.heads < 1 || c->q.heads % c->k.heads || c->q.heads / c->k.heads > 64) return false;
   if (c->tokens >= 1ull << 31 || c->tokens * (c->q.heads / c->k.heads) >= (1ull << 31) - 256) return false;
-  return ((c->tokens * (c->q.heads / c->k.heads)) / kRows + c->tokens / kTile + c->sequences + 2) * c->k.heads < 1ull << 31;
+  return ((c->tokens * (c->q.heads / c->k.heads)) / kRows + c->sequences + 2) * c->k.heads < 1ull << 24;          // workgroups of 256 threads, which 32 bits count
+}
+bool backward_fine(const conqur_attention_call* c) {
+  return call_fine(c) && (c->tokens / kTile + c->sequences + 2) * c->k.heads < 1ull << 23;          // ... of 512
 }
 
 uint64_t lay_bytes(const conqur_attention_call& c, const conqur_heads& h) { return plain(h) ? 0 : (c.tokens * h.heads * c.width * 2 + 255) / 256 * 256; }
@@ -366,13 +369,13 @@ extern "C" conqur_status conqur_attention(const conqur_attention_call* c, void* 
 }
 
 extern "C" uint64_t conqur_attention_backward_workspace(const conqur_attention_call* c) {
-  if (!call_fine(c)) return 0;
+  if (!backward_fine(c)) return 0;
   const BackwardSizes z = backward_sizes(*c);
   return z.stat + z.seen + z.span + z.part + lay_bytes(*c, c->q) + lay_bytes(*c, c->k) + lay_bytes(*c, c->v) + lay_bytes(*c, c->out) + lay_bytes(*c, c->out_grad);
 }
 
 extern "C" conqur_status conqur_attention_backward(const conqur_attention_call* c, void* stream) {
-  if (!call_fine(c)) return CONQUR_EINVAL;
+  if (!backward_fine(c)) return CONQUR_EINVAL;
   if (c->tokens == 0) return CONQUR_OK;
   const uint64_t q = c->q.heads, k = c->k.heads;
   if (!heads_fine(c->q, q, c->width, c->tokens, false) || !heads_fine(c->k, k, c->width, c->tokens, false) ||

@@ -141,3 +141,22 @@ def test_rows_in_parts(counts, heads, kv, width, options):
 
 def test_contiguous_rows():
     check([100, 30], 4, 4, 128, seed=24, strided=False)
+
+
+@pytest.mark.parametrize("cap", [200.0, 4096.0])
+def test_large_caps(cap):
+    """Scores next to zero under a cap that is far from them: what is left of cap - 2 cap / (1 + e^(2 u / cap)) is off by cap 2^-23, twice that with the
+    products before it, and the weights and their sum by so much of themselves."""
+    from paper_2605_10793_amd import attention as A
+    counts, heads, kv, width = [150, 70], 4, 2, 64
+    host, dev, start = inputs(counts, heads, kv, width, 5)
+    out, lse = A.attention(*dev[:3], start, cap=cap, lse=True)
+    at = 0
+    for n in counts:
+        rows = slice(at, at + n)
+        seen = seen_of(n, None, None, 0)
+        want, free = (attend(*(x[rows] for x in host[:3]), seen, torch.arange(n), width ** -0.5, c) for c in (cap, 0.0))
+        more = cap * 2.0 ** -22
+        close(out[rows], want["out"], free["out_tol"] + 2 * more * host[2][rows].abs().max().double(), "out")
+        close(lse[rows], want["lse"], free["lse_tol"] + more, "lse")
+        at += n

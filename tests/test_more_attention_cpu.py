@@ -65,6 +65,31 @@ def test_attention_arguments():
         assert lib.conqur_attention_backward(attention_call(**room), None) == binding.EINVAL
 
 
+@pytest.mark.parametrize("cap,scale,fine", [(4096.0, 0.1, True), (4100.0, 0.1, False), (1e30, 0.1, False), (1e-37, 0.1, True), (1e-40, 0.1, False), (1e-20, 1e20, False),
+                                            (0.0, 1e38, True), (0.0, 3e38, False), (50.0, 0.0, True), (50.0, -0.1, True)])
+def test_caps_and_scales_that_32_bits_hold(cap, scale, fine):
+    """A capped score is off by cap 2^-23, and what is divided by the cap must not overflow."""
+    lib = binding.load()
+    want = binding.OK if fine else binding.EINVAL
+    assert lib.conqur_attention(attention_call(cap=cap, scale=scale, tokens=0), None) == want
+    assert lib.conqur_attention_backward(attention_call(cap=cap, scale=scale, tokens=0), None) == want
+    assert lib.conqur_chunk_attention(chunk_call(cap=cap, scale=scale, tokens=0), None) == want
+
+
+def test_workgroups_that_32_bits_count():
+    """Sequences times key heads, however few the tokens: a launch holds fewer than 2^32 threads."""
+    lib = binding.load()
+
+    def call(sequences, heads, tokens=0):
+        return attention_call(sequences=sequences, tokens=tokens, q=(0x10000, heads * 128, 128, heads), k=(0x20000, heads * 128, 128, heads),
+                              v=(0x30000, heads * 128, 128, heads), out=(0x40000, heads * 128, 128, heads))
+    for sequences, heads, forward, backward in ((65535, 64, True, True), (65535, 200, True, False), (65535, 256, False, False), (1000, 65535, False, False),
+                                                (120, 65535, True, True), (250, 65535, True, False)):
+        assert lib.conqur_attention(call(sequences, heads), None) == (binding.OK if forward else binding.EINVAL)
+        assert lib.conqur_attention_backward(call(sequences, heads), None) == (binding.OK if backward else binding.EINVAL)
+        assert bool(lib.conqur_attention_backward_workspace(call(sequences, heads, 1))) == backward
+
+
 def test_workspace_of_rows_that_are_laid_out():
     """None for rows at multiples of 16 bytes; a copy for each tensor whose are not, or lie far apart."""
     lib = binding.load()
