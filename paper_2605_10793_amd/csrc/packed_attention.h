@@ -163,6 +163,31 @@ struct Tile {
   static __device__ __forceinline__ bf16x8 rows(uint32_t at, int s) {
     return *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)(anew(at ^ (uint32_t)(s << 5)) + BEHIND);
   }
+  // The same from a lane's places in one tile, made once for all operands.
+  struct RowsAt {
+    uint32_t at[KS];
+    __device__ __forceinline__ explicit RowsAt(uint32_t x) {
+#pragma unroll
+      for (int s = 0; s < KS; ++s) at[s] = anew(x ^ (uint32_t)(s << 5));
+    }
+    template <int BEHIND>
+    __device__ __forceinline__ bf16x8 get(int s) const { return *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)(at[s] + BEHIND); }
+  };
+  struct TurnedAt {
+    uint32_t at[2 * kTiles];
+    __device__ __forceinline__ explicit TurnedAt(uint32_t x) {
+#pragma unroll
+      for (int t = 0; t < 2 * kTiles; ++t) at[t] = anew(x ^ (uint32_t)(t << 5));
+    }
+    template <int BEHIND>
+    __device__ __forceinline__ bf16x8 get(int t) const {
+      typedef __attribute__((address_space(3))) s16x4* P;
+      const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(at[2 * t] + BEHIND));
+      const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(at[2 * t + 1] + BEHIND + 8 * kPitch));
+      const u32x2 p = __builtin_bit_cast(u32x2, a), q = __builtin_bit_cast(u32x2, b);
+      return frag_of(p[0], p[1], q[0], q[1]);
+    }
+  };
   // Turned round: lane's entry 32 t + (lane & 31), rows {4 h .. 4 h + 3, 8 + 4 h .. 8 + 4 h + 3}.
   static __device__ __forceinline__ uint32_t turned_at(int lane) {
     const int l = lane & 15, half = lane >> 5, part = (lane >> 4) & 1, row = 4 * half + (l >> 2);
@@ -299,6 +324,17 @@ __device__ __forceinline__ bool clear_nonfinite(uint32_t tile, int wave, int lan
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float x;
   asm("v_max3_f32 %0, %1, %2, %3" : "=v"(x) : "v"(a), "v"(b), "v"(c));
+  return x;
+}
+
+// The largest of 16 and one more.  (In one piece: between two instructions of its own assembly the compiler leaves a pause.)
+__device__ __forceinline__ float max17(const f32x16& s, float more) {
+  float x;
+  asm("v_max3_f32 %0, %1, %2, %3\n\tv_max3_f32 %0, %0, %4, %5\n\tv_max3_f32 %0, %0, %6, %7\n\tv_max3_f32 %0, %0, %8, %9\n\t"
+      "v_max3_f32 %0, %0, %10, %11\n\tv_max3_f32 %0, %0, %12, %13\n\tv_max3_f32 %0, %0, %14, %15\n\tv_max3_f32 %0, %0, %16, %17"
+      : "=&v"(x)
+      : "v"(s[0]), "v"(s[1]), "v"(s[2]), "v"(s[3]), "v"(s[4]), "v"(s[5]), "v"(s[6]), "v"(s[7]), "v"(s[8]), "v"(s[9]), "v"(s[10]), "v"(s[11]), "v"(s[12]), "v"(s[13]),
+        "v"(s[14]), "v"(s[15]), "v"(more));
   return x;
 }
 

@@ -96,18 +96,14 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed(const PackedArgs) {
     const bool all = kb >= low_all && kb + kTile <= high_all;
 
     const int here = lane_anew();
-    const uint32_t row_at = sk + T::row_at(here), turned_at = sv + T::turned_at(here);
+    const typename T::RowsAt row_at(sk + T::row_at(here));
+    const uint32_t turned_at = sv + T::turned_at(here);
     f32x16 s[2] = {f32x16{}, f32x16{}};
-    in_turn<2 * KS>([&](auto i) { return T::template rows<decltype(i)::value % 2 * 32 * T::kPitch>(row_at, decltype(i)::value / 2); },
+    in_turn<2 * KS>([&](auto i) { return row_at.template get<decltype(i)::value % 2 * 32 * T::kPitch>(decltype(i)::value / 2); },
                     [&](auto i, bf16x8 f) { s[decltype(i)::value % 2] = mfma32(f, qf[decltype(i)::value / 2], s[decltype(i)::value % 2]); });
 
     const float base = m == -INFINITY ? 0.0f : m;
-    if (!OPTIONS && all) {
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[u][r] = fmaf(s[u][r], scale, -base);
-    } else {
+    {
       if (OPTIONS && cap != 0.0f) {
 #pragma unroll
         for (int u = 0; u < 2; ++u)
@@ -120,7 +116,11 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed(const PackedArgs) {
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[u][r] = fmaf(s[u][r], scale, -base);
+          for (int r = 0; r < 16; ++r) {
+            float x = fmaf(s[u][r], scale, -base);
+            asm volatile("" : "+v"(x));
+            s[u][r] = x;
+          }
       }
       if (OPTIONS && slope != 0.0f) {
         const float at = (float)(token - kb - 4 * h);
@@ -138,10 +138,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed(const PackedArgs) {
       }
     }
 
-    float top = max3(s[0][0], s[1][0], s[0][1]);
-#pragma unroll
-    for (int r = 1; r < 15; ++r) top = max3(top, s[1][r], s[0][r + 1]);
-    top = fmaxf(top, s[1][15]);
+    float top = max17(s[1], max17(s[0], -INFINITY));
     if (__any(top > (m == -INFINITY ? -INFINITY : kRise))) {
       top = halves(top, [](float x, float y) { return fmaxf(x, y); });
       const bool unset = m == -INFINITY;
@@ -164,10 +161,11 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed(const PackedArgs) {
         p[u][r] = f32x2_to_bf16x2(__builtin_amdgcn_exp2f(s[u][2 * r]), __builtin_amdgcn_exp2f(s[u][2 * r + 1]));
         l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, p[u][r]), ones, l, false);
       }
+    const typename T::TurnedAt values(turned_at);
     // Operand i of V: 16 keys, 32 entries.
     auto value = [&](auto i) {
       constexpr int I = decltype(i)::value, K = I / T::kTiles;
-      return T::template turned<K * 16 * T::kPitch>(turned_at, I % T::kTiles);
+      return values.template get<K * 16 * T::kPitch>(I % T::kTiles);
     };
     in_turn<4 * T::kTiles>(value, [&](auto i, bf16x8 f) {
       constexpr int I = decltype(i)::value, K = I / T::kTiles;
