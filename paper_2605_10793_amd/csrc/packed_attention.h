@@ -16,6 +16,7 @@ constexpr int kWaves = 4;
 constexpr int kTile = 64;                         // keys, or rows, that lie in LDS at a time
 constexpr int kRows = 32 * kWaves;                // rows of a workgroup: query heads of a key head, token by token
 constexpr float kRise = 16.0f;                    // by how much (log2) scores may exceed the maximum they are taken against, before it and all results are raised
+enum { kBiased = 1, kCapped = 2 };                // OPTIONS of the kernels: a bias by distance, capped scores; both (of the gradients: kCapped, too)
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct Rows {
@@ -206,6 +207,10 @@ struct Tile {
 // N products whose operands come from LDS: RING of them are on their way ahead of the products that take them, and nothing but arithmetic passes from one to
 // the next (the compiler would hold more of them than there are registers).  load(i), use(i, operand): i as a constant.
 constexpr int kArithmetic = 0x6;
+template <int FROM, int TO, typename F>
+__device__ __forceinline__ void each_from(F&& f) {
+  each<TO - FROM>([&](auto i) { f(std::integral_constant<int, FROM + decltype(i)::value>{}); });
+}
 template <int N, int RING = 4, typename Load, typename Use>
 __device__ __forceinline__ void in_turn(Load load, Use use) {
   decltype(load(std::integral_constant<int, 0>{})) ring[RING];
@@ -328,7 +333,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 
 // The largest of 16 and one more.  (In one piece: between two instructions of its own assembly the compiler leaves a pause.)
-__device__ __forceinline__ float max17(const f32x16& s, float more) {
+__device__ __forceinline__ float max17(const float (&s)[16], float more) {
   float x;
   asm("v_max3_f32 %0, %1, %2, %3\n\tv_max3_f32 %0, %0, %4, %5\n\tv_max3_f32 %0, %0, %6, %7\n\tv_max3_f32 %0, %0, %8, %9\n\t"
       "v_max3_f32 %0, %0, %10, %11\n\tv_max3_f32 %0, %0, %12, %13\n\tv_max3_f32 %0, %0, %14, %15\n\tv_max3_f32 %0, %0, %16, %17"

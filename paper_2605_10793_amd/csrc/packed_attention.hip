@@ -6,8 +6,14 @@
 // in one pass over the keys, with running maxima and sums (in base 2).  The rows of a key head are its query heads times the tokens, token by token, so
 // that a workgroup's 128 rows are few tokens whose keys nearly coincide.  Both products run transposed, S^T = K Q^T and O^T = V^T P^T (32x32x16 bf16 MFMA): a
 // column is a row of the call, so that a lane holds scores of one row, the maximum needs one exchange, factors on O^T are the lane's own, and S^T leaves the
-// first product as P^T has to enter the second: weights stay in registers.  64 keys and values at a time come to LDS without passing registers, one block
-// ahead of the products; V is turned round as it is read from there.
+// first product as P^T has to enter the second: weights stay in registers.  64 keys and values at a time come to LDS without passing registers, a block
+// (keys: two) ahead of the products; V is turned round as it is read from there.
+//
+// Bound by the matrix units' and the vector units' shares of a SIMD and by the clock that their load allows (the same calls over zeros take 0.85 of the time).
+// So that a wavefront gives both work at once, a block's scores become weights between the products of the next block's scores, and those become scores between
+// the products with V: 8 sequences of 2048 tokens, 32 and 8 heads of 128, 331 us for 348 (830 TFLOP/s over what is seen), one of 16384 at 1020 TFLOP/s.
+// Eight wavefronts to a workgroup (348 us), more operands on their way from LDS (340 for 339) and a fourth wavefront to a SIMD where registers leave
+// room for it (85.0 for 85.8) gave nothing.
 #include "packed_attention.h"
 
 namespace conqur {
@@ -15,7 +21,7 @@ namespace packed {
 
 namespace {
 
-template <int KS, bool OPTIONS>
+template <int KS, int OPTIONS>
 __global__ void __launch_bounds__(64 * kWaves, 2) k_packed(const PackedArgs) {
   using T = Tile<KS>;
   Args a = kernel_args();
@@ -60,135 +66,163 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed(const PackedArgs) {
   const int k_stride = (int)(a->k.ts * 2), v_stride = (int)(a->v.ts * 2);
   const bf16_bits* const k0 = a->k.data + (int64_t)item.first * a->k.ts + head * a->k.hs;
   const bf16_bits* const v0 = a->v.data + (int64_t)item.first * a->v.ts + head * a->v.hs;
-  const uint32_t lds = lds_of(shared);
-  auto send = [&](int kb, int which) {
-    send_tile<KS>(k0 + (int64_t)kb * a->k.ts, k_stride, item.count - kb, lds + which * 2 * T::kBytes, wave);
-    send_tile<KS>(v0 + (int64_t)kb * a->v.ts, v_stride, item.count - kb, lds + which * 2 * T::kBytes + T::kBytes, wave);
-  };
+  const uint32_t lds = lds_of(shared);          // two tiles of keys, two of values
+  auto send_keys = [&](int kb, int which) { send_tile<KS>(k0 + (int64_t)kb * a->k.ts, k_stride, item.count - kb, lds + which * T::kBytes, wave); };
+  auto send_values = [&](int kb, int which) { send_tile<KS>(v0 + (int64_t)kb * a->v.ts, v_stride, item.count - kb, lds + (2 + which) * T::kBytes, wave); };
 
   f32x16 o[T::kTiles];
 #pragma unroll
   for (int t = 0; t < T::kTiles; ++t) o[t] = f32x16{};
-  float m = -INFINITY, l = 0.0f;
-  const float scale = a->scale_log2, cap = a->cap_log2, cap_in = a->cap_in, slope = OPTIONS && a->slopes ? a->slopes[q_head] * kLog2e : 0.0f;
+  float m = -INFINITY, l = 0.0f, top = -INFINITY;
+  const float scale = a->scale_log2, cap = a->cap_log2, cap_in = a->cap_in, slope = OPTIONS & kBiased ? a->slopes[q_head] * kLog2e : 0.0f;
   const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+  float s[2][16];
+  f32x16 next[2];          // scores of a block, less the maximum so far; products of the next
+  // The wavefront's own blocks.
+  const int from = max(begin, low / kTile * kTile), to_end = min(high, end);
 
-  if (threadIdx.x == 0) *s_odd = 0;
-  if (begin < end) send(begin, 0);
-  int which = 0;
-  for (int kb = begin; kb < end; kb += kTile, which ^= 1) {
-    wait_loads<0>();
-    pipeline_barrier();
-    if (kb + kTile < end) send(kb + kTile, which ^ 1);
-    const uint32_t sk = lds + which * 2 * T::kBytes, sv = sk + T::kBytes;
-    // Values that are not finite must not meet rows that do not see them, for 0 * NaN is NaN: where some rows of the workgroup do not see all of the block they
-    // become zeros, and are added by themselves to the rows that do.
-    bool odd = false;
-    if (kb < low_both || kb + kTile > high_both) {
-      const int me = lane_anew();
-      const bool bad = clear_nonfinite<KS, kTile / kWaves>(sv, wave, me);
-      if (bad) *s_odd = 1;
-      if ((me & 3) == 0) s_bad[which * kTile + wave * 16 + (me >> 2)] = bad;
-      pipeline_barrier();
-      odd = *(volatile int*)s_odd;
-    }
-    if (kb >= high || kb + kTile <= low) continue;
-    const bool all = kb >= low_all && kb + kTile <= high_all;
-
-    const int here = lane_anew();
-    const typename T::RowsAt row_at(sk + T::row_at(here));
-    const uint32_t turned_at = sv + T::turned_at(here);
-    f32x16 s[2] = {f32x16{}, f32x16{}};
-    in_turn<2 * KS>([&](auto i) { return row_at.template get<decltype(i)::value % 2 * 32 * T::kPitch>(decltype(i)::value / 2); },
-                    [&](auto i, bf16x8 f) { s[decltype(i)::value % 2] = mfma32(f, qf[decltype(i)::value / 2], s[decltype(i)::value % 2]); });
-
+  // A score of the block at kb from its product; the block's maximum, and what is not seen.
+  auto score = [&](int kb, auto i) __attribute__((always_inline)) {
+    constexpr int u = decltype(i)::value / 16, r = decltype(i)::value % 16;
     const float base = m == -INFINITY ? 0.0f : m;
-    {
-      if (OPTIONS && cap != 0.0f) {
+    float x;
+    if constexpr (OPTIONS & kCapped) {
+      float none;
+      x = capped(next[u][r], cap, cap_in, base, &none);
+    } else {
+      x = fmaf(next[u][r], scale, -base);
+    }
+    if constexpr (OPTIONS & kBiased) x = fmaf(-slope, fabsf((float)(token - kb - 4 * h) - (float)(32 * u + row_of(r, 0))), x);
+    asm volatile("" : "+v"(x));
+    s[u][r] = x;
+  };
+  auto finish = [&](int kb) __attribute__((always_inline)) {
+    if (!(kb >= low_all && kb + kTile <= high_all)) {
+      const int lo = mine.x - kb - 4 * h, hi = mine.y - kb - 4 * h;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[u][r] = 32 * u + row_of(r, 0) >= lo && 32 * u + row_of(r, 0) < hi ? s[u][r] : -INFINITY;
+    }
+    top = max17(s[1], max17(s[0], -INFINITY));
+  };
+  // A block's weights and results (NOW), and the next one's products (NEXT): the products of one run while the other's scores become weights, and the other way round.
+  auto step = [&](int kb, int which, bool odd, auto now_, auto next_) __attribute__((always_inline)) {
+    constexpr bool NOW = decltype(now_)::value, NEXT = decltype(next_)::value;
+    if constexpr (NOW) {
+      if (__any(top > (m == -INFINITY ? -INFINITY : kRise))) {
+        top = halves(top, [](float x, float y) { return fmaxf(x, y); });
+        const bool unset = m == -INFINITY;
+        const float by = unset ? (top == -INFINITY ? 0.0f : top) : fmaxf(top, 0.0f);
+        m = unset ? top : m + by;
+        const float f = __builtin_amdgcn_exp2f(-fmaxf(by, 0.0f));          // (before the first score the sums are 0)
+        l *= f;
+#pragma unroll
+        for (int t = 0; t < T::kTiles; ++t) o[t] *= f;
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            float x;
-            s[u][r] = capped(s[u][r], cap, cap_in, base, &x);
-          }
-      } else {
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            float x = fmaf(s[u][r], scale, -base);
-            asm volatile("" : "+v"(x));
-            s[u][r] = x;
-          }
-      }
-      if (OPTIONS && slope != 0.0f) {
-        const float at = (float)(token - kb - 4 * h);
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[u][r] = fmaf(-slope, fabsf(at - (float)(32 * u + row_of(r, 0))), s[u][r]);
-      }
-      if (!all) {
-        const int lo = mine.x - kb - 4 * h, hi = mine.y - kb - 4 * h;
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[u][r] = 32 * u + row_of(r, 0) >= lo && 32 * u + row_of(r, 0) < hi ? s[u][r] : -INFINITY;
+          for (int r = 0; r < 16; ++r) s[u][r] -= by;
       }
     }
-
-    float top = max17(s[1], max17(s[0], -INFINITY));
-    if (__any(top > (m == -INFINITY ? -INFINITY : kRise))) {
-      top = halves(top, [](float x, float y) { return fmaxf(x, y); });
-      const bool unset = m == -INFINITY;
-      const float by = unset ? (top == -INFINITY ? 0.0f : top) : fmaxf(top, 0.0f);
-      m = unset ? top : m + by;
-      const float f = __builtin_amdgcn_exp2f(-fmaxf(by, 0.0f));          // (before the first score the sums are 0)
-      l *= f;
-#pragma unroll
-      for (int t = 0; t < T::kTiles; ++t) o[t] *= f;
-#pragma unroll
-      for (int u = 0; u < 2; ++u) s[u] -= by;
-    }
-
+    const int here = lane_anew();
     // Weights rounded to bf16, as the second product takes them; the sum that divides takes them so, too.
     uint32_t p[2][8];
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int r = 0; r < 8; ++r) {
-        p[u][r] = f32x2_to_bf16x2(__builtin_amdgcn_exp2f(s[u][2 * r]), __builtin_amdgcn_exp2f(s[u][2 * r + 1]));
-        l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, p[u][r]), ones, l, false);
-      }
-    const typename T::TurnedAt values(turned_at);
-    // Operand i of V: 16 keys, 32 entries.
-    auto value = [&](auto i) {
-      constexpr int I = decltype(i)::value, K = I / T::kTiles;
-      return values.template get<K * 16 * T::kPitch>(I % T::kTiles);
+    auto weigh = [&](auto i) __attribute__((always_inline)) {
+      constexpr int u = decltype(i)::value / 8, r = decltype(i)::value % 8;
+      p[u][r] = f32x2_to_bf16x2(__builtin_amdgcn_exp2f(s[u][2 * r]), __builtin_amdgcn_exp2f(s[u][2 * r + 1]));
+      l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, p[u][r]), ones, l, false);
     };
-    in_turn<4 * T::kTiles>(value, [&](auto i, bf16x8 f) {
-      constexpr int I = decltype(i)::value, K = I / T::kTiles;
-      const uint32_t* w = &p[K / 2][K % 2 * 4];
-      o[I % T::kTiles] = mfma32(f, frag_of(w[0], w[1], w[2], w[3]), o[I % T::kTiles]);
-    });
-    if (odd) {
-      for (int j = 0; j < kTile; ++j) {
-        const int key = kb + j;
-        if (!s_bad[which * kTile + j] || key >= item.count) continue;
-        const bool see = key >= mine.x && key < mine.y;
-        const bf16_bits* const from = v0 + (int64_t)key * a->v.ts + 4 * h;
+    if constexpr (NEXT) {
+      const typename T::RowsAt keys(lds + (which ^ 1) * T::kBytes + T::row_at(here));
+      next[0] = next[1] = f32x16{};
+      in_turn<2 * KS>([&](auto i) { return keys.template get<decltype(i)::value % 2 * 32 * T::kPitch>(decltype(i)::value / 2); },
+                         [&](auto i, bf16x8 f) {
+                           constexpr int I = decltype(i)::value;
+                           next[I % 2] = mfma32(f, qf[I / 2], next[I % 2]);
+                           if constexpr (NOW) each_from<I * 16 / (2 * KS), (I + 1) * 16 / (2 * KS)>(weigh);
+                         });
+    } else {
+      each<16>(weigh);
+    }
+    if constexpr (NOW) {
+      const typename T::TurnedAt values(lds + (2 + which) * T::kBytes + T::turned_at(here));
+      constexpr int N = 4 * T::kTiles;
+      // Operand i of V: 16 keys, 32 entries.
+      in_turn<N>(
+          [&](auto i) {
+            constexpr int I = decltype(i)::value, K = I / T::kTiles;
+            return values.template get<K * 16 * T::kPitch>(I % T::kTiles);
+          },
+          [&](auto i, bf16x8 f) {
+            constexpr int I = decltype(i)::value, K = I / T::kTiles;
+            const uint32_t* w = &p[K / 2][K % 2 * 4];
+            o[I % T::kTiles] = mfma32(f, frag_of(w[0], w[1], w[2], w[3]), o[I % T::kTiles]);
+            if constexpr (NEXT) each_from<(I * 32 / N), ((I + 1) * 32 / N)>([&](auto j) __attribute__((always_inline)) { score(kb + kTile, j); });
+          });
+      if (odd) {
+        for (int j = 0; j < kTile; ++j) {
+          const int key = kb + j;
+          if (!s_bad[which * kTile + j] || key >= item.count) continue;
+          const bool see = key >= mine.x && key < mine.y;
+          const bf16_bits* const from_v = v0 + (int64_t)key * a->v.ts + 4 * h;
 #pragma unroll
-        for (int t = 0; t < T::kTiles; ++t)
+          for (int t = 0; t < T::kTiles; ++t)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int entry = 32 * t + row_of(r, 0);
-            const uint32_t x = entry < KS * 16 ? from[entry] : 0;
-            o[t][r] += see && (x & 0x7f80u) == 0x7f80u ? __uint_as_float(x << 16) : 0.0f;
-          }
+            for (int r = 0; r < 16; ++r) {
+              const int entry = 32 * t + row_of(r, 0);
+              const uint32_t x = entry < KS * 16 ? from_v[entry] : 0;
+              o[t][r] += see && (x & 0x7f80u) == 0x7f80u ? __uint_as_float(x << 16) : 0.0f;
+            }
+        }
       }
     }
+    if constexpr (NEXT) {
+      if constexpr (!NOW) each<32>([&](auto j) __attribute__((always_inline)) { score(kb + kTile, j); });
+      finish(kb + kTile);
+    }
+  };
+
+  // What all wavefronts do at a block: wait for its values and the next keys, send for those behind.  Values that are not finite must not meet rows that do not see
+  // them, for 0 * NaN is NaN: where some rows of the workgroup do not see all of the block they become zeros, and are added by themselves to the rows that do.
+  auto arrive = [&](int kb, int which) __attribute__((always_inline)) {
+    wait_loads<0>();
+    pipeline_barrier();
+    if (kb + kTile < end) send_values(kb + kTile, which ^ 1);
+    if (kb + 2 * kTile < end) send_keys(kb + 2 * kTile, which);
+    if (kb >= low_both && kb + kTile <= high_both) return false;
+    const int me = lane_anew();
+    const bool bad = clear_nonfinite<KS, kTile / kWaves>(lds + (2 + which) * T::kBytes, wave, me);
+    if (bad) *s_odd = 1;
+    if ((me & 3) == 0) s_bad[which * kTile + wave * 16 + (me >> 2)] = bad;
+    pipeline_barrier();
+    return *(volatile int*)s_odd != 0;
+  };
+  if (threadIdx.x == 0) *s_odd = 0;
+  int which = 0, kb = begin;
+  if (begin < end) {
+    send_keys(begin, 0);
+    send_values(begin, 0);
+    if (begin + kTile < end) {
+      send_keys(begin + kTile, 1);
+      wait_loads<2 * T::kLoads>();
+    } else {
+      wait_loads<T::kLoads>();
+    }
+    pipeline_barrier();
   }
+  if (from < to_end) {
+    for (; kb < from; kb += kTile, which ^= 1) arrive(kb, which);
+    step(kb - kTile, which ^ 1, false, std::false_type{}, std::true_type{});
+    for (; kb + kTile < to_end; kb += kTile, which ^= 1) {
+      const bool odd = arrive(kb, which);
+      step(kb, which, odd, std::true_type{}, std::true_type{});
+    }
+    const bool odd = arrive(kb, which);
+    step(kb, which, odd, std::true_type{}, std::false_type{});
+    kb += kTile, which ^= 1;
+  }
+  for (; kb < end; kb += kTile, which ^= 1) arrive(kb, which);
 
   a = kernel_args();
   if (row >= rows) return;
@@ -200,7 +234,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed(const PackedArgs) {
   if (a->lse && h == 0) a->lse[row_token * (a->heads * group) + q_head] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * (1.0f / kLog2e);
 }
 
-template <int KS, bool OPTIONS>
+template <int KS, int OPTIONS>
 hipError_t launch(const PackedArgs& a, hipStream_t s) {
   constexpr int kShared = 4 * Tile<KS>::kBytes + 2 * kTile * 4 + 16;
   static PerDeviceOnce once;
@@ -211,7 +245,10 @@ hipError_t launch(const PackedArgs& a, hipStream_t s) {
 }
 
 template <int KS>
-hipError_t launch(const PackedArgs& a, hipStream_t s) { return a.cap_log2 != 0.0f || a.slopes ? launch<KS, true>(a, s) : launch<KS, false>(a, s); }
+hipError_t launch(const PackedArgs& a, hipStream_t s) {
+  if (a.cap_log2 != 0.0f) return a.slopes ? launch<KS, kBiased | kCapped>(a, s) : launch<KS, kCapped>(a, s);
+  return a.slopes ? launch<KS, kBiased>(a, s) : launch<KS, 0>(a, s);
+}
 
 }  // namespace
 

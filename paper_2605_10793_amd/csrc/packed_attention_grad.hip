@@ -19,7 +19,6 @@ __device__ __forceinline__ bf16x8 pack8(const f32x16& x, int k) {
                  f32x2_to_bf16x2(x[8 * k + 6], x[8 * k + 7]));
 }
 
-enum { kBiased = 1, kCapped = 2 };      // OPTIONS: a bias by distance; capped scores, with or without it
 constexpr int kKeys = 32;          // keys that lie in LDS at a time for k_packed_dq
 
 // Operands that each lane keeps in LDS because its registers are full: what goes to scratch memory instead comes back behind all that is on its way to LDS.
