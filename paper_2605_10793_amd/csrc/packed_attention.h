@@ -157,14 +157,9 @@ struct Tile {
   static __device__ __forceinline__ int f(int row) {
     return kChunks == 16 ? ((row & 3) << 2 | ((row >> 2) & 3)) : (((row >> 1) & 1) << 2 | ((row >> 2) & 3));
   }
-  // Operands from LDS.  `at`: a tile's place (a multiple of 256 bytes, more rows or tiles behind it as a constant) plus what the lane adds, row_at() or turned_at().
-  // Lane's row (lane & 31), entries 16 s + 8 h to 16 s + 8 h + 7.
+  // Operands from LDS.  A lane's places in a tile that lies at a multiple of 256 bytes are made once; more rows or tiles behind it are a constant (BEHIND).
+  // Of a lane: row (lane & 31), entries 16 s + 8 h to 16 s + 8 h + 7.
   static __device__ __forceinline__ uint32_t row_at(int lane) { return (lane & 31) * kPitch + ((((lane >> 5) ^ f(lane & 31))) << 4); }
-  template <int BEHIND>
-  static __device__ __forceinline__ bf16x8 rows(uint32_t at, int s) {
-    return *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)(anew(at ^ (uint32_t)(s << 5)) + BEHIND);
-  }
-  // The same from a lane's places in one tile, made once for all operands.
   struct RowsAt {
     uint32_t at[KS];
     __device__ __forceinline__ explicit RowsAt(uint32_t x) {
@@ -174,6 +169,11 @@ struct Tile {
     template <int BEHIND>
     __device__ __forceinline__ bf16x8 get(int s) const { return *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)(at[s] + BEHIND); }
   };
+  // Turned round: lane's entry 32 t + (lane & 31), rows {4 h .. 4 h + 3, 8 + 4 h .. 8 + 4 h + 3}.
+  static __device__ __forceinline__ uint32_t turned_at(int lane) {
+    const int l = lane & 15, half = lane >> 5, part = (lane >> 4) & 1, row = 4 * half + (l >> 2);
+    return row * kPitch + (((2 * part + ((l & 3) >> 1)) ^ f(row)) << 4) + (l & 1) * 8;
+  }
   struct TurnedAt {
     uint32_t at[2 * kTiles];
     __device__ __forceinline__ explicit TurnedAt(uint32_t x) {
@@ -189,19 +189,6 @@ struct Tile {
       return frag_of(p[0], p[1], q[0], q[1]);
     }
   };
-  // Turned round: lane's entry 32 t + (lane & 31), rows {4 h .. 4 h + 3, 8 + 4 h .. 8 + 4 h + 3}.
-  static __device__ __forceinline__ uint32_t turned_at(int lane) {
-    const int l = lane & 15, half = lane >> 5, part = (lane >> 4) & 1, row = 4 * half + (l >> 2);
-    return row * kPitch + (((2 * part + ((l & 3) >> 1)) ^ f(row)) << 4) + (l & 1) * 8;
-  }
-  template <int BEHIND>
-  static __device__ __forceinline__ bf16x8 turned(uint32_t at, int t) {
-    typedef __attribute__((address_space(3))) s16x4* P;
-    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(anew(at ^ (uint32_t)(t << 6)) + BEHIND));
-    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(anew(at ^ (uint32_t)(t << 6) ^ 32u) + BEHIND + 8 * kPitch));
-    const u32x2 p = __builtin_bit_cast(u32x2, a), q = __builtin_bit_cast(u32x2, b);
-    return frag_of(p[0], p[1], q[0], q[1]);
-  }
 };
 
 // N products whose operands come from LDS: RING of them are on their way ahead of the products that take them, and nothing but arithmetic passes from one to
@@ -325,14 +312,8 @@ __device__ __forceinline__ bool clear_nonfinite(uint32_t tile, int wave, int lan
   return (found >> (lane / kLanes * kLanes)) & ((1 << kLanes) - 1);
 }
 
-// The largest of three, whatever their sign; a NaN loses.  (For fmaxf of fmaxf the compiler first makes each argument canonical, an instruction more for each.)
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float x;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(x) : "v"(a), "v"(b), "v"(c));
-  return x;
-}
-
-// The largest of 16 and one more.  (In one piece: between two instructions of its own assembly the compiler leaves a pause.)
+// The largest of 16 and one more, whatever their sign; a NaN loses.  (For fmaxf of fmaxf the compiler first makes each argument canonical, an instruction more for
+// each; between two pieces of assembly it leaves a pause.)
 __device__ __forceinline__ float max17(const float (&s)[16], float more) {
   float x;
   asm("v_max3_f32 %0, %1, %2, %3\n\tv_max3_f32 %0, %0, %4, %5\n\tv_max3_f32 %0, %0, %6, %7\n\tv_max3_f32 %0, %0, %8, %9\n\t"

@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dq(const PackedArgs) 
     if (kb >= high || kb + kKeys <= low) continue;
     const bool all = kb >= low_all && kb + kKeys <= high_all;
     const int here = lane_anew();
-    const uint32_t row_at = sk + T::row_at(here), turned_at = sk + T::turned_at(here);
+    const typename T::RowsAt row_at(sk + T::row_at(here));
     struct Operands {
       bf16x8 rows, mine;
     };
@@ -146,11 +146,11 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dq(const PackedArgs) 
         [&](auto i) {
           constexpr int I = decltype(i)::value / 2;
           if constexpr (decltype(i)::value % 2)
-            return Operands{T::template rows<kBytes>(row_at, I), own(std::integral_constant<int, I>{})};
+            return Operands{row_at.template get<kBytes>(I), own(std::integral_constant<int, I>{})};
           else if constexpr (I < kQueriesInLds)
-            return Operands{T::template rows<0>(row_at, I), own(std::integral_constant<int, KS + I>{})};
+            return Operands{row_at.template get<0>(I), own(std::integral_constant<int, KS + I>{})};
           else
-            return Operands{T::template rows<0>(row_at, I), qf[I - kQueriesInLds]};
+            return Operands{row_at.template get<0>(I), qf[I - kQueriesInLds]};
         },
         [&](auto i, const Operands& f) {
           if constexpr (decltype(i)::value % 2)
@@ -205,7 +205,8 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dq(const PackedArgs) 
     const bf16x8 rest[2] = {pack8(d, 0), pack8(d, 1)};
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_setprio(1);
-    in_turn<2 * T::kTiles>([&](auto i) { return T::template turned<decltype(i)::value / T::kTiles * 16 * T::kPitch>(turned_at, decltype(i)::value % T::kTiles); },
+    const typename T::TurnedAt turned_at(sk + T::turned_at(here));
+    in_turn<2 * T::kTiles>([&](auto i) { return turned_at.template get<decltype(i)::value / T::kTiles * 16 * T::kPitch>(decltype(i)::value % T::kTiles); },
                            [&](auto i, bf16x8 f) {
                              constexpr int I = decltype(i)::value, t = I % T::kTiles;
                              dq[t] = mfma32(f, df[I / T::kTiles], dq[t]);
@@ -365,6 +366,7 @@ __global__ void __launch_bounds__(64 * kKeyWaves, 2) k_packed_dkv(const PackedAr
   Step now, then;
   bool more = next(&now);
   if (more) send(now.sub, 0);
+  if (wave >= 4) __builtin_amdgcn_s_setprio(1);          // of two wavefronts that share a SIMD, and begin a step together, one goes first: 376 -> 370 us, uneven prefixes
   for (int which = 0; more; which ^= 1, now = then) {
     more = next(&then);
     wait_loads<0>();
@@ -383,14 +385,9 @@ __global__ void __launch_bounds__(64 * kKeyWaves, 2) k_packed_dkv(const PackedAr
     const uint32_t sq = lds + which * kBuffer + at_rows * 32 * T::kPitch;           // the gradients lie behind the queries
     const unsigned char* const s_rows = shared + which * kBuffer + 2 * kBytes;
     const int here = lane_anew();
-    const uint32_t row_at = sq + T::row_at(here), turned_at = sq + T::turned_at(here);
+    const typename T::RowsAt row_at(sq + T::row_at(here));
     const int half = here >> 5;
 
-    // Operands of the queries and, odd ones, of the gradients: 16 rows, 32 entries.
-    auto turned = [&](auto i) {
-      constexpr int I = decltype(i)::value;
-      return T::template turned<I % 2 * kBytes + I / 2 / T::kTiles * 16 * T::kPitch>(turned_at, I / 2 % T::kTiles);
-    };
     f32x16 s = f32x16{}, d = f32x16{};
     struct Operands {
       bf16x8 rows, keys;
@@ -399,11 +396,11 @@ __global__ void __launch_bounds__(64 * kKeyWaves, 2) k_packed_dkv(const PackedAr
         [&](auto i) {
           constexpr int I = decltype(i)::value / 2;
           if constexpr (decltype(i)::value % 2)
-            return Operands{T::template rows<kBytes>(row_at, I), vf[I]};
+            return Operands{row_at.template get<kBytes>(I), vf[I]};
           else if constexpr (I < kKeysInLds)
-            return Operands{T::template rows<0>(row_at, I), *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)(keys_lds + I * 1024)};
+            return Operands{row_at.template get<0>(I), *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)(keys_lds + I * 1024)};
           else
-            return Operands{T::template rows<0>(row_at, I), kf[I - kKeysInLds]};
+            return Operands{row_at.template get<0>(I), kf[I - kKeysInLds]};
         },
         [&](auto i, const Operands& f) {
           if constexpr (decltype(i)::value % 2)
@@ -457,6 +454,12 @@ __global__ void __launch_bounds__(64 * kKeyWaves, 2) k_packed_dkv(const PackedAr
     }
     const bf16x8 pf[2] = {pack8(s, 0), pack8(s, 1)}, df[2] = {pack8(d, 0), pack8(d, 1)};
     __builtin_amdgcn_sched_barrier(0);
+    const typename T::TurnedAt turned_at(sq + T::turned_at(here));
+    // Operands of the queries and, odd ones, of the gradients: 16 rows, 32 entries.
+    auto turned = [&](auto i) {
+      constexpr int I = decltype(i)::value;
+      return turned_at.template get<I % 2 * kBytes + I / 2 / T::kTiles * 16 * T::kPitch>(I / 2 % T::kTiles);
+    };
     in_turn<4 * T::kTiles>(turned, [&](auto i, bf16x8 f) {
       constexpr int I = decltype(i)::value, t = I / 2 % T::kTiles, k = I / 2 / T::kTiles;
       if constexpr (I % 2)
