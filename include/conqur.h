@@ -548,7 +548,8 @@ typedef struct {
   uint64_t workspace_bytes;
 } conqur_attention_call;
 
-/* Bytes of workspace: none for rows that start at multiples of 16 bytes (and lie less than 8 MiB apart); others are laid out there first. */
+/* Bytes of workspace: none for rows that start at multiples of 16 bytes (and lie less than 8 MiB apart); others are laid out there first.  Calls of few rows with many keys
+ * leave their parts of results there, too. */
 uint64_t conqur_attention_workspace(const conqur_attention_call* call);
 conqur_status conqur_attention(const conqur_attention_call* call, void* stream);
 

@@ -43,6 +43,10 @@ struct PackedArgs {
   int4* span;                // [32 rows of an item] lowest first, highest last, highest first, lowest last (a row that sees nothing: highest first is INT_MAX)
   float* part;               // [part of the rows][64 keys][key head][32 of them][dk, dv]: sums over the part, as registers hold them
   int parts;                 // in which the rows that see 64 keys are taken
+  // Of keys that several workgroups share (splits > 1): what each made of its own, as registers hold it, and four numbers a row.
+  float* shared;             // [split][128 rows][key head][wavefront] ...
+  float4* shared_row;        // [split][128 rows][key head][row]
+  int splits;
 };
 
 // The arguments as a kernel reads them, where they lie: what a part of a kernel needs of them is read there and not kept in registers.
@@ -330,6 +334,22 @@ __device__ __forceinline__ float capped(float dot, float cap_log2, float cap_in,
   return fmaf(-2.0f * cap_log2, *r, cap_log2 - base);
 }
 
+// The part [*begin, *end) of a workgroup's keys, `tile` at a time, that is workgroup blockIdx.y's of gridDim.y.
+__device__ __forceinline__ void share_keys(int* begin, int* end, int tile) {
+  if (gridDim.y == 1 || *begin >= *end) return;
+  const int tiles = (*end - *begin + tile - 1) / tile, per = (tiles + (int)gridDim.y - 1) / (int)gridDim.y;
+  *begin += (int)blockIdx.y * per * tile;
+  *end = min(*end, *begin + per * tile);
+}
+// Where a wavefront's registers go: N float4 a lane.
+template <int N>
+__device__ __forceinline__ f32x4* shared_of(Args a, int split, int wave) {
+  return reinterpret_cast<f32x4*>(a->shared) + (((int64_t)split * gridDim.x + blockIdx.x) * kWaves + wave) * (N * 64) + ((int)threadIdx.x & 63);
+}
+__device__ __forceinline__ float4* shared_row_of(Args a, int split, int row) {
+  return a->shared_row + ((int64_t)split * gridDim.x + blockIdx.x) * kRows + row;
+}
+
 // Four neighbouring entries of a row's result.
 __device__ __forceinline__ void store4(bf16_bits* to, f32x4 x, bool wide) {
   const uint32_t a = f32x2_to_bf16x2(x[0], x[1]), b = f32x2_to_bf16x2(x[2], x[3]);
@@ -360,6 +380,14 @@ __device__ __forceinline__ void store_row(bf16_bits* to, const f32x16 (&x)[(KS +
     all(true);
   else
     all(false);
+}
+
+// The 32 entries t of a row.
+template <int KS>
+__device__ __forceinline__ void store_tile(bf16_bits* to, int t, const f32x16& x, float by, bool wide) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    if (32 * t + 8 * r < KS * 16) store4(to + 32 * t + 8 * r, f32x4{x[4 * r], x[4 * r + 1], x[4 * r + 2], x[4 * r + 3]} * by, wide);
 }
 
 // Items of the rows, and of the keys, of a call.

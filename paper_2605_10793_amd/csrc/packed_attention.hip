@@ -57,6 +57,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed(const PackedArgs) {
     if (part * kRows + wave * 32 >= rows) high = 0;
   }
   begin = begin / kTile * kTile;
+  share_keys(&begin, &end, kTile);
 
   const int64_t row_token = item.first + token;
   const int q_head = head * group + (row < rows ? row : rows - 1) - token * group;
@@ -225,13 +226,54 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed(const PackedArgs) {
   for (; kb < end; kb += kTile, which ^= 1) arrive(kb, which);
 
   a = kernel_args();
-  if (row >= rows) return;
   l = halves(l, [](float x, float y) { return x + y; });
+  if (gridDim.y > 1) {
+    f32x4* const to = shared_of<4 * T::kTiles>(a, (int)blockIdx.y, wave);
+#pragma unroll
+    for (int t = 0; t < T::kTiles; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) to[(t * 4 + r) * 64] = f32x4{o[t][4 * r], o[t][4 * r + 1], o[t][4 * r + 2], o[t][4 * r + 3]};
+    if (h == 0) *shared_row_of(a, (int)blockIdx.y, wave * 32 + lane) = make_float4(m, l, 0.0f, 0.0f);
+    return;
+  }
+  if (row >= rows) return;
   // Nothing seen, or every score -inf: zeros.
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   bf16_bits* const to = a->out.data + row_token * a->out.ts + q_head * a->out.hs + 4 * h;
   store_row<KS>(to, o, inv, wide8(a->out.data, a->out.ts, a->out.hs));
   if (a->lse && h == 0) a->lse[row_token * (a->heads * group) + q_head] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * (1.0f / kLog2e);
+}
+
+// What workgroups that share keys made, joined, for 32 entries of a row (blockIdx.y).
+template <int KS>
+__global__ void __launch_bounds__(64 * kWaves) k_packed_join(const PackedArgs) {
+  using T = Tile<KS>;
+  const Args a = kernel_args();
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5, t = blockIdx.y;
+  const int head = blockIdx.x % a->heads, group = a->group;
+  Item item;
+  if (!item.find(a, blockIdx.x / a->heads, 7, group)) return;
+  const int row = (item.parts - 1 - item.part) * kRows + wave * 32 + (lane & 31);
+  if (row >= item.count * group) return;
+  float top = -INFINITY, l = 0.0f;
+  for (int i = 0; i < a->splits; ++i) top = fmaxf(top, shared_row_of(a, i, wave * 32 + (lane & 31))->x);
+  f32x16 o = {};
+  for (int i = 0; i < a->splits; ++i) {
+    const float4 x = *shared_row_of(a, i, wave * 32 + (lane & 31));
+    const float by = x.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(x.x - top);
+    const f32x4* const from = shared_of<4 * T::kTiles>(a, i, wave) + t * 4 * 64;
+    l = fmaf(x.y, by, l);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const f32x4 y = from[r * 64];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[4 * r + j] = fmaf(y[j], by, o[4 * r + j]);
+    }
+  }
+  const int token = (int)((uint32_t)row / (uint32_t)group), q_head = head * group + row - token * group;
+  const int64_t row_token = item.first + token;
+  store_tile<KS>(a->out.data + row_token * a->out.ts + q_head * a->out.hs + 4 * h, t, o, l == 0.0f ? 0.0f : 1.0f / l, wide8(a->out.data, a->out.ts, a->out.hs));
+  if (a->lse && h == 0 && t == 0) a->lse[row_token * (a->heads * group) + q_head] = l == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * (1.0f / kLog2e);
 }
 
 template <int KS, int OPTIONS>
@@ -240,7 +282,11 @@ hipError_t launch(const PackedArgs& a, hipStream_t s) {
   static PerDeviceOnce once;
   const hipError_t e = once.run([] { return hipFuncSetAttribute(reinterpret_cast<const void*>(k_packed<KS, OPTIONS>), hipFuncAttributeMaxDynamicSharedMemorySize, kShared); });
   if (e != hipSuccess) return e;
-  k_packed<KS, OPTIONS><<<dim3((uint32_t)(row_items(a) * a.heads)), 64 * kWaves, kShared, s>>>(a);
+  const uint32_t workgroups = (uint32_t)(row_items(a) * a.heads);
+  k_packed<KS, OPTIONS><<<dim3(workgroups, (uint32_t)a.splits), 64 * kWaves, kShared, s>>>(a);
+  const hipError_t x = hipGetLastError();
+  if (x != hipSuccess || a.splits == 1) return x;
+  k_packed_join<KS><<<dim3(workgroups, Tile<KS>::kTiles), 64 * kWaves, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -302,14 +348,37 @@ bool backward_fine(const conqur_attention_call* c) {
 }
 
 uint64_t lay_bytes(const conqur_attention_call& c, const conqur_heads& h) { return plain(h) ? 0 : (c.tokens * h.heads * c.width * 2 + 255) / 256 * 256; }
+// How many workgroups share the keys of 128 rows, whose results a second launch joins.  A workgroup takes the keys that its rows see one block after the other;
+// with fewer workgroups than the device takes at a time (two to a compute unit), the last rows' keys are what all wait for.  As many as make 512, of 256 keys or more
+// each, if that saves the wait for 1024 keys or more: 4000 tokens, 4 heads, 1 key head, width 128: 80 us in one part, 46 in four, its gradients 376 and 236; one head of width
+// 64: 62 and 26 in fifteen; 8 heads, 8 key heads: 80 and 72 in two.  1000 tokens, 32 heads, 8 key heads: 27, and 33 in two.
+int key_splits(const conqur_attention_call& c) {
+  if (!c.sequences || !c.k.heads) return 1;
+  uint64_t seeing = c.tokens / c.sequences;
+  if (c.window && c.window < seeing) seeing = c.window;
+  const uint64_t rows = c.tokens * (c.q.heads / c.k.heads), workgroups = (rows / kRows + c.sequences) * c.k.heads;
+  const uint64_t fill = workgroups ? 512 / workgroups : 1, most = fill < 16 ? fill : 16, n = seeing / 256 < most ? seeing / 256 : most;
+  return n < 2 || seeing - seeing / n < 1024 ? 1 : (int)n;
+}
+struct ShareSizes {
+  uint64_t rows, registers;
+};
+// each: entries that a row leaves.
+ShareSizes share_sizes(const conqur_attention_call& c, int splits, int each) {
+  if (splits == 1) return {0, 0};
+  const uint64_t rows = (c.tokens * (c.q.heads / c.k.heads) / kRows + c.sequences + 2) * c.k.heads * kRows * splits, width = (c.width + 31) / 32 * 32;
+  return {rows * sizeof(float4), rows * width * each * sizeof(float)};
+}
+
 struct BackwardSizes {
   uint64_t stat, seen, span, part;
-  int parts;
+  int parts, splits;
+  ShareSizes share;
 };
 // In how many parts the rows of 64 keys are taken, by as many workgroups, whose sums a kernel of its own adds up.  A workgroup takes what sees its keys one step
 // of 128 rows after the other; with fewer workgroups than the device takes at a time (one to a compute unit), the first keys' rows are what the others wait for.
 // As many parts as make 512 workgroups (half the rows see a key, on average), of four steps or more: gradients of 2000 tokens, 8 heads, 1 key head, width 128:
-// 344 us in one part, 200 in 15; 1000 tokens, 32 heads, 8 key heads: 125 and 115; 2 of 1500 tokens, 40 heads, 8 key heads (384 workgroups): 280, and 314 in two.
+// 344 us in one part, 200 in 15 (164 since keys are shared, too); 1000 tokens, 32 heads, 8 key heads: 125 and 115; 2 of 1500 tokens, 40 heads, 8 key heads (384 workgroups): 280, and 314 in two.
 int key_parts(const conqur_attention_call& c, uint64_t workgroups) {
   if (!c.sequences) return 1;
   uint64_t seeing = c.tokens / c.sequences;
@@ -324,7 +393,7 @@ BackwardSizes backward_sizes(const conqur_attention_call& c) {
   const uint64_t items = (c.tokens / kTile + c.sequences + 2) * c.k.heads, width = (c.width + 31) / 32 * 32;
   const int parts = key_parts(c, items);
   return {up((rows * c.k.heads + 128) * stat), up((rows + 128) * sizeof(int2)), up((rows / kRows + c.sequences + 2) * kWaves * sizeof(int4)),
-          parts > 1 ? parts * items * kTile * width * 2 * sizeof(float) : 0, parts};
+          parts > 1 ? parts * items * kTile * width * 2 * sizeof(float) : 0, parts, key_splits(c), share_sizes(c, key_splits(c), 2)};
 }
 
 PackedArgs args_of(const conqur_attention_call& c) {
@@ -346,6 +415,7 @@ PackedArgs args_of(const conqur_attention_call& c) {
   a.width = (int)c.width;
   a.window = (int)c.window;
   a.rest = c.zero_rest != 0;
+  a.splits = key_splits(c);
   a.scale = c.scale;
   a.scale_log2 = c.scale * kLog2e;
   a.cap_log2 = c.cap * kLog2e;
@@ -383,7 +453,8 @@ using namespace conqur::packed;
 
 extern "C" uint64_t conqur_attention_workspace(const conqur_attention_call* c) {
   if (!call_fine(c)) return 0;
-  return lay_bytes(*c, c->q) + lay_bytes(*c, c->k) + lay_bytes(*c, c->v);
+  const ShareSizes share = share_sizes(*c, key_splits(*c), 1);
+  return share.rows + share.registers + lay_bytes(*c, c->q) + lay_bytes(*c, c->k) + lay_bytes(*c, c->v);
 }
 
 extern "C" conqur_status conqur_attention(const conqur_attention_call* c, void* stream) {
@@ -396,6 +467,10 @@ extern "C" conqur_status conqur_attention(const conqur_attention_call* c, void* 
   PackedArgs a = args_of(*c);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   unsigned char* at = static_cast<unsigned char*>(c->workspace);
+  const ShareSizes share = share_sizes(*c, a.splits, 1);
+  a.shared_row = reinterpret_cast<float4*>(at);
+  a.shared = reinterpret_cast<float*>(at + share.rows);
+  at += share.rows + share.registers;
   hipError_t e = lay(*c, c->q, &a.q, &at, s);
   if (e == hipSuccess) e = lay(*c, c->k, &a.k, &at, s);
   if (e == hipSuccess) e = lay(*c, c->v, &a.v, &at, s);
@@ -406,7 +481,7 @@ extern "C" conqur_status conqur_attention(const conqur_attention_call* c, void* 
 extern "C" uint64_t conqur_attention_backward_workspace(const conqur_attention_call* c) {
   if (!backward_fine(c)) return 0;
   const BackwardSizes z = backward_sizes(*c);
-  return z.stat + z.seen + z.span + z.part + lay_bytes(*c, c->q) + lay_bytes(*c, c->k) + lay_bytes(*c, c->v) + lay_bytes(*c, c->out) + lay_bytes(*c, c->out_grad);
+  return z.stat + z.seen + z.span + z.part + z.share.rows + z.share.registers + lay_bytes(*c, c->q) + lay_bytes(*c, c->k) + lay_bytes(*c, c->v) + lay_bytes(*c, c->out) + lay_bytes(*c, c->out_grad);
 }
 
 extern "C" conqur_status conqur_attention_backward(const conqur_attention_call* c, void* stream) {
@@ -432,6 +507,9 @@ extern "C" conqur_status conqur_attention_backward(const conqur_attention_call* 
   a.part = reinterpret_cast<float*>(at + z.stat + z.seen + z.span);
   a.parts = z.parts;
   at += z.stat + z.seen + z.span + z.part;
+  a.shared_row = reinterpret_cast<float4*>(at);
+  a.shared = reinterpret_cast<float*>(at + z.share.rows);
+  at += z.share.rows + z.share.registers;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   hipError_t e = lay(*c, c->q, &a.q, &at, s);
   if (e == hipSuccess) e = lay(*c, c->k, &a.k, &at, s);

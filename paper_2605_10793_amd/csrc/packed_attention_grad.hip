@@ -19,6 +19,18 @@ __device__ __forceinline__ bf16x8 pack8(const f32x16& x, int k) {
                  f32x2_to_bf16x2(x[8 * k + 6], x[8 * k + 7]));
 }
 
+// What the other kernel needs of a row: `off` is D's error.
+template <int OPTIONS>
+__device__ __forceinline__ void leave_row(Args a, const Item& item, int head, int row, int token, int2 mine, float sum, float off, float lse, float dot, float slope) {
+  const int64_t at = (int64_t)item.first * a->group + row, to = (int64_t)head * a->tokens * a->group + at;
+  const float2 stat = make_float2(sum == 0.0f ? INFINITY : lse + __builtin_amdgcn_logf(sum), dot + off);
+  if constexpr (OPTIONS)
+    reinterpret_cast<float4*>(a->stat)[to] = make_float4(stat.x, stat.y, slope, (float)token);
+  else
+    a->stat[to] = stat;
+  if (head == 0) a->seen[at] = mine;
+}
+
 constexpr int kKeys = 32;          // keys that lie in LDS at a time for k_packed_dq
 
 // Operands that each lane keeps in LDS because its registers are full: what goes to scratch memory instead comes back behind all that is on its way to LDS.
@@ -60,7 +72,8 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dq(const PackedArgs) 
     if (part * kRows + wave * 32 >= rows) high = 0;
   }
   begin = begin / kKeys * kKeys;
-  if (head == 0 && lane == 0) a->span[(int64_t)(item.base + part) * kWaves + wave] = make_int4(low, high, low_all, high_all);
+  share_keys(&begin, &end, kKeys);
+  if (head == 0 && lane == 0 && blockIdx.y == 0) a->span[(int64_t)(item.base + part) * kWaves + wave] = make_int4(low, high, low_all, high_all);
 
   const int64_t row_token = item.first + token;
   const int q_head = head * group + (row < rows ? row : rows - 1) - token * group;
@@ -218,24 +231,63 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_packed_dq(const PackedArgs) 
 
   sum = halves(sum, [](float x, float y) { return x + y; });
   off = halves(off, [](float x, float y) { return x + y; });
+  a = kernel_args();
+  if (gridDim.y > 1) {
+    f32x4* const to = shared_of<8 * T::kTiles>(a, (int)blockIdx.y, wave);
+#pragma unroll
+    for (int t = 0; t < T::kTiles; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        to[(8 * t + r) * 64] = f32x4{dq[t][4 * r], dq[t][4 * r + 1], dq[t][4 * r + 2], dq[t][4 * r + 3]};
+        to[(8 * t + 4 + r) * 64] = f32x4{pk[t][4 * r], pk[t][4 * r + 1], pk[t][4 * r + 2], pk[t][4 * r + 3]};
+      }
+    if (h == 0) *shared_row_of(a, (int)blockIdx.y, wave * 32 + lane) = make_float4(sum, off, lse, dot);
+    return;
+  }
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
   off *= inv;
-  a = kernel_args();
   if (row >= rows) return;
-  if (h == 0) {
-    const int64_t at = (int64_t)item.first * group + row;
-    const float2 stat = make_float2(sum == 0.0f ? INFINITY : lse + __builtin_amdgcn_logf(sum), dot + off);
-    const int64_t to = (int64_t)head * a->tokens * group + at;
-    if constexpr (OPTIONS)
-      reinterpret_cast<float4*>(a->stat)[to] = make_float4(stat.x, stat.y, slope, (float)token);
-    else
-      a->stat[to] = stat;
-    if (head == 0) a->seen[at] = mine;
-  }
+  if (h == 0) leave_row<OPTIONS>(a, item, head, row, token, mine, sum, off, lse, dot, slope);
   bf16_bits* const to = a->q_grad.data + row_token * a->q_grad.ts + q_head * a->q_grad.hs + 4 * h;
 #pragma unroll
   for (int t = 0; t < T::kTiles; ++t) dq[t] -= off * pk[t];
   store_row<KS>(to, dq, a->scale * inv, wide8(a->q_grad.data, a->q_grad.ts, a->q_grad.hs));
+}
+
+// What workgroups that share keys made, added up in their order, for 32 entries of a row (blockIdx.y).
+template <int KS, int OPTIONS>
+__global__ void __launch_bounds__(64 * kWaves) k_packed_dq_join(const PackedArgs) {
+  using T = Tile<KS>;
+  const Args a = kernel_args();
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5, t = blockIdx.y;
+  const int head = blockIdx.x % a->heads, group = a->group;
+  Item item;
+  if (!item.find(a, blockIdx.x / a->heads, 7, group)) return;
+  const int row = (item.parts - 1 - item.part) * kRows + wave * 32 + (lane & 31);
+  if (row >= item.count * group) return;
+  float4 all = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  f32x16 dq = {}, pk = {};
+  for (int i = 0; i < a->splits; ++i) {
+    const float4 x = *shared_row_of(a, i, wave * 32 + (lane & 31));
+    all = make_float4(all.x + x.x, all.y + x.y, x.z, x.w);
+    const f32x4* const from = shared_of<8 * T::kTiles>(a, i, wave) + 8 * t * 64;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const f32x4 y = from[r * 64], z = from[(4 + r) * 64];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        dq[4 * r + j] += y[j];
+        pk[4 * r + j] += z[j];
+      }
+    }
+  }
+  const float inv = all.x == 0.0f ? 0.0f : 1.0f / all.x, off = all.y * inv;
+  const int token = (int)((uint32_t)row / (uint32_t)group), q_head = head * group + row - token * group;
+  if (h == 0 && t == 0)
+    leave_row<OPTIONS>(a, item, head, row, token, keys_of(a, item, token), all.x, off, all.z, all.w, OPTIONS && a->slopes ? a->slopes[q_head] * kLog2e : 0.0f);
+  dq -= off * pk;
+  store_tile<KS>(a->q_grad.data + (item.first + (int64_t)token) * a->q_grad.ts + q_head * a->q_grad.hs + 4 * h, t, dq, a->scale * inv,
+                 wide8(a->q_grad.data, a->q_grad.ts, a->q_grad.hs));
 }
 
 // Where the sums over part `p` of the rows are, of 32 keys of a workgroup.
@@ -520,37 +572,33 @@ __global__ void __launch_bounds__(64 * kKeyWaves, 2) k_packed_dkv(const PackedAr
   store_row<KS>(to_v, dv, 1.0f, v_wide);
 }
 
-// The sums of the rows' parts, in their order.
+// The sums of the rows' parts, in their order, for 32 entries of a key (blockIdx.y).
 template <int KS>
 __global__ void __launch_bounds__(128) k_packed_sum(const PackedArgs) {
   using T = Tile<KS>;
   const Args a = kernel_args();
-  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5, t = blockIdx.y;
   const int head = blockIdx.x % a->heads;
   Item item;
   if (!item.find(a, blockIdx.x / a->heads, 6, 1)) return;
   const int key = item.part * kTile + 32 * wave + (lane & 31);
-  f32x16 dk[T::kTiles], dv[T::kTiles];
-#pragma unroll
-  for (int t = 0; t < T::kTiles; ++t) dk[t] = dv[t] = f32x16{};
+  f32x16 dk = {}, dv = {};
   for (int p = 0; p < a->parts; ++p) {
-    const f32x4* const from = part_of<KS>(a, p, (int)blockIdx.x, wave) + lane;
+    const f32x4* const from = part_of<KS>(a, p, (int)blockIdx.x, wave) + t * 4 * 64 + lane;
 #pragma unroll
-    for (int t = 0; t < T::kTiles; ++t)
+    for (int r = 0; r < 4; ++r) {
+      const f32x4 x = from[r * 64], y = from[(T::kTiles * 4 + r) * 64];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const f32x4 x = from[(t * 4 + r) * 64], y = from[((T::kTiles + t) * 4 + r) * 64];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          dk[t][4 * r + j] += x[j];
-          dv[t][4 * r + j] += y[j];
-        }
+      for (int j = 0; j < 4; ++j) {
+        dk[4 * r + j] += x[j];
+        dv[4 * r + j] += y[j];
       }
+    }
   }
   if (key >= item.count) return;
   const int64_t token = item.first + key;
-  store_row<KS>(a->k_grad.data + token * a->k_grad.ts + head * a->k_grad.hs + 4 * h, dk, a->scale, wide8(a->k_grad.data, a->k_grad.ts, a->k_grad.hs));
-  store_row<KS>(a->v_grad.data + token * a->v_grad.ts + head * a->v_grad.hs + 4 * h, dv, 1.0f, wide8(a->v_grad.data, a->v_grad.ts, a->v_grad.hs));
+  store_tile<KS>(a->k_grad.data + token * a->k_grad.ts + head * a->k_grad.hs + 4 * h, t, dk, a->scale, wide8(a->k_grad.data, a->k_grad.ts, a->k_grad.hs));
+  store_tile<KS>(a->v_grad.data + token * a->v_grad.ts + head * a->v_grad.hs + 4 * h, t, dv, 1.0f, wide8(a->v_grad.data, a->v_grad.ts, a->v_grad.hs));
 }
 
 template <int KS, int OPTIONS>
@@ -562,14 +610,20 @@ hipError_t launch(const PackedArgs& a, hipStream_t s) {
     return x != hipSuccess ? x : hipFuncSetAttribute(reinterpret_cast<const void*>(k_packed_dkv<KS, OPTIONS>), hipFuncAttributeMaxDynamicSharedMemorySize, kDkv);
   });
   if (e != hipSuccess) return e;
-  k_packed_dq<KS, OPTIONS><<<dim3((uint32_t)(row_items(a) * a.heads)), 64 * kWaves, kDq, s>>>(a);
+  const uint32_t of_rows = (uint32_t)(row_items(a) * a.heads);
+  k_packed_dq<KS, OPTIONS><<<dim3(of_rows, (uint32_t)a.splits), 64 * kWaves, kDq, s>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
+  if (a.splits > 1) {
+    k_packed_dq_join<KS, OPTIONS><<<dim3(of_rows, Tile<KS>::kTiles), 64 * kWaves, 0, s>>>(a);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
   const uint32_t workgroups = (uint32_t)(key_items(a) * a.heads);
   k_packed_dkv<KS, OPTIONS><<<dim3(workgroups, (uint32_t)a.parts), 64 * kKeyWaves, kDkv, s>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess || a.parts == 1) return e;
-  k_packed_sum<KS><<<dim3(workgroups), 128, 0, s>>>(a);
+  k_packed_sum<KS><<<dim3(workgroups, Tile<KS>::kTiles), 128, 0, s>>>(a);
   return hipGetLastError();
 }
 

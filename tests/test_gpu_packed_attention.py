@@ -160,3 +160,36 @@ def test_large_caps(cap):
         close(out[rows], want["out"], free["out_tol"] + 2 * more * host[2][rows].abs().max().double(), "out")
         close(lse[rows], want["lse"], free["lse_tol"] + more, "lse")
         at += n
+
+
+@pytest.mark.parametrize("width", [32, 64, 80, 96, 128])
+@pytest.mark.parametrize("counts, heads, kv", [([1300], 2, 1), ([1500, 1400], 2, 2)])
+@pytest.mark.parametrize("kind, window, cap, biased", [("causal", 0, 0.0, False), ("both", 0, 0.0, True), ("holes", 0, 30.0, False), ("causal", 1290, 20.0, True)])
+def test_few_rows_whose_keys_are_shared(width, counts, heads, kv, kind, window, cap, biased):
+    """So few rows that several workgroups take parts of their keys, some of them none."""
+    check(counts, heads, kv, width, kind=kind, window=window, cap=cap, biased=biased, seed=width, lead=5, behind=3, strided=width != 80)
+
+
+def test_shared_keys_that_are_not_finite():
+    """Reach the rows that see them and no others, in every part."""
+    from paper_2605_10793_amd import attention as A
+    n, heads, width = 2048, 2, 128
+    (q, k, v, grad), _, start = inputs([n], heads, 1, width, 11)
+    first = (torch.arange(n) // 1024 * 1024).to(torch.int32).to(DEV)
+
+    def run(k, v, grad):
+        k, v, grad = (x.to(DEV) for x in (k, v, grad))
+        out, lse = A.attention(q.to(DEV), k, v, start, first=first, lse=True)
+        return (out, *A.attention_backward(q.to(DEV), k, v, out, lse, grad, start, first=first))
+    clean = run(k, v, grad)
+    bad_k, bad_v, bad_grad = k.clone(), v.clone(), grad.clone()
+    bad_v[1400, 0, 3] = math.nan
+    out, *_ = run(k, bad_v, grad)
+    assert torch.equal(out[:1400], clean[0][:1400]) and bool(out[1400:, :, 3].isnan().all()) and not bool(out[1400:, :, 4].isnan().any())
+    bad_k[1200] = math.inf
+    out, dq, _, _ = run(bad_k, v, grad)
+    assert torch.equal(out[:1200], clean[0][:1200]) and torch.equal(dq[:1200], clean[1][:1200]) and bool(out[1200:].isnan().any())
+    bad_grad[600, 1] = math.nan
+    _, dq, dk, dv = run(k, v, bad_grad)
+    assert torch.equal(dq[:600], clean[1][:600]) and torch.equal(dq[601:], clean[1][601:]) and torch.equal(dq[600, 0], clean[1][600, 0])
+    assert torch.equal(dk[601:], clean[2][601:]) and torch.equal(dv[601:], clean[3][601:]) and bool(dv[:601].isnan().any())

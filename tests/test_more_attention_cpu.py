@@ -239,3 +239,17 @@ def test_gradients_are_not_lost(library):
             A.attention(**a)
     with pytest.raises(ValueError, match="autograd"):
         A.chunk_attention(**chunk_arguments(q=Fake(3, 4, 64, grad=True)))
+
+
+def test_workspace_of_keys_that_are_shared():
+    """Few rows with many keys leave their parts of results there: 4 numbers a row and its entries, twice those of the gradients."""
+    lib = binding.load()
+
+    def call(tokens, heads, kv, **change):
+        return attention_call(tokens=tokens, q=(0x10000, heads * 128, 128, heads), k=(0x20000, kv * 128, 128, kv), v=(0x30000, kv * 128, 128, kv),
+                              out=(0x40000, heads * 128, 128, heads), **change)
+    rows = (2048 * 2 // 128 + 1 + 2) * 128 * 8          # eight parts of 256 keys
+    assert lib.conqur_attention_workspace(call(2048, 2, 1)) == rows * (16 + 128 * 4)
+    assert lib.conqur_attention_workspace(call(1200, 2, 1)) == lib.conqur_attention_workspace(call(2048, 2, 1, window=1200)) == 0
+    assert lib.conqur_attention_workspace(call(8192, 32, 8)) == 0
+    assert lib.conqur_attention(call(2048, 2, 1, workspace=0x1000, bytes=rows * (16 + 128 * 4) - 1), None) == binding.EINVAL
