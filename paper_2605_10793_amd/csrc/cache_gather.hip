@@ -4,7 +4,8 @@
 // neighbouring slots of the target (they lie at multiples of 64 of their sequence), whose tokens come from anywhere in the source, of one head, and has all of
 // them under way before it stores any (one after the other, keys, pairs, values: 83 us for 77, 32 sequences that keep three quarters of 501 to 8000 tokens in 4 bits; several heads to a workgroup cost more than finding the tokens
 // anew for each).  Keys go in 16 bytes a lane; values lie with the tokens of a page side by side, so a lane takes four
-// neighbouring target tokens of a V row: four reads of one entry each, one where the four lie side by side in the source too, and one store.
+// neighbouring target tokens of a V row: four reads of one entry each, one where the four lie side by side in the source too, or (codes) close to each other, and one
+// store.  (Codes, one read for four close ones: 67 us for 72, those sequences in 4 bits, 115 for 140 in 8; for 16 bits, two reads, 236 for 240, is left out.)
 #include "../../include/conqur.h"
 #include "common.h"
 
@@ -81,7 +82,29 @@ __global__ void __launch_bounds__(256) k_gather(const GatherArgs a) {
   }
   side_by_side = side_by_side && at[0] % 4 == 0 && ((s_from[t0] ^ s_from[t0 + 3]) >> shift) == 0;
   units values[kValues];
-  if (side_by_side) {
+  // Codes of four tokens that lie within 16 of a page, as those of a sequence that drops some do, come with one read for the four.
+  int64_t window = 0;
+  bool near = false;
+  if constexpr (BITS != 16) {
+    const int64_t low = min(min(s_from[t0], s_from[t0 + 1]), min(s_from[t0 + 2], s_from[t0 + 3])), high = max(max(s_from[t0], s_from[t0 + 1]), max(s_from[t0 + 2], s_from[t0 + 3]));
+    const int slot = (int)(low & (page_tokens - 1)) & ~3, from = slot < page_tokens - 16 ? slot : page_tokens - 16;      // (pages hold 16 tokens or more)
+    near = every && (low >> shift) == (high >> shift) && (int)(high & (page_tokens - 1)) - from < 16;
+    window = in_v((low >> shift << shift) + from);
+  }
+  if (near && !side_by_side) {
+    u32x4 all[kValues];
+#pragma unroll
+    for (int i = 0; i < kValues; ++i) __builtin_memcpy(&all[i], __builtin_assume_aligned(v + window + ((int64_t)(i * (256 / kFours)) << shift), 4), 16);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int byte = (int)(at[j] - window);
+#pragma unroll
+      for (int i = 0; i < kValues; ++i) {
+        const uint32_t a = byte & 4 ? all[i][1] : all[i][0], b = byte & 4 ? all[i][3] : all[i][2];
+        values[i][j] = (Unit)((byte & 8 ? b : a) >> (byte & 3) * 8);
+      }
+    }
+  } else if (side_by_side) {
 #pragma unroll
     for (int i = 0; i < kValues; ++i) values[i] = *reinterpret_cast<const units*>(v + at[0] + ((int64_t)(i * (256 / kFours)) << shift));
   } else {

@@ -265,3 +265,32 @@ def test_gather_of_many_sequences_and_heads():
         k[to, :, :3] = k[0][:, [9, 2, 11]]
         v[to, :, :, :3] = v[0][:, :, [9, 2, 11]]
     assert torch.equal(k, cache.k.view(torch.int16)) and torch.equal(v, cache.v.view(torch.int16))
+
+
+@pytest.mark.parametrize("bits, page, width", [(8, 16, 64), (8, 64, 128), (4, 16, 128), (4, 32, 64), (4, 256, 128), (16, 32, 128)])
+def test_gather_of_tokens_close_to_each_other(bits, page, width):
+    """Fours within 16 tokens of a page, at its ends, in any order, one token over and over, fours that are not, and the pool's very last tokens."""
+    from paper_2605_10793_amd import attention as A
+    g = torch.Generator().manual_seed(bits + page)
+    cache = A.KVCache.empty(6, 2, page, width, bits, DEV)
+    for x in (cache.k, cache.v, cache.k_scale, cache.v_scale):
+        if x is not None:
+            x.copy_(torch.randint(0, 255, x.shape, generator=g).to(x.dtype))
+    last = page - 1
+    picks = [last, last, last, last, last - 3, last, last - 1, last - 2, last - 15, last, last - 7, last - 8, 0, 15, 3, 8, 5, 1, 1, 2, page, last, page + 1, page - 2]
+    picks += sorted(torch.randperm(2 * page, generator=g)[:page].tolist()) + torch.randint(0, 2 * page, (page,), generator=g).tolist()
+    tokens = torch.tensor(picks[:4 * page], dtype=torch.int32)
+    table, to_table = torch.tensor([[3, 5]], dtype=torch.int32), torch.tensor([[0, 4, 2, 1]], dtype=torch.int32)
+    start = torch.tensor([0, tokens.shape[0]], dtype=torch.int32)
+    want = [None if x is None else x.cpu().clone() for x in (cache.k, cache.v, cache.k_scale, cache.v_scale)]
+    for i, t in enumerate(tokens.tolist()):
+        f, to = int(table[0, t // page]), int(to_table[0, i // page])
+        for side, x in enumerate(want):
+            if x is not None and side == 1:
+                x[to, :, :, i % page] = x[f, :, :, t % page]
+            elif x is not None:
+                x[to, :, i % page] = x[f, :, t % page]
+    A.gather(cache, tokens.to(DEV), start.to(DEV), table.to(DEV), to_table.to(DEV))
+    for x, y in zip(want, (cache.k, cache.v, cache.k_scale, cache.v_scale)):
+        if x is not None:
+            assert torch.equal(x.view(torch.uint8), y.cpu().view(torch.uint8))

@@ -207,3 +207,43 @@ def test_streams_and_graphs():
         torch.cuda.synchronize()
         for mine, theirs in zip((one, two), eager):
             assert all(torch.equal(x, y) for x, y in zip(mine, theirs))
+
+
+def test_shared_keys_on_streams_in_graphs_and_in_place():
+    """Calls whose keys several workgroups share: two under way at once, captured ones between eager ones, results over the queries, rows anywhere."""
+    from paper_2605_10793_amd import attention as A
+    counts = [1700]
+    made = [case(counts, heads=2, kv=1, width=64, seed=s) for s in range(4)]
+    want = [both(*x) for x in made]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in made]
+    got = []
+    for _ in range(3):
+        for stream, x in zip(streams, made):
+            with torch.cuda.stream(stream):
+                got.append(both(*x))
+    torch.cuda.synchronize()
+    for i, x in enumerate(got):
+        assert all(torch.equal(a, b) for a, b in zip(x, want[i % len(made)]))
+    sq, sk, sv, sg, start = (x.clone() for x in made[0])
+    graph, other = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        one = both(sq, sk, sv, sg, start)
+    with torch.cuda.graph(other):
+        two = both(sq, sk, sv, sg, start, cap=30.0)
+    for i in (1, 2, 3):
+        for x, y in zip((sq, sk, sv, sg), made[i]):
+            x.copy_(y)
+        graph.replay()
+        other.replay()
+        capped = both(*made[i], cap=30.0)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(one, want[i])) and all(torch.equal(x, y) for x, y in zip(two, capped))
+    q, k, v, grad, start = made[0]
+    over = q.clone()
+    A.attention(over, k, v, start, out=over)
+    odd = torch.zeros(q.numel() + 1, dtype=torch.bfloat16, device=DEV)[1:].view(q.shape).copy_(q)          # rows at multiples of 2 bytes
+    into = torch.zeros(q.numel() + 3, dtype=torch.bfloat16, device=DEV)[3:].view(q.shape)
+    A.attention(odd, k, v, start, out=into)
+    assert torch.equal(over, want[0][0]) and torch.equal(into, want[0][0])
+    assert all(torch.equal(x, y) for x, y in zip(both(odd, k, v, grad, start), want[0]))
