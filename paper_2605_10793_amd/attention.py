@@ -451,11 +451,16 @@ def _attention_call(q, k, v, out, start, first, last, window: int, cap: float, s
             tokens, sequences, width, window, cap, width ** -0.5 if scale is None else scale, 1 if zero_rest else 0), device
 
 
-def _with_room(call, size_of, fields, x, device: int) -> int:
-    """A call's status, with the workspace that it asks for, if any."""
-    size = size_of(_ATTENTION.pack(*fields, 0, 0))
+def _with_room(call, size_of, fields, x, device: int, without: bool) -> int:
+    """A call's status, with the workspace that it asks for, if any; without: most such calls need none, and only one that is refused is asked."""
+    alone = _ATTENTION.pack(*fields, 0, 0)
+    if without:
+        status = _run(call, device, alone)
+        if status != binding.EINVAL:
+            return status
+    size = size_of(alone)
     if not size:
-        return _run(call, device, _ATTENTION.pack(*fields, 0, 0))
+        return binding.EINVAL if without else _run(call, device, alone)
     room = torch.empty(size, dtype=torch.uint8, device=x.device)
     return _run(call, device, _ATTENTION.pack(*fields, room.data_ptr(), size))
 
@@ -477,7 +482,7 @@ def attention(q, k, v, start, first=None, last=None, window: int = 0, cap: float
     sums = torch.empty((q.shape[0], q.shape[1]), dtype=float32, device=q.device) if lse else None
     fields, device = _attention_call(q, k, v, out, start, first, last, window, cap, slopes, scale, 0 if sums is None else sums.data_ptr(), new)
     lib = binding.load()
-    _check(_with_room(lib.conqur_attention, lib.conqur_attention_workspace, fields, q, device), "conqur_attention")
+    _check(_with_room(lib.conqur_attention, lib.conqur_attention_workspace, fields, q, device, True), "conqur_attention")
     return (out, sums) if lse else out
 
 
@@ -492,5 +497,5 @@ def attention_backward(q, k, v, out, lse, grad, start, first=None, last=None, wi
     gradients = grad, _like(q), _like(k), _like(v)
     fields, device = _attention_call(q, k, v, out, start, first, last, window, cap, slopes, scale, lse.data_ptr(), True, gradients)
     lib = binding.load()
-    _check(_with_room(lib.conqur_attention_backward, lib.conqur_attention_backward_workspace, fields, q, device), "conqur_attention_backward")
+    _check(_with_room(lib.conqur_attention_backward, lib.conqur_attention_backward_workspace, fields, q, device, False), "conqur_attention_backward")
     return gradients[1:]
