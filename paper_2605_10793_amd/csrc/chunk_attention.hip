@@ -90,8 +90,11 @@ Plan plan_of(const conqur_chunk_call& c) {
   // (Short sequences: a wavefront that takes two blocks, of codes for up to 16 rows four, one after the other costs less than the join: a token of one sequence of 500 tokens, 4 bits, 11.7 us for
   // 14.5, 16 bits, capped, 17.2 for 17.9; 3 tokens of 4 of 1000, 8 bits, width 64, 11.8 for 17.8; but one token at 777 in 16 bits, capped, 21.8 for 16.1,
   // 8 tokens at 900 in 4 bits 22.0 for 18.9.)
+  // (Nor is it worth cutting 16 blocks where a quarter of the workgroups that the device holds have them, or 32 where half have: 8 tokens of 32 sequences of 300 to 1000, 4 bits,
+  // 21.9 us for 38.7, one token of 16 of them, 16 bits, 23.0 for 26.5; 4 tokens of 32 of 2000, 8 bits with a bias, 33.2 for 39.7.)
   const int64_t short_blocks = p.wide ? kWaves : (c.cache.bits == 16 || rows > 16 ? 2 : 4) * kWaves;
-  const bool alone = splits < 2 || blocks <= short_blocks || (blocks <= 32 && workgroups >= kSlots) || (blocks <= 128 && workgroups >= 4 * kSlots);
+  const bool alone = splits < 2 || blocks <= short_blocks || (blocks <= 32 && workgroups >= (p.wide ? kSlots : kSlots / 2)) || (!p.wide && blocks <= 16 && workgroups >= kSlots / 4) ||
+                     (blocks <= 128 && workgroups >= 4 * kSlots);
   p.tail = p.wide || (c.cache.bits != 16 && blocks * sequences >= 8 * splits) ? 4 : 0;
   p.splits = alone || sequences > kMaxScan || (blocks + p.tail) * sequences + 2 * kMaxSplits >= 1ll << 31 ? 0 : (int)splits;
   return p;
