@@ -294,3 +294,10 @@ def test_gather_of_tokens_close_to_each_other(bits, page, width):
     for x, y in zip(want, (cache.k, cache.v, cache.k_scale, cache.v_scale)):
         if x is not None:
             assert torch.equal(x.view(torch.uint8), y.cpu().view(torch.uint8))
+
+
+@pytest.mark.parametrize("bits, page, width", FORMATS)
+@pytest.mark.parametrize("kind, window, cap, biased", [("causal", 0, 0.0, False), ("causal", 1200, 0.0, True), ("holes", 0, 30.0, False)])
+def test_few_over_longer_contexts(bits, page, width, kind, window, cap, biased):
+    """Contexts that are cut into runs, whatever the format, next to short ones."""
+    check(bits, page, width, [2500, 70, 1300], [1, 3, 2], 4, 2, kind=kind, window=window, cap=cap, biased=biased, seed=bits + width, closer=True)

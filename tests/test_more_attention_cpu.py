@@ -113,15 +113,16 @@ def chunk_call(tokens=4, q=(0x60000, 1024, 128, 8), out=(0x70000, 1024, 128, 8),
 def test_chunk_arguments():
     lib = binding.load()
     assert lib.conqur_chunk_attention(chunk_call(tokens=0), None) == binding.OK
-    size = lib.conqur_chunk_attention_workspace(chunk_call())
-    assert size > 0
+    long = dict(columns=100, stride=100, context=6400)          # (short contexts are not cut into runs, and need no room)
+    size = lib.conqur_chunk_attention_workspace(chunk_call(**long))
+    assert size > 0 and lib.conqur_chunk_attention_workspace(chunk_call()) == 0
     for bad in BAD_CACHES + BAD_BATCHES + (dict(max_query=0), dict(max_query=1 << 22), dict(scale=float("inf")), dict(cap=-0.5), dict(cap=float("nan")),
                                            dict(window=1 << 31), dict(q=(0x60000, 1024, 128, 7)), dict(out=(0x70000, 1024, 128, 4)), dict(context=1 << 31)):
         assert lib.conqur_chunk_attention(chunk_call(**bad), None) == binding.EINVAL, bad
         assert lib.conqur_chunk_attention_workspace(chunk_call(**bad)) == 0, bad
     for bad in (dict(q=(0, 1024, 128, 8)), dict(out=(0x70000, 1024, 64, 8)), dict(first=0x102), dict(last=0x102), dict(slopes=0x102), dict(workspace=(0, 1 << 40)),
                 dict(workspace=(0x8008, 1 << 40)), dict(workspace=(0x8000, size - 1))):
-        assert lib.conqur_chunk_attention(chunk_call(**bad), None) == binding.EINVAL, bad
+        assert lib.conqur_chunk_attention(chunk_call(**long, **bad), None) == binding.EINVAL, bad
 
 
 def gather_call(count=4, tokens=0x6000, start=0x7000, table=0x8000, to_table=0x9000, stride=8, to_stride=4, columns=8, to_columns=4, sequences=2, **change):
