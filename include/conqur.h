@@ -411,8 +411,8 @@ typedef struct {
 
 /* New tokens of several sequences, packed: sequence b's are [start[b], start[b + 1]) of the call's rows and become the tokens prefix[b],
  * prefix[b] + 1, ... of that sequence.  Entries are clamped to [0, tokens]; a negative count means none; tokens beyond the table's
- * row (table_columns * page_tokens) are dropped.  conqur_cache_append with more than 512 sequences: no start may lie below one before it
- * (where one does, which tokens are written is unspecified).                                                            */
+ * row (table_columns * page_tokens) are dropped.  conqur_cache_append and conqur_chunk_attention with more than 512 sequences: no start may lie
+ * below one before it (where one does, which tokens are written, or have a result, is unspecified).                     */
 typedef struct {
   const int32_t* start;      /* sequences + 1 */
   const int32_t* prefix;     /* sequences: tokens committed already, >= 0 */
@@ -510,7 +510,8 @@ typedef struct {
 /*
  * Attention of a chunk of new tokens of each sequence, one or thousands, over a cache that holds them already: the token in place i of its
  * sequence sees keys max(0, first, i - window + 1) <= j < min(length, last) with the score cap tanh(scale q_i k_j / cap) (cap 0: scale q_i k_j) -
- * slope |i - j|.  Arithmetic, rounding, missing pages and rows that see nothing as in conqur_tree_attention.
+ * slope |i - j|.  Arithmetic, rounding, missing pages and rows that see nothing as in conqur_tree_attention.  Sequences must not have rows of the call in
+ * common, as they may where a start falls (which rows get a result is then unspecified).
  */
 uint64_t conqur_chunk_attention_workspace(const conqur_chunk_call* call);
 conqur_status conqur_chunk_attention(const conqur_chunk_call* call, void* stream);

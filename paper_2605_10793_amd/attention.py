@@ -392,12 +392,12 @@ def _in_room(call, size_of, form, fields, tail, x, what: str) -> None:
 def chunk_attention(q, cache: KVCache, start, prefix, table, first=None, last=None, window: int = 0, cap: float = 0.0, slopes=None,
                     max_query: Optional[int] = None, max_context: Optional[int] = None, scale: Optional[float] = None, out=None):
     """Attention of any number of new tokens q (bf16 [tokens, heads, width]; packed as in `append`, which has put their keys and values into the
-    cache) over their sequences' tokens, committed and new.  A token sees itself and those before it, or those from first on up to, not including, last
-    (int32, one per row of q, counted in tokens of the sequence; first >= last: nothing, zeros); window: and at most that many, itself the last.
-    cap (up to 4096): scores become cap tanh(score / cap); slopes (fp32 [heads]): less slope times the distance.  max_query: most new tokens of a
-    sequence, max_context: most tokens, committed and new (default: what q and the table hold; closer bounds choose the quicker kernel and share the work
-    out better).  scale: 1 / sqrt(width) unless given.  Returns out.  Rows beyond max_query of a sequence and rows of no sequence are zeros in a new tensor and stay as
-    they are in a given `out`."""
+    cache; no row two sequences') over their sequences' tokens, committed and new.  A token sees itself and those before it, or those from first on up
+    to, not including, last (int32, one per row of q, counted in tokens of the sequence; first >= last: nothing, zeros); window: and at most that many, itself
+    the last.  cap (up to 4096): scores become cap tanh(score / cap); slopes (fp32 [heads]): less slope times the distance.  max_query: most new tokens of
+    a sequence, max_context: most tokens, committed and new (default: what q and the table hold; closer bounds choose the quicker kernel and share the work
+    out better).  scale: 1 / sqrt(width) unless given.  Returns out.  Rows beyond max_query of a sequence and rows of no sequence are zeros in a new tensor and
+    stay as they are in a given `out`."""
     if q.requires_grad and torch.is_grad_enabled():
         _no_gradient("chunk_attention", "it has no gradient")
     if q.dim() != 3:

@@ -164,6 +164,7 @@ extern "C" conqur_status conqur_chunk_attention(const conqur_chunk_call* c, void
   a.tile_rows = p.tile_rows;
   a.row_tiles = p.row_tiles;
   a.row_shift = p.row_shift;
+  a.tile_inverse = (uint32_t)(((1ull << 32) + p.tile_rows - 1) / p.tile_rows);
   a.part = static_cast<float*>(c->workspace);
   a.part_ml = reinterpret_cast<float2*>(a.part + (uint64_t)c->cache.heads * p.row_tiles * 2 * p.splits * p.tile_rows * c->cache.width);
   a.scale_log2 = c->scale * 1.4426950408889634f;

@@ -45,7 +45,9 @@ struct TreeArgs {
   float scale_log2;
   // Of a chunk of new tokens (kinds kChunk and kOptions): keys by bounds, a window, a cap in base 2 and 2 / cap in base 2, a bias by distance.
   int chunk, window, zero_rest;
-  int row_shift;             // with no runs: row tiles of all sequences are numbered one behind the other, 2^row_shift rows (a tile's at most) to a number
+  // With no runs, row tiles of all sequences are numbered one behind the other.
+  uint32_t tile_inverse;     // 2^32 / tile_rows, rounded up: of rows (fewer than 2^24) it makes tiles
+  int row_shift;             // more than kMaxScan sequences: 2^row_shift rows (a tile's at most) to a number
   const int32_t* first;
   const int32_t* last;
   const float* slopes;
@@ -231,10 +233,43 @@ struct Pages {
   }
 };
 
+// The sequence (-1: none) and the row tile of it that is the id-th of all sequences' row tiles, wherever their rows lie, for up to kMaxScan sequences, each of
+// which has a tile more where its rows end with one (64 prompts of 512: 371 us, 383 without).  All starts are read at once.  By a whole wavefront; the same for
+// all lanes.
+__device__ __forceinline__ void place_among(Args a, int id, int* b, int* row_tile) {
+  const int lane = (int)threadIdx.x & 63, sequences = (int)a->batch.sequences, tokens = (int)a->tokens, most = a->max_query, group = a->group;
+  const uint32_t inverse = a->tile_inverse;
+  const int32_t* const start = a->batch.start;
+  int x[kScanChunks], y[kScanChunks];
+#pragma unroll
+  for (int c = 0; c < kScanChunks; ++c)
+    if (c * 64 < sequences) {
+      x[c] = start[min(c * 64 + lane, sequences)];
+      y[c] = start[min(c * 64 + lane + 1, sequences)];
+    }
+  *b = -1;
+  int before = 0;
+#pragma unroll
+  for (int c = 0; c < kScanChunks; ++c) {
+    if (c * 64 < sequences && *b < 0) {
+      const int n = min(max(y[c], 0), tokens) - min(max(x[c], 0), tokens);
+      const int tiles = c * 64 + lane < sequences ? (int)__umulhi((uint32_t)(min(max(n, 0), most) * group), inverse) + 1 : 0;
+      const int end = before + wave_scan(tiles), all = __builtin_amdgcn_readlane(end, 63);
+      if (id < all) {
+        const int i = __popcll(__ballot(end <= id));
+        *b = c * 64 + i;
+        *row_tile = id - (i ? __builtin_amdgcn_readlane(end, i - 1) : before);
+      }
+      before = all;
+    }
+  }
+}
+
 // The head and the row tile of a workgroup, and, if there are no runs, its sequence (-1: none).  A chunk's heads come first, so that with eight of them, or a
 // multiple, a cache head's workgroups share an L2 (four chunks of 700 to 1024 tokens over 16 bits: 412 us for 421); with no runs, sequences have the row tiles
 // that their own tokens make, for one prompt among many single tokens would give each of them a prompt's (2000 tokens and 255 single ones over 500 to 2500: 352 us
-// for 505; 64 prompts of 512: 374 for 452).
+// for 505; 64 prompts of 512: 374 for 452).  Up to kMaxScan sequences' tiles are counted, for their starts may fall (500 of 40 tokens over up to 60: 288 us,
+// 283 if numbered by their starts, as those of more are).
 template <int KIND>
 __device__ __forceinline__ void place_of(Args a, int* head, int* row_tile, int* b) {
   if constexpr (KIND == kMasks) {
@@ -245,6 +280,10 @@ __device__ __forceinline__ void place_of(Args a, int* head, int* row_tile, int* 
     if (a->splits) return;
     if (a->row_tiles == 1) {
       *b = id, *row_tile = 0;
+      return;
+    }
+    if ((int)a->batch.sequences <= kMaxScan) {
+      place_among(a, id, b, row_tile);
       return;
     }
     int first, next;
