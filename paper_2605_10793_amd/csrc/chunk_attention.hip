@@ -170,7 +170,8 @@ extern "C" conqur_status conqur_chunk_attention(const conqur_chunk_call* c, void
   a.scale_log2 = c->scale * 1.4426950408889634f;
   a.chunk = 1;
   a.window = (int)c->window;
-  a.zero_rest = c->zero_rest != 0;
+  a.looks = c->zero_rest ? (int)((c->tokens - 1) / rows_of_look((int)c->batch.sequences) + 1) : 0;
+  a.workgroups = (int)workgroups * (p.splits ? p.splits : 1);
   a.first = c->first;
   a.last = c->last;
   a.slopes = c->slopes;

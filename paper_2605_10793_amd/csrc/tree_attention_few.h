@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree(const TreeArgs) {
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int row0 = row_tile * 16 * QT;
   if constexpr (KIND != kMasks) {
-    if (a->zero_rest && blockIdx.x < a->cache.heads && blockIdx.y == 0) zero_rows(a, head);
+    if (a->looks) zero_rows(a);
   }
   const bf16x8 ones = as_frag(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);      // a row of the sums of the weights as they are rounded
   Pieces piece;

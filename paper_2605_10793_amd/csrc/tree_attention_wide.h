@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs) {
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int row0 = (row_tile * kWaves + wave) * 16 * QT;
   if constexpr (KIND != kMasks) {
-    if (a->zero_rest && blockIdx.x < a->cache.heads && blockIdx.y == 0) zero_rows(a, head);
+    if (a->looks) zero_rows(a);
   }
   Pieces piece;
   piece.b = own;

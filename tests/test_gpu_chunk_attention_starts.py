@@ -45,7 +45,10 @@ FALLING = [([0, 200, 0, 0], 200, [30, 0, 9]),                                   
            (backwards(5, 70), 350, [(i * 37) % 90 for i in range(9)])]
 
 
-@pytest.mark.parametrize("bits, page, width", [(16, 64, 128), (8, 32, 64), (4, 16, 128)])
+FORMATS = [(16, 64, 128), (8, 32, 64), (4, 16, 128)]
+
+
+@pytest.mark.parametrize("bits, page, width", FORMATS)
 @pytest.mark.parametrize("start, tokens, committed", FALLING, ids=lambda x: str(x) if isinstance(x, list) else None)
 def test_row_tiles_of_every_sequence(bits, page, width, start, tokens, committed):
     """Several row tiles and no runs."""
@@ -70,3 +73,33 @@ def test_runs(bits, size):
     """Contexts that are cut into runs."""
     check(bits, 64, 128, 8, 2, [0, size, 0, 0], size, [3000, 9, 0], True)
     check(bits, 64, 128, 8, 2, backwards(3, size), 3 * size, [2500, 0, 900, 4, 3000], True)
+
+
+@pytest.mark.parametrize("bits, page, width", FORMATS)
+@pytest.mark.parametrize("start, tokens, committed", [*FALLING, ([0, 1, 2, 0, 0], 2, [7, 100, 3, 4]), ([3, 4, 1, 2, 0, 1], 6, [7, 0, 3, 4, 90])],
+                         ids=lambda x: str(x) if isinstance(x, list) else None)
+def test_rows_without_a_result_are_zeros(bits, page, width, start, tokens, committed):
+    """In a new tensor; no others are."""
+    check(bits, page, width, 8, 2, start, tokens, committed, False, max_query=400 if tokens > 9 else None, seed=tokens)
+
+
+@pytest.mark.parametrize("bits, committed", [(16, 10), (16, 3000), (8, 3000), (4, 40)])
+@pytest.mark.parametrize("size, max_query", [(1, 1), (3, 2), (50, 40)])
+def test_many_rows_without_a_result(bits, committed, size, max_query):
+    """Behind the sequences and before them, beyond the most new tokens, with runs and without."""
+    for start, tokens in (([0, size, 2 * size], 4001), ([4000 - size, 4000, 0], 4000), ([1700, 1700 + size, 0], 1701 + size), ([900, 900, 900 + size], 4000)):
+        check(bits, 64, 128, 8, 2, start, tokens, [committed, 20], False, max_query=max_query)
+
+
+@pytest.mark.parametrize("sequences", [511, 512, 513, 700])
+def test_rows_without_a_result_among_many_sequences(sequences):
+    """Around the most sequences whose starts may fall: sequences of none, of more than have results, rows before and behind them."""
+    counts = [(i * 7) % 4 if i % 5 else 0 for i in range(sequences)]
+    start = [37 + sum(counts[:b]) for b in range(sequences + 1)]
+    check(16, 16, 64, 2, 1, start, start[-1] + 70, [i % 3 for i in range(sequences)], False, max_query=2)
+
+
+def test_rows_without_a_result_at_any_strides(monkeypatch):
+    from paper_2605_10793_amd import attention as A
+    monkeypatch.setattr(A, "_like", lambda x: torch.full((x.shape[1], x.shape[0], x.shape[2] + 1), 7, dtype=x.dtype, device=x.device)[..., 1:].transpose(0, 1))
+    check(16, 64, 64, 4, 2, [5, 9, 0], 300, [30, 0], False, max_query=3)
