@@ -39,7 +39,8 @@ class AttentionLayer:
 
     def step(self, fused, start, depth=None, mask=None, max_query: int = 64, max_context: Optional[int] = None):
         """New tokens of every sequence, at most max_query each (64 at most of a tree): fused [tokens, heads + 2 cache heads, width] holds their queries, keys and
-        values, start (int32 [sequences + 1]) the first row of each sequence.  A tree of drafted tokens has its tokens' depths (int64) and masks
+        values, start (int32 [sequences + 1], 0 or more) the first row of each sequence, in their order; a start below one before it: a sequence of none, as if
+        that had been repeated.  A tree of drafted tokens has its tokens' depths (int64) and masks
         (attention.tree_attention); without them they are a chain.  max_query: the most of a sequence, so that every token has a result.  Returns
         [tokens, heads, width].  Nothing is committed."""
         tokens, kv = fused.shape[0], self.cache.heads
@@ -50,7 +51,8 @@ class AttentionLayer:
             raise ValueError("a layer with a window, capped scores or slopes takes chains of tokens, no trees")
         q, k, v = self._split(fused)
         rows = torch.arange(tokens, dtype=torch.int32, device=fused.device)
-        sequence = torch.searchsorted(start[1:], rows, right=True).clamp_(max=self.table.shape[0] - 1)      # (rows of no sequence: the last)
+        # (rows of no sequence: the last; where a start falls, those behind it begin where rows end)
+        sequence = torch.searchsorted(start.cummax(0).values[1:-1], rows, right=True)
         first = self.prefix if depth is not None else self.prefix - start[:-1]
         positions = first[sequence] + (rows.long() if depth is None else depth)
         q_out, k_out = attention.qk_norm_rotary(self.plan, q, k, self.q_weight, self.k_weight, positions, eps=self.eps)

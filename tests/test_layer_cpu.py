@@ -110,3 +110,19 @@ def test_starts_that_do_not_fit_the_tokens(positions_of):
     assert len(got) == 6 and prefix == [14, 20, 34]
     got, prefix = positions_of([10, 20], [-5, -2, 6], 6)
     assert prefix == [10, 26]
+
+
+def test_positions_where_starts_fall(positions_of):
+    """Starts padded by zeros, sequences of none among others."""
+    assert positions_of([10, 20, 30, 40], [0, 1, 3, 0, 0], 3) == ([10, 20, 21], [11, 22, 30, 40])
+    assert positions_of([10, 20, 30, 40, 50], [2, 4, 4, 0, 0, 0], 4)[0][2:] == [10, 11]
+    assert positions_of([10, 20], [0, 3, 0], 3, torch.tensor([0, 1, 1])) == ([10, 11, 11], [13, 20])
+    assert positions_of([10], [0, 3], 3) == ([10, 11, 12], [13])
+
+
+@pytest.mark.parametrize("sequences", [64, 2000])
+def test_positions_of_many_sequences(positions_of, sequences):
+    counts = [b % 3 for b in range(sequences)]
+    start = [sum(counts[:b]) for b in range(sequences + 1)]
+    got, prefix = positions_of([7 * b for b in range(sequences)], start, start[-1])
+    assert got == [7 * b + i for b in range(sequences) for i in range(counts[b])] and prefix == [7 * b + n for b, n in enumerate(counts)]
