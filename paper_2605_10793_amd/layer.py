@@ -34,6 +34,7 @@ class AttentionLayer:
             raise ValueError(f"the calibrator is on cuda:{calibrator.device}, the cache on cuda:{cache.device}")
         self.calibrator = calibrator
         self.prefix = torch.zeros(table.shape[0], dtype=torch.int32, device=table.device)      # committed tokens
+        self._ahead = None             # by how much the sequences' next positions lie ahead of that; None: nowhere
         self.window, self.cap, self.slopes = window, cap, slopes
         self._last = self._trained = None
 
@@ -53,7 +54,9 @@ class AttentionLayer:
         rows = torch.arange(tokens, dtype=torch.int32, device=fused.device)
         # (rows of no sequence: the last; where a start falls, those behind it begin where rows end)
         sequence = torch.searchsorted(start.cummax(0).values[1:-1], rows, right=True)
-        first = self.prefix if depth is not None else self.prefix - start[:-1]
+        first = self.prefix if self._ahead is None else self.prefix + self._ahead
+        if depth is None:
+            first = first - start[:-1]
         positions = first[sequence] + (rows.long() if depth is None else depth)
         q_out, k_out = attention.qk_norm_rotary(self.plan, q, k, self.q_weight, self.k_weight, positions, eps=self.eps)
         attention.append(self.cache, k_out, v, start, self.prefix, self.table)
@@ -83,11 +86,23 @@ class AttentionLayer:
         attention.gather(self.cache, tokens.flatten(), start, old, begun)
         self.table = torch.where(torch.arange(table.shape[1], device=prefix.device) < full, old, table)
         self.prefix = prefix
+        if self._ahead is not None:
+            self._ahead = self._ahead[parents]
 
-    def keep(self, tokens, start, table):
-        """The sequences keep these of their tokens (as in attention.gather), in the pages of `table`, which nothing reads; positions stay in the keys."""
+    @property
+    def position(self):
+        """Of each sequence (int32), the position that its next token gets: the number of committed tokens, unless `keep` was told another."""
+        return self.prefix.clone() if self._ahead is None else self.prefix + self._ahead
+
+    def keep(self, tokens, start, table, position=None):
+        """The sequences keep these of their tokens (as in attention.gather), in the pages of `table`, which nothing reads.  The keys keep their positions: where
+        tokens were dropped that others stood behind, `position` (int32 [sequences]) says where those that follow stand, for them to be as far from each key as
+        they would have been: `layer.position`, if they follow the last one.  None: they get positions from the number of tokens that are left on, which is right
+        where a sequence keeps its first ones.  Windows and slopes go by the tokens that are left."""
         attention.gather(self.cache, tokens, start, self.table, table)
+        start = start.clamp(0, tokens.shape[0])        # as gather reads it
         self.table, self.prefix = table, start[1:] - start[:-1]
+        self._ahead = None if position is None else position - self.prefix
 
     def packed(self, fused, start, first=None, last=None):
         """Whole sequences, packed, for training: fused as in step, start (int32 [sequences + 1], any number of them) the first row of each, first and last the

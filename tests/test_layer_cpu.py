@@ -126,3 +126,32 @@ def test_positions_of_many_sequences(positions_of, sequences):
     start = [sum(counts[:b]) for b in range(sequences + 1)]
     got, prefix = positions_of([7 * b for b in range(sequences)], start, start[-1])
     assert got == [7 * b + i for b in range(sequences) for i in range(counts[b])] and prefix == [7 * b + n for b, n in enumerate(counts)]
+
+
+def test_positions_behind_dropped_tokens(monkeypatch, positions_of):
+    """The next tokens stand where they would have, through commits and branches, or where those that are left end."""
+    from paper_2605_10793_amd import layer as module
+    moved, positions = [], []
+    monkeypatch.setattr(module.attention, "gather", lambda *a: moved.append(a))
+    monkeypatch.setattr(module.attention, "qk_norm_rotary", lambda plan, q, k, qw, kw, p, eps: positions.append(p.tolist()) or (q, k))
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32)  # noqa: E731
+    layer = layer_of(sequences=3)
+    layer.cache.page_tokens = 16
+    layer.prefix = i32([100, 40, 7])
+    fused, start = torch.zeros(5, 8, 64), i32([0, 2, 3, 5])
+    kept, edges, to = i32(list(range(0, 100, 2)) + list(range(40)) + [6]), i32([0, 50, 90, 91]), torch.ones(3, 3, dtype=torch.int32)
+    layer.keep(kept, edges, to, position=layer.position)
+    assert moved[0][1:] == (kept, edges, moved[0][3], to) and layer.table is to
+    assert layer.prefix.tolist() == [50, 40, 1] and layer.position.tolist() == [100, 40, 7]
+    layer.step(fused, start)
+    layer.commit(start)
+    assert layer.prefix.tolist() == [52, 41, 3] and layer.position.tolist() == [102, 41, 9]
+    layer.step(fused, start, depth=torch.tensor([0, 1, 0, 0, 1]))
+    layer.branch(torch.tensor([2, 0, 0]), to)
+    assert layer.prefix.tolist() == [3, 52, 52] and layer.position.tolist() == [9, 102, 102]
+    layer.step(fused, start)
+    assert positions == [[100, 101, 40, 7, 8], [102, 103, 41, 9, 10], [9, 10, 102, 102, 103]]
+    layer.keep(i32([0, 1, 2]), i32([0, 2, 3, 9]), to)          # (a start behind the tokens that are named)
+    assert layer.prefix.tolist() == layer.position.tolist() == [2, 1, 0]
+    layer.step(fused, start)
+    assert positions[-1] == [2, 3, 1, 0, 1]
