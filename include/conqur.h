@@ -497,7 +497,7 @@ typedef struct {
   const float* slopes;       /* one per query head; NULL: none */
   uint64_t tokens;           /* rows of q, below 2^31; 0: nothing is done */
   uint64_t max_context;      /* as in conqur_tree_call */
-  void* workspace;           /* 16-byte aligned, conqur_chunk_attention_workspace bytes; as in conqur_tree_call */
+  void* workspace;           /* 16-byte aligned, conqur_chunk_attention_workspace bytes, at most 2^29; as in conqur_tree_call */
   uint64_t workspace_bytes;
   uint32_t max_query;        /* largest count of new tokens of a sequence, times the query heads of a cache head below 2^24; tokens beyond it get no result */
   uint32_t window;           /* tokens that a token sees at most, itself the last; 0: no such limit */

@@ -397,7 +397,7 @@ def chunk_attention(q, cache: KVCache, start, prefix, table, first=None, last=No
     the last.  cap (up to 4096): scores become cap tanh(score / cap); slopes (fp32 [heads]): less slope times the distance.  max_query: most new tokens of
     a sequence, max_context: most tokens, committed and new (default: what q and the table hold; closer bounds choose the quicker kernel and share the work
     out better).  scale: 1 / sqrt(width) unless given.  Returns out.  Rows beyond max_query of a sequence and rows of no sequence are zeros in a new tensor and
-    stay as they are in a given `out`."""
+    stay as they are in a given `out`.  Calls over long contexts need a workspace, up to 512 MiB, which the thread keeps for the stream."""
     if q.requires_grad and torch.is_grad_enabled():
         _no_gradient("chunk_attention", "it has no gradient")
     if q.dim() != 3:

@@ -36,6 +36,7 @@ hipError_t launch(const TreeArgs& a, int qt, dim3 grid, hipStream_t s) {
 }
 
 constexpr int64_t kMaxStride = 1ll << 40;
+constexpr uint64_t kMostRoom = 512ull << 20;          // bytes of workspace that a call may take to be cut into more runs than fill the device
 
 struct Plan {
   bool wide;
@@ -43,6 +44,11 @@ struct Plan {
   uint64_t tiles;            // row tiles of all sequences at most
   int64_t context;
 };
+
+// What `splits` runs leave there: a row's sum of values, its maximum and sum of weights, of two pieces each, or of one where there is one sequence.
+uint64_t room_of(const conqur_chunk_call& c, const Plan& p, int64_t splits) {
+  return (uint64_t)c.cache.heads * p.row_tiles * (c.batch.sequences > 1 ? 2 : 1) * splits * p.tile_rows * (c.cache.width + 2) * sizeof(float);
+}
 
 Plan plan_of(const conqur_chunk_call& c) {
   Plan p;
@@ -73,16 +79,16 @@ Plan plan_of(const conqur_chunk_call& c) {
   const int64_t blocks = p.context > kBlock ? (p.context + kBlock - 1) / kBlock : 1;
   p.min_blocks = kWaves;
   // As many runs as fill the device, or a few times that: the smallest number whose last turn leaves less than a tenth of it idle (17 tiles of 8 heads, 30011
-  // tokens in 8 bits: 3 runs 870 us with 408 workgroups, 7 runs 650).
-  const int64_t most = (blocks * sequences + p.min_blocks - 1) / p.min_blocks;
-  int64_t splits = kSlots / groups < 1 ? 1 : kSlots / groups;
-  for (int64_t s = splits, least = 0; s <= 16; ++s) {
-    const int64_t share = 1000 * groups * s / ((groups * s + kSlots - 1) / kSlots * kSlots);
-    if (share > least) {
-      least = share;
-      splits = s;
-    }
-    if (share >= 900) break;
+  // tokens in 8 bits: 3 runs 870 us with 408 workgroups, 7 runs 650), or the best of those whose parts take no more than kMostRoom and are written and read in
+  // the time that is saved, at 400 operations a byte.  (Without regard to that, 8256 tokens of one sequence by themselves took 784 us with parts of 786 MiB, and now 691 with none;
+  // 2112 120, now 89.  Over 30000, 8256 take 5.08 ms with parts of 393 MiB, 5.52 with none.  24600 tokens, 8 bits, over 40000: 28.5 ms with none, 27.4 with 1563 MiB.)
+  const int64_t most = (blocks * sequences + p.min_blocks - 1) / p.min_blocks, fill = kSlots / groups < 1 ? 1 : kSlots / groups;
+  auto share_of = [&](int64_t s) { return (double)(groups * s) / (double)((groups * s + kSlots - 1) / kSlots * kSlots); };
+  const double work = 4.0 * c.cache.width * c.q.heads * (double)c.tokens * ((double)p.context - 0.5 * (double)(c.max_query < p.context ? c.max_query : p.context));
+  int64_t splits = fill;
+  for (int64_t s = fill + 1; s <= 16 && share_of(splits) < 0.9; ++s) {
+    const uint64_t room = room_of(c, p, s);
+    if (share_of(s) > share_of(splits) && room <= kMostRoom && work * (1.0 - share_of(fill) / share_of(s)) > 400.0 * (double)room) splits = s;
   }
   if (splits > most) splits = most;
   if (splits > kMaxSplits) splits = kMaxSplits;
@@ -98,10 +104,6 @@ Plan plan_of(const conqur_chunk_call& c) {
   p.tail = p.wide || (c.cache.bits != 16 && blocks * sequences >= 8 * splits) ? 4 : 0;
   p.splits = alone || sequences > kMaxScan || (blocks + p.tail) * sequences + 2 * kMaxSplits >= 1ll << 31 ? 0 : (int)splits;
   return p;
-}
-
-uint64_t workspace_of(const conqur_chunk_call& c, const Plan& p) {
-  return (uint64_t)c.cache.heads * p.row_tiles * 2 * p.splits * p.tile_rows * (c.cache.width + 2) * sizeof(float);
 }
 
 bool call_fine(const conqur_chunk_call* c) {
@@ -130,7 +132,8 @@ hipError_t conqur::tree::launch_chunk_few(const TreeArgs& a, int qt, dim3 grid, 
 
 extern "C" uint64_t conqur_chunk_attention_workspace(const conqur_chunk_call* call) {
   if (!call_fine(call)) return 0;
-  return workspace_of(*call, plan_of(*call));
+  const Plan p = plan_of(*call);
+  return room_of(*call, p, p.splits);
 }
 
 extern "C" conqur_status conqur_chunk_attention(const conqur_chunk_call* c, void* stream) {
@@ -139,7 +142,7 @@ extern "C" conqur_status conqur_chunk_attention(const conqur_chunk_call* c, void
   if (!rows_fine(c->q, c->cache.width, c->tokens, false) || !rows_fine(c->out, c->cache.width, c->tokens, true)) return CONQUR_EINVAL;
   if (reinterpret_cast<uintptr_t>(c->first) % 4 || reinterpret_cast<uintptr_t>(c->last) % 4 || reinterpret_cast<uintptr_t>(c->slopes) % 4) return CONQUR_EINVAL;
   const Plan p = plan_of(*c);
-  const uint64_t need = workspace_of(*c, p);
+  const uint64_t need = room_of(*c, p, p.splits);
   if (need && (!c->workspace || reinterpret_cast<uintptr_t>(c->workspace) % 16 || c->workspace_bytes < need)) return CONQUR_EINVAL;
   const uint64_t workgroups = c->cache.heads * (p.splits ? (uint64_t)p.row_tiles : p.tiles);
   if (workgroups >= 1u << 24) return CONQUR_EINVAL;          // (of 256 threads, which 32 bits count)
@@ -166,7 +169,7 @@ extern "C" conqur_status conqur_chunk_attention(const conqur_chunk_call* c, void
   a.row_shift = p.row_shift;
   a.tile_inverse = (uint32_t)(((1ull << 32) + p.tile_rows - 1) / p.tile_rows);
   a.part = static_cast<float*>(c->workspace);
-  a.part_ml = reinterpret_cast<float2*>(a.part + (uint64_t)c->cache.heads * p.row_tiles * 2 * p.splits * p.tile_rows * c->cache.width);
+  a.part_ml = reinterpret_cast<float2*>(a.part + need / sizeof(float) / (c->cache.width + 2) * c->cache.width);
   a.scale_log2 = c->scale * 1.4426950408889634f;
   a.chunk = 1;
   a.window = (int)c->window;

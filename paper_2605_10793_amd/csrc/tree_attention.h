@@ -220,7 +220,8 @@ struct Layout {
 
 // Where a row's results of a piece are.
 __device__ __forceinline__ int64_t part_at(Args a, int head, int row_tile, int slot, int row_in_tile) {
-  return (((int64_t)head * a->row_tiles + row_tile) * 2 * a->splits + slot) * a->tile_rows + row_in_tile;
+  const int one = a->batch.sequences == 1;          // (which has first pieces only)
+  return (((int64_t)head * a->row_tiles + row_tile) * (2 * a->splits >> one) + (slot >> one)) * a->tile_rows + row_in_tile;
 }
 
 // Pages of a block's four groups of 16 keys, -1 where there is none; the same for a whole wavefront.
