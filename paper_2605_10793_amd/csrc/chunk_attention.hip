@@ -40,7 +40,7 @@ constexpr uint64_t kMostRoom = 512ull << 20;          // bytes of workspace that
 
 struct Plan {
   bool wide;
-  int qt, tile_rows, row_tiles, row_shift, splits, min_blocks, tail;
+  int qt, tile_rows, row_tiles, row_shift, splits, min_blocks, tail, tile_by_tile;
   uint64_t tiles;            // row tiles of all sequences at most
   int64_t context;
 };
@@ -78,6 +78,7 @@ Plan plan_of(const conqur_chunk_call& c) {
   const int64_t groups = (int64_t)c.cache.heads * p.row_tiles, sequences = c.batch.sequences;
   const int64_t blocks = p.context > kBlock ? (p.context + kBlock - 1) / kBlock : 1;
   p.min_blocks = kWaves;
+  p.tile_by_tile = 0;
   // As many runs as fill the device, or a few times that: the smallest number whose last turn leaves less than a tenth of it idle (17 tiles of 8 heads, 30011
   // tokens in 8 bits: 3 runs 870 us with 408 workgroups, 7 runs 650), or the best of those whose parts take no more than kMostRoom and are written and read in
   // the time that is saved, at 400 operations a byte.  (Without regard to that, 8256 tokens of one sequence by themselves took 784 us with parts of 786 MiB, and now 691 with none;
@@ -91,6 +92,20 @@ Plan plan_of(const conqur_chunk_call& c) {
     if (share_of(s) > share_of(splits) && room <= kMostRoom && work * (1.0 - share_of(fill) / share_of(s)) > 400.0 * (double)room) splits = s;
   }
   if (splits > most) splits = most;
+  // Row tiles are all cut into as many runs, and the first of them has every sequence, the others only those with as many new tokens.  Where a call's tokens make fewer
+  // tiles than so many sequences could, there are as many runs as give the first tile the share of the device that it has of all of them, and they are taken
+  // first; other tiles' are not shorter than a quarter of them, or 16 blocks.  16 bits, 640 new tokens of one of 64 sequences of 8000 and one of the others: 4400 us, 611 so (1405
+  // without an order); 512 of 4 of them 3890 and 846; 300 of one of 64 of 1000, one of which has 60000: 635 and 149.
+  if (p.row_tiles > 1 && splits > 1) {
+    const int64_t held = (int64_t)(kMostRoom / room_of(c, p, 1)), uneven = kSlots * sequences / ((int64_t)c.cache.heads * (int64_t)p.tiles);
+    const int64_t n = uneven < held ? (uneven < most ? uneven : most) : (held < most ? held : most);
+    if (n > splits) {
+      splits = n;
+      const int64_t quarter = blocks * sequences / splits / 4;
+      if (quarter > p.min_blocks) p.min_blocks = (int)(quarter < 16 ? quarter : 16);
+      p.tile_by_tile = 1;
+    }
+  }
   if (splits > kMaxSplits) splits = kMaxSplits;
   const int64_t workgroups = (int64_t)c.cache.heads * (sequences * p.row_tiles < (int64_t)p.tiles ? sequences * p.row_tiles : (int64_t)p.tiles);
   // (Short sequences: a wavefront that takes two blocks, of codes for up to 16 rows four, one after the other costs less than the join: a token of one sequence of 500 tokens, 4 bits, 11.7 us for
@@ -161,6 +176,7 @@ extern "C" conqur_status conqur_chunk_attention(const conqur_chunk_call* c, void
   a.context = p.context;
   a.splits = p.splits;
   a.min_blocks = p.min_blocks;
+  a.tile_by_tile = p.tile_by_tile;
   a.tail = p.splits ? p.tail : 0;
   a.max_query = (int)c->max_query;
   a.group = (int)(c->q.heads / c->cache.heads);

@@ -46,6 +46,7 @@ struct TreeArgs {
   // Of a chunk of new tokens (kinds kChunk and kOptions): keys by bounds, a window, a cap in base 2 and 2 / cap in base 2, a bias by distance.
   int chunk, window;
   int looks, workgroups;     // rows that get no result get zeros: how often zero_rows looks at some (0: they stay as they are), workgroups of the launch
+  int tile_by_tile;          // of the runs, all of the first row tile come first
   // With no runs, row tiles of all sequences are numbered one behind the other.
   uint32_t tile_inverse;     // 2^32 / tile_rows, rounded up: of rows (fewer than 2^24) it makes tiles
   int row_shift;             // more than kMaxScan sequences: 2^row_shift rows (a tile's at most) to a number
@@ -273,13 +274,20 @@ __device__ __forceinline__ void place_among(Args a, int id, int* b, int* row_til
 // for 505; 64 prompts of 512: 374 for 452).  Up to kMaxScan sequences' tiles are counted, for their starts may fall (500 of 40 tokens over up to 60: 288 us,
 // 283 if numbered by their starts, as those of more are).
 template <int KIND>
-__device__ __forceinline__ void place_of(Args a, int* head, int* row_tile, int* b) {
+__device__ __forceinline__ void place_of(Args a, int* head, int* row_tile, int* b, int* run) {
+  *run = blockIdx.y;
   if constexpr (KIND == kMasks) {
     *head = blockIdx.x / a->row_tiles, *row_tile = blockIdx.x % a->row_tiles, *b = blockIdx.y;
   } else {
     const int heads = (int)a->cache.heads, id = (int)blockIdx.x / heads;
     *head = (int)blockIdx.x % heads, *row_tile = id, *b = 0;
-    if (a->splits) return;
+    if (a->splits) {
+      if (a->tile_by_tile) {
+        const int at = (int)blockIdx.y * a->row_tiles + id;
+        *row_tile = at / a->splits, *run = at % a->splits;
+      }
+      return;
+    }
     if (a->row_tiles == 1) {
       *b = id, *row_tile = 0;
       return;
@@ -303,10 +311,11 @@ __device__ __forceinline__ void place_of(Args a, int* head, int* row_tile, int* 
 
 // What a workgroup has to do, piece by piece: blocks [first, last) of sequence b.
 struct Pieces {
+  int run;                   // number of the workgroup's
   int x, stop;               // in the blocks of all sequences
   int b, first, last, slot;
   bool whole;
-  // False: nothing left.  Begins with the workgroup's own sequence in b, if there are no runs.  Called by whole wavefronts, with the same results in all of them.
+  // False: nothing left.  Begins with the workgroup's own run, or, if there are none, its sequence in b.  Called by whole wavefronts, with the same results in all of them.
   __device__ __forceinline__ bool next(Args a, int row0, bool begin) {
     if (a->splits == 0) {
       if (!begin || b < 0) return false;
@@ -317,7 +326,7 @@ struct Pieces {
     }
     if (begin) {
       const Layout l(a, row0, lane_anew());
-      x = (int)blockIdx.y * l.each;
+      x = run * l.each;
       stop = l.all - x < l.each ? l.all : x + l.each;
       if (x >= stop) return false;
       int from = 0, to = 0;
@@ -325,7 +334,7 @@ struct Pieces {
       first = x - from;
       last = (to < stop ? to : stop) - from;
       whole = first == 0 && from + last == to;
-      slot = 2 * (int)blockIdx.y;
+      slot = 2 * run;
       x = from + last;
       return true;
     }
@@ -339,7 +348,7 @@ struct Pieces {
     first = 0;
     last = n < stop - x ? n : stop - x;
     whole = last == n;
-    slot = 2 * (int)blockIdx.y + 1;
+    slot = 2 * run + 1;
     x += last;
     return true;
   }

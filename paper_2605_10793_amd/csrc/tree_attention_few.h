@@ -107,16 +107,15 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree(const TreeArgs) {
   __shared__ __attribute__((aligned(16))) float s_o[2][QT * kTiles][64][4];
   __shared__ float s_ml[2][QT][2][64];
 
-  int head, row_tile, own;
-  place_of<KIND>(a, &head, &row_tile, &own);
+  int head, row_tile;
+  Pieces piece;
+  place_of<KIND>(a, &head, &row_tile, &piece.b, &piece.run);
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int row0 = row_tile * 16 * QT;
   if constexpr (KIND != kMasks) {
     if (a->looks) zero_rows(a);
   }
   const bf16x8 ones = as_frag(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);      // a row of the sums of the weights as they are rounded
-  Pieces piece;
-  piece.b = own;
   for (bool first = true; piece.next(a, row0, first); first = false) {
     int lane, col, g;
     auto number = [&] {

@@ -93,15 +93,14 @@ __global__ void __launch_bounds__(64 * kWaves, 2) k_tree_wide(const TreeArgs) {
   int* const s_flag = reinterpret_cast<int*>(shared + D::kFlagAt);          // of a pair's slot: K's tokens, V's tokens have rests
   uint16_t* const s_later = reinterpret_cast<uint16_t*>(s_flag + 2 * kDepth);
 
-  int head, row_tile, own;
-  place_of<KIND>(a, &head, &row_tile, &own);
+  int head, row_tile;
+  Pieces piece;
+  place_of<KIND>(a, &head, &row_tile, &piece.b, &piece.run);
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int row0 = (row_tile * kWaves + wave) * 16 * QT;
   if constexpr (KIND != kMasks) {
     if (a->looks) zero_rows(a);
   }
-  Pieces piece;
-  piece.b = own;
   for (bool first = true; piece.next(a, row_tile * 64 * QT, first); first = false) {
   int tid, lane, col, g;
   auto number = [&] {

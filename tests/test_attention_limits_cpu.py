@@ -40,3 +40,10 @@ def test_room_that_runs_of_chunk_attention_take():
     assert chunk_room(16, 4160, 4160) == chunk_room(8, 3120, 3120) == chunk_room(8, 24600, 65536) == 0
     assert chunk_room(8, 777, 30788) == 17 * 192 * 8 * 7 * 130 * 4
     assert chunk_room(16, 1024 * 4, 9024, 4) == 32 * 128 * 8 * 2 * 2 * 130 * 4
+
+
+def test_runs_of_calls_that_bring_very_different_numbers_of_tokens():
+    """The first row tile, which has every sequence, gets the runs that it needs, as far as their room goes; where all bring as many, all tiles get the same."""
+    assert chunk_room(16, 640 + 63, 8640, 64, max_query=640) == 20 * 128 * 8 * 2 * 25 * 130 * 4
+    assert chunk_room(16, 300 + 7, 8300, 8, max_query=300) == 10 * 128 * 8 * 2 * 30 * 130 * 4
+    assert chunk_room(16, 300 * 8, 8300, 8, max_query=300) == 10 * 128 * 8 * 2 * 6 * 130 * 4
