@@ -558,8 +558,9 @@ conqur_status conqur_attention(const conqur_attention_call* call, void* stream);
  * Its gradients, for the gradient g of the result: with D_i = sum g_i out_i, ds_ij = p_ij (g_i v_j - D_i), du_ij = ds_ij (1 - tanh^2 of that score),
  *   q_grad_i = scale sum_j du_ij k_j,  k_grad_j = scale sum_i du_ij q_i,  v_grad_j = sum_i p_ij g_i,
  * the latter two over all query heads of the key head, each sum in 32 bits and in an order that depends on the call's sizes and starts alone; p and du are
- * rounded to bf16 as factors.  A row that sees nothing has no part in any, whatever its gradient holds; keys that no row sees get zeros.  A gradient that is
- * not finite reaches nothing that its row does not see; what it sees may become NaN throughout.
+ * rounded to bf16 as factors.  A row that sees nothing has no part in any, whatever its gradient holds; keys that no row sees get zeros.  What is not finite
+ * in a row's query or gradient, or in a key or value that it sees, reaches that row and what it sees, which may become NaN throughout, even where the result is
+ * finite (a score of -inf has no weight in it), and nothing else.
  */
 uint64_t conqur_attention_backward_workspace(const conqur_attention_call* call);
 conqur_status conqur_attention_backward(const conqur_attention_call* call, void* stream);

@@ -489,7 +489,8 @@ def attention(q, k, v, start, first=None, last=None, window: int = 0, cap: float
 def attention_backward(q, k, v, out, lse, grad, start, first=None, last=None, window: int = 0, cap: float = 0.0, slopes=None,
                        scale: Optional[float] = None):
     """Gradients of attention (of q, of k, of v) for the gradient `grad` of its result `out` (bf16), with the lse that it gave and the other arguments as
-    it took them.  Rows of no sequence get zeros."""
+    it took them.  Rows of no sequence get zeros.  What is not finite in a row's query or gradient, or in a key or value that it sees, may make NaN of the
+    gradients of that row and of all that it sees, also where its result is finite; of no others."""
     if lse.dtype is not float32 or q.dim() != 3 or lse.shape != (q.shape[0], q.shape[1]) or not lse.is_contiguous():
         raise ValueError("lse must be a contiguous fp32 device tensor [tokens, heads]")
     if lse.get_device() != q.get_device():

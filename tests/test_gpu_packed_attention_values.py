@@ -104,6 +104,37 @@ def test_scores_of_minus_infinity():
     assert bool(torch.isfinite(out).all())
 
 
+@pytest.mark.parametrize("width", [64, 80, 128])
+@pytest.mark.parametrize("t", [0, 40, 99])
+def test_gradients_of_scores_of_minus_infinity(width, t):
+    """A key whose scores are all -inf, in the first of two documents: its rows and what they see have the gradients that they would have without it, or NaN (0 times
+    an infinity); rows before it, and the other document and sequence, have those of a call without it, bit by bit."""
+    n, edge, scale = 170, 100, width ** -0.5
+    q, k, v, grad, start = case([n, 30], heads=2, kv=1, width=width, seed=t)
+    q.abs_()
+    place = torch.arange(n + 30)
+    first = torch.where(place < edge, 0, torch.where(place < n, edge, 0)).to(torch.int32)
+    last = (torch.where(place < n, place, place - n) + 1).to(torch.int32)
+    options = dict(first=first.to(DEV), last=last.to(DEV))
+    clean = both(q, k, v, grad, start, **options)
+    k[t] = -math.inf
+    out, dq, dk, dv = both(q, k, v, grad, start, **options)
+    assert bool(torch.isfinite(out).all()) and (t or not out[0].any())
+    for x, y in zip((out, dq), clean):
+        assert torch.equal(x[:t], y[:t])
+    for x, y in zip((out, dq, dk, dv), clean):
+        assert torch.equal(x[edge:], y[edge:])
+    seen = seen_of(edge, None, None, 0)
+    seen[:, t] = False
+    finite = k[:edge].clone()
+    finite[t] = 0
+    want = attend(q[:edge].cpu(), finite.cpu(), v[:edge].cpu(), seen, place[:edge], scale, grad=grad[:edge].cpu())
+    close(out[:edge], want["out"], want["out_tol"], "out")
+    for name, x in (("dq", dq), ("dk", dk), ("dv", dv)):
+        nan = torch.isnan(x[:edge]).cpu()
+        close(torch.where(nan, want[name], x[:edge].cpu().double()), want[name], want[name + "_tol"], name)
+
+
 @pytest.mark.parametrize("how", ["odd strides", "unaligned", "heads first", "one row for all"])
 def test_rows_anywhere(how):
     """Rows that do not start at multiples of 16 bytes, heads that lie further apart than tokens, broadcast rows."""
