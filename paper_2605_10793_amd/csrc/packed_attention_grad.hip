@@ -25,7 +25,7 @@ __device__ __forceinline__ void leave_row(Args a, const Item& item, int head, in
   const int64_t at = (int64_t)item.first * a->group + row, to = (int64_t)head * a->tokens * a->group + at;
   const float2 stat = make_float2(sum == 0.0f ? INFINITY : lse + __builtin_amdgcn_logf(sum), dot + off);
   if constexpr (OPTIONS)
-    reinterpret_cast<float4*>(a->stat)[to] = make_float4(stat.x, stat.y, slope, (float)token);
+    reinterpret_cast<float4*>(a->stat)[to] = make_float4(stat.x, stat.y, slope, __int_as_float(token));
   else
     a->stat[to] = stat;
   if (head == 0) a->seen[at] = mine;
@@ -413,7 +413,6 @@ __global__ void __launch_bounds__(64 * kKeyWaves, 2) k_packed_dkv(const PackedAr
 #pragma unroll
   for (int t = 0; t < T::kTiles; ++t) dk[t] = dv[t] = f32x16{};
   const float scale = a->scale_log2, cap = a->cap_log2, cap_in = a->cap_in;
-  const float place = (float)key;
 
   Step now, then;
   bool more = next(&now);
@@ -467,10 +466,11 @@ __global__ void __launch_bounds__(64 * kKeyWaves, 2) k_packed_dkv(const PackedAr
     {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        float lse, dot, slope = 0.0f, token = 0.0f;
+        float lse, dot, slope = 0.0f;
+        int token = 0;
         if constexpr (OPTIONS) {
           const f32x4 x = *reinterpret_cast<const f32x4*>(s_rows + (at_rows * 32 + row_of(r, half)) * kStat);
-          lse = x[0], dot = x[1], slope = x[2], token = x[3];
+          lse = x[0], dot = x[1], slope = x[2], token = __float_as_int(x[3]);
         } else {
           const f32x2 x = *reinterpret_cast<const f32x2*>(s_rows + (at_rows * 32 + row_of(r, half)) * kStat);
           lse = x[0], dot = x[1];
@@ -480,7 +480,7 @@ __global__ void __launch_bounds__(64 * kKeyWaves, 2) k_packed_dkv(const PackedAr
           y = capped(s[r], cap, cap_in, lse, &x);
         else
           y = fmaf(s[r], scale, -lse);
-        if constexpr (OPTIONS) y = fmaf(-slope, fabsf(token - place), y);
+        if constexpr (OPTIONS) y = fmaf(-slope, fabsf((float)(token - key)), y);          // (24 bits do not hold every token)
         const float p = __builtin_amdgcn_exp2f(y);
         float e = (d[r] - dot) * p;
         if constexpr (OPTIONS == kCapped) e *= 4.0f * (x - x * x);
