@@ -76,6 +76,8 @@ class AttentionLayer:
         """Every sequence goes on from one of them, parents (int64 [sequences]), in the pages of `table` (as large as the present one): the parent's full pages
         stand in front of it, shared, whatever it holds there, and the page that the parent has begun is copied to the one behind them.  That and what
         follows must be pages that nothing else uses (attention.Pages keeps count)."""
+        if table.shape != self.table.shape:
+            raise ValueError(f"table must be {list(self.table.shape)}, as the present one")
         page, sequences = self.cache.page_tokens, self.table.shape[0]
         prefix, old = self.prefix[parents], self.table[parents]
         full = (prefix // page)[:, None]

@@ -155,3 +155,16 @@ def test_positions_behind_dropped_tokens(monkeypatch, positions_of):
     assert layer.prefix.tolist() == layer.position.tolist() == [2, 1, 0]
     layer.step(fused, start)
     assert positions[-1] == [2, 3, 1, 0, 1]
+
+
+@pytest.mark.parametrize("shape", [(3, 2), (3, 4), (2, 3)])
+def test_a_branch_into_another_number_of_pages_is_refused(monkeypatch, shape):
+    """Before anything is moved."""
+    from paper_2605_10793_amd import layer as module
+    moved = []
+    monkeypatch.setattr(module.attention, "gather", lambda *a: moved.append(a))
+    layer = layer_of(sequences=3)
+    layer.cache.page_tokens = 16
+    with pytest.raises(ValueError):
+        layer.branch(torch.tensor([0, 0, 1]), torch.zeros(shape, dtype=torch.int32))
+    assert not moved and layer.prefix.tolist() == [0, 0, 0]
