@@ -37,6 +37,7 @@ class AttentionLayer:
         self._ahead = None             # by how much the sequences' next positions lie ahead of that; None: nowhere
         self.window, self.cap, self.slopes = window, cap, slopes
         self._last = self._trained = None
+        self._moved = False            # whether sequences went on from others, or dropped tokens, since the last step
 
     def step(self, fused, start, depth=None, mask=None, max_query: int = 64, max_context: Optional[int] = None):
         """New tokens of every sequence, at most max_query each (64 at most of a tree): fused [tokens, heads + 2 cache heads, width] holds their queries, keys and
@@ -65,7 +66,7 @@ class AttentionLayer:
                                             max_query=max_query, max_context=max_context)
         else:
             out = attention.tree_attention(q_out, self.cache, start, self.prefix, self.table, mask=mask, max_query=max_query, max_context=max_context)
-        self._last = q, k, v, k_out, positions, out
+        self._last, self._moved = (q, k, v, k_out, positions, out), False
         return out
 
     def _split(self, fused):
@@ -87,7 +88,7 @@ class AttentionLayer:
         begun = table.gather(1, full.long().clamp_(max=table.shape[1] - 1))
         attention.gather(self.cache, tokens.flatten(), start, old, begun)
         self.table = torch.where(torch.arange(table.shape[1], device=prefix.device) < full, old, table)
-        self.prefix = prefix
+        self.prefix, self._moved = prefix, True
         if self._ahead is not None:
             self._ahead = self._ahead[parents]
 
@@ -103,7 +104,7 @@ class AttentionLayer:
         where a sequence keeps its first ones.  Windows and slopes go by the tokens that are left."""
         attention.gather(self.cache, tokens, start, self.table, table)
         start = start.clamp(0, tokens.shape[0])        # as gather reads it
-        self.table, self.prefix = table, start[1:] - start[:-1]
+        self.table, self.prefix, self._moved = table, start[1:] - start[:-1], True
         self._ahead = None if position is None else position - self.prefix
 
     def packed(self, fused, start, first=None, last=None):
@@ -128,7 +129,9 @@ class AttentionLayer:
     def commit(self, start, rows=None):
         """The tokens of the last step that stay.  rows (int64): their row numbers there, each sequence's from its root on, start (int32
         [sequences + 1]) the first entry of each sequence; None: all rows, as they were passed.  Kept keys and values move to the places
-        behind the committed ones, and their outputs go to the calibrator."""
+        behind the committed ones, and their outputs go to the calibrator.  Not after a branch or `keep`, which take committed tokens alone."""
+        if self._moved:
+            raise ValueError("the last step's tokens were not committed before sequences went on from others or dropped tokens")
         _, _, v, k_out, _, out = self._last
         if rows is not None:
             out = out[rows]

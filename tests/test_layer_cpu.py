@@ -168,3 +168,23 @@ def test_a_branch_into_another_number_of_pages_is_refused(monkeypatch, shape):
     with pytest.raises(ValueError):
         layer.branch(torch.tensor([0, 0, 1]), torch.zeros(shape, dtype=torch.int32))
     assert not moved and layer.prefix.tolist() == [0, 0, 0]
+
+
+@pytest.mark.parametrize("how", ["branch", "keep"])
+def test_tokens_that_were_left_behind_are_not_committed(monkeypatch, positions_of, how):
+    """A step's keys and values stand behind the committed ones in the pages that its sequences had then."""
+    from paper_2605_10793_amd import layer as module
+    monkeypatch.setattr(module.attention, "gather", lambda *a: None)
+    layer, fused, start = layer_of(sequences=2), torch.zeros(3, 8, 64), torch.tensor([0, 2, 3], dtype=torch.int32)
+    layer.cache.page_tokens = 16
+    layer.step(fused, start)
+    if how == "branch":
+        layer.branch(torch.tensor([1, 1]), layer.table)
+    else:
+        layer.keep(torch.tensor([], dtype=torch.int32), torch.zeros(3, dtype=torch.int32), layer.table)
+    with pytest.raises(ValueError):
+        layer.commit(start)
+    assert layer.prefix.tolist() == [0, 0]
+    layer.step(fused, start)
+    layer.commit(start)
+    assert layer.prefix.tolist() == [2, 1]
