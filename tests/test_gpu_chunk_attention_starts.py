@@ -103,3 +103,35 @@ def test_rows_without_a_result_at_any_strides(monkeypatch):
     from paper_2605_10793_amd import attention as A
     monkeypatch.setattr(A, "_like", lambda x: torch.full((x.shape[1], x.shape[0], x.shape[2] + 1), 7, dtype=x.dtype, device=x.device)[..., 1:].transpose(0, 1))
     check(16, 64, 64, 4, 2, [5, 9, 0], 300, [30, 0], False, max_query=3)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("max_query, context", [(4, 40), (4, 2000), (200, 250)])
+def test_a_captured_call_of_batches_of_any_size(bits, max_query, context):
+    """One graph, replayed with other starts, prefixes and queries, the batch padded by sequences of none and rows of no sequence."""
+    from paper_2605_10793_amd import attention as A
+    sequences, tokens = 6, 3 * max_query
+    cache, table, _ = filled(bits, 2, 64, 128, [context] * sequences, seed=1)
+    table = table.to(DEV)
+    q, start, prefix = (torch.zeros(s, dtype=t, device=DEV) for s, t in (((tokens, 8, 128), torch.bfloat16), ((sequences + 1,), torch.int32), ((sequences,), torch.int32)))
+    call = lambda q, s, p: A.chunk_attention(q, cache, s, p, table[:p.shape[0]], max_query=max_query, max_context=context)  # noqa: E731
+    call(q, start, prefix)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = call(q, start, prefix)
+    g = torch.Generator().manual_seed(2)
+    for counts in ([max_query] * 3, [1], [2, 0, max_query, 1], [], [max_query, 1, 1, 1, 1, 1], [0, max_query]):
+        n, total = len(counts), sum(counts)
+        edges = [sum(counts[:b]) for b in range(n + 1)]
+        q.copy_(torch.randn(tokens, 8, 128, generator=g))
+        start.copy_(torch.tensor(edges + [0] * (sequences - n)))
+        prefix.copy_(torch.tensor([(37 * b + 11) % (context - max_query) for b in range(sequences)]))
+        graph.replay()
+        eager = call(q, start, prefix)
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager) and not out[total:].any()
+        for b, (x, y) in enumerate(zip(edges, edges[1:])):          # each by itself: two results, off by two roundings of 2^-8 each at most
+            if y > x:
+                own = A.chunk_attention(q[x:y], cache, torch.tensor([0, y - x], dtype=torch.int32, device=DEV), prefix[b:b + 1].clone(), table[b:b + 1],
+                                        max_query=max_query, max_context=context)
+                assert float((own.double() - out[x:y].double()).norm()) <= 4 * 2.0 ** -8 * float(own.double().norm())
