@@ -22,7 +22,9 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-u
          "-Rpass-analysis=kernel-resource-usage"]
 
 
-MAX_SCRATCH = 64   # bytes per lane; attention over 16-bit pages of less than 64 tokens, 128 wide, has 32, every other kernel 0
+# Bytes per lane.  128 wide, tree attention over 16-bit pages of less than 64 tokens has 20, chunk attention over them 16 and of 17 to 32 rows of 8-bit codes (without a
+# cap or slopes) 12; every other kernel 0.
+MAX_SCRATCH = 64
 
 
 def hipcc() -> str:

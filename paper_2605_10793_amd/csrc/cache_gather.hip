@@ -1,6 +1,7 @@
 // Moving tokens of a paged cache into other pages: forks of sequences, tokens that a sequence keeps, states of beams.
 //
-// Nothing is computed: bound by HBM, or by the chain of reads (starts, token, page, entry) behind which a token's values are found.  A workgroup takes 64
+// Nothing is computed: bound by HBM, in 4 bits by the vector instructions that find 64 tokens' places for 9 KiB, too (62 to 66 % of the SIMDs' time), or by the chain of
+// reads (starts, token, page, entry) behind which a token's values are found.  A workgroup takes 64
 // neighbouring slots of the target (they lie at multiples of 64 of their sequence), whose tokens come from anywhere in the source, of one head, and has all of
 // them under way before it stores any (one after the other, keys, pairs, values: 83 us for 77, 32 sequences that keep three quarters of 501 to 8000 tokens in 4 bits; several heads to a workgroup cost more than finding the tokens
 // anew for each).  Keys go in 16 bytes a lane; values lie with the tokens of a page side by side, so a lane takes four

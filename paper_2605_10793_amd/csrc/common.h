@@ -129,9 +129,9 @@ __device__ __forceinline__ int sequence_of_part(int id, int edges, int shift, in
   }
 }
 
-// Scales and caps of scores that the kernels take.  A capped score is cap - 2 cap / (1 + e^(2 u / cap)): as each of exponential, sum and reciprocal is a unit or
-// less off in its last place, the quotient is by up to 2^-24, next to u = 0 where it is one half, and the score by cap 2^-23.  Up to 4096 that is 2^-11, a quarter of what
-// rounding a weight to bf16 may take; above, the difference would lose what scores say.
+// Scales and caps of scores that the kernels take.  A capped score is cap - 2 cap / (1 + e^(2 u / cap)).  Next to u = 0, where the quotient is one half, an exponential
+// that is a unit off in its last place makes 2^-25 of it, the sum's half unit 2^-25 more, and the reciprocal's unit 2^-24: the score is off by up to cap 2^-22.
+// Up to 4096 that is 2^-10, a quarter of what rounding a weight to bf16 may take; above, the difference would lose what scores say.
 constexpr float kMostCap = 4096.0f;
 static inline bool scores_fine(float scale, float cap) {
   const float most = 3.0f * scale;          // (2 log2 e is less)

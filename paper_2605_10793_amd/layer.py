@@ -108,8 +108,9 @@ class AttentionLayer:
         self._ahead = None if position is None else position - self.prefix
 
     def packed(self, fused, start, first=None, last=None):
-        """Whole sequences, packed, for training: fused as in step, start (int32 [sequences + 1], any number of them) the first row of each, first and last the
-        bounds of what tokens see (attention.attention).  Returns [tokens, heads, width]; the cache is not used."""
+        """Whole sequences, packed, for training: fused as in step, start (int32 [sequences + 1], any number of them, not falling) the first row of each, first and
+        last the bounds of what tokens see (attention.attention).  Returns [tokens, heads, width], which a calibrator may take as it takes a step's; the cache is not
+        used."""
         q, k, v = self._split(fused)
         rows = torch.arange(fused.shape[0], dtype=torch.int32, device=fused.device)
         positions = (rows - start[(torch.searchsorted(start, rows, right=True) - 1).clamp_(min=0)]).long()
